@@ -20,6 +20,14 @@
  *                     routing split over two streams on disjoint SM sets
  *   cr_shadow_replay  routed requests -> per-destination LRU hits and load
  *
+ * What a destination does with the prefix it was chosen for:
+ *
+ *   cr_pages_*        pages of its key/value cache: extend, fork, free, compact
+ *   cr_kv_write       keys and values of new tokens -> pages
+ *   cr_attn_packed, cr_attn_paged, cr_attn_decode
+ *                     attention over whole prompts, over cached prefixes, and of single
+ *                     tokens whose sequences share a prefix
+ *
  * Conventions shared by every call:
  *   - Pointers named d_* are DEVICE pointers owned by the caller (any CUDA
  *     allocation, e.g. a torch tensor's storage on the context's device).
@@ -34,8 +42,9 @@
  *     the context's CUDA stream unless documented as blocking.  Device-side
  *     checks (for example an arithmetic overflow found in a kernel) are
  *     reported by the next blocking call (cr_sync, *_export, *_info).
- *   - All quantities are unsigned integers: results are exact and
- *     deterministic (bit-identical run to run).
+ *   - All quantities of the routing path and of the pages are integers:
+ *     results are exact; those of the attention calls are floating point.  All
+ *     are deterministic (bit-identical run to run on one GPU).
  *   - A call whose scratch buffers are already large enough allocates
  *     nothing and does not synchronise, so a sequence of non-blocking calls
  *     can be captured into a CUDA graph after one pass over the same sizes
@@ -472,6 +481,139 @@ CR_API int cr_replay_export_state(cr_ctx *ctx, const cr_replay *rp, uint32_t rep
  * replay), CR_ECUDA. */
 CR_API int cr_replay_import_state(cr_ctx *ctx, cr_replay *rp, uint32_t rep, uint32_t r, const uint64_t *keys,
                                   uint32_t fill);
+
+/* ==== pages of a destination's key/value cache ========================= */
+/*
+ * The prefix cache that the plan places prefixes in (paper sec. 3.2: the
+ * engine-native cache that admitted and cold-tail traffic share), as pages of
+ * `page` tokens.  A sequence's tokens lie in the pages its table row lists;
+ * sequences with a common prefix list the same pages for it.  Everything is
+ * the caller's device memory; the calls keep it consistent:
+ *   d_ref    int32[n_pages]            table entries that name the page; 0: free
+ *   d_table  int32[n_seqs][max_pages]  pages of each sequence, ceil(len / page) of
+ *                                      them, the rest is -1
+ *   d_lens   int32[n_seqs]             tokens of each sequence (0: the row is empty)
+ *   d_cache  keys and values: token t of page p, head h, of layer l (keys: c = 0,
+ *            values: c = 1) starts at element
+ *            l*layer_stride + c*kv_stride + p*page_stride + t*token_stride + h*head_stride
+ *            and holds head_dim consecutive elements.
+ * Only the last page of a sequence is ever partly filled, and it is the
+ * sequence's own (its count is 1), so that a sequence always grows in place.
+ * Free pages are taken lowest first, for the entries of a call in list order.
+ * A call that needs more pages than are free changes nothing and makes the next
+ * blocking call return CR_EOVERFLOW.  An entry that names a row or a page that
+ * does not exist, a fork into a row in use, one that keeps no token or more than
+ * its parent has, or a length that its row cannot hold is skipped (the others
+ * are carried out), and the next blocking call returns CR_EINVAL.
+ *
+ * Limits: page a power of two, 8..256; head_dim a multiple of 8, 8..128; d_cache
+ * 16-byte aligned and every stride a multiple of 8 elements; a page's tokens and
+ * heads are dense in either order (token_stride = kv_heads*head_dim and
+ * head_stride = head_dim, or head_stride = page*head_dim and token_stride =
+ * head_dim).  n_pages * page < 2^31, n_seqs * max_pages < 2^40.
+ */
+#define CR_DTYPE_BF16 0 /* bfloat16 */
+#define CR_DTYPE_FP16 1 /* IEEE half */
+
+typedef struct {
+    void *d_cache;
+    int32_t *d_ref, *d_table, *d_lens;
+    uint32_t dtype; /* CR_DTYPE_* */
+    uint32_t layers, n_pages, page, kv_heads, head_dim, n_seqs, max_pages;
+    uint64_t layer_stride, kv_stride, page_stride, token_stride, head_stride; /* elements */
+} cr_kv_pages;
+
+/* The rows d_seqs[n] get pages for d_add[i] (>= 0) more tokens each, and are that
+ * much longer.  A row that stands in the list twice is extended once (CR_EINVAL).
+ * Errors: CR_EINVAL (pool out of limits, n >= 2^24), CR_ENOMEM, CR_ECUDA. */
+CR_API int cr_pages_extend(cr_ctx *ctx, const cr_kv_pages *pages, const int32_t *d_seqs, const int32_t *d_add,
+                           uint32_t n);
+/* The empty rows d_dst[i] become the first d_keep[i] tokens of rows d_src[i]: the
+ * pages that are full of them are shared, the tokens that are left are copied, in
+ * every layer, into a page of the row's own.  No row may stand in d_dst twice, nor
+ * in both lists.  Errors as cr_pages_extend. */
+CR_API int cr_pages_fork(cr_ctx *ctx, const cr_kv_pages *pages, const int32_t *d_src, const int32_t *d_dst,
+                         const int32_t *d_keep, uint32_t n);
+/* The rows d_seqs[n] become empty; pages that no row names any more are free.  An
+ * empty row stays empty.  Errors as cr_pages_extend. */
+CR_API int cr_pages_free(cr_ctx *ctx, const cr_kv_pages *pages, const int32_t *d_seqs, uint32_t n);
+/* Live pages move to the front: with L live pages, the k-th live page at or above L
+ * goes, in every layer, to the k-th free page below L (both ascending).
+ *   d_ref_out    int32[n_pages]            the counts afterwards
+ *   d_table_out  int32[n_seqs][max_pages]  the tables afterwards
+ *   d_map        int32[n_pages]            each page's new place, -1 for free ones
+ *   d_live       int32[1]                  L
+ * d_ref_out and d_table_out are arrays of their own (not d_ref, d_table); d_ref and
+ * d_table are left as they are, and no longer describe d_cache.  Errors as
+ * cr_pages_extend. */
+CR_API int cr_pages_compact(cr_ctx *ctx, const cr_kv_pages *pages, int32_t *d_ref_out, int32_t *d_table_out,
+                            int32_t *d_map, int32_t *d_live);
+
+/* Keys and values of new tokens into the pages of one layer.  The tokens of entry i
+ * are d_cu[i] .. d_cu[i+1]-1 of d_k and d_v (d_cu: int32[n+1], ascending from 0 to
+ * n_tokens); they are the last ones of row d_seqs[i] (NULL: of row i), whose length
+ * already counts them.  Token t, head h of d_k starts at element t*k_token +
+ * h*k_head (d_v alike), strides multiples of 8, pointers 16-byte aligned.  Tokens
+ * that fall outside their row are skipped and reported as CR_EINVAL by the next
+ * blocking call.  Errors: CR_EINVAL, CR_ECUDA. */
+CR_API int cr_kv_write(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t layer, const void *d_k, uint64_t k_token,
+                       uint64_t k_head, const void *d_v, uint64_t v_token, uint64_t v_head, const int32_t *d_cu,
+                       const int32_t *d_seqs, uint32_t n, uint32_t n_tokens);
+
+/* ==== attention ======================================================== */
+/*
+ * For every query head a and query token i of a sequence with m query and n key
+ * tokens, with key head h = a / (q_heads / kv_heads):
+ *
+ *   o_i = sum_j p_ij v_jh,  p_ij = exp(scale q_ia.k_jh) / sum_j' exp(scale q_ia.k_j'h)
+ *
+ * over the j that i sees: j < n and, if causal, j <= i + (n - m): the last query
+ * token sees every key.  A query that sees no key gets o = 0 and lse = -infinity.
+ * Products are of 16-bit operands with 32-bit sums; the softmax is in 32 bits, its
+ * weights are rounded to the 16-bit type for the product with v, o once at the end.
+ * Nothing behind a sequence's end is read into its result, whatever it holds.  A
+ * NaN or infinity in k_j or v_j reaches the queries that see j, and may reach
+ * others of the same sequence.
+ *
+ *   d_q, d_o  token t, head a at element t*q_token + a*q_head (o alike), 16-byte
+ *             aligned, strides multiples of 8
+ *   d_lse     NULL, or float[n_tokens][q_heads]: log of the sum of exp(scale q.k)
+ *   d_cu_q    int32[n+1]: query tokens of entry i are d_cu_q[i] .. d_cu_q[i+1]-1
+ *             (ascending from 0 to n_tokens)
+ *   d_seqs    paged calls: int32[n] rows of the table, NULL: row i
+ * q_heads a multiple of kv_heads, at most 128 times it; scale finite and > 0.
+ * d_o overlaps no input.
+ * Errors: CR_EINVAL, CR_ENOMEM, CR_ECUDA; CR_EINVAL by the next blocking call for a
+ * row that does not exist (its output is that of a row without keys), CR_ETIMEOUT
+ * for a wait that gave up (outputs are not meaningful).
+ */
+typedef struct {
+    const void *d_q;
+    void *d_o;
+    float *d_lse;
+    const int32_t *d_cu_q, *d_seqs;
+    uint32_t n, n_tokens, q_heads, causal;
+    float scale;
+    uint32_t reserved; /* 0 */
+    uint64_t q_token, q_head, o_token, o_head; /* elements */
+} cr_attn_args;
+
+/* Keys and values packed as the queries are: those of entry i are tokens
+ * d_cu_k[i] .. d_cu_k[i+1]-1 (NULL: d_cu_q) of d_k and d_v, n_kv tokens in all;
+ * strides as d_q's. */
+CR_API int cr_attn_packed(cr_ctx *ctx, const cr_attn_args *args, uint32_t dtype, uint32_t kv_heads, uint32_t head_dim,
+                          const void *d_k, uint64_t k_token, uint64_t k_head, const void *d_v, uint64_t v_token,
+                          uint64_t v_head, const int32_t *d_cu_k, uint32_t n_kv);
+/* Keys and values are those of the rows' d_lens tokens in one layer's pages (written
+ * by cr_kv_write before, the query tokens' own among them). */
+CR_API int cr_attn_paged(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t layer, const cr_attn_args *args);
+/* One query token per entry (d_cu_q and causal are not read, n_tokens = n).  With
+ * n_groups > 0 the entries d_group_off[g] .. d_group_off[g+1]-1 (int32[n_groups+1],
+ * ascending from 0 to n) are sequences whose first d_shared[g] tokens lie in the same
+ * pages: these are read once for all of them.  d_shared[g] is at most the shortest
+ * of their lengths. */
+CR_API int cr_attn_decode(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t layer, const cr_attn_args *args,
+                          const int32_t *d_group_off, const int32_t *d_shared, uint32_t n_groups);
 
 /* ==== allocation-free key histogram ================================== */
 /*

@@ -13,6 +13,14 @@ fails loudly otherwise.
   Ring            ring of the bounded-load policy               (cr_ring_create)
   plan_diff       churn between two plans                       (cr_plan_diff)
   shadow_replay   routed requests -> LRU hit / load counters    (cr_shadow_replay)
+
+What a destination does with the prefixes it holds:
+
+  KVPages         pages of a key/value cache, and pages_extend, pages_fork, pages_free, pages_compact
+  kv_write        keys and values of new tokens -> pages        (cr_kv_write)
+  attn_packed     attention over whole prompts                  (cr_attn_packed)
+  attn_paged      attention over cached pages                   (cr_attn_paged)
+  attn_decode     of single tokens that share prefixes          (cr_attn_decode)
 """
 from __future__ import annotations
 
@@ -42,7 +50,9 @@ EXPORTS = ("cr_create", "cr_destroy", "cr_set_stream", "cr_sync", "cr_last_error
            "cr_ring_create", "cr_ring_destroy", "cr_ring_export", "cr_plan_diff",
            "cr_replay_create_tokens", "cr_set_resolve_stream", "cr_partition_create", "cr_partition_destroy",
            "cr_profile_enable", "cr_profile_read", "cr_plan_import", "cr_replay_import_state",
-           "cr_replay_input_create", "cr_replay_input_destroy", "cr_replay_partition", "cr_replay_simulate")
+           "cr_replay_input_create", "cr_replay_input_destroy", "cr_replay_partition", "cr_replay_simulate",
+           "cr_pages_extend", "cr_pages_fork", "cr_pages_free", "cr_pages_compact", "cr_kv_write",
+           "cr_attn_packed", "cr_attn_paged", "cr_attn_decode")
 PROF = {"hash": 0, "plan": 1, "route_cand": 2, "route_resolve": 3, "partition": 4, "replay": 5}
 CR_NOALLOC_MAX_KEYS = 65536
 
@@ -68,6 +78,20 @@ class PlanDiff(C.Structure):
     _fields_ = [(f, C.c_uint64) for f in ("keys_a", "keys_b", "keys_common", "pairs_a", "pairs_b",
                                           "pairs_common", "adm_k_changed", "adm_set_changed", "hist_keys",
                                           "hist_kb_changed")]
+
+
+class KVPagesDesc(C.Structure):
+    _fields_ = ([(f, C.c_void_p) for f in ("d_cache", "d_ref", "d_table", "d_lens")] +
+                [(f, C.c_uint32) for f in ("dtype", "layers", "n_pages", "page", "kv_heads", "head_dim", "n_seqs",
+                                           "max_pages")] +
+                [(f, C.c_uint64) for f in ("layer_stride", "kv_stride", "page_stride", "token_stride", "head_stride")])
+
+
+class AttnArgs(C.Structure):
+    _fields_ = ([(f, C.c_void_p) for f in ("d_q", "d_o", "d_lse", "d_cu_q", "d_seqs")] +
+                [(f, C.c_uint32) for f in ("n", "n_tokens", "q_heads", "causal")] +
+                [("scale", C.c_float), ("reserved", C.c_uint32)] +
+                [(f, C.c_uint64) for f in ("q_token", "q_head", "o_token", "o_head")])
 
 
 class Replica(C.Structure):
@@ -130,6 +154,14 @@ def lib() -> C.CDLL:
         "cr_replay_simulate": ([vp, vp, vp, vp], i32),
         "cr_profile_enable": ([vp, u32], i32),
         "cr_profile_read": ([vp, u32, C.POINTER(C.c_uint64), C.POINTER(C.c_double)], i32),
+        "cr_pages_extend": ([vp, vp, vp, vp, u32], i32),
+        "cr_pages_fork": ([vp, vp, vp, vp, vp, u32], i32),
+        "cr_pages_free": ([vp, vp, vp, u32], i32),
+        "cr_pages_compact": ([vp, vp, vp, vp, vp, vp], i32),
+        "cr_kv_write": ([vp, vp, u32, vp, u64, u64, vp, u64, u64, vp, vp, u32, u32], i32),
+        "cr_attn_packed": ([vp, vp, u32, u32, u32, vp, u64, u64, vp, u64, u64, vp, u32], i32),
+        "cr_attn_paged": ([vp, vp, u32, vp], i32),
+        "cr_attn_decode": ([vp, vp, u32, vp, vp, vp, u32], i32),
     }
     for name, (args, res) in sig.items():
         f = getattr(L, name)
@@ -515,3 +547,217 @@ def shadow_replay(ctx: Context, replay: Replay, keys, plen, slen, dest, ctr):
     ctx.check(lib().cr_shadow_replay(ctx.handle, replay.handle, _ptr(keys), _ptr(plen), _ptr(slen), _ptr(dest),
                                      n, _ptr(ctr)), "cr_shadow_replay")
     return ctr
+
+
+# ---- what a destination does with the prefixes it holds ------------------------------------------------------------
+def _dtype_code(t) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return 0
+    if t.dtype == torch.float16:
+        return 1
+    raise ValueError(f"keys, values and queries are bfloat16 or float16, got {t.dtype}")
+
+
+def _out(ctx: Context, shape, like, dtype=None):
+    """An output of a call: its memory is not handed out again before ctx's stream has written it."""
+    import torch
+    t = torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
+    if ctx._stream_obj != torch.cuda.current_stream(ctx.device):
+        t.record_stream(ctx._stream_obj)
+    return t
+
+
+def _need_int32(name, t, n=None):
+    import torch
+    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 CUDA tensor")
+    if n is not None and t.numel() != n:
+        raise ValueError(f"{name} must have {n} elements, got {t.numel()}")
+
+
+def _need_heads(name, t, dtype, shape):
+    """[tokens, heads, head_dim] of the given dtype, head_dim contiguous."""
+    if not t.is_cuda or t.dtype != dtype or t.dim() != 3 or t.stride(2) != 1:
+        raise ValueError(f"{name} must be a {dtype} CUDA tensor [tokens, heads, head_dim] with contiguous head_dim")
+    for have, want in zip(t.shape, shape):
+        if want is not None and have != want:
+            raise ValueError(f"{name} must have shape {tuple(shape)} (None: any), got {tuple(t.shape)}")
+
+
+class KVPages:
+    """Pages of a destination's key/value cache, tables and lengths of its sequences (tensors the caller keeps).
+
+    ``cache`` [layers, 2, n_pages, page, kv_heads, head_dim] (keys, values; bfloat16 or float16; a page's tokens and
+    heads may be stored in either order), ``ref`` int32[n_pages] counts the table entries that name a page (0: free),
+    ``table`` int32[n_seqs, max_pages] lists each sequence's pages (-1 behind them), ``lens`` int32[n_seqs] its
+    tokens.  ``KVPages.empty`` makes an empty pool."""
+
+    def __init__(self, cache, ref, table, lens):
+        if cache.dim() != 6 or cache.shape[1] != 2 or not cache.is_cuda or cache.stride(5) != 1:
+            raise ValueError("cache must be a CUDA tensor [layers, 2, n_pages, page, kv_heads, head_dim]")
+        layers, _, n_pages, page, heads, dim = cache.shape
+        _need_int32("ref", ref, n_pages)
+        _need_int32("table", table)
+        if table.dim() != 2:
+            raise ValueError("table must have two dimensions")
+        _need_int32("lens", lens, table.shape[0])
+        self.cache, self.ref, self.table, self.lens = cache, ref, table, lens
+        self.layers, self.n_pages, self.page, self.kv_heads, self.head_dim = layers, n_pages, page, heads, dim
+        self._code = _dtype_code(cache)
+        self._bind()
+
+    def _bind(self):
+        st = self.cache.stride()
+        d = KVPagesDesc(_ptr(self.cache), _ptr(self.ref), _ptr(self.table), _ptr(self.lens), self._code, self.layers,
+                        self.n_pages, self.page, self.kv_heads, self.head_dim, self.table.shape[0],
+                        self.table.shape[1], st[0], st[1], st[2], st[3], st[4])
+        self._desc, self._addr = d, C.addressof(d)
+
+    @classmethod
+    def empty(cls, n_pages: int, page: int, n_seqs: int, max_pages: int, layers: int, kv_heads: int, head_dim: int,
+              dtype=None, device="cuda"):
+        import torch
+        cache = torch.zeros((layers, 2, n_pages, page, kv_heads, head_dim), dtype=dtype or torch.bfloat16,
+                            device=device)
+        return cls(cache, torch.zeros(n_pages, dtype=torch.int32, device=device),
+                   torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device),
+                   torch.zeros(n_seqs, dtype=torch.int32, device=device))
+
+    def replace(self, ref, table):
+        """Take the counts and tables that ``pages_compact`` gave (the cache's pages have moved already)."""
+        _need_int32("ref", ref, self.n_pages)
+        _need_int32("table", table)
+        if table.shape != self.table.shape:
+            raise ValueError("table must have the old table's shape")
+        self.ref, self.table = ref, table
+        self._bind()
+
+
+def pages_extend(ctx: Context, pages: KVPages, seqs, add):
+    """The sequences ``seqs`` get pages for ``add`` more tokens each (cr_pages_extend)."""
+    n = int(seqs.shape[0])
+    _need_int32("seqs", seqs, n)
+    _need_int32("add", add, n)
+    ctx.check(lib().cr_pages_extend(ctx.handle, pages._addr, _ptr(seqs), _ptr(add), n), "cr_pages_extend")
+
+
+def pages_fork(ctx: Context, pages: KVPages, src, dst, keep):
+    """The empty rows ``dst`` become the first ``keep`` tokens of the rows ``src`` (cr_pages_fork)."""
+    n = int(src.shape[0])
+    _need_int32("src", src, n)
+    _need_int32("dst", dst, n)
+    _need_int32("keep", keep, n)
+    ctx.check(lib().cr_pages_fork(ctx.handle, pages._addr, _ptr(src), _ptr(dst), _ptr(keep), n), "cr_pages_fork")
+
+
+def pages_free(ctx: Context, pages: KVPages, seqs):
+    """The rows ``seqs`` become empty (cr_pages_free)."""
+    n = int(seqs.shape[0])
+    _need_int32("seqs", seqs, n)
+    ctx.check(lib().cr_pages_free(ctx.handle, pages._addr, _ptr(seqs), n), "cr_pages_free")
+
+
+def pages_compact(ctx: Context, pages: KVPages):
+    """Move live pages to the front (cr_pages_compact): (ref, table, page_map, n_live), new tensors;
+    ``pages.replace(ref, table)`` takes them."""
+    import torch
+    ref = _out(ctx, pages.ref.shape, pages.ref)
+    table = _out(ctx, pages.table.shape, pages.table)
+    page_map = _out(ctx, pages.ref.shape, pages.ref)
+    live = _out(ctx, (1,), pages.ref)
+    ctx.check(lib().cr_pages_compact(ctx.handle, pages._addr, _ptr(ref), _ptr(table), _ptr(page_map), _ptr(live)),
+              "cr_pages_compact")
+    return ref, table, page_map, live
+
+
+def kv_write(ctx: Context, pages: KVPages, layer: int, k, v, cu, seqs=None):
+    """Write the keys and values [tokens, kv_heads, head_dim] of every sequence's last tokens into its pages:
+    entry i's tokens are cu[i] .. cu[i+1]-1, its row seqs[i] (None: i) (cr_kv_write)."""
+    n = int(cu.shape[0]) - 1
+    _need_int32("cu", cu)
+    if seqs is not None:
+        _need_int32("seqs", seqs, n)
+    shape = (k.shape[0], pages.kv_heads, pages.head_dim)
+    _need_heads("k", k, pages.cache.dtype, shape)
+    _need_heads("v", v, pages.cache.dtype, shape)
+    ks, vs = k.stride(), v.stride()
+    ctx.check(lib().cr_kv_write(ctx.handle, pages._addr, layer, _ptr(k), ks[0], ks[1], _ptr(v), vs[0], vs[1],
+                                _ptr(cu), _ptr(seqs), max(n, 0), int(k.shape[0])), "cr_kv_write")
+
+
+def _attn_args(ctx: Context, q, n, cu, seqs, causal, scale, out, lse):
+    import torch
+    T, heads, dim = q.shape
+    if out is None:
+        out = _out(ctx, (T, heads, dim), q)
+    else:
+        _need_heads("out", out, q.dtype, (T, heads, dim))
+    if lse is True:
+        lse = _out(ctx, (T, heads), q, torch.float32)
+    elif lse is not None and lse is not False:
+        _need_cuda("lse", lse, torch.float32)
+        if tuple(lse.shape) != (T, heads):
+            raise ValueError(f"lse must have shape {(T, heads)}")
+    else:
+        lse = None
+    if seqs is not None:
+        _need_int32("seqs", seqs, n)
+    qs, os_ = q.stride(), out.stride()
+    a = AttnArgs(_ptr(q), _ptr(out), _ptr(lse), _ptr(cu), _ptr(seqs), n, T, heads, 1 if causal else 0,
+                 dim ** -0.5 if scale is None else scale, 0, qs[0], qs[1], os_[0], os_[1])
+    return a, out, lse
+
+
+def attn_packed(ctx: Context, q, k, v, cu, cu_k=None, causal: bool = True, scale: Optional[float] = None, out=None,
+                lse=None):
+    """Attention over whole prompts packed back to back: q [tokens, heads, head_dim], k and v [tokens, kv_heads,
+    head_dim]; sequence i's queries are cu[i] .. cu[i+1]-1, its keys cu_k[i] .. (None: the same) (cr_attn_packed).
+    Returns the output, or (output, lse) with ``lse=True`` (or a tensor for it)."""
+    _need_heads("q", q, q.dtype, (None, None, None))
+    _need_int32("cu", cu)
+    n = max(int(cu.shape[0]) - 1, 0)
+    if cu_k is not None:
+        _need_int32("cu_k", cu_k, n + 1)
+    elif k.shape[0] != q.shape[0]:
+        raise ValueError("as many keys as queries, or cu_k")
+    shape = (k.shape[0], k.shape[1], q.shape[2])
+    _need_heads("k", k, q.dtype, shape)
+    _need_heads("v", v, q.dtype, shape)
+    code = _dtype_code(q)
+    a, out, lse = _attn_args(ctx, q, n, cu, None, causal, scale, out, lse)
+    ks, vs = k.stride(), v.stride()
+    ctx.check(lib().cr_attn_packed(ctx.handle, C.addressof(a), code, int(k.shape[1]), int(q.shape[2]), _ptr(k), ks[0],
+                                   ks[1], _ptr(v), vs[0], vs[1], _ptr(cu_k), int(k.shape[0])), "cr_attn_packed")
+    return out if lse is None else (out, lse)
+
+
+def attn_paged(ctx: Context, q, pages: KVPages, layer: int, cu, seqs=None, causal: bool = True,
+               scale: Optional[float] = None, out=None, lse=None):
+    """Attention of every sequence's last tokens over its pages (cr_attn_paged): q [tokens, heads, head_dim], entry
+    i's queries cu[i] .. cu[i+1]-1, its row seqs[i] (None: i).  Returns as ``attn_packed``."""
+    _need_heads("q", q, pages.cache.dtype, (None, None, pages.head_dim))
+    _need_int32("cu", cu)
+    n = max(int(cu.shape[0]) - 1, 0)
+    a, out, lse = _attn_args(ctx, q, n, cu, seqs, causal, scale, out, lse)
+    ctx.check(lib().cr_attn_paged(ctx.handle, pages._addr, layer, C.addressof(a)), "cr_attn_paged")
+    return out if lse is None else (out, lse)
+
+
+def attn_decode(ctx: Context, q, pages: KVPages, layer: int, seqs=None, group_off=None, shared=None,
+                scale: Optional[float] = None, out=None, lse=None):
+    """Attention of one token per sequence, q [n, heads, head_dim], over its pages (cr_attn_decode).  Sequences
+    group_off[g] .. group_off[g+1]-1 of the batch share their first shared[g] tokens' pages, which are read once for
+    all of them.  Returns as ``attn_packed``."""
+    _need_heads("q", q, pages.cache.dtype, (None, None, pages.head_dim))
+    ng = 0
+    if group_off is not None:
+        ng = max(int(group_off.shape[0]) - 1, 0)
+        _need_int32("group_off", group_off)
+        if shared is None:
+            raise ValueError("group_off without shared")
+        _need_int32("shared", shared, ng)
+    a, out, lse = _attn_args(ctx, q, int(q.shape[0]), None, seqs, False, scale, out, lse)
+    ctx.check(lib().cr_attn_decode(ctx.handle, pages._addr, layer, C.addressof(a), _ptr(group_off), _ptr(shared), ng),
+              "cr_attn_decode")
+    return out if lse is None else (out, lse)

@@ -311,6 +311,11 @@ extern "C" int cr_sync(cr_ctx *ctx)
         if (flags & CR_FLAG_BOUNDS)
             return cr_fail(ctx, CR_EINVAL, "debug build: an index outside its array was skipped (results of that "
                                            "call are not meaningful)");
+        if (flags & CR_FLAG_NOPAGES)
+            return cr_fail(ctx, CR_EOVERFLOW, "a call needed more pages than are free (it changed nothing)");
+        if (flags & CR_FLAG_BADPAGES)
+            return cr_fail(ctx, CR_EINVAL, "a row, page, length or offset of a page or attention call was out of range "
+                                           "(skipped)");
         if (flags & CR_FLAG_INTERNAL)
             return cr_fail(ctx, CR_ECUDA, "a kernel found its state inconsistent (results of that call are not "
                                           "meaningful)");

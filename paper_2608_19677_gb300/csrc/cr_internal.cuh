@@ -23,6 +23,8 @@ struct cr_nvtx_range {
 #define CR_FLAG_BADSIZE 8u   // token-weighted replay: a key came back with another prefix length
 #define CR_FLAG_INTERNAL 16u // a kernel found its own state inconsistent and skipped the access
 #define CR_FLAG_BOUNDS 32u   // debug build: an index outside its array was skipped
+#define CR_FLAG_NOPAGES 64u  // a call needed more pages than are free: nothing was changed
+#define CR_FLAG_BADPAGES 128u // a row, page, length or offset outside its array was skipped
 
 // Debug build (compiled with -DCR_DEBUG_CHECKS, see buildlib.py): data-dependent
 // indices are checked before use; a failing check raises CR_FLAG_BOUNDS in the
@@ -48,6 +50,11 @@ enum cr_scratch_slot {
     SCR_REPLAY_REST,   // replay items left to the window kernels, and their number
     SCR_ROUTE_DESC,    // route candidates, or the keys of a split route call
     SCR_DIFF,          // plan-difference counters
+    SCR_PAGES,         // free pages and entries of a page call
+    SCR_ATTN_PLAN,     // attention: list of work
+    SCR_ATTN_PART,     // attention: pieces of blocks that several CTAs share
+    SCR_ATTN_FEW,      //   of single tokens
+    SCR_ATTN_PFX,      // attention: results over shared prefixes
     SCR_NUM
 };
 
