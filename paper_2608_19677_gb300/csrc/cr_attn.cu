@@ -8,7 +8,8 @@
 // Work is therefore a list of (key head, block of query rows) with a number of key tiles each,
 // laid end to end; every CTA takes an equal stretch of it, wherever that begins or ends.  What a
 // CTA has of a block that it shares with others goes to scratch, and a second kernel joins the
-// pieces in order (k_attn_plan writes the list and the stretches, one CTA).
+// pieces in order (k_attn_plan writes the list and the stretches, one CTA).  A block counts for its tiles
+// and for kExtra more: its queries, its first scores and its result, which no other work hides.
 //
 // Two kernels do the work:
 //   k_attn_rows  many query rows per key head: 256 rows (tokens x grouped heads) against tiles of
@@ -24,6 +25,7 @@ namespace {
 constexpr int kRowsTile = 128;  // query rows of a tile, and keys of one
 constexpr int kFewTile = 64;    // keys of a tile of k_attn_few
 constexpr int kFewWarps = 4;
+constexpr uint32_t kExtra = 1;
 
 // A block of query rows of one key head.
 struct __align__(16) attn_blk {
@@ -33,17 +35,14 @@ struct __align__(16) attn_blk {
     int kbase;  // packed: first key token; paged: row of the table
     int diag;   // keys before the one that its first query token sees last (causal)
     int lo;     // k_attn_few: keys below are already counted (the shared prefix)
-    int pad0, pad1;
+    int nt;     // its key tiles
+    int pad;
 };
 // Where a CTA's stretch begins.
 struct __align__(16) attn_start {
-    unsigned long long pos;
-    uint32_t head, blk, tile, pad[3];
-};
-struct __align__(16) attn_plan {
-    unsigned long long N, Nb;  // key tiles in all, and of one head
-    uint32_t nblk, ncta;
-    uint32_t pad[2];
+    unsigned long long pos, N;  // N: key tiles of all stretches
+    uint32_t head, blk, tile, nblk;
+    attn_blk k;                 // its first block
 };
 
 // What the plan kernel reads.
@@ -57,12 +56,13 @@ struct plan_in {
     uint32_t tok_blk;      // query tokens per block
     uint32_t max_len;      // paged: tokens that a row can hold
     uint32_t min_tiles;    // key tiles that a CTA is worth
-    attn_plan *plan;
     attn_blk *blk;
-    unsigned long long *cum;  // [max_blk + 1] key tiles before each block
     attn_start *start;        // [max_cta + 1]
+    // of long lists only (the plan kernel's shared memory holds the others)
+    unsigned long long *cum;  // [max_blk + 1] key tiles before each block
     uint32_t *first;          // [n + 1] first block of each entry
 };
+constexpr uint32_t kPlanShared = 1024;
 
 enum { PLAN_PACKED, PLAN_PAGED, PLAN_GROUPS, PLAN_FEW };
 
@@ -130,8 +130,12 @@ __device__ __forceinline__ uint32_t upper(const unsigned long long *a, uint32_t 
 template <int KIND>
 __device__ void plan_build(const plan_in &A, uint32_t *status)
 {
+    __shared__ unsigned long long cum_near[kPlanShared + 1];
+    __shared__ uint32_t first_near[kPlanShared + 1];
     const uint32_t tid = threadIdx.x;
     const uint32_t n = KIND == PLAN_GROUPS ? A.n_groups : A.n;
+    uint32_t *first = n <= kPlanShared ? first_near : A.first;
+    unsigned long long *cum = A.max_blk <= kPlanShared ? cum_near : A.cum;
     unsigned long long total, base = 0;
     // blocks of every entry
     uint32_t nblk;
@@ -147,7 +151,7 @@ __device__ void plan_build(const plan_in &A, uint32_t *status)
                 nb = ((uint32_t)(hi - lo) + A.tok_blk - 1) / A.tok_blk;
             }
             const unsigned long long at = base + scan1024(nb, &total);
-            if (i < n) A.first[i] = (uint32_t)(at < A.max_blk ? at : A.max_blk);
+            if (i < n) first[i] = (uint32_t)(at < A.max_blk ? at : A.max_blk);
             base += total;
         }
         if (base > A.max_blk) {  // entries that overlap: not ascending
@@ -155,7 +159,7 @@ __device__ void plan_build(const plan_in &A, uint32_t *status)
             base = A.max_blk;
         }
         nblk = (uint32_t)base;
-        if (tid == 0) A.first[n] = nblk;
+        if (tid == 0) first[n] = nblk;
         __syncthreads();
     }
     // their keys
@@ -169,7 +173,7 @@ __device__ void plan_build(const plan_in &A, uint32_t *status)
                 uint32_t l = 0, h = n;
                 while (l < h) {
                     const uint32_t m = (l + h) >> 1;
-                    if (A.first[m] <= b)
+                    if (first[m] <= b)
                         l = m + 1;
                     else
                         h = m;
@@ -183,7 +187,7 @@ __device__ void plan_build(const plan_in &A, uint32_t *status)
                 k.row0 = (int)i;
                 k.ntok = 1;
             } else {
-                const int t0 = (int)((b - A.first[i]) * A.tok_blk);
+                const int t0 = (int)((b - first[i]) * A.tok_blk);
                 k.row0 = lo + t0;
                 k.ntok = clampi(hi - lo - t0, 0, (int)A.tok_blk);
             }
@@ -238,13 +242,14 @@ __device__ void plan_build(const plan_in &A, uint32_t *status)
                 nt = (uint32_t)((end + kRowsTile - 1) / kRowsTile);
                 if (nt == 0 && KIND != PLAN_GROUPS) nt = 1;  // rows without keys: zeros
             }
+            k.nt = (int)nt;
             A.blk[b] = k;
         }
-        const unsigned long long at = base + scan1024(nt, &total);
-        if (b < nblk) A.cum[b] = at;
+        const unsigned long long at = base + scan1024(nt ? nt + kExtra : 0, &total);
+        if (b < nblk) cum[b] = at;
         base += total;
     }
-    if (tid == 0) A.cum[nblk] = base;
+    if (tid == 0) cum[nblk] = base;
     __syncthreads();
     // stretches
     const unsigned long long Nb = base, N = Nb * A.heads;
@@ -257,10 +262,10 @@ __device__ void plan_build(const plan_in &A, uint32_t *status)
         if (s.pos < N) {
             s.head = (uint32_t)(s.pos / Nb);
             const unsigned long long rem = s.pos - s.head * Nb;
-            s.blk = upper(A.cum, nblk + 1, rem) - 1;
-            const unsigned long long t = rem - A.cum[s.blk], left = A.cum[s.blk + 1] - rem;
-            s.tile = (uint32_t)t;
-            if (t <= snap) {
+            s.blk = upper(cum, nblk + 1, rem) - 1;
+            const unsigned long long t = rem - cum[s.blk], left = cum[s.blk + 1] - rem;
+            s.tile = (uint32_t)(t - kExtra);
+            if (t <= snap || t <= kExtra) {
                 s.pos -= t;
                 s.tile = 0;
             } else if (left <= snap) {
@@ -272,15 +277,17 @@ __device__ void plan_build(const plan_in &A, uint32_t *status)
                 }
             }
         }
+        s.N = N;
+        s.nblk = nblk;
+        if (s.pos < N) {
+            while (cum[s.blk + 1] == cum[s.blk])  // blocks without keys
+                if (++s.blk == nblk) {
+                    s.blk = 0;
+                    ++s.head;
+                }
+            s.k = A.blk[s.blk];
+        }
         A.start[c] = s;
-    }
-    if (tid == 0) {
-        attn_plan p = {};
-        p.N = N;
-        p.Nb = Nb;
-        p.nblk = nblk;
-        p.ncta = ncta;
-        *A.plan = p;
     }
 }
 
@@ -288,6 +295,7 @@ template <int KIND>
 __global__ void __launch_bounds__(1024) k_attn_plan(const __grid_constant__ plan_in a, const __grid_constant__ plan_in b,
                                                     uint32_t *status)
 {
+    asm volatile("griddepcontrol.launch_dependents;");  // the next kernel's prologue needs nothing of this
     if (blockIdx.x == 0)
         plan_build<KIND>(a, status);
     else
@@ -296,126 +304,151 @@ __global__ void __launch_bounds__(1024) k_attn_plan(const __grid_constant__ plan
 
 // What the attention kernels read.
 struct attn_in {
-    const attn_plan *plan;
     const attn_blk *blk;
-    const unsigned long long *cum;
     const attn_start *start;
     const int32_t *table;  // paged
     uint32_t max_pages, page_log2, box_rows, box_log2;
     uint32_t paged, causal, G, nsub, tq, q_heads, head_dim;
     float c;               // scale * log2(e)
-    const void *q;         // k_attn_few
-    uint64_t q_token, q_head;
     void *o;
     float *lse;
     uint64_t o_token, o_head;
     float *part, *part_ml; // pieces
     float *pfx, *pfx_lse;  // shared prefix: o and log2 of the sum, [token][head]
     uint32_t to_pfx;       // k_attn_rows, its join: write those instead of o
+    uint32_t o_wide;       // rows of o begin at multiples of 32 bytes
+    uint32_t o_copy;       // whole tiles of o are written by copies
     uint32_t *status;
 };
 
-// A CTA's stretch, a block at a time.
+// A CTA's stretch, a block at a time; the next block's description is on its way while one is worked on.
 struct walk {
-    unsigned long long pos, end;
-    uint32_t h, b, t0, t1, nt, nblk;
-    attn_blk k;
-    const attn_in *A;
-    __device__ void begin(const attn_in &a)
+    unsigned long long left;
+    uint32_t h, next_h, b, t0, t1, begin_tile, nblk;  // b: of next_k
+    attn_blk k, next_k;
+    const attn_blk *blk;
+    __device__ __forceinline__ void fetch(uint32_t i)
     {
-        A = &a;
-        const attn_start s = a.start[blockIdx.x];
-        pos = s.pos;
-        h = s.head;
-        b = s.blk;
-        t1 = s.tile;
-        end = a.start[blockIdx.x + 1].pos;
-        nblk = a.plan->nblk;
-    }
-    __device__ bool next()
-    {
-        if (pos >= end) return false;
-        for (;;) {
-            if (b == nblk) {
-                b = 0;
-                ++h;
-            }
-            nt = (uint32_t)(A->cum[b + 1] - A->cum[b]);
-            if (nt) break;
-            ++b;
-        }
-        const int4 *g = reinterpret_cast<const int4 *>(A->blk + b);
-        int4 *d = reinterpret_cast<int4 *>(&k);
+        const int4 *g = reinterpret_cast<const int4 *>(blk + i);
+        int4 *d = reinterpret_cast<int4 *>(&next_k);
         d[0] = g[0];
         d[1] = g[1];
-        t0 = t1;
-        const unsigned long long left = end - pos;
-        t1 = nt - t0 < left ? nt : t0 + (uint32_t)left;
-        pos += t1 - t0;
+    }
+    __device__ __forceinline__ void begin(const attn_start *start, const attn_blk *list)
+    {
+        const attn_start *s = start + blockIdx.x;
+        blk = list;
+        next_h = s->head;
+        b = s->blk;
+        begin_tile = s->tile;
+        nblk = s->nblk;
+        next_k = s->k;
+        left = s[1].pos - s->pos;
+    }
+    __device__ __forceinline__ bool next()
+    {
+        if (left == 0) return false;
+        while (next_k.nt == 0) step();
+        k = next_k;
+        h = next_h;
+        t0 = begin_tile;
+        begin_tile = 0;
+        if (t0 == 0) left -= kExtra;
+        t1 = (uint32_t)k.nt - t0 < left ? (uint32_t)k.nt : t0 + (uint32_t)left;
+        left -= t1 - t0;
+        if (left) step();  // a piece that does not end its block is the last
         return true;
     }
-    __device__ void done()
+    __device__ __forceinline__ void step()
     {
-        if (t1 == nt) {
-            ++b;
-            t1 = 0;
+        if (++b == nblk) {
+            b = 0;
+            ++next_h;
         }
+        fetch(b);
     }
     // scratch place of this piece, or -1: the block is all here
-    __device__ int slot() const { return t0 ? 2 * (int)blockIdx.x : (t1 < nt ? 2 * (int)blockIdx.x + 1 : -1); }
+    __device__ __forceinline__ int slot() const
+    {
+        return t0 ? 2 * (int)blockIdx.x : (t1 < (uint32_t)k.nt ? 2 * (int)blockIdx.x + 1 : -1);
+    }
 };
 
 // ---- many rows --------------------------------------------------------------------------------
 // 256 query rows in two tiles of 128 (row r of a tile: token r / G, head r % G of the key head's
-// group), one warpgroup of softmax threads each (a thread owns a row), a warp that issues the
-// products and one that issues the copies.  Scores of tile X are in columns X*128 .. of tensor
-// memory; their weights, 16 bits wide, take the first half of the same columns and are the left
-// operand of the product with v, which adds to columns 256 + X*D ...  While one tile's scores are
-// in the softmax, the tensor cores work on the other's.
+// group).  Scores of tile X are in columns X*128 .. of tensor memory; the weights of 64 keys, 16 bits
+// wide, take the first half of the same columns and are the left operand of the product with v, which
+// adds to columns 256 + X*D ...  While one tile's scores are in the softmax, the tensor cores work
+// on the other's, so the softmax has to be as short as a tile's two products (1,024 cycles each way):
+// a row belongs to two threads, 64 keys each, which exchange their maxima through shared memory, and
+// the product with v begins when half of the weights are there.
 template <int D>
 struct rows_cfg {
     static constexpr int kChunks = D / 64;               // 64 elements: a 128-byte row
     static constexpr int kTile = kRowsTile * D * 2;      // bytes of 128 rows
-    static constexpr int kStages = D == 128 ? 5 : 8;
-    static constexpr int kSmem = (2 + kStages) * kTile + 1024;
+    // a stage holds the values of one tile and the keys of the next: what one turn of the products uses
+    static constexpr int kStages = D == 128 ? 2 : 4;
+    // after the tiles: one of outputs, a value per (tile, half, row), pieces, barriers, two words
+    static constexpr int kOut = (2 + 2 * kStages) * kTile, kXch = kOut + kTile, kPieces = kXch + 4 * kRowsTile * 4, kBars = kPieces + 2 * 48;
+    static constexpr int kSmem = kBars + 8 * (22 + 2 * kStages) + 16;
+    static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
 };
-// Warps 0-3 and 4-7: softmax; 8: products; 9: copies; 10, 11 only make the warpgroup whole, so that
-// its registers can go to the softmax threads (128 scores each): 2 x 128 x 208 + 128 x 80 of the
-// launch's 384 x 168.
-constexpr int kRowsThreads = 384;
+// Warps 0-15: softmax (tile, half of the keys, 32 rows); 16: products; 17: copies; 18: copies of outputs;
+// 19 makes the warpgroup whole, whose registers go to the softmax threads: 512 x 104 + 128 x 64 = 640 x 96.
+constexpr int kRowsThreads = 640;
 
-enum { B_QFULL, B_QEMPTY, B_SFULL, B_PREADY = B_SFULL + 2, B_OFULL = B_PREADY + 2, B_OEMPTY = B_OFULL + 2,
-       B_DONE = B_OEMPTY + 2, B_FULL };
+enum { B_QFULL, B_QEMPTY, B_DONE, B_SFULL, B_PREADY = B_SFULL + 2, B_OFULL = B_PREADY + 4, B_OEMPTY = B_OFULL + 2,
+       B_PFULL = B_OEMPTY + 2, B_PEMPTY = B_PFULL + 2, B_OUT = B_PEMPTY + 2, B_OUTFREE = B_OUT + 2, B_FULL };
+
+// What the copying warp tells the others of a piece (two of them are kept).
+struct rows_piece {
+    int row0, ntok, klen, diag;
+    int h, t0, n, slot;  // n: key tiles, 0: no more pieces
+    int stage, phase;    // of the ring, at its first keys
+    int whole;           // bit x: tile x is written as a whole, by a copy
+    int outs;            // such tiles before
+};
+static_assert(sizeof(rows_piece) == 48, "shared memory of the pieces");
 
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kRowsThreads, 1)
     k_attn_rows(const __grid_constant__ attn_in A, const __grid_constant__ CUtensorMap map_q,
-                const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
+                const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                const __grid_constant__ CUtensorMap map_o)
 {
     using cfg = rows_cfg<D>;
-    extern __shared__ unsigned char dyn[];
-    __shared__ __align__(8) unsigned long long bars[B_FULL + 2 * cfg::kStages];
-    __shared__ uint32_t tmem_at;
-    __shared__ int gave_up;
+    static_assert(B_FULL <= 22, "barriers");
+    extern __shared__ __align__(1024) unsigned char dyn[];
+    volatile rows_piece *piece = reinterpret_cast<volatile rows_piece *>(dyn + cfg::kPieces);
+    float(*xch)[kRowsTile] = reinterpret_cast<float(*)[kRowsTile]>(dyn + cfg::kXch);
+    uint32_t &tmem_at = *reinterpret_cast<uint32_t *>(dyn + cfg::kSmem - 16);
+    int &gave_up = *reinterpret_cast<int *>(dyn + cfg::kSmem - 12);
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t smem = (cr_smem(dyn) + 1023u) & ~1023u;
-    const uint32_t sq = smem, ring = smem + 2 * cfg::kTile;
-    const uint32_t bar = cr_smem(bars);
+    const uint32_t sq = cr_smem(dyn), ring = sq + 2 * cfg::kTile;
+    const uint32_t bar = sq + cfg::kBars;
+    if (sq & 1023u) {  // the swizzled tiles begin at multiples of 1,024 bytes
+        if (threadIdx.x == 0) atomicOr(A.status, CR_FLAG_INTERNAL);
+        return;
+    }
 #define BAR(i) (bar + 8u * (uint32_t)(i))
 #define FULL(s) BAR(B_FULL + (s))
 #define EMPTY(s) BAR(B_FULL + cfg::kStages + (s))
 
-    if (A.start[blockIdx.x].pos >= A.start[blockIdx.x + 1].pos) return;  // nothing for this CTA
     if (threadIdx.x == 0) {
         gave_up = 0;
         cr_bar_init(BAR(B_QFULL), 1);
         cr_bar_init(BAR(B_QEMPTY), 1);
         cr_bar_init(BAR(B_DONE), 1);
+        cr_bar_init(BAR(B_OUTFREE), 1);
         for (int x = 0; x < 2; ++x) {
             cr_bar_init(BAR(B_SFULL + x), 1);
-            cr_bar_init(BAR(B_PREADY + x), 4);
+            cr_bar_init(BAR(B_PREADY + 2 * x), 8);
+            cr_bar_init(BAR(B_PREADY + 2 * x + 1), 8);
             cr_bar_init(BAR(B_OFULL + x), 1);
-            cr_bar_init(BAR(B_OEMPTY + x), 4);
+            cr_bar_init(BAR(B_OEMPTY + x), 8);
+            cr_bar_init(BAR(B_PFULL + x), 1);
+            cr_bar_init(BAR(B_PEMPTY + x), 18);
+            cr_bar_init(BAR(B_OUT + x), 8);
         }
         for (int s = 0; s < cfg::kStages; ++s) {
             cr_bar_init(FULL(s), 1);
@@ -424,32 +457,60 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     // query rows that no copy writes (128 is not a multiple of G) are zeros
-    for (uint32_t i = threadIdx.x; i < 2u * cfg::kTile / 16; i += kRowsThreads)
-        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(sq + 16 * i), "r"(0));
+    if (A.G * A.tq < kRowsTile)
+        for (uint32_t i = threadIdx.x; i < 2u * cfg::kTile / 16; i += kRowsThreads)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(sq + 16 * i), "r"(0));
     cr_fence_async_smem();
-    if (warp == 8) cr_tmem_alloc(cr_smem(&tmem_at), 512);
+    if (warp == 16) cr_tmem_alloc(cr_smem(&tmem_at), 512);
     cr_tc_before();
     __syncthreads();
     cr_tc_after();
     const uint32_t tmem = tmem_at;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    walk w;
-    w.begin(A);
-    const uint32_t q_bytes = A.G * A.tq * 128 * cfg::kChunks;
+    uint32_t pieces = 0;  // their number so far; they take two places in turn
 
-    if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    if (warp == 9) {
+    if (warp >= 16) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (warp == 17) {
         // ---- copies ----
         if (lane == 0) {
             cr_tma_prefetch_map(&map_q);
             cr_tma_prefetch_map(&map_k);
             cr_tma_prefetch_map(&map_v);
         }
-        uint32_t stage = 0, phase = 0, qphase = 0;
-        while (w.next()) {
+        const uint32_t q_bytes = A.G * A.tq * 128 * cfg::kChunks;
+        uint32_t stage = 0, phase = 0, outs = 0;
+        walk w;
+        w.begin(A.start, A.blk);
+        for (;;) {
+            const bool more = w.next();
+            if (!cr_bar_wait(BAR(B_PEMPTY + (pieces & 1)), ((pieces >> 1) & 1) ^ 1, &gave_up)) goto out;
+            // tiles whose rows are all queries of the block, in a piece that ends its block
+            const int whole = A.o_copy && more && w.slot() < 0 ? (w.k.ntok >= (int)A.tq) + 2 * (w.k.ntok == 2 * (int)A.tq) : 0;
+            if (lane == 0) {
+                volatile rows_piece *p = piece + (pieces & 1);
+                p->n = more ? (int)(w.t1 - w.t0) : 0;
+                if (more) {
+                    p->whole = whole;
+                    p->outs = (int)outs;
+                    p->row0 = w.k.row0;
+                    p->ntok = w.k.ntok;
+                    p->klen = w.k.klen;
+                    p->diag = w.k.diag;
+                    p->h = (int)w.h;
+                    p->t0 = (int)w.t0;
+                    p->slot = w.slot();
+                    p->stage = (int)stage;
+                    p->phase = (int)phase;
+                }
+                cr_bar_arrive(BAR(B_PFULL + (pieces & 1)));
+            }
+            __syncwarp();
+            if (!more) break;
+            outs += __popc(whole);
             const int two = w.k.ntok > (int)A.tq;
-            if (!cr_bar_wait(BAR(B_QEMPTY), qphase ^ 1, &gave_up)) goto out;
-            qphase ^= 1;
+            if (!cr_bar_wait(BAR(B_QEMPTY), (pieces & 1) ^ 1, &gave_up)) goto out;
+            ++pieces;
             if (lane == 0) {
                 cr_bar_expect(BAR(B_QFULL), q_bytes * (1 + two));
                 for (int x = 0; x <= two; ++x)
@@ -460,292 +521,365 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             // lane: one box of one column block of a tile
             const uint32_t boxes = kRowsTile >> A.box_log2;
             const uint32_t box = lane & (boxes - 1), ch = lane / boxes;
-            for (uint32_t t = w.t0; t < w.t1; ++t) {
+            const uint32_t at = ch * (kRowsTile * 128) + ((box << A.box_log2) * 128);
+            const int32_t *row = A.paged ? A.table + (uint64_t)w.k.kbase * A.max_pages : nullptr;
+            bool on_v = false;  // of the tile whose values come next
+            int y_v = 0, pg_v = 0;
+            for (uint32_t t = w.t0; t <= w.t1; ++t) {
                 const int key = (int)(t * kRowsTile + (box << A.box_log2));
                 // packed keys come as one box; its rows behind the sequence are never used
-                const bool on = lane < boxes * cfg::kChunks && (!A.paged || key < w.k.klen);
-                const uint32_t bytes = __popc(__ballot_sync(~0u, on)) * A.box_rows * 128;
-                int y, pg = 0;
+                const bool on = t < w.t1 && lane < boxes * cfg::kChunks && (!A.paged || key < w.k.klen);
+                int y = w.k.kbase + key, pg = 0;
                 if (A.paged) {
-                    const uint32_t pi = (uint32_t)key >> A.page_log2;
-                    if (on) pg = __ldg(A.table + (uint64_t)w.k.kbase * A.max_pages + pi);
+                    if (on) pg = __ldg(row + ((uint32_t)key >> A.page_log2));
                     y = key & ((1 << A.page_log2) - 1);
-                } else {
-                    y = w.k.kbase + key;
                 }
-                for (int v = 0; v < 2; ++v) {
-                    if (!cr_bar_wait(EMPTY(stage), phase ^ 1, &gave_up)) goto out;
-                    if (lane == 0) cr_bar_expect(FULL(stage), bytes);
-                    __syncwarp();
-                    if (on)
-                        cr_tma_load(ring + stage * cfg::kTile + ch * (kRowsTile * 128) + ((box << A.box_log2) * 128),
-                                    v ? &map_v : &map_k, FULL(stage), (int)ch * 64, y, (int)w.h, pg);
-                    if (++stage == cfg::kStages) {
-                        stage = 0;
-                        phase ^= 1;
-                    }
-                }
-            }
-            w.done();
-        }
-    } else if (warp == 8) {
-        // ---- products ----
-        if (lane == 0) {
-            const uint32_t id_s = cr_idesc(BF16, 128, 128, false), id_o = cr_idesc(BF16, 128, D, true);
-            uint32_t stage = 0, phase = 0, qphase = 0, pphase[2] = {0, 0}, ophase[2] = {0, 0};
-            auto scores = [&](int x, uint32_t st) {
-                const uint32_t a = sq + x * cfg::kTile, b = ring + st * cfg::kTile;
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    const uint32_t off = (i / 4) * (kRowsTile * 128) + (i % 4) * 32;
-                    cr_mma_ss(tmem + x * 128, cr_sdesc(a + off, 16, 1024), cr_sdesc(b + off, 16, 1024), id_s, i > 0);
-                }
-            };
-            auto values = [&](int x, uint32_t st, bool first) {
-                const uint32_t b = ring + st * cfg::kTile;
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    cr_mma_ts(tmem + 256 + x * D, tmem + x * 128 + i * 8,
-                              cr_sdesc(b + i * 2048, kRowsTile * 128, 1024), id_o, !(first && i == 0));
-            };
-            while (w.next()) {
-                const int two = w.k.ntok > (int)A.tq;
-                const uint32_t n = w.t1 - w.t0;
-                if (!cr_bar_wait(BAR(B_QFULL), qphase, &gave_up)) goto out;
-                qphase ^= 1;
-                if (!cr_bar_wait(FULL(stage), phase, &gave_up)) goto out;
-                cr_tc_after();
-                for (int x = 0; x <= two; ++x) {
-                    scores(x, stage);
-                    cr_tc_commit(BAR(B_SFULL + x));
-                }
-                cr_tc_commit(EMPTY(stage));
-                if (n == 1) cr_tc_commit(BAR(B_QEMPTY));
+                const uint32_t bytes =
+                    (__popc(__ballot_sync(~0u, on)) + __popc(__ballot_sync(~0u, on_v))) * A.box_rows * 128;
+                if (!cr_bar_wait(EMPTY(stage), phase ^ 1, &gave_up)) goto out;
+                if (lane == 0) cr_bar_expect(FULL(stage), bytes);
+                __syncwarp();
+                const uint32_t dst = ring + stage * 2 * cfg::kTile + at;
+                if (on_v) cr_tma_load(dst, &map_v, FULL(stage), (int)ch * 64, y_v, (int)w.h, pg_v);
+                if (on) cr_tma_load(dst + cfg::kTile, &map_k, FULL(stage), (int)ch * 64, y, (int)w.h, pg);
+                on_v = on;
+                y_v = y;
+                pg_v = pg;
                 if (++stage == cfg::kStages) {
                     stage = 0;
                     phase ^= 1;
                 }
-                for (uint32_t j = 0; j < n; ++j) {
-                    const uint32_t vs = stage;
-                    if (!cr_bar_wait(FULL(vs), phase, &gave_up)) goto out;
-                    if (++stage == cfg::kStages) {
-                        stage = 0;
-                        phase ^= 1;
-                    }
-                    const uint32_t ks = stage;
-                    const bool more = j + 1 < n;
-                    if (more) {
-                        if (!cr_bar_wait(FULL(ks), phase, &gave_up)) goto out;
-                        if (++stage == cfg::kStages) {
-                            stage = 0;
-                            phase ^= 1;
-                        }
-                    }
-                    for (int x = 0; x <= two; ++x) {
-                        if (j == 0) {
-                            if (!cr_bar_wait(BAR(B_OEMPTY + x), ophase[x] ^ 1, &gave_up)) goto out;
-                            ophase[x] ^= 1;
-                        }
-                        if (!cr_bar_wait(BAR(B_PREADY + x), pphase[x], &gave_up)) goto out;
-                        pphase[x] ^= 1;
-                        cr_tc_after();
-                        values(x, vs, j == 0);
-                        if (more) {
-                            scores(x, ks);
-                            cr_tc_commit(BAR(B_SFULL + x));
-                        } else {
-                            cr_tc_commit(BAR(B_OFULL + x));
-                        }
-                    }
-                    cr_tc_commit(EMPTY(vs));
-                    if (more) {
-                        cr_tc_commit(EMPTY(ks));
-                        if (j + 2 == n) cr_tc_commit(BAR(B_QEMPTY));
-                    }
-                }
-                w.done();
             }
-            cr_tc_commit(BAR(B_DONE));  // the shared memory is in use until the last product has ended
-            cr_bar_wait(BAR(B_DONE), 0, &gave_up);
         }
-    } else if (warp < 8) {
-        // ---- softmax: a thread owns a row ----
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-        const int x = (int)(warp >> 2);
-        const uint32_t row = threadIdx.x & 127;
-        const uint32_t lanes = (warp & 3) << 21;  // this warp's lanes of tensor memory
-        const uint32_t ts = tmem + x * 128 + lanes, to = tmem + 256 + x * D + lanes;
-        const int tok = (int)(row / A.G), g = (int)(row % A.G);
+    } else if (warp == 16) {
+        // ---- products ----
+        const uint32_t me = cr_elect();
+        const uint32_t id_s = cr_idesc(BF16, 128, 128, false), id_o = cr_idesc(BF16, 128, D, true);
+        uint32_t stage = 0, phase = 0, pphase[2] = {0, 0}, ophase[2] = {0, 0};
+        auto scores = [&](int x, uint32_t st) {
+            const uint32_t a = sq + x * cfg::kTile, b = ring + st * 2 * cfg::kTile + cfg::kTile;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                const uint32_t off = (i / 4) * (kRowsTile * 128) + (i % 4) * 32;
+                cr_mma_ss(tmem + x * 128, cr_sdesc(a + off, 16, 1024), cr_sdesc(b + off, 16, 1024), id_s, i > 0, me);
+            }
+        };
+        // 16 keys a step: of each thread's 64 keys the first half (part 0), then the second
+        auto values = [&](int x, uint32_t st, int part, bool first) {
+            const uint32_t b = ring + st * 2 * cfg::kTile;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = (e >> 1) * 4 + part * 2 + (e & 1);
+                cr_mma_ts(tmem + 256 + x * D, tmem + x * 128 + (e >> 1) * 64 + (part * 2 + (e & 1)) * 8,
+                          cr_sdesc(b + i * 2048, kRowsTile * 128, 1024), id_o, !(first && part == 0 && e == 0), me);
+            }
+        };
+        auto forward = [&]() {
+            if (++stage == cfg::kStages) {
+                stage = 0;
+                phase ^= 1;
+            }
+        };
+        // weights x values of a tile, then the next scores
+        auto turn = [&](int x, bool first, bool more) {
+            if (first) {
+                if (!cr_bar_wait(BAR(B_OEMPTY + x), ophase[x] ^ 1, &gave_up)) return false;
+                ophase[x] ^= 1;
+            }
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                if (!cr_bar_wait(BAR(B_PREADY + 2 * x + part), pphase[x], &gave_up)) return false;
+                cr_tc_after();
+                values(x, stage, part, first);
+            }
+            pphase[x] ^= 1;
+            if (more) {
+                scores(x, stage);
+                cr_tc_commit(BAR(B_SFULL + x), me);
+            } else {
+                cr_tc_commit(BAR(B_OFULL + x), me);
+            }
+            return true;
+        };
+        for (;; ++pieces) {
+            if (!cr_bar_wait(BAR(B_PFULL + (pieces & 1)), (pieces >> 1) & 1, &gave_up)) goto out;
+            const volatile rows_piece *p = piece + (pieces & 1);
+            const uint32_t n = __shfl_sync(~0u, p->n, 0);
+            const bool two = __shfl_sync(~0u, p->ntok, 0) > (int)A.tq;
+            if (lane == 0) cr_bar_arrive(BAR(B_PEMPTY + (pieces & 1)));
+            if (n == 0) break;
+            if (!cr_bar_wait(BAR(B_QFULL), pieces & 1, &gave_up)) goto out;
+            if (!cr_bar_wait(FULL(stage), phase, &gave_up)) goto out;
+            cr_tc_after();
+            scores(0, stage);
+            cr_tc_commit(BAR(B_SFULL), me);
+            if (two) {
+                scores(1, stage);
+                cr_tc_commit(BAR(B_SFULL + 1), me);
+            }
+            cr_tc_commit(EMPTY(stage), me);
+            if (n == 1) cr_tc_commit(BAR(B_QEMPTY), me);
+            forward();
+            for (uint32_t j = 0; j < n; ++j) {
+                const bool more = j + 1 < n;
+                if (!cr_bar_wait(FULL(stage), phase, &gave_up)) goto out;
+                if (!turn(0, j == 0, more)) goto out;
+                if (two && !turn(1, j == 0, more)) goto out;
+                cr_tc_commit(EMPTY(stage), me);
+                if (j + 2 == n) cr_tc_commit(BAR(B_QEMPTY), me);
+                forward();
+            }
+        }
+        cr_tc_commit(BAR(B_DONE), me);  // the shared memory is in use until the last product has ended
+        cr_bar_wait(BAR(B_DONE), 0, &gave_up);
+    } else if (warp == 18) {
+        // ---- copies of outputs ----
+        uint32_t done[2] = {0, 0};
+        for (;; ++pieces) {
+            if (!cr_bar_wait(BAR(B_PFULL + (pieces & 1)), (pieces >> 1) & 1, &gave_up)) goto out;
+            const volatile rows_piece *p = piece + (pieces & 1);
+            const int n = p->n, whole = p->whole, h = p->h, row0 = p->row0;
+            __syncwarp();
+            if (lane == 0) cr_bar_arrive(BAR(B_PEMPTY + (pieces & 1)));
+            if (n == 0) break;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                if (!(whole >> x & 1)) continue;
+                if (!cr_bar_wait(BAR(B_OUT + x), done[x] & 1, &gave_up)) goto out;
+                ++done[x];
+                if (lane == 0) {
+                    for (int ch = 0; ch < cfg::kChunks; ++ch)
+                        cr_tma_store(&map_o, sq + cfg::kOut + ch * (kRowsTile * 128), ch * 64, 0, h, row0 + x * (int)A.tq);
+                    cr_tma_store_read();
+                    cr_bar_arrive(BAR(B_OUTFREE));
+                }
+                __syncwarp();
+            }
+        }
+        if (lane == 0) cr_tma_store_done();
+    } else if (warp < 16) {
+        // ---- softmax: two threads a row ----
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+        const int x = (int)(warp >> 3), half = (int)(warp >> 2) & 1;
+        const uint32_t row = (warp & 3) * 32 + lane;
+        // this warp's lanes of tensor memory, its scores (and weights), its columns of the accumulator
+        const uint32_t ts = tmem + ((warp & 3) << 21) + x * 128 + half * 64;
+        const uint32_t to = tmem + ((warp & 3) << 21) + 256 + x * D + half * (D / 2);
+        const uint32_t pair = 1 + x * 4 + (warp & 3);  // barrier of the two warps that share rows
         const float c = A.c;
         const unsigned long long c2 = cr_pair(c, c);
-        uint32_t sphase = 0, ophase = 0, stage = 0, phase = 0;  // stage, phase: of the piece's first key tile
-        while (w.next()) {
-            const int two = w.k.ntok > (int)A.tq;
-            const uint32_t n = w.t1 - w.t0;
-            if (x <= two) {
-                const int mine = x * (int)A.tq + tok;  // token of the block
-                const bool valid = row < A.G * A.tq && mine < w.k.ntok;
-                int lim = w.k.klen;  // keys that this row sees
-                if (A.causal) lim = min(lim, w.k.diag + mine + 1);
-                float m = -INFINITY, l = 0.f;
-                for (uint32_t j = 0; j < n; ++j) {
-                    const int k0 = (int)(w.t0 + j) * kRowsTile;
-                    if (!cr_bar_wait(BAR(B_SFULL + x), sphase, &gave_up)) goto out;
-                    sphase ^= 1;
-                    cr_tc_after();
-                    uint32_t s[128];
+        uint32_t sphase = 0;
+        // The other half's value of this row.  The next value is written only after the other warp has read this
+        // one: the next scores come after both warps' weights, and a piece ends with another meeting.
+        auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(pair) : "memory"); };
+        auto exchange = [&](float v) {
+            xch[x * 2 + half][row] = v;
+            meet();
+            return xch[x * 2 + (half ^ 1)][row];
+        };
+        for (uint32_t ophase = 0;; ++pieces) {
+            if (!cr_bar_wait(BAR(B_PFULL + (pieces & 1)), (pieces >> 1) & 1, &gave_up)) goto left;
+            const volatile rows_piece *p = piece + (pieces & 1);
+            const int n = p->n;
+            if (n == 0) break;
+            if (x == 1 && p->ntok <= (int)A.tq) {
+                __syncwarp();
+                if (lane == 0) cr_bar_arrive(BAR(B_PEMPTY + (pieces & 1)));
+                continue;
+            }
+            // keys that this row sees, from the first tile's on; the tile with the sequence's end
+            int seen = p->klen - p->t0 * kRowsTile - half * 64;
+            const int tail = x == 0 && half < cfg::kChunks ? (p->klen >> 7) - p->t0 : -1;
+            if (A.causal) seen = min(seen, p->diag + x * (int)A.tq + (int)(row / A.G) + 1 - p->t0 * kRowsTile - half * 64);
+            float m = -INFINITY, l = 0.f;
+            for (int j = 0; j < n; ++j, seen -= kRowsTile) {
+                if (!cr_bar_wait(BAR(B_SFULL + x), sphase, &gave_up)) goto left;
+                sphase ^= 1;
+                cr_tc_after();
+                uint32_t s[64];
+                cr_tmem_ld(ts, s);
+                cr_tmem_ld(ts + 32, s + 32);
+                cr_tmem_ld_wait();
+                if (__any_sync(~0u, seen < 64)) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) cr_tmem_ld(ts + 32 * i, s + 32 * i);
-                    cr_tmem_ld_wait();
-                    const int seen = lim - k0;
-                    if (__any_sync(~0u, seen < kRowsTile)) {
+                    for (int i = 0; i < 64; ++i) s[i] = i < seen ? s[i] : 0xff800000u;
+                }
+                float mx[4];
 #pragma unroll
-                        for (int i = 0; i < 128; ++i) s[i] = i < seen ? s[i] : 0xff800000u;
-                    }
-                    float mx[4];
+                for (int i = 0; i < 4; ++i) {
+                    mx[i] = __uint_as_float(s[i]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        mx[i] = __uint_as_float(s[i]);
-#pragma unroll
-                        for (int e = 4; e < 124; e += 8)
-                            mx[i] = cr_max3(mx[i], __uint_as_float(s[e + i]), __uint_as_float(s[e + 4 + i]));
-                        mx[i] = fmaxf(mx[i], __uint_as_float(s[124 + i]));
-                    }
-                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-                    // The maximum may lag by 2^8: weights stay below 2^8, sums below 2^31, and the
-                    // accumulator is scaled a few times per row instead of at every tile.
-                    const bool grow = j == 0 || !((top - m) * c <= 8.f || top == m);
-                    if (__any_sync(~0u, grow)) {
-                        const float m_new = fmaxf(m, top);
-                        if (j > 0) {
-                            const float f = m_new == m ? 1.f : cr_exp2((m - m_new) * c);
-                            l *= f;
+                    for (int e = 4; e < 60; e += 8)
+                        mx[i] = cr_max3(mx[i], __uint_as_float(s[e + i]), __uint_as_float(s[e + 4 + i]));
+                    mx[i] = fmaxf(mx[i], __uint_as_float(s[60 + i]));
+                }
+                float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                top = fmaxf(top, exchange(top));
+                // The maximum may lag by 2^8: weights stay below 2^8, sums below 2^31, and the
+                // accumulator is scaled a few times per row instead of at every tile.
+                const bool grow = j == 0 || !((top - m) * c <= 8.f || top == m);
+                if (__any_sync(~0u, grow)) {
+                    const float m_new = fmaxf(m, top);
+                    if (j > 0) {
+                        const float f = m_new == m ? 1.f : cr_exp2((m - m_new) * c);
+                        l *= f;
 #pragma unroll 1
-                            for (int i = 0; i < D / 32; ++i) {
-                                uint32_t o[32];
-                                cr_tmem_ld(to + 32 * i, o);
-                                cr_tmem_ld_wait();
+                        for (int i = 0; i < D / 2; i += 16) {
+                            uint32_t o[16];
+                            cr_tmem_ld16(to + i, o);
+                            cr_tmem_ld_wait();
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                                cr_tmem_st(to + 32 * i, o);
-                            }
-                            cr_tmem_st_wait();
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            cr_tmem_st16(to + i, o);
                         }
-                        m = m_new;
+                        cr_tmem_st_wait();
                     }
-                    const float off = m == -INFINITY ? 0.f : -m * c;
-                    const unsigned long long off2 = cr_pair(off, off);
-                    unsigned long long sum[2] = {0ull, 0ull};
+                    m = m_new;
+                }
+                // keys behind the sequence's end have weight zero, but what stands there may be
+                // no number: their rows of v become zeros
+                if (j == tail) {
+                    const uint32_t at = (uint32_t)p->stage + j + 1;
+                    const uint32_t st = at % cfg::kStages, ph = (uint32_t)p->phase ^ ((at / cfg::kStages) & 1);
+                    if (!cr_bar_wait(FULL(st), ph, &gave_up)) goto left;
+                    if ((int)row >= (p->klen & (kRowsTile - 1))) {
 #pragma unroll
-                    for (int i = 0; i < 128; i += 64) {
-                        uint32_t p[32];
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            float a, b;
-                            cr_unpair(cr_fma2(cr_pair(__uint_as_float(s[i + 2 * e]), __uint_as_float(s[i + 2 * e + 1])), c2,
-                                              off2),
-                                      a, b);
-                            a = cr_exp2(a);
-                            b = cr_exp2(b);
-                            sum[e & 1] = cr_add2(sum[e & 1], cr_pair(a, b));
-                            p[e] = cr_pack16<BF16>(a, b);
-                        }
-                        cr_tmem_st(ts + i / 2, p);
+                        for (int i = 0; i < 8; ++i)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(
+                                             ring + st * 2 * cfg::kTile + half * (kRowsTile * 128) + row * 128 + i * 16),
+                                         "r"(0)
+                                         : "memory");
                     }
-                    float s0, s1;
-                    cr_unpair(cr_add2(sum[0], sum[1]), s0, s1);
-                    l += s0 + s1;
-                    // keys behind the sequence's end have weight zero, but what stands there may be
-                    // no number: their rows of v become zeros
-                    if (x == 0 && k0 + kRowsTile > w.k.klen) {
-                        const uint32_t at = stage + 2 * j + 1;
-                        const uint32_t st = at % cfg::kStages, ph = phase ^ ((at / cfg::kStages) & 1);
-                        if (!cr_bar_wait(FULL(st), ph, &gave_up)) goto out;
-                        if (k0 + (int)row >= w.k.klen) {
+                    cr_fence_async_smem();
+                }
+                const float off = m == -INFINITY ? 0.f : -m * c;
+                const unsigned long long off2 = cr_pair(off, off);
+                unsigned long long sum[2] = {0ull, 0ull};
 #pragma unroll
-                            for (int i = 0; i < D / 8; ++i)
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(
-                                                 ring + st * cfg::kTile + (i / 8) * (kRowsTile * 128) + row * 128 + (i % 8) * 16),
-                                             "r"(0)
-                                             : "memory");
-                        }
-                        cr_fence_async_smem();
+                for (int part = 0; part < 2; ++part) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int i = part * 32 + 2 * e;
+                        float a, b;
+                        cr_unpair(cr_fma2(cr_pair(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), c2, off2), a, b);
+                        a = cr_exp2(a);
+                        b = cr_exp2(b);
+                        sum[e & 1] = cr_add2(sum[e & 1], cr_pair(a, b));
+                        w[e] = cr_pack16<BF16>(a, b);
                     }
+                    cr_tmem_st16(ts + part * 16, w);
                     cr_tmem_st_wait();
                     cr_tc_before();
                     __syncwarp();
-                    if (lane == 0) cr_bar_arrive(BAR(B_PREADY + x));
+                    if (lane == 0) cr_bar_arrive(BAR(B_PREADY + 2 * x + part));
                 }
-                // ---- the piece's result ----
-                if (!cr_bar_wait(BAR(B_OFULL + x), ophase, &gave_up)) goto out;
-                ophase ^= 1;
-                cr_tc_after();
-                const int slot = w.slot();
-                const int head = (int)(w.h * A.G) + g;
-                const uint64_t tk = (uint64_t)(w.k.row0 + mine);
-                if (slot >= 0) {
-                    const uint64_t at = (uint64_t)(2 * slot + x);
-                    float4 *dst = reinterpret_cast<float4 *>(A.part) + at * (D / 4) * kRowsTile + row;
+                float s0, s1;
+                cr_unpair(cr_add2(sum[0], sum[1]), s0, s1);
+                l += s0 + s1;
+            }
+            // ---- the piece's result ----
+            if (!cr_bar_wait(BAR(B_OFULL + x), ophase, &gave_up)) goto left;
+            ophase ^= 1;
+            cr_tc_after();
+            const float l2 = exchange(l);
+            meet();
+            l = half ? l2 + l : l + l2;
+            const int mine = x * (int)A.tq + (int)(row / A.G);  // token of the block
+            const bool valid = row < A.G * A.tq && mine < p->ntok;
+            const int slot = p->slot;
+            const int head = p->h * (int)A.G + (int)(row % A.G);
+            const uint64_t tk = (uint64_t)(p->row0 + mine);
+            if (slot >= 0) {
+                constexpr int RP = 2 * kRowsTile;  // rows of a piece
+                const uint32_t r = x * kRowsTile + row;
+                float4 *dst = reinterpret_cast<float4 *>(A.part) + ((uint64_t)slot * (D / 4) + half * (D / 8)) * RP + r;
 #pragma unroll 1
-                    for (int i = 0; i < D / 32; ++i) {
-                        uint32_t o[32];
-                        cr_tmem_ld(to + 32 * i, o);
-                        cr_tmem_ld_wait();
+                for (int i = 0; i < D / 2; i += 16) {
+                    uint32_t o[16];
+                    cr_tmem_ld16(to + i, o);
+                    cr_tmem_ld_wait();
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        dst[(i / 4 + e) * RP] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]),
+                                                            __uint_as_float(o[4 * e + 2]), __uint_as_float(o[4 * e + 3]));
+                }
+                if (half == 0)
+                    reinterpret_cast<float2 *>(A.part_ml)[(uint64_t)slot * RP + r] =
+                        make_float2(m == -INFINITY ? m : m * c, l);
+            } else {
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                const bool copied = p->whole >> x & 1;
+                if (copied) {  // the last tile that was copied has been read
+                    const int use = p->outs + (x && (p->whole & 1));
+                    if (!cr_bar_wait(BAR(B_OUTFREE), (use & 1) ^ 1, &gave_up)) goto left;
+                }
+#pragma unroll 1
+                for (int i = 0; i < D / 2; i += 16) {
+                    uint32_t o[16];
+                    cr_tmem_ld16(to + i, o);
+                    cr_tmem_ld_wait();
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[e] = l == 0.f ? 0u : __float_as_uint(__uint_as_float(o[e]) * inv);
+                    const int d0 = half * (D / 2) + i;
+                    if (copied) {
+                        const uint32_t at = sq + cfg::kOut + (d0 / 64) * (kRowsTile * 128) + row * 128;
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t u = (uint32_t)(d0 % 64) / 8 + e;
+                            const uint32_t *f = o + 8 * e;
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + ((u ^ (row & 7)) << 4)),
+                                         "r"(cr_pack16<BF16>(__uint_as_float(f[0]), __uint_as_float(f[1]))),
+                                         "r"(cr_pack16<BF16>(__uint_as_float(f[2]), __uint_as_float(f[3]))),
+                                         "r"(cr_pack16<BF16>(__uint_as_float(f[4]), __uint_as_float(f[5]))),
+                                         "r"(cr_pack16<BF16>(__uint_as_float(f[6]), __uint_as_float(f[7])))
+                                         : "memory");
+                        }
+                        continue;
+                    }
+                    if (!valid) continue;
+                    if (A.to_pfx) {
+                        float *dst = A.pfx + (tk * A.q_heads + head) * D + d0;
+                        cr_store32(dst, o);
+                        cr_store32(dst + 8, o + 8);
+                    } else {
+                        uint16_t *dst = static_cast<uint16_t *>(A.o) + tk * A.o_token + head * A.o_head + d0;
+                        uint32_t v[8];
 #pragma unroll
                         for (int e = 0; e < 8; ++e)
-                            dst[(i * 8 + e) * kRowsTile] =
-                                make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]),
-                                            __uint_as_float(o[4 * e + 2]), __uint_as_float(o[4 * e + 3]));
-                    }
-                    reinterpret_cast<float2 *>(A.part_ml)[at * kRowsTile + row] =
-                        make_float2(m == -INFINITY ? m : m * c, l);
-                } else {
-                    const float inv = l == 0.f ? 0.f : 1.f / l;
-                    const float lse2 = l == 0.f ? -INFINITY : m * c + log2f(l);
-#pragma unroll 1
-                    for (int i = 0; i < D / 32; ++i) {
-                        uint32_t o[32];
-                        cr_tmem_ld(to + 32 * i, o);
-                        cr_tmem_ld_wait();
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            o[e] = l == 0.f ? 0u : __float_as_uint(__uint_as_float(o[e]) * inv);
-                        if (!valid) continue;
-                        if (A.to_pfx) {
-                            float *dst = A.pfx + (tk * A.q_heads + head) * D + 32 * i;
-#pragma unroll
-                            for (int e = 0; e < 32; e += 4)
-                                *reinterpret_cast<uint4 *>(dst + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                            v[e] = cr_pack16<BF16>(__uint_as_float(o[2 * e]), __uint_as_float(o[2 * e + 1]));
+                        if (A.o_wide && d0 + 16 <= (int)A.head_dim) {
+                            cr_store32(dst, v);
                         } else {
-                            uint16_t *dst = static_cast<uint16_t *>(A.o) + tk * A.o_token + head * A.o_head + 32 * i;
-#pragma unroll
-                            for (int e = 0; e < 32; e += 8)
-                                if (32 * i + e < (int)A.head_dim) {
-                                    uint4 v;
-                                    v.x = cr_pack16<BF16>(__uint_as_float(o[e]), __uint_as_float(o[e + 1]));
-                                    v.y = cr_pack16<BF16>(__uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
-                                    v.z = cr_pack16<BF16>(__uint_as_float(o[e + 4]), __uint_as_float(o[e + 5]));
-                                    v.w = cr_pack16<BF16>(__uint_as_float(o[e + 6]), __uint_as_float(o[e + 7]));
-                                    *reinterpret_cast<uint4 *>(dst + e) = v;
-                                }
+                            if (d0 < (int)A.head_dim) *reinterpret_cast<uint4 *>(dst) = make_uint4(v[0], v[1], v[2], v[3]);
+                            if (d0 + 8 < (int)A.head_dim)
+                                *reinterpret_cast<uint4 *>(dst + 8) = make_uint4(v[4], v[5], v[6], v[7]);
                         }
                     }
-                    if (valid) {
-                        if (A.to_pfx)
-                            A.pfx_lse[tk * A.q_heads + head] = lse2;
-                        else if (A.lse)
-                            A.lse[tk * A.q_heads + head] = lse2 * 0.693147180559945309f;
-                    }
                 }
-                cr_tc_before();
-                __syncwarp();
-                if (lane == 0) cr_bar_arrive(BAR(B_OEMPTY + x));
+                if (valid && half == 0) {
+                    const float lse2 = l == 0.f ? -INFINITY : m * c + log2f(l);
+                    if (A.to_pfx)
+                        A.pfx_lse[tk * A.q_heads + head] = lse2;
+                    else if (A.lse)
+                        A.lse[tk * A.q_heads + head] = lse2 * 0.693147180559945309f;
+                }
+                if (copied) {
+                    cr_fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) cr_bar_arrive(BAR(B_OUT + x));
+                }
             }
-            stage += 2 * n;
-            phase ^= (stage / cfg::kStages) & 1;
-            stage %= cfg::kStages;
-            w.done();
+            cr_tc_before();
+            __syncwarp();
+            if (lane == 0) {
+                cr_bar_arrive(BAR(B_OEMPTY + x));
+                cr_bar_arrive(BAR(B_PEMPTY + (pieces & 1)));
+            }
         }
+    left:
+        // a wait that has given up: the other warp of the pair must not wait for this one
+        if (gave_up) asm volatile("bar.arrive %0, 64;" ::"r"(pair) : "memory");
     }
 out:
     __syncwarp();
@@ -755,7 +889,8 @@ out:
     }
     cr_tc_before();
     __syncthreads();
-    if (warp == 8) {
+    asm volatile("griddepcontrol.launch_dependents;");
+    if (warp == 16) {
         cr_tc_after();
         cr_tmem_free(tmem, 512);
     }
@@ -764,69 +899,117 @@ out:
 #undef BAR
 }
 
-// First stretch that begins inside a block: true for the CTA that joins the block's pieces.
-__device__ __forceinline__ bool join_here(const attn_in &A, uint32_t c, attn_start &s, unsigned long long &begin,
-                                          unsigned long long &end)
+// Joins the pieces of blocks that several CTAs worked on: blockIdx.x + 1 is the first stretch that begins
+// inside the block, blockIdx.y a share of its rows.  Pieces lie in scratch as [D / 4][rows][4] with (m, l) per
+// row; a thread joins four columns of a row, the pieces' weights are in shared memory, 32 pieces at a time.
+// RP rows of a piece, RW of them here.
+template <int D, bool BF16, int RP, int RW>
+__global__ void __launch_bounds__(256) k_attn_join(const __grid_constant__ attn_in A)
 {
-    if (c == 0 || c >= A.plan->ncta) return false;
-    s = A.start[c];
-    if (s.pos >= A.plan->N || s.tile == 0) return false;
-    begin = s.pos - s.tile;
-    end = begin + (A.cum[s.blk + 1] - A.cum[s.blk]);
-    return A.start[c - 1].pos <= begin;
-}
-
-// Joins the pieces of blocks that several CTAs worked on: blockIdx.x + 1 is the stretch that begins
-// inside the block, blockIdx.y 32 of its rows.  A thread joins four columns of one row at a time.
-template <int D, bool BF16>
-__global__ void __launch_bounds__(256) k_attn_rows_join(const __grid_constant__ attn_in A)
-{
+    constexpr int kGroups = 256 / RW, kPer = D / 4 / kGroups;  // threads of a row, columns / 4 of each
+    __shared__ float wgt[32][RW];
+    __shared__ float red[2][kGroups][RW];
+    __shared__ uint32_t ends;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t c = blockIdx.x + 1;
-    attn_start s;
-    unsigned long long begin, end;
-    if (!join_here(A, c, s, begin, end)) return;
-    const attn_blk k = A.blk[s.blk];
-    const uint32_t x = blockIdx.y >> 2, row = (blockIdx.y & 3) * 32 + (threadIdx.x & 31);
-    const int tok = (int)(x * A.tq + row / A.G);
-    if (row >= A.G * A.tq || tok >= k.ntok) return;
+    const attn_start s = A.start[c];
+    if (s.pos >= s.N || s.tile == 0) return;
+    const unsigned long long begin = s.pos - s.tile - kExtra, end = begin + kExtra + (uint32_t)s.k.nt;
+    if (A.start[c - 1].pos > begin) return;
+    // row of the piece
+    const uint32_t r = blockIdx.y * RW + threadIdx.x % RW, grp = threadIdx.x / RW;
+    bool valid;
+    uint32_t head;
+    uint64_t tk;
+    if (RP == 16) {
+        head = s.head / A.nsub * A.G + s.head % A.nsub * 16 + r;
+        valid = s.head % A.nsub * 16 + r < A.G;
+        tk = (uint64_t)s.k.row0;
+    } else {
+        const uint32_t x = r / kRowsTile, rr = r % kRowsTile;
+        const uint32_t tok = x * A.tq + rr / A.G;
+        valid = rr < A.G * A.tq && (int)tok < s.k.ntok;
+        head = s.head * A.G + rr % A.G;
+        tk = (uint64_t)s.k.row0 + tok;
+    }
+    // its pieces: stretches c-1 .. last
+    if (threadIdx.x < 32) {
+        uint32_t last = c;
+        for (uint32_t p0 = c;; p0 += 32) {
+            const uint32_t p = p0 + threadIdx.x;
+            const bool in = p < gridDim.x + 1 && A.start[p].pos < end;
+            const uint32_t b = __ballot_sync(~0u, in);
+            last = p0 + __popc(b);
+            if (b != ~0u) break;
+        }
+        if (threadIdx.x == 0) ends = last;
+    }
+    __syncthreads();
+    const uint32_t np = ends - (c - 1);
+    if (blockIdx.y * RW / kRowsTile && !__syncthreads_or(valid)) return;  // the second tile is not in use
     const float2 *ml = reinterpret_cast<const float2 *>(A.part_ml);
     const float4 *part = reinterpret_cast<const float4 *>(A.part);
+    auto place = [&](uint32_t i) { return (uint64_t)(i == 0 ? 2 * c - 1 : 2 * (c - 1 + i)); };
+    auto is_empty = [&](uint32_t i) { return i && A.start[c - 1 + i].pos == A.start[c + i].pos; };
     float m = -INFINITY;
-    for (uint32_t p = c - 1; A.start[p].pos < end; ++p) {
-        if (A.start[p].pos == A.start[p + 1].pos) continue;
-        const uint64_t at = 2ull * (p == c - 1 ? 2 * p + 1 : 2 * p) + x;
-        m = fmaxf(m, ml[at * kRowsTile + row].x);
-    }
-    const int head = (int)(s.head * A.G + row % A.G);
-    const uint64_t tk = (uint64_t)(k.row0 + tok);
-    for (uint32_t d4 = threadIdx.x >> 5; d4 < D / 4; d4 += 8) {
-        float l = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (uint32_t p = c - 1; A.start[p].pos < end; ++p) {
-            if (A.start[p].pos == A.start[p + 1].pos) continue;
-            const uint64_t at = 2ull * (p == c - 1 ? 2 * p + 1 : 2 * p) + x;
-            const float2 q = ml[at * kRowsTile + row];
-            if (q.x == -INFINITY) continue;  // sees none of these keys
-            const float f = cr_exp2(q.x - m);
-            const float4 v = part[(at * (D / 4) + d4) * kRowsTile + row];
+    for (uint32_t i = grp; i < np; i += kGroups)
+        if (!is_empty(i)) m = fmaxf(m, ml[place(i) * RP + r].x);
+    red[0][grp][threadIdx.x % RW] = m;
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < kGroups; ++e) m = fmaxf(m, red[0][e][threadIdx.x % RW]);
+    float l = 0.f;
+    float4 o[kPer];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) o[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (uint32_t i0 = 0; i0 < np; i0 += 32) {
+        const uint32_t ni = min(32u, np - i0);
+        __syncthreads();
+        for (uint32_t i = grp; i < ni; i += kGroups) {
+            float2 q = make_float2(-INFINITY, 0.f);
+            if (!is_empty(i0 + i)) q = ml[place(i0 + i) * RP + r];
+            const float f = q.x == -INFINITY ? 0.f : cr_exp2(q.x - m);
+            wgt[i][threadIdx.x % RW] = f;
             l += q.y * f;
-            o.x += v.x * f;
-            o.y += v.y * f;
-            o.z += v.z * f;
-            o.w += v.w * f;
         }
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-        const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
-        if (A.to_pfx) {
-            *reinterpret_cast<float4 *>(A.pfx + (tk * A.q_heads + head) * D + 4 * d4) = o;
-            if (d4 == 0) A.pfx_lse[tk * A.q_heads + head] = lse2;
-        } else {
-            if (4 * d4 < A.head_dim)
-                *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(A.o) + tk * A.o_token + head * A.o_head + 4 * d4) =
-                    make_uint2(cr_pack16<BF16>(o.x, o.y), cr_pack16<BF16>(o.z, o.w));
-            if (d4 == 0 && A.lse) A.lse[tk * A.q_heads + head] = lse2 * 0.693147180559945309f;
+        __syncthreads();
+#pragma unroll 4
+        for (uint32_t i = 0; i < ni; ++i) {
+            const float f = wgt[i][threadIdx.x % RW];
+            if (f == 0.f) continue;  // sees none of these keys, or no piece
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                const float4 v = part[(place(i0 + i) * (D / 4) + grp + e * kGroups) * RP + r];
+                o[e].x += v.x * f;
+                o[e].y += v.y * f;
+                o[e].z += v.z * f;
+                o[e].w += v.w * f;
+            }
         }
+    }
+    red[1][grp][threadIdx.x % RW] = l;
+    __syncthreads();
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < kGroups; ++e) l += red[1][e][threadIdx.x % RW];
+    if (!valid) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        const uint32_t d = 4 * (grp + e * kGroups);
+        const float4 v = make_float4(o[e].x * inv, o[e].y * inv, o[e].z * inv, o[e].w * inv);
+        if (A.to_pfx)
+            *reinterpret_cast<float4 *>(A.pfx + (tk * A.q_heads + head) * D + d) = v;
+        else if (d < A.head_dim)
+            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(A.o) + tk * A.o_token + head * A.o_head + d) =
+                make_uint2(cr_pack16<BF16>(v.x, v.y), cr_pack16<BF16>(v.z, v.w));
+    }
+    if (grp == 0) {
+        if (A.to_pfx)
+            A.pfx_lse[tk * A.q_heads + head] = lse2;
+        else if (A.lse)
+            A.lse[tk * A.q_heads + head] = lse2 * 0.693147180559945309f;
     }
 }
 
@@ -834,14 +1017,15 @@ __global__ void __launch_bounds__(256) k_attn_rows_join(const __grid_constant__ 
 // One token's query heads of a key head, 16 at most.  Here the bytes of k and v are the bound
 // (each is used for a few rows only), so the small register-operand products do: four warps take
 // 16 keys each of a tile of 64 that a fifth warp's copies bring, with the softmax state of the
-// rows in every warp, joined at the piece's end.
-template <int D, bool WIDE>
+// rows in every warp, joined at the piece's end.  The next piece's queries are copied meanwhile.
+template <int D>
 struct few_cfg {
     static constexpr int kChunks = D / 64;
-    static constexpr int kTile = kFewTile * D * 2;  // bytes of 64 keys
+    static constexpr int kTile = kFewTile * D * 2;       // bytes of 64 keys
     static constexpr int kStages = D == 128 ? 3 : 6;
-    static constexpr int kJoin = kFewWarps * 8 * D * 4;  // eight rows of every warp
-    static constexpr int kSmem = kStages * 2 * kTile + kJoin + 1024;
+    static constexpr int kQ = 16 * D * 2;                // bytes of 16 query rows
+    static constexpr int kJoin = kFewWarps * 8 * 64 * 4; // eight rows, 64 columns of every warp
+    static constexpr int kSmem = kStages * 2 * kTile + kQ + kJoin + 1024;
 };
 constexpr int kFewThreads = 32 * (kFewWarps + 1);
 
@@ -876,41 +1060,62 @@ __device__ __forceinline__ void ldsm4(uint32_t *r, uint32_t addr)
 
 template <int D, bool BF16, bool WIDE>
 __global__ void __launch_bounds__(kFewThreads, 2)
-    k_attn_few(const __grid_constant__ attn_in A, const __grid_constant__ CUtensorMap map_k,
-               const __grid_constant__ CUtensorMap map_v)
+    k_attn_few(const __grid_constant__ attn_in A, const __grid_constant__ CUtensorMap map_q,
+               const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
 {
-    using cfg = few_cfg<D, WIDE>;
+    using cfg = few_cfg<D>;
     extern __shared__ unsigned char dyn[];
-    __shared__ __align__(8) unsigned long long bars[2 * cfg::kStages];
+    __shared__ __align__(8) unsigned long long bars[2 * cfg::kStages + 3];
     __shared__ float2 join_ml[kFewWarps][16];
     __shared__ int gave_up;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t base = cr_smem(dyn), ring = (base + 1023u) & ~1023u;
-    float *join = reinterpret_cast<float *>(dyn + (ring - base) + cfg::kStages * 2 * cfg::kTile);
+    const uint32_t base = cr_smem(dyn), ring = (base + 1023u) & ~1023u, sq = ring + cfg::kStages * 2 * cfg::kTile;
+    float *join = reinterpret_cast<float *>(dyn + (sq - base) + cfg::kQ);
     const uint32_t bar = cr_smem(bars);
 #define FULL(s) (bar + 8u * (s))
 #define EMPTY(s) (bar + 8u * (cfg::kStages + (s)))
+#define QFULL (bar + 8u * (2 * cfg::kStages))
+#define QEMPTY (bar + 8u * (2 * cfg::kStages + 1))
+#define JOIN (bar + 8u * (2 * cfg::kStages + 2))
 
-    if (A.start[blockIdx.x].pos >= A.start[blockIdx.x + 1].pos) return;
     if (threadIdx.x == 0) {
         gave_up = 0;
         for (int s = 0; s < cfg::kStages; ++s) {
             cr_bar_init(FULL(s), 1);
             cr_bar_init(EMPTY(s), kFewWarps);
         }
+        cr_bar_init(QFULL, 1);
+        cr_bar_init(QEMPTY, kFewWarps);
+        cr_bar_init(JOIN, kFewWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    for (uint32_t i = threadIdx.x; i < cfg::kQ / 16; i += kFewThreads)  // rows that no copy writes
+        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(sq + 16 * i), "r"(0));
+    cr_fence_async_smem();
     __syncthreads();
+    asm volatile("griddepcontrol.wait;" ::: "memory");
 
     walk w;
-    w.begin(A);
-    uint32_t stage = 0, phase = 0;
+    w.begin(A.start, A.blk);
+    uint32_t stage = 0, phase = 0, qphase = 0;
     if (warp == kFewWarps) {
-        // ---- copies: a lane brings one box of one column block, keys then values ----
+        // ---- copies: a lane brings one box of one column block, keys and values ----
+        if (lane == 0) {
+            cr_tma_prefetch_map(&map_q);
+            cr_tma_prefetch_map(&map_k);
+            cr_tma_prefetch_map(&map_v);
+        }
         const uint32_t boxes = kFewTile >> A.box_log2;
         const uint32_t box = lane & (boxes - 1), ch = lane / boxes;
         while (w.next()) {
             const int kv = (int)(w.h / A.nsub);
+            if (!cr_bar_wait(QEMPTY, qphase ^ 1, &gave_up)) goto out;
+            qphase ^= 1;
+            if (lane == 0) {
+                cr_bar_expect(QFULL, min(16u, A.G) * 128 * cfg::kChunks);
+                for (int c = 0; c < cfg::kChunks; ++c)
+                    cr_tma_load(sq + c * 16 * 128, &map_q, QFULL, c * 64, (int)(w.h % A.nsub) * 16, kv, w.k.row0);
+            }
             for (uint32_t t = w.t0; t < w.t1; ++t) {
                 const int key = (int)((w.k.lo / kFewTile + t) * kFewTile + (box << A.box_log2));
                 const bool on = lane < boxes * cfg::kChunks && key < w.k.klen;
@@ -931,26 +1136,36 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                     phase ^= 1;
                 }
             }
-            w.done();
         }
     } else {
         const uint32_t r4 = lane >> 2, q4 = lane & 3;
         const float c = A.c;
+        uint32_t jphase = 0;
+        auto meet = [&]() {  // of the four warps
+            __syncwarp();
+            if (lane == 0) cr_bar_arrive(JOIN);
+            const bool ok = cr_bar_wait(JOIN, jphase, &gave_up);
+            jphase ^= 1;
+            return ok;
+        };
         while (w.next()) {
-            const uint32_t kv = w.h / A.nsub, sub = w.h % A.nsub;
-            const uint32_t h0 = kv * A.G + sub * 16;                       // first query head of the rows
+            const uint32_t sub = w.h % A.nsub;
+            const uint32_t h0 = w.h / A.nsub * A.G + sub * 16;  // first query head of the rows
             const uint32_t rows = min(16u, A.G - sub * 16);
-            const uint16_t *q = static_cast<const uint16_t *>(A.q) + (uint64_t)w.k.row0 * A.q_token;
             uint32_t qa[D / 16][4];
+            if (!cr_bar_wait(QFULL, qphase, &gave_up)) goto out;
+            qphase ^= 1;
+            {
+                const uint32_t r = lane & 15;
 #pragma unroll
-            for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t r = r4 + (e & 1) * 8, d = i * 16 + q4 * 2 + (e >> 1) * 8;
-                    qa[i][e] = 0;
-                    if ((WIDE || !(e & 1)) && r < rows && d < A.head_dim)
-                        qa[i][e] = *reinterpret_cast<const uint32_t *>(q + (uint64_t)(h0 + r) * A.q_head + d);
+                for (int i = 0; i < D / 16; ++i) {
+                    const uint32_t u = i * 2 + (lane >> 4);
+                    ldsm4<false>(qa[i], sq + (u >> 3) * (16 * 128) + r * 128 + (((u & 7) ^ (r & 7)) << 4));
+                    if (!WIDE) qa[i][1] = qa[i][3] = 0;
                 }
+            }
+            __syncwarp();
+            if (lane == 0) cr_bar_arrive(QEMPTY);
             float o[D / 8][4];
 #pragma unroll
             for (int i = 0; i < D / 8; ++i)
@@ -1029,7 +1244,7 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                     phase ^= 1;
                 }
             }
-            // ---- the four warps' states join, eight rows at a time ----
+            // ---- the four warps' states join: eight rows and 64 columns at a time, four columns a thread ----
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 l[r] += __shfl_xor_sync(~0u, l[r], 1);
@@ -1039,16 +1254,16 @@ __global__ void __launch_bounds__(kFewThreads, 2)
             const int slot = w.slot();
             const bool from_pfx = w.k.lo > 0 && w.t0 == 0;
 #pragma unroll
-            for (int r = 0; r < (WIDE ? 2 : 1); ++r) {
+            for (int pass = 0; pass < (WIDE ? 2 : 1) * cfg::kChunks; ++pass) {
+                const int r = pass / cfg::kChunks, ch = pass % cfg::kChunks;
                 if (rows <= 8u * r) break;
 #pragma unroll
-                for (int i = 0; i < D / 8; ++i)
-                    *reinterpret_cast<float2 *>(join + (warp * 8 + r4) * D + i * 8 + q4 * 2) =
-                        make_float2(o[i][2 * r], o[i][2 * r + 1]);
-                asm volatile("bar.sync 1, 128;" ::: "memory");
-                for (uint32_t e = threadIdx.x; e < 8 * D / 4; e += 128) {
-                    const uint32_t rr = e / (D / 4), d4 = e % (D / 4), row = 8 * r + rr;
-                    if (row >= rows) continue;
+                for (int i = 0; i < 8; ++i)
+                    *reinterpret_cast<float2 *>(join + (warp * 8 + r4) * 64 + i * 8 + q4 * 2) =
+                        make_float2(o[ch * 8 + i][2 * r], o[ch * 8 + i][2 * r + 1]);
+                if (!meet()) goto out;
+                const uint32_t rr = threadIdx.x >> 4, d4 = ch * 16 + (threadIdx.x & 15), row = 8 * r + rr;
+                if (row < rows) {
                     const uint64_t oh = (uint64_t)w.k.row0 * A.q_heads + h0 + row;
                     float mm = -INFINITY, ll = 0.f;
                     for (int v = 0; v < kFewWarps; ++v) mm = fmaxf(mm, join_ml[v][row].x);
@@ -1058,11 +1273,11 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                         mm = fmaxf(mm, px);
                     }
                     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
                     for (int v = 0; v < kFewWarps; ++v) {
                         const float2 ml = join_ml[v][row];
-                        if (ml.x == -INFINITY) continue;
-                        const float f = cr_exp2(ml.x - mm);
-                        const float4 x = *reinterpret_cast<const float4 *>(join + (v * 8 + rr) * D + 4 * d4);
+                        const float f = ml.x == -INFINITY ? 0.f : cr_exp2(ml.x - mm);
+                        const float4 x = *reinterpret_cast<const float4 *>(join + (v * 8 + rr) * 64 + 4 * (threadIdx.x & 15));
                         ll += ml.y * f;
                         s.x += x.x * f;
                         s.y += x.y * f;
@@ -1079,9 +1294,8 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                         s.w += x.w * f;
                     }
                     if (slot >= 0) {
-                        const uint64_t at = (uint64_t)slot * 16 + row;
-                        *reinterpret_cast<float4 *>(A.part + at * D + 4 * d4) = s;
-                        if (d4 == 0) reinterpret_cast<float2 *>(A.part_ml)[at] = make_float2(mm, ll);
+                        reinterpret_cast<float4 *>(A.part)[((uint64_t)slot * (D / 4) + d4) * 16 + row] = s;
+                        if (d4 == 0) reinterpret_cast<float2 *>(A.part_ml)[(uint64_t)slot * 16 + row] = make_float2(mm, ll);
                     } else {
                         const float inv = ll == 0.f ? 0.f : 1.f / ll;
                         if (4 * d4 < A.head_dim)
@@ -1092,9 +1306,8 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                             A.lse[oh] = (ll == 0.f ? -INFINITY : mm + log2f(ll)) * 0.693147180559945309f;
                     }
                 }
-                asm volatile("bar.sync 1, 128;" ::: "memory");
+                if (!meet()) goto out;
             }
-            w.done();
         }
     }
 out:
@@ -1103,50 +1316,12 @@ out:
         if (lane == 0) atomicOr(A.status, CR_FLAG_TIMEOUT);
         for (int i = 0; i < 2000; ++i) __nanosleep(1000);
     }
+    asm volatile("griddepcontrol.launch_dependents;");
 #undef FULL
 #undef EMPTY
-}
-
-// Joins the pieces of blocks that several CTAs of k_attn_few worked on: 16 rows by D columns.
-template <int D, bool BF16>
-__global__ void __launch_bounds__(128) k_attn_few_join(const __grid_constant__ attn_in A)
-{
-    const uint32_t c = blockIdx.x + 1;
-    attn_start s;
-    unsigned long long begin, end;
-    if (!join_here(A, c, s, begin, end)) return;
-    const attn_blk k = A.blk[s.blk];
-    const uint32_t kv = s.head / A.nsub, sub = s.head % A.nsub;
-    const uint32_t h0 = kv * A.G + sub * 16, rows = min(16u, A.G - sub * 16);
-    const float2 *ml = reinterpret_cast<const float2 *>(A.part_ml);
-    for (uint32_t e = threadIdx.x; e < rows * (D / 4); e += 128) {
-        const uint32_t row = e / (D / 4), d4 = e % (D / 4);
-        float m = -INFINITY, l = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (uint32_t p = c - 1; A.start[p].pos < end; ++p)
-            if (A.start[p].pos != A.start[p + 1].pos)
-                m = fmaxf(m, ml[(uint64_t)(p == c - 1 ? 2 * p + 1 : 2 * p) * 16 + row].x);
-        for (uint32_t p = c - 1; A.start[p].pos < end; ++p) {
-            if (A.start[p].pos == A.start[p + 1].pos) continue;
-            const uint64_t at = (uint64_t)(p == c - 1 ? 2 * p + 1 : 2 * p) * 16 + row;
-            const float2 q = ml[at];
-            if (q.x == -INFINITY) continue;
-            const float f = cr_exp2(q.x - m);
-            const float4 v = *reinterpret_cast<const float4 *>(A.part + at * D + 4 * d4);
-            l += q.y * f;
-            o.x += v.x * f;
-            o.y += v.y * f;
-            o.z += v.z * f;
-            o.w += v.w * f;
-        }
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        if (4 * d4 < A.head_dim)
-            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(A.o) + (uint64_t)k.row0 * A.o_token +
-                                       (uint64_t)(h0 + row) * A.o_head + 4 * d4) =
-                make_uint2(cr_pack16<BF16>(o.x * inv, o.y * inv), cr_pack16<BF16>(o.z * inv, o.w * inv));
-        if (d4 == 0 && A.lse)
-            A.lse[(uint64_t)k.row0 * A.q_heads + h0 + row] = (l == 0.f ? -INFINITY : m + log2f(l)) * 0.693147180559945309f;
-    }
+#undef QFULL
+#undef QEMPTY
+#undef JOIN
 }
 
 // ---- host -------------------------------------------------------------------------------------
@@ -1226,7 +1401,7 @@ uint32_t ilog2(uint32_t v)
 // Scratch of one list of work.
 struct plan_mem {
     size_t bytes;
-    size_t plan, blk, cum, start, first;
+    size_t blk, cum, start, first;
     plan_mem(uint32_t max_blk, uint32_t max_cta, uint32_t n)
     {
         bytes = 0;
@@ -1235,22 +1410,18 @@ struct plan_mem {
             bytes += (b + 255) & ~(size_t)255;
             return at;
         };
-        plan = take(sizeof(attn_plan));
         blk = take(sizeof(attn_blk) * ((size_t)max_blk + 1));
-        cum = take(8 * ((size_t)max_blk + 2));
+        cum = take(max_blk > kPlanShared ? 8 * ((size_t)max_blk + 2) : 0);
         start = take(sizeof(attn_start) * ((size_t)max_cta + 2));
-        first = take(4 * ((size_t)n + 1));
+        first = take(n > kPlanShared ? 4 * ((size_t)n + 1) : 0);
     }
     void point(char *base, plan_in &p, attn_in &a) const
     {
-        p.plan = reinterpret_cast<attn_plan *>(base + plan);
         p.blk = reinterpret_cast<attn_blk *>(base + blk);
         p.cum = reinterpret_cast<unsigned long long *>(base + cum);
         p.start = reinterpret_cast<attn_start *>(base + start);
         p.first = reinterpret_cast<uint32_t *>(base + first);
-        a.plan = p.plan;
         a.blk = p.blk;
-        a.cum = p.cum;
         a.start = p.start;
     }
 };
@@ -1282,12 +1453,10 @@ void fill_common(attn_in &A, cr_ctx *ctx, const cr_attn_args *a, const kv_desc &
     A.head_dim = K.dim;
     A.c = a->scale * 1.44269504088896341f;
     A.causal = a->causal != 0;
-    A.q = a->d_q;
-    A.q_token = a->q_token;
-    A.q_head = a->q_head;
     A.o = a->d_o;
     A.o_token = a->o_token;
     A.o_head = a->o_head;
+    A.o_wide = !((uintptr_t)a->d_o & 31) && !((a->o_token | a->o_head) & 15);
     A.lse = a->d_lse;
     A.status = ctx->d_status;
     if (K.paged) {
@@ -1297,57 +1466,85 @@ void fill_common(attn_in &A, cr_ctx *ctx, const cr_attn_args *a, const kv_desc &
     }
 }
 
-template <int D, bool BF16>
-int launch_rows(cr_ctx *ctx, const attn_in &A, const kv_desc &K, const cr_attn_args *a, uint32_t ctas, bool join)
+// Launches whose prologue may run before the kernel ahead of them on the stream has ended; they wait for its
+// end (griddepcontrol.wait) before they read anything of it.
+template <typename... P, typename... T>
+int launch_early(cr_ctx *ctx, const char *what, void (*kern)(P...), dim3 grid, uint32_t block, size_t smem, T... args)
 {
-    CUtensorMap mq, mk, mv;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = ctx->stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kern, args...) != cudaSuccess) return cr_check_launch(ctx, what);
+    ctx->launches++;
+    return CR_OK;
+}
+
+int query_map(cr_ctx *ctx, CUtensorMap *map, const attn_in &A, const kv_desc &K, const cr_attn_args *a, uint32_t heads,
+              uint32_t tokens)
+{
     const uint64_t dim[4] = {K.dim, A.G, K.heads, a->n_tokens}, st[3] = {a->q_head, a->q_head * A.G, a->q_token};
-    const uint32_t box[3] = {A.G, 1, A.tq};
-    CR_TRY(encode_map(ctx, &mq, BF16, a->d_q, dim, st, box, false));
+    const uint32_t box[3] = {heads, 1, tokens};
+    return encode_map(ctx, map, K.bf16, a->d_q, dim, st, box, false);
+}
+
+template <int D, bool BF16>
+int launch_rows(cr_ctx *ctx, const attn_in &A, const kv_desc &K, const cr_attn_args *a, uint32_t ctas)
+{
+    CUtensorMap mq, mk, mv, mo;
+    CR_TRY(query_map(ctx, &mq, A, K, a, A.G, A.tq));
     CR_TRY(kv_map(ctx, &mk, K, false, A.box_rows));
     CR_TRY(kv_map(ctx, &mv, K, true, A.box_rows));
+    // outputs as the queries: same dims and boxes
+    const uint64_t dim[4] = {K.dim, A.G, K.heads, a->n_tokens}, st[3] = {a->o_head, a->o_head * A.G, a->o_token};
+    const uint32_t box[3] = {A.G, 1, A.tq};
+    CR_TRY(encode_map(ctx, &mo, BF16, a->d_o, dim, st, box, false));
     auto kern = k_attn_rows<D, BF16>;
-    CR_CUDA(ctx, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, rows_cfg<D>::kSmem));
-    CR_LAUNCH(ctx, kern, ctas, kRowsThreads, rows_cfg<D>::kSmem, A, mq, mk, mv);
-    if (join && ctas > 1) {
-        auto kj = k_attn_rows_join<D, BF16>;
-        CR_LAUNCH(ctx, kj, dim3(ctas - 1, 8), 256, 0, A);
-    }
+    static const cudaError_t raised = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, rows_cfg<D>::kSmem);
+    if (raised != cudaSuccess) return cr_fail(ctx, CR_ECUDA, "k_attn_rows: %s", cudaGetErrorString(raised));
+    CR_TRY(launch_early(ctx, "k_attn_rows", kern, dim3(ctas), kRowsThreads, rows_cfg<D>::kSmem, A, mq, mk, mv, mo));
+    if (ctas > 1)
+        CR_TRY(launch_early(ctx, "k_attn_join", k_attn_join<D, BF16, 2 * kRowsTile, 32>, dim3(ctas - 1, 8), 256, 0, A));
     return CR_OK;
 }
 
 int rows(cr_ctx *ctx, const attn_in &A, const kv_desc &K, const cr_attn_args *a, uint32_t ctas)
 {
-    if (K.dim <= 64)
-        return K.bf16 ? launch_rows<64, true>(ctx, A, K, a, ctas, true) : launch_rows<64, false>(ctx, A, K, a, ctas, true);
-    return K.bf16 ? launch_rows<128, true>(ctx, A, K, a, ctas, true) : launch_rows<128, false>(ctx, A, K, a, ctas, true);
+    if (K.dim <= 64) return K.bf16 ? launch_rows<64, true>(ctx, A, K, a, ctas) : launch_rows<64, false>(ctx, A, K, a, ctas);
+    return K.bf16 ? launch_rows<128, true>(ctx, A, K, a, ctas) : launch_rows<128, false>(ctx, A, K, a, ctas);
 }
 
 template <int D, bool BF16, bool WIDE>
-int launch_few(cr_ctx *ctx, const attn_in &A, const kv_desc &K, uint32_t ctas)
+int launch_few(cr_ctx *ctx, const attn_in &A, const kv_desc &K, const cr_attn_args *a, uint32_t ctas)
 {
-    CUtensorMap mk, mv;
+    CUtensorMap mq, mk, mv;
+    CR_TRY(query_map(ctx, &mq, A, K, a, A.G < 16 ? A.G : 16, 1));
     CR_TRY(kv_map(ctx, &mk, K, false, A.box_rows));
     CR_TRY(kv_map(ctx, &mv, K, true, A.box_rows));
     auto kern = k_attn_few<D, BF16, WIDE>;
-    CR_CUDA(ctx, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, few_cfg<D, WIDE>::kSmem));
-    CR_LAUNCH(ctx, kern, ctas, kFewThreads, (few_cfg<D, WIDE>::kSmem), A, mk, mv);
-    if (ctas > 1) {
-        auto kj = k_attn_few_join<D, BF16>;
-        CR_LAUNCH(ctx, kj, ctas - 1, 128, 0, A);
-    }
+    static const cudaError_t raised = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, few_cfg<D>::kSmem);
+    if (raised != cudaSuccess) return cr_fail(ctx, CR_ECUDA, "k_attn_few: %s", cudaGetErrorString(raised));
+    CR_TRY(launch_early(ctx, "k_attn_few", kern, dim3(ctas), kFewThreads, few_cfg<D>::kSmem, A, mq, mk, mv));
+    if (ctas > 1)
+        CR_TRY(launch_early(ctx, "k_attn_join", k_attn_join<D, BF16, 16, 16>, dim3(ctas - 1), 256, 0, A));
     return CR_OK;
 }
 
-int few(cr_ctx *ctx, const attn_in &A, const kv_desc &K, uint32_t ctas)
+int few(cr_ctx *ctx, const attn_in &A, const kv_desc &K, const cr_attn_args *a, uint32_t ctas)
 {
     const bool wide = A.G > 8;
     if (K.dim <= 64) {
-        if (K.bf16) return wide ? launch_few<64, true, true>(ctx, A, K, ctas) : launch_few<64, true, false>(ctx, A, K, ctas);
-        return wide ? launch_few<64, false, true>(ctx, A, K, ctas) : launch_few<64, false, false>(ctx, A, K, ctas);
+        if (K.bf16) return wide ? launch_few<64, true, true>(ctx, A, K, a, ctas) : launch_few<64, true, false>(ctx, A, K, a, ctas);
+        return wide ? launch_few<64, false, true>(ctx, A, K, a, ctas) : launch_few<64, false, false>(ctx, A, K, a, ctas);
     }
-    if (K.bf16) return wide ? launch_few<128, true, true>(ctx, A, K, ctas) : launch_few<128, true, false>(ctx, A, K, ctas);
-    return wide ? launch_few<128, false, true>(ctx, A, K, ctas) : launch_few<128, false, false>(ctx, A, K, ctas);
+    if (K.bf16) return wide ? launch_few<128, true, true>(ctx, A, K, a, ctas) : launch_few<128, true, false>(ctx, A, K, a, ctas);
+    return wide ? launch_few<128, false, true>(ctx, A, K, a, ctas) : launch_few<128, false, false>(ctx, A, K, a, ctas);
 }
 
 // Pieces of a list of work: two per CTA at most.
@@ -1387,6 +1584,7 @@ int attn_many(cr_ctx *ctx, const cr_attn_args *a, const kv_desc &K)
         p.n_seqs = K.pg->n_seqs;
         p.max_len = K.pg->max_pages * K.pg->page;
     }
+    A.o_copy = 1;
     p.max_cta = (uint32_t)ctx->num_sms;
     const plan_mem mem(p.max_blk, p.max_cta, a->n);
     void *base;
@@ -1531,5 +1729,5 @@ extern "C" int cr_attn_decode(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t la
     } else {
         CR_LAUNCH(ctx, k_attn_plan<PLAN_FEW>, 1, 1024, 0, f, f, ctx->d_status);
     }
-    return few(ctx, F, K, f.max_cta);
+    return few(ctx, F, K, args, f.max_cta);
 }

@@ -66,6 +66,18 @@ __device__ __forceinline__ void cr_tma_load(uint32_t dst, const CUtensorMap *map
         ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w)
         : "memory");
 }
+__device__ __forceinline__ void cr_tma_store(const CUtensorMap *map, uint32_t src, int x, int y, int z, int w)
+{
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(map),
+                 "r"(src), "r"(x), "r"(y), "r"(z), "r"(w)
+                 : "memory");
+}
+// This thread's stores have read shared memory; have been written.
+__device__ __forceinline__ void cr_tma_store_read()
+{
+    asm volatile("cp.async.bulk.commit_group;\n\tcp.async.bulk.wait_group.read 0;" ::: "memory");
+}
+__device__ __forceinline__ void cr_tma_store_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void cr_tma_prefetch_map(const CUtensorMap *map)
 {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
@@ -83,27 +95,40 @@ __device__ __forceinline__ void cr_tmem_free(uint32_t tmem, uint32_t cols)
 }
 __device__ __forceinline__ void cr_tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void cr_tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// The barrier gets one arrival when every tcgen05 operation this thread issued before has finished.
-__device__ __forceinline__ void cr_tc_commit(uint32_t bar)
+// Products and commits are issued by one thread of a warp that runs the surrounding code as a whole: so the
+// operands' descriptors stay in uniform registers (issued from a branch of one lane, every product waits for
+// its descriptors to be moved there, and the tensor cores for the products).
+__device__ __forceinline__ uint32_t cr_elect()
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r;
 }
-// D += A B (acc = 0: D = A B), A and B through shared-memory descriptors
-__device__ __forceinline__ void cr_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc)
+// The barrier gets one arrival when every tcgen05 operation the elected thread issued before has finished.
+__device__ __forceinline__ void cr_tc_commit(uint32_t bar, uint32_t elected)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc)
+        "{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %1, 0;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
+        ::"r"(bar), "r"(elected)
+        : "memory");
+}
+// D += A B (acc = 0: D = A B), A and B through shared-memory descriptors
+__device__ __forceinline__ void cr_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc, uint32_t elected)
+{
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(elected)
         : "memory");
 }
 // the same with A in tensor memory
-__device__ __forceinline__ void cr_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc)
+__device__ __forceinline__ void cr_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc, uint32_t elected)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc)
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc), "r"(elected)
         : "memory");
 }
 
@@ -131,15 +156,6 @@ __device__ __forceinline__ uint64_t cr_sdesc(uint32_t addr, uint32_t lead, uint3
         "=r"((a)[(o) + 20]), "=r"((a)[(o) + 21]), "=r"((a)[(o) + 22]), "=r"((a)[(o) + 23]), "=r"((a)[(o) + 24]),   \
         "=r"((a)[(o) + 25]), "=r"((a)[(o) + 26]), "=r"((a)[(o) + 27]), "=r"((a)[(o) + 28]), "=r"((a)[(o) + 29]),   \
         "=r"((a)[(o) + 30]), "=r"((a)[(o) + 31])
-#define CR_ST32(a, o)                                                                                              \
-    "r"((a)[(o) + 0]), "r"((a)[(o) + 1]), "r"((a)[(o) + 2]), "r"((a)[(o) + 3]), "r"((a)[(o) + 4]),                 \
-        "r"((a)[(o) + 5]), "r"((a)[(o) + 6]), "r"((a)[(o) + 7]), "r"((a)[(o) + 8]), "r"((a)[(o) + 9]),             \
-        "r"((a)[(o) + 10]), "r"((a)[(o) + 11]), "r"((a)[(o) + 12]), "r"((a)[(o) + 13]), "r"((a)[(o) + 14]),        \
-        "r"((a)[(o) + 15]), "r"((a)[(o) + 16]), "r"((a)[(o) + 17]), "r"((a)[(o) + 18]), "r"((a)[(o) + 19]),        \
-        "r"((a)[(o) + 20]), "r"((a)[(o) + 21]), "r"((a)[(o) + 22]), "r"((a)[(o) + 23]), "r"((a)[(o) + 24]),        \
-        "r"((a)[(o) + 25]), "r"((a)[(o) + 26]), "r"((a)[(o) + 27]), "r"((a)[(o) + 28]), "r"((a)[(o) + 29]),        \
-        "r"((a)[(o) + 30]), "r"((a)[(o) + 31])
-
 // 32 consecutive columns of the calling thread's lane of tensor memory (warp-collective)
 __device__ __forceinline__ void cr_tmem_ld(uint32_t addr, uint32_t *v)
 {
@@ -150,17 +166,39 @@ __device__ __forceinline__ void cr_tmem_ld(uint32_t addr, uint32_t *v)
         : CR_LD32(v, 0)
         : "r"(addr));
 }
-__device__ __forceinline__ void cr_tmem_st(uint32_t addr, const uint32_t *v)
+#define CR_LD16(a)                                                                                                 \
+    "=r"((a)[0]), "=r"((a)[1]), "=r"((a)[2]), "=r"((a)[3]), "=r"((a)[4]), "=r"((a)[5]), "=r"((a)[6]),              \
+        "=r"((a)[7]), "=r"((a)[8]), "=r"((a)[9]), "=r"((a)[10]), "=r"((a)[11]), "=r"((a)[12]), "=r"((a)[13]),      \
+        "=r"((a)[14]), "=r"((a)[15])
+#define CR_ST16(a)                                                                                                 \
+    "r"((a)[0]), "r"((a)[1]), "r"((a)[2]), "r"((a)[3]), "r"((a)[4]), "r"((a)[5]), "r"((a)[6]), "r"((a)[7]),        \
+        "r"((a)[8]), "r"((a)[9]), "r"((a)[10]), "r"((a)[11]), "r"((a)[12]), "r"((a)[13]), "r"((a)[14]), "r"((a)[15])
+__device__ __forceinline__ void cr_tmem_ld16(uint32_t addr, uint32_t *v)
 {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
-        ::CR_ST32(v, 0), "r"(addr)
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : CR_LD16(v)
+        : "r"(addr));
+}
+__device__ __forceinline__ void cr_tmem_st16(uint32_t addr, const uint32_t *v)
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+        ::CR_ST16(v), "r"(addr)
         : "memory");
 }
 __device__ __forceinline__ void cr_tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cr_tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// 32 bytes, aligned so
+__device__ __forceinline__ void cr_store32(void *p, const uint32_t *v)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]),
+                 "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
 
 // ---- arithmetic ----------------------------------------------------------------------------
 __device__ __forceinline__ float cr_exp2(float x)
