@@ -581,7 +581,7 @@ CR_API int cr_kv_write(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t layer, co
  *   d_cu_q    int32[n+1]: query tokens of entry i are d_cu_q[i] .. d_cu_q[i+1]-1
  *             (ascending from 0 to n_tokens)
  *   d_seqs    paged calls: int32[n] rows of the table, NULL: row i
- * q_heads a multiple of kv_heads, at most 128 times it; scale finite and > 0.
+ * kv_heads at most 4,096, q_heads a multiple of it, at most 128 times it; scale finite and > 0.
  * d_o overlaps no input.
  * Errors: CR_EINVAL, CR_ENOMEM, CR_ECUDA; CR_EINVAL by the next blocking call for a
  * row that does not exist (its output is that of a row without keys), CR_ETIMEOUT

@@ -26,6 +26,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -85,13 +86,6 @@ class KVPagesDesc(C.Structure):
                 [(f, C.c_uint32) for f in ("dtype", "layers", "n_pages", "page", "kv_heads", "head_dim", "n_seqs",
                                            "max_pages")] +
                 [(f, C.c_uint64) for f in ("layer_stride", "kv_stride", "page_stride", "token_stride", "head_stride")])
-
-
-class AttnArgs(C.Structure):
-    _fields_ = ([(f, C.c_void_p) for f in ("d_q", "d_o", "d_lse", "d_cu_q", "d_seqs")] +
-                [(f, C.c_uint32) for f in ("n", "n_tokens", "q_heads", "causal")] +
-                [("scale", C.c_float), ("reserved", C.c_uint32)] +
-                [(f, C.c_uint64) for f in ("q_token", "q_head", "o_token", "o_head")])
 
 
 class Replica(C.Structure):
@@ -550,6 +544,7 @@ def shadow_replay(ctx: Context, replay: Replay, keys, plen, slen, dest, ctr):
 
 
 # ---- what a destination does with the prefixes it holds ------------------------------------------------------------
+# These calls are made once per layer and step, so their checks take one look at each tensor.
 def _dtype_code(t) -> int:
     import torch
     if t.dtype == torch.bfloat16:
@@ -563,26 +558,34 @@ def _out(ctx: Context, shape, like, dtype=None):
     """An output of a call: its memory is not handed out again before ctx's stream has written it."""
     import torch
     t = torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
-    if ctx._stream_obj != torch.cuda.current_stream(ctx.device):
+    if ctx._stream_obj.cuda_stream != torch._C._cuda_getCurrentRawStream(ctx.device):
         t.record_stream(ctx._stream_obj)
     return t
 
 
-def _need_int32(name, t, n=None):
+def _int32(name, t, n=None):
+    """Address of a contiguous int32 CUDA tensor, of n elements."""
     import torch
     if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 CUDA tensor")
     if n is not None and t.numel() != n:
         raise ValueError(f"{name} must have {n} elements, got {t.numel()}")
+    return t.data_ptr()
 
 
-def _need_heads(name, t, dtype, shape):
-    """[tokens, heads, head_dim] of the given dtype, head_dim contiguous."""
-    if not t.is_cuda or t.dtype != dtype or t.dim() != 3 or t.stride(2) != 1:
-        raise ValueError(f"{name} must be a {dtype} CUDA tensor [tokens, heads, head_dim] with contiguous head_dim")
-    for have, want in zip(t.shape, shape):
-        if want is not None and have != want:
-            raise ValueError(f"{name} must have shape {tuple(shape)} (None: any), got {tuple(t.shape)}")
+def _heads(name, t, dtype, want):
+    """(tokens, address, token stride, head stride) of a tensor [tokens, heads, head_dim], contiguous in head_dim;
+    ``want``: (tokens, heads, head_dim), None for any."""
+    shape = t.shape
+    if t.dtype != dtype or not t.is_cuda or len(shape) != 3:
+        raise ValueError(f"{name} must be a {dtype} CUDA tensor [tokens, heads, head_dim]")
+    if ((want[0] is not None and shape[0] != want[0]) or (want[1] is not None and shape[1] != want[1]) or
+            (want[2] is not None and shape[2] != want[2])):
+        raise ValueError(f"{name} must have shape {tuple(want)} (None: any), got {tuple(shape)}")
+    st = t.stride()
+    if st[2] != 1:
+        raise ValueError(f"{name} must be contiguous in head_dim")
+    return shape[0], t.data_ptr(), st[0], st[1]
 
 
 class KVPages:
@@ -597,13 +600,14 @@ class KVPages:
         if cache.dim() != 6 or cache.shape[1] != 2 or not cache.is_cuda or cache.stride(5) != 1:
             raise ValueError("cache must be a CUDA tensor [layers, 2, n_pages, page, kv_heads, head_dim]")
         layers, _, n_pages, page, heads, dim = cache.shape
-        _need_int32("ref", ref, n_pages)
-        _need_int32("table", table)
+        _int32("ref", ref, n_pages)
+        _int32("table", table)
         if table.dim() != 2:
             raise ValueError("table must have two dimensions")
-        _need_int32("lens", lens, table.shape[0])
+        _int32("lens", lens, table.shape[0])
         self.cache, self.ref, self.table, self.lens = cache, ref, table, lens
         self.layers, self.n_pages, self.page, self.kv_heads, self.head_dim = layers, n_pages, page, heads, dim
+        self.dtype = cache.dtype
         self._code = _dtype_code(cache)
         self._bind()
 
@@ -626,8 +630,8 @@ class KVPages:
 
     def replace(self, ref, table):
         """Take the counts and tables that ``pages_compact`` gave (the cache's pages have moved already)."""
-        _need_int32("ref", ref, self.n_pages)
-        _need_int32("table", table)
+        _int32("ref", ref, self.n_pages)
+        _int32("table", table)
         if table.shape != self.table.shape:
             raise ValueError("table must have the old table's shape")
         self.ref, self.table = ref, table
@@ -636,76 +640,77 @@ class KVPages:
 
 def pages_extend(ctx: Context, pages: KVPages, seqs, add):
     """The sequences ``seqs`` get pages for ``add`` more tokens each (cr_pages_extend)."""
-    n = int(seqs.shape[0])
-    _need_int32("seqs", seqs, n)
-    _need_int32("add", add, n)
-    ctx.check(lib().cr_pages_extend(ctx.handle, pages._addr, _ptr(seqs), _ptr(add), n), "cr_pages_extend")
+    n = seqs.shape[0]
+    st = lib().cr_pages_extend(ctx._h, pages._addr, _int32("seqs", seqs, n), _int32("add", add, n), n)
+    if st:
+        ctx.check(st, "cr_pages_extend")
 
 
 def pages_fork(ctx: Context, pages: KVPages, src, dst, keep):
     """The empty rows ``dst`` become the first ``keep`` tokens of the rows ``src`` (cr_pages_fork)."""
-    n = int(src.shape[0])
-    _need_int32("src", src, n)
-    _need_int32("dst", dst, n)
-    _need_int32("keep", keep, n)
-    ctx.check(lib().cr_pages_fork(ctx.handle, pages._addr, _ptr(src), _ptr(dst), _ptr(keep), n), "cr_pages_fork")
+    n = src.shape[0]
+    st = lib().cr_pages_fork(ctx._h, pages._addr, _int32("src", src, n), _int32("dst", dst, n),
+                             _int32("keep", keep, n), n)
+    if st:
+        ctx.check(st, "cr_pages_fork")
 
 
 def pages_free(ctx: Context, pages: KVPages, seqs):
     """The rows ``seqs`` become empty (cr_pages_free)."""
-    n = int(seqs.shape[0])
-    _need_int32("seqs", seqs, n)
-    ctx.check(lib().cr_pages_free(ctx.handle, pages._addr, _ptr(seqs), n), "cr_pages_free")
+    n = seqs.shape[0]
+    st = lib().cr_pages_free(ctx._h, pages._addr, _int32("seqs", seqs, n), n)
+    if st:
+        ctx.check(st, "cr_pages_free")
 
 
 def pages_compact(ctx: Context, pages: KVPages):
     """Move live pages to the front (cr_pages_compact): (ref, table, page_map, n_live), new tensors;
     ``pages.replace(ref, table)`` takes them."""
-    import torch
     ref = _out(ctx, pages.ref.shape, pages.ref)
     table = _out(ctx, pages.table.shape, pages.table)
     page_map = _out(ctx, pages.ref.shape, pages.ref)
     live = _out(ctx, (1,), pages.ref)
-    ctx.check(lib().cr_pages_compact(ctx.handle, pages._addr, _ptr(ref), _ptr(table), _ptr(page_map), _ptr(live)),
-              "cr_pages_compact")
+    st = lib().cr_pages_compact(ctx._h, pages._addr, ref.data_ptr(), table.data_ptr(), page_map.data_ptr(),
+                                live.data_ptr())
+    if st:
+        ctx.check(st, "cr_pages_compact")
     return ref, table, page_map, live
 
 
 def kv_write(ctx: Context, pages: KVPages, layer: int, k, v, cu, seqs=None):
     """Write the keys and values [tokens, kv_heads, head_dim] of every sequence's last tokens into its pages:
     entry i's tokens are cu[i] .. cu[i+1]-1, its row seqs[i] (None: i) (cr_kv_write)."""
-    n = int(cu.shape[0]) - 1
-    _need_int32("cu", cu)
-    if seqs is not None:
-        _need_int32("seqs", seqs, n)
-    shape = (k.shape[0], pages.kv_heads, pages.head_dim)
-    _need_heads("k", k, pages.cache.dtype, shape)
-    _need_heads("v", v, pages.cache.dtype, shape)
-    ks, vs = k.stride(), v.stride()
-    ctx.check(lib().cr_kv_write(ctx.handle, pages._addr, layer, _ptr(k), ks[0], ks[1], _ptr(v), vs[0], vs[1],
-                                _ptr(cu), _ptr(seqs), max(n, 0), int(k.shape[0])), "cr_kv_write")
+    n = max(cu.shape[0] - 1, 0)
+    T, kp, kt, kh = _heads("k", k, pages.dtype, (None, pages.kv_heads, pages.head_dim))
+    _, vp, vt, vh = _heads("v", v, pages.dtype, (T, pages.kv_heads, pages.head_dim))
+    st = lib().cr_kv_write(ctx._h, pages._addr, layer, kp, kt, kh, vp, vt, vh, _int32("cu", cu),
+                           None if seqs is None else _int32("seqs", seqs, n), n, T)
+    if st:
+        ctx.check(st, "cr_kv_write")
 
 
-def _attn_args(ctx: Context, q, n, cu, seqs, causal, scale, out, lse):
+_pack_attn = struct.Struct("@5P4IfI4Q").pack  # cr_attn_args
+
+
+def _attn_args(ctx: Context, q, dtype, dim, n, cu, seqs, causal, scale, out, lse):
+    """cr_attn_args as bytes, and the outputs."""
     import torch
-    T, heads, dim = q.shape
+    T, qp, qt, qh = _heads("q", q, dtype, (None, None, dim))
+    heads, dim = q.shape[1], q.shape[2]
     if out is None:
         out = _out(ctx, (T, heads, dim), q)
-    else:
-        _need_heads("out", out, q.dtype, (T, heads, dim))
+    _, op, ot, oh = _heads("out", out, dtype, (T, heads, dim))
     if lse is True:
         lse = _out(ctx, (T, heads), q, torch.float32)
-    elif lse is not None and lse is not False:
+    elif lse is False:
+        lse = None
+    elif lse is not None:
         _need_cuda("lse", lse, torch.float32)
         if tuple(lse.shape) != (T, heads):
             raise ValueError(f"lse must have shape {(T, heads)}")
-    else:
-        lse = None
-    if seqs is not None:
-        _need_int32("seqs", seqs, n)
-    qs, os_ = q.stride(), out.stride()
-    a = AttnArgs(_ptr(q), _ptr(out), _ptr(lse), _ptr(cu), _ptr(seqs), n, T, heads, 1 if causal else 0,
-                 dim ** -0.5 if scale is None else scale, 0, qs[0], qs[1], os_[0], os_[1])
+    a = _pack_attn(qp, op, 0 if lse is None else lse.data_ptr(), 0 if cu is None else _int32("cu", cu),
+                   0 if seqs is None else _int32("seqs", seqs, n), n, T, heads, 1 if causal else 0,
+                   dim ** -0.5 if scale is None else scale, 0, qt, qh, ot, oh)
     return a, out, lse
 
 
@@ -714,21 +719,17 @@ def attn_packed(ctx: Context, q, k, v, cu, cu_k=None, causal: bool = True, scale
     """Attention over whole prompts packed back to back: q [tokens, heads, head_dim], k and v [tokens, kv_heads,
     head_dim]; sequence i's queries are cu[i] .. cu[i+1]-1, its keys cu_k[i] .. (None: the same) (cr_attn_packed).
     Returns the output, or (output, lse) with ``lse=True`` (or a tensor for it)."""
-    _need_heads("q", q, q.dtype, (None, None, None))
-    _need_int32("cu", cu)
-    n = max(int(cu.shape[0]) - 1, 0)
-    if cu_k is not None:
-        _need_int32("cu_k", cu_k, n + 1)
-    elif k.shape[0] != q.shape[0]:
-        raise ValueError("as many keys as queries, or cu_k")
-    shape = (k.shape[0], k.shape[1], q.shape[2])
-    _need_heads("k", k, q.dtype, shape)
-    _need_heads("v", v, q.dtype, shape)
+    n = max(cu.shape[0] - 1, 0)
     code = _dtype_code(q)
-    a, out, lse = _attn_args(ctx, q, n, cu, None, causal, scale, out, lse)
-    ks, vs = k.stride(), v.stride()
-    ctx.check(lib().cr_attn_packed(ctx.handle, C.addressof(a), code, int(k.shape[1]), int(q.shape[2]), _ptr(k), ks[0],
-                                   ks[1], _ptr(v), vs[0], vs[1], _ptr(cu_k), int(k.shape[0])), "cr_attn_packed")
+    a, out, lse = _attn_args(ctx, q, q.dtype, None, n, cu, None, causal, scale, out, lse)
+    dim = q.shape[2]
+    S, kp, kt, kh = _heads("k", k, q.dtype, (None if cu_k is not None else q.shape[0], None, dim))
+    heads = k.shape[1]
+    _, vp, vt, vh = _heads("v", v, q.dtype, (S, heads, dim))
+    st = lib().cr_attn_packed(ctx._h, a, code, heads, dim, kp, kt, kh, vp, vt, vh,
+                              None if cu_k is None else _int32("cu_k", cu_k, n + 1), S)
+    if st:
+        ctx.check(st, "cr_attn_packed")
     return out if lse is None else (out, lse)
 
 
@@ -736,11 +737,11 @@ def attn_paged(ctx: Context, q, pages: KVPages, layer: int, cu, seqs=None, causa
                scale: Optional[float] = None, out=None, lse=None):
     """Attention of every sequence's last tokens over its pages (cr_attn_paged): q [tokens, heads, head_dim], entry
     i's queries cu[i] .. cu[i+1]-1, its row seqs[i] (None: i).  Returns as ``attn_packed``."""
-    _need_heads("q", q, pages.cache.dtype, (None, None, pages.head_dim))
-    _need_int32("cu", cu)
-    n = max(int(cu.shape[0]) - 1, 0)
-    a, out, lse = _attn_args(ctx, q, n, cu, seqs, causal, scale, out, lse)
-    ctx.check(lib().cr_attn_paged(ctx.handle, pages._addr, layer, C.addressof(a)), "cr_attn_paged")
+    n = max(cu.shape[0] - 1, 0)
+    a, out, lse = _attn_args(ctx, q, pages.dtype, pages.head_dim, n, cu, seqs, causal, scale, out, lse)
+    st = lib().cr_attn_paged(ctx._h, pages._addr, layer, a)
+    if st:
+        ctx.check(st, "cr_attn_paged")
     return out if lse is None else (out, lse)
 
 
@@ -749,15 +750,14 @@ def attn_decode(ctx: Context, q, pages: KVPages, layer: int, seqs=None, group_of
     """Attention of one token per sequence, q [n, heads, head_dim], over its pages (cr_attn_decode).  Sequences
     group_off[g] .. group_off[g+1]-1 of the batch share their first shared[g] tokens' pages, which are read once for
     all of them.  Returns as ``attn_packed``."""
-    _need_heads("q", q, pages.cache.dtype, (None, None, pages.head_dim))
-    ng = 0
+    ng = go = sh = 0
     if group_off is not None:
-        ng = max(int(group_off.shape[0]) - 1, 0)
-        _need_int32("group_off", group_off)
         if shared is None:
             raise ValueError("group_off without shared")
-        _need_int32("shared", shared, ng)
-    a, out, lse = _attn_args(ctx, q, int(q.shape[0]), None, seqs, False, scale, out, lse)
-    ctx.check(lib().cr_attn_decode(ctx.handle, pages._addr, layer, C.addressof(a), _ptr(group_off), _ptr(shared), ng),
-              "cr_attn_decode")
+        ng = max(group_off.shape[0] - 1, 0)
+        go, sh = _int32("group_off", group_off), _int32("shared", shared, ng)
+    a, out, lse = _attn_args(ctx, q, pages.dtype, pages.head_dim, q.shape[0], None, seqs, False, scale, out, lse)
+    st = lib().cr_attn_decode(ctx._h, pages._addr, layer, a, go, sh, ng)
+    if st:
+        ctx.check(st, "cr_attn_decode")
     return out if lse is None else (out, lse)

@@ -25,7 +25,7 @@ namespace {
 constexpr int kRowsTile = 128;  // query rows of a tile, and keys of one
 constexpr int kFewTile = 64;    // keys of a tile of k_attn_few
 constexpr int kFewWarps = 4;
-constexpr uint32_t kExtra = 1;
+constexpr uint32_t kExtra = 1, kPieceCost = 3;
 
 // A block of query rows of one key head.
 struct __align__(16) attn_blk {
@@ -36,14 +36,17 @@ struct __align__(16) attn_blk {
     int diag;   // keys before the one that its first query token sees last (causal)
     int lo;     // k_attn_few: keys below are already counted (the shared prefix)
     int nt;     // its key tiles
-    int pad;
+    uint32_t at;  // place in a head's list
 };
 // Where a CTA's stretch begins.
 struct __align__(16) attn_start {
     unsigned long long pos, N;  // N: key tiles of all stretches
     uint32_t head, blk, tile, nblk;
     attn_blk k;                 // its first block
+    // where the stretch is the first to begin inside that block: the block's pieces (from the stretch before on)
+    uint32_t pieces, pad[3];
 };
+constexpr uint32_t kMaxCtas = 512;
 
 // What the plan kernel reads.
 struct plan_in {
@@ -58,9 +61,11 @@ struct plan_in {
     uint32_t min_tiles;    // key tiles that a CTA is worth
     attn_blk *blk;
     attn_start *start;        // [max_cta + 1]
+    unsigned long long *pos;  // [max_cta + 1] their places alone
     // of long lists only (the plan kernel's shared memory holds the others)
     unsigned long long *cum;  // [max_blk + 1] key tiles before each block
     uint32_t *first;          // [n + 1] first block of each entry
+    int32_t *of_token;        // groups: block of each query token
 };
 constexpr uint32_t kPlanShared = 1024;
 
@@ -132,6 +137,7 @@ __device__ void plan_build(const plan_in &A, uint32_t *status)
 {
     __shared__ unsigned long long cum_near[kPlanShared + 1];
     __shared__ uint32_t first_near[kPlanShared + 1];
+    __shared__ unsigned long long pos_near[kMaxCtas + 1];
     const uint32_t tid = threadIdx.x;
     const uint32_t n = KIND == PLAN_GROUPS ? A.n_groups : A.n;
     uint32_t *first = n <= kPlanShared ? first_near : A.first;
@@ -163,6 +169,7 @@ __device__ void plan_build(const plan_in &A, uint32_t *status)
         __syncthreads();
     }
     // their keys
+    uint32_t filled = 0;  // blocks that have any
     base = 0;
     for (uint32_t b0 = 0; b0 < nblk; b0 += 1024) {
         const uint32_t b = b0 + tid;
@@ -244,9 +251,15 @@ __device__ void plan_build(const plan_in &A, uint32_t *status)
             }
             k.nt = (int)nt;
             A.blk[b] = k;
+            if (KIND == PLAN_GROUPS)
+                for (int t = 0; t < k.ntok; ++t) A.of_token[k.row0 + t] = (int)b;
         }
+        filled += __syncthreads_count(nt > 0);
         const unsigned long long at = base + scan1024(nt ? nt + kExtra : 0, &total);
-        if (b < nblk) cum[b] = at;
+        if (b < nblk) {
+            cum[b] = at;
+            A.blk[b].at = (uint32_t)at;
+        }
         base += total;
     }
     if (tid == 0) cum[nblk] = base;
@@ -254,11 +267,18 @@ __device__ void plan_build(const plan_in &A, uint32_t *status)
     // stretches
     const unsigned long long Nb = base, N = Nb * A.heads;
     unsigned long long want = N / A.min_tiles;
-    const uint32_t ncta = want < 1 ? 1u : (want < A.max_cta ? (uint32_t)want : A.max_cta);
+    uint32_t ncta = want < 1 ? 1u : (want < A.max_cta ? (uint32_t)want : A.max_cta);
+    // Few blocks: as many stretches for each, so that most of them are within one block and leave one piece instead
+    // of two, where that makes them longer by less than a piece costs (its result's way to scratch and back).
+    const unsigned long long blocks = (unsigned long long)filled * A.heads;
+    if (blocks && blocks <= ncta) {
+        const uint32_t even = (uint32_t)(ncta / blocks * blocks);
+        if (N / even <= N / ncta + kPieceCost) ncta = even;
+    }
     const unsigned long long snap = N / ncta / 8;  // a stretch ends with its block where that is near
     for (uint32_t c = tid; c <= A.max_cta; c += 1024) {
         attn_start s = {};
-        s.pos = c < ncta ? (unsigned long long)((unsigned __int128)N * c / ncta) : N;
+        s.pos = c < ncta ? N * c / ncta : N;  // N < 2^54, c <= 512
         if (s.pos < N) {
             s.head = (uint32_t)(s.pos / Nb);
             const unsigned long long rem = s.pos - s.head * Nb;
@@ -288,6 +308,15 @@ __device__ void plan_build(const plan_in &A, uint32_t *status)
             s.k = A.blk[s.blk];
         }
         A.start[c] = s;
+        pos_near[c] = A.pos[c] = s.pos;
+    }
+    __syncthreads();
+    for (uint32_t c = 1 + tid; c < ncta; c += 1024) {
+        const attn_start &s = A.start[c];
+        const unsigned long long begin = s.pos - s.tile - kExtra, end = begin + kExtra + (uint32_t)s.k.nt;
+        uint32_t n = 0;
+        if (s.tile && s.pos < N && pos_near[c - 1] <= begin) n = upper(pos_near, A.max_cta + 1, end - 1) - (c - 1);
+        A.start[c].pieces = n;
     }
 }
 
@@ -295,7 +324,8 @@ template <int KIND>
 __global__ void __launch_bounds__(1024) k_attn_plan(const __grid_constant__ plan_in a, const __grid_constant__ plan_in b,
                                                     uint32_t *status)
 {
-    asm volatile("griddepcontrol.launch_dependents;");  // the next kernel's prologue needs nothing of this
+    cr_launch_next();
+    cr_wait_previous();
     if (blockIdx.x == 0)
         plan_build<KIND>(a, status);
     else
@@ -306,6 +336,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan(const __grid_constant__ plan
 struct attn_in {
     const attn_blk *blk;
     const attn_start *start;
+    const unsigned long long *pos;
     const int32_t *table;  // paged
     uint32_t max_pages, page_log2, box_rows, box_log2;
     uint32_t paged, causal, G, nsub, tq, q_heads, head_dim;
@@ -315,9 +346,11 @@ struct attn_in {
     uint64_t o_token, o_head;
     float *part, *part_ml; // pieces
     float *pfx, *pfx_lse;  // shared prefix: o and log2 of the sum, [token][head]
+    float *own, *own_ml;   // k_attn_few: whole blocks that a shared prefix still joins
+    const int32_t *of_token;  // groups: block of each query token
+    uint32_t few_heads, ncta, after_rows;
     uint32_t to_pfx;       // k_attn_rows, its join: write those instead of o
     uint32_t o_wide;       // rows of o begin at multiples of 32 bytes
-    uint32_t o_copy;       // whole tiles of o are written by copies
     uint32_t *status;
 };
 
@@ -386,38 +419,35 @@ template <int D>
 struct rows_cfg {
     static constexpr int kChunks = D / 64;               // 64 elements: a 128-byte row
     static constexpr int kTile = kRowsTile * D * 2;      // bytes of 128 rows
-    // a stage holds the values of one tile and the keys of the next: what one turn of the products uses
-    static constexpr int kStages = D == 128 ? 2 : 4;
-    // after the tiles: one of outputs, a value per (tile, half, row), pieces, barriers, two words
-    static constexpr int kOut = (2 + 2 * kStages) * kTile, kXch = kOut + kTile, kPieces = kXch + 4 * kRowsTile * 4, kBars = kPieces + 2 * 48;
-    static constexpr int kSmem = kBars + 8 * (22 + 2 * kStages) + 16;
+    static constexpr int kStages = D == 128 ? 5 : 10;    // of a tile's keys or values
+    // after the tiles: a value per (tile, half, row), pieces, barriers, two words
+    static constexpr int kXch = (2 + kStages) * kTile, kPieces = kXch + 4 * kRowsTile * 4, kBars = kPieces + 2 * 48;
+    static constexpr int kSmem = kBars + 8 * (18 + 2 * kStages) + 16;
     static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
 };
-// Warps 0-15: softmax (tile, half of the keys, 32 rows); 16: products; 17: copies; 18: copies of outputs;
-// 19 makes the warpgroup whole, whose registers go to the softmax threads: 512 x 104 + 128 x 64 = 640 x 96.
+// Warps 0-15: softmax (tile, half of the keys, 32 rows); 16: products; 17: copies; 18, 19 make the
+// warpgroup whole, whose registers go to the softmax threads: 512 x 104 + 128 x 64 = 640 x 96.
 constexpr int kRowsThreads = 640;
 
 enum { B_QFULL, B_QEMPTY, B_DONE, B_SFULL, B_PREADY = B_SFULL + 2, B_OFULL = B_PREADY + 4, B_OEMPTY = B_OFULL + 2,
-       B_PFULL = B_OEMPTY + 2, B_PEMPTY = B_PFULL + 2, B_OUT = B_PEMPTY + 2, B_OUTFREE = B_OUT + 2, B_FULL };
+       B_PFULL = B_OEMPTY + 2, B_PEMPTY = B_PFULL + 2, B_FULL = B_PEMPTY + 2 };
 
 // What the copying warp tells the others of a piece (two of them are kept).
 struct rows_piece {
     int row0, ntok, klen, diag;
     int h, t0, n, slot;  // n: key tiles, 0: no more pieces
     int stage, phase;    // of the ring, at its first keys
-    int whole;           // bit x: tile x is written as a whole, by a copy
-    int outs;            // such tiles before
+    int pad[2];
 };
 static_assert(sizeof(rows_piece) == 48, "shared memory of the pieces");
 
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kRowsThreads, 1)
     k_attn_rows(const __grid_constant__ attn_in A, const __grid_constant__ CUtensorMap map_q,
-                const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                const __grid_constant__ CUtensorMap map_o)
+                const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
 {
     using cfg = rows_cfg<D>;
-    static_assert(B_FULL <= 22, "barriers");
+    static_assert(B_FULL <= 18, "barriers");
     extern __shared__ __align__(1024) unsigned char dyn[];
     volatile rows_piece *piece = reinterpret_cast<volatile rows_piece *>(dyn + cfg::kPieces);
     float(*xch)[kRowsTile] = reinterpret_cast<float(*)[kRowsTile]>(dyn + cfg::kXch);
@@ -434,12 +464,16 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
 #define FULL(s) BAR(B_FULL + (s))
 #define EMPTY(s) BAR(B_FULL + cfg::kStages + (s))
 
+    if (threadIdx.x == 32) {
+        cr_tma_prefetch_map(&map_q);
+        cr_tma_prefetch_map(&map_k);
+        cr_tma_prefetch_map(&map_v);
+    }
     if (threadIdx.x == 0) {
         gave_up = 0;
         cr_bar_init(BAR(B_QFULL), 1);
         cr_bar_init(BAR(B_QEMPTY), 1);
         cr_bar_init(BAR(B_DONE), 1);
-        cr_bar_init(BAR(B_OUTFREE), 1);
         for (int x = 0; x < 2; ++x) {
             cr_bar_init(BAR(B_SFULL + x), 1);
             cr_bar_init(BAR(B_PREADY + 2 * x), 8);
@@ -447,8 +481,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             cr_bar_init(BAR(B_OFULL + x), 1);
             cr_bar_init(BAR(B_OEMPTY + x), 8);
             cr_bar_init(BAR(B_PFULL + x), 1);
-            cr_bar_init(BAR(B_PEMPTY + x), 18);
-            cr_bar_init(BAR(B_OUT + x), 8);
+            cr_bar_init(BAR(B_PEMPTY + x), 17);
         }
         for (int s = 0; s < cfg::kStages; ++s) {
             cr_bar_init(FULL(s), 1);
@@ -466,33 +499,25 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     __syncthreads();
     cr_tc_after();
     const uint32_t tmem = tmem_at;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    cr_wait_previous();
+    if (A.to_pfx) cr_launch_next();  // k_attn_few of the same call takes the SMs as they come free
 
     uint32_t pieces = 0;  // their number so far; they take two places in turn
 
     if (warp >= 16) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp == 17) {
         // ---- copies ----
-        if (lane == 0) {
-            cr_tma_prefetch_map(&map_q);
-            cr_tma_prefetch_map(&map_k);
-            cr_tma_prefetch_map(&map_v);
-        }
         const uint32_t q_bytes = A.G * A.tq * 128 * cfg::kChunks;
-        uint32_t stage = 0, phase = 0, outs = 0;
+        uint32_t stage = 0, phase = 0;
         walk w;
         w.begin(A.start, A.blk);
         for (;;) {
             const bool more = w.next();
             if (!cr_bar_wait(BAR(B_PEMPTY + (pieces & 1)), ((pieces >> 1) & 1) ^ 1, &gave_up)) goto out;
-            // tiles whose rows are all queries of the block, in a piece that ends its block
-            const int whole = A.o_copy && more && w.slot() < 0 ? (w.k.ntok >= (int)A.tq) + 2 * (w.k.ntok == 2 * (int)A.tq) : 0;
             if (lane == 0) {
                 volatile rows_piece *p = piece + (pieces & 1);
                 p->n = more ? (int)(w.t1 - w.t0) : 0;
                 if (more) {
-                    p->whole = whole;
-                    p->outs = (int)outs;
                     p->row0 = w.k.row0;
                     p->ntok = w.k.ntok;
                     p->klen = w.k.klen;
@@ -507,7 +532,6 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             }
             __syncwarp();
             if (!more) break;
-            outs += __popc(whole);
             const int two = w.k.ntok > (int)A.tq;
             if (!cr_bar_wait(BAR(B_QEMPTY), (pieces & 1) ^ 1, &gave_up)) goto out;
             ++pieces;
@@ -523,31 +547,28 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             const uint32_t box = lane & (boxes - 1), ch = lane / boxes;
             const uint32_t at = ch * (kRowsTile * 128) + ((box << A.box_log2) * 128);
             const int32_t *row = A.paged ? A.table + (uint64_t)w.k.kbase * A.max_pages : nullptr;
-            bool on_v = false;  // of the tile whose values come next
-            int y_v = 0, pg_v = 0;
-            for (uint32_t t = w.t0; t <= w.t1; ++t) {
+            for (uint32_t t = w.t0; t < w.t1; ++t) {
                 const int key = (int)(t * kRowsTile + (box << A.box_log2));
                 // packed keys come as one box; its rows behind the sequence are never used
-                const bool on = t < w.t1 && lane < boxes * cfg::kChunks && (!A.paged || key < w.k.klen);
+                const bool on = lane < boxes * cfg::kChunks && (!A.paged || key < w.k.klen);
                 int y = w.k.kbase + key, pg = 0;
                 if (A.paged) {
                     if (on) pg = __ldg(row + ((uint32_t)key >> A.page_log2));
                     y = key & ((1 << A.page_log2) - 1);
                 }
-                const uint32_t bytes =
-                    (__popc(__ballot_sync(~0u, on)) + __popc(__ballot_sync(~0u, on_v))) * A.box_rows * 128;
-                if (!cr_bar_wait(EMPTY(stage), phase ^ 1, &gave_up)) goto out;
-                if (lane == 0) cr_bar_expect(FULL(stage), bytes);
-                __syncwarp();
-                const uint32_t dst = ring + stage * 2 * cfg::kTile + at;
-                if (on_v) cr_tma_load(dst, &map_v, FULL(stage), (int)ch * 64, y_v, (int)w.h, pg_v);
-                if (on) cr_tma_load(dst + cfg::kTile, &map_k, FULL(stage), (int)ch * 64, y, (int)w.h, pg);
-                on_v = on;
-                y_v = y;
-                pg_v = pg;
-                if (++stage == cfg::kStages) {
-                    stage = 0;
-                    phase ^= 1;
+                const uint32_t bytes = __popc(__ballot_sync(~0u, on)) * A.box_rows * 128;
+#pragma unroll
+                for (int v = 0; v < 2; ++v) {
+                    if (!cr_bar_wait(EMPTY(stage), phase ^ 1, &gave_up)) goto out;
+                    if (lane == 0) cr_bar_expect(FULL(stage), bytes);
+                    __syncwarp();
+                    if (on)
+                        cr_tma_load(ring + stage * cfg::kTile + at, v ? &map_v : &map_k, FULL(stage), (int)ch * 64, y,
+                                    (int)w.h, pg);
+                    if (++stage == cfg::kStages) {
+                        stage = 0;
+                        phase ^= 1;
+                    }
                 }
             }
         }
@@ -557,7 +578,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         const uint32_t id_s = cr_idesc(BF16, 128, 128, false), id_o = cr_idesc(BF16, 128, D, true);
         uint32_t stage = 0, phase = 0, pphase[2] = {0, 0}, ophase[2] = {0, 0};
         auto scores = [&](int x, uint32_t st) {
-            const uint32_t a = sq + x * cfg::kTile, b = ring + st * 2 * cfg::kTile + cfg::kTile;
+            const uint32_t a = sq + x * cfg::kTile, b = ring + st * cfg::kTile;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {
                 const uint32_t off = (i / 4) * (kRowsTile * 128) + (i % 4) * 32;
@@ -566,7 +587,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         };
         // 16 keys a step: of each thread's 64 keys the first half (part 0), then the second
         auto values = [&](int x, uint32_t st, int part, bool first) {
-            const uint32_t b = ring + st * 2 * cfg::kTile;
+            const uint32_t b = ring + st * cfg::kTile;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int i = (e >> 1) * 4 + part * 2 + (e & 1);
@@ -581,7 +602,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             }
         };
         // weights x values of a tile, then the next scores
-        auto turn = [&](int x, bool first, bool more) {
+        auto turn = [&](int x, uint32_t vs, bool first, bool more) {
             if (first) {
                 if (!cr_bar_wait(BAR(B_OEMPTY + x), ophase[x] ^ 1, &gave_up)) return false;
                 ophase[x] ^= 1;
@@ -590,7 +611,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             for (int part = 0; part < 2; ++part) {
                 if (!cr_bar_wait(BAR(B_PREADY + 2 * x + part), pphase[x], &gave_up)) return false;
                 cr_tc_after();
-                values(x, stage, part, first);
+                values(x, vs, part, first);
             }
             pphase[x] ^= 1;
             if (more) {
@@ -622,41 +643,22 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             forward();
             for (uint32_t j = 0; j < n; ++j) {
                 const bool more = j + 1 < n;
+                const uint32_t vs = stage;
                 if (!cr_bar_wait(FULL(stage), phase, &gave_up)) goto out;
-                if (!turn(0, j == 0, more)) goto out;
-                if (two && !turn(1, j == 0, more)) goto out;
-                cr_tc_commit(EMPTY(stage), me);
-                if (j + 2 == n) cr_tc_commit(BAR(B_QEMPTY), me);
                 forward();
+                if (more && !cr_bar_wait(FULL(stage), phase, &gave_up)) goto out;
+                if (!turn(0, vs, j == 0, more)) goto out;
+                if (two && !turn(1, vs, j == 0, more)) goto out;
+                cr_tc_commit(EMPTY(vs), me);
+                if (more) {
+                    cr_tc_commit(EMPTY(stage), me);
+                    forward();
+                }
+                if (j + 2 == n) cr_tc_commit(BAR(B_QEMPTY), me);
             }
         }
         cr_tc_commit(BAR(B_DONE), me);  // the shared memory is in use until the last product has ended
         cr_bar_wait(BAR(B_DONE), 0, &gave_up);
-    } else if (warp == 18) {
-        // ---- copies of outputs ----
-        uint32_t done[2] = {0, 0};
-        for (;; ++pieces) {
-            if (!cr_bar_wait(BAR(B_PFULL + (pieces & 1)), (pieces >> 1) & 1, &gave_up)) goto out;
-            const volatile rows_piece *p = piece + (pieces & 1);
-            const int n = p->n, whole = p->whole, h = p->h, row0 = p->row0;
-            __syncwarp();
-            if (lane == 0) cr_bar_arrive(BAR(B_PEMPTY + (pieces & 1)));
-            if (n == 0) break;
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                if (!(whole >> x & 1)) continue;
-                if (!cr_bar_wait(BAR(B_OUT + x), done[x] & 1, &gave_up)) goto out;
-                ++done[x];
-                if (lane == 0) {
-                    for (int ch = 0; ch < cfg::kChunks; ++ch)
-                        cr_tma_store(&map_o, sq + cfg::kOut + ch * (kRowsTile * 128), ch * 64, 0, h, row0 + x * (int)A.tq);
-                    cr_tma_store_read();
-                    cr_bar_arrive(BAR(B_OUTFREE));
-                }
-                __syncwarp();
-            }
-        }
-        if (lane == 0) cr_tma_store_done();
     } else if (warp < 16) {
         // ---- softmax: two threads a row ----
         asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
@@ -739,14 +741,14 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                 // keys behind the sequence's end have weight zero, but what stands there may be
                 // no number: their rows of v become zeros
                 if (j == tail) {
-                    const uint32_t at = (uint32_t)p->stage + j + 1;
+                    const uint32_t at = (uint32_t)p->stage + 2 * j + 1;
                     const uint32_t st = at % cfg::kStages, ph = (uint32_t)p->phase ^ ((at / cfg::kStages) & 1);
                     if (!cr_bar_wait(FULL(st), ph, &gave_up)) goto left;
                     if ((int)row >= (p->klen & (kRowsTile - 1))) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
                             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(
-                                             ring + st * 2 * cfg::kTile + half * (kRowsTile * 128) + row * 128 + i * 16),
+                                             ring + st * cfg::kTile + half * (kRowsTile * 128) + row * 128 + i * 16),
                                          "r"(0)
                                          : "memory");
                     }
@@ -809,11 +811,6 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                         make_float2(m == -INFINITY ? m : m * c, l);
             } else {
                 const float inv = l == 0.f ? 0.f : 1.f / l;
-                const bool copied = p->whole >> x & 1;
-                if (copied) {  // the last tile that was copied has been read
-                    const int use = p->outs + (x && (p->whole & 1));
-                    if (!cr_bar_wait(BAR(B_OUTFREE), (use & 1) ^ 1, &gave_up)) goto left;
-                }
 #pragma unroll 1
                 for (int i = 0; i < D / 2; i += 16) {
                     uint32_t o[16];
@@ -822,21 +819,6 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) o[e] = l == 0.f ? 0u : __float_as_uint(__uint_as_float(o[e]) * inv);
                     const int d0 = half * (D / 2) + i;
-                    if (copied) {
-                        const uint32_t at = sq + cfg::kOut + (d0 / 64) * (kRowsTile * 128) + row * 128;
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const uint32_t u = (uint32_t)(d0 % 64) / 8 + e;
-                            const uint32_t *f = o + 8 * e;
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + ((u ^ (row & 7)) << 4)),
-                                         "r"(cr_pack16<BF16>(__uint_as_float(f[0]), __uint_as_float(f[1]))),
-                                         "r"(cr_pack16<BF16>(__uint_as_float(f[2]), __uint_as_float(f[3]))),
-                                         "r"(cr_pack16<BF16>(__uint_as_float(f[4]), __uint_as_float(f[5]))),
-                                         "r"(cr_pack16<BF16>(__uint_as_float(f[6]), __uint_as_float(f[7])))
-                                         : "memory");
-                        }
-                        continue;
-                    }
                     if (!valid) continue;
                     if (A.to_pfx) {
                         float *dst = A.pfx + (tk * A.q_heads + head) * D + d0;
@@ -864,11 +846,6 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                     else if (A.lse)
                         A.lse[tk * A.q_heads + head] = lse2 * 0.693147180559945309f;
                 }
-                if (copied) {
-                    cr_fence_async_smem();
-                    __syncwarp();
-                    if (lane == 0) cr_bar_arrive(BAR(B_OUT + x));
-                }
             }
             cr_tc_before();
             __syncwarp();
@@ -889,7 +866,7 @@ out:
     }
     cr_tc_before();
     __syncthreads();
-    asm volatile("griddepcontrol.launch_dependents;");
+    cr_launch_next();
     if (warp == 16) {
         cr_tc_after();
         cr_tmem_free(tmem, 512);
@@ -909,13 +886,12 @@ __global__ void __launch_bounds__(256) k_attn_join(const __grid_constant__ attn_
     constexpr int kGroups = 256 / RW, kPer = D / 4 / kGroups;  // threads of a row, columns / 4 of each
     __shared__ float wgt[32][RW];
     __shared__ float red[2][kGroups][RW];
-    __shared__ uint32_t ends;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    cr_launch_next();
+    cr_wait_previous();
     const uint32_t c = blockIdx.x + 1;
+    const uint32_t np = A.start[c].pieces;
+    if (np == 0) return;
     const attn_start s = A.start[c];
-    if (s.pos >= s.N || s.tile == 0) return;
-    const unsigned long long begin = s.pos - s.tile - kExtra, end = begin + kExtra + (uint32_t)s.k.nt;
-    if (A.start[c - 1].pos > begin) return;
     // row of the piece
     const uint32_t r = blockIdx.y * RW + threadIdx.x % RW, grp = threadIdx.x / RW;
     bool valid;
@@ -932,28 +908,13 @@ __global__ void __launch_bounds__(256) k_attn_join(const __grid_constant__ attn_
         head = s.head * A.G + rr % A.G;
         tk = (uint64_t)s.k.row0 + tok;
     }
-    // its pieces: stretches c-1 .. last
-    if (threadIdx.x < 32) {
-        uint32_t last = c;
-        for (uint32_t p0 = c;; p0 += 32) {
-            const uint32_t p = p0 + threadIdx.x;
-            const bool in = p < gridDim.x + 1 && A.start[p].pos < end;
-            const uint32_t b = __ballot_sync(~0u, in);
-            last = p0 + __popc(b);
-            if (b != ~0u) break;
-        }
-        if (threadIdx.x == 0) ends = last;
-    }
-    __syncthreads();
-    const uint32_t np = ends - (c - 1);
     if (blockIdx.y * RW / kRowsTile && !__syncthreads_or(valid)) return;  // the second tile is not in use
     const float2 *ml = reinterpret_cast<const float2 *>(A.part_ml);
     const float4 *part = reinterpret_cast<const float4 *>(A.part);
     auto place = [&](uint32_t i) { return (uint64_t)(i == 0 ? 2 * c - 1 : 2 * (c - 1 + i)); };
-    auto is_empty = [&](uint32_t i) { return i && A.start[c - 1 + i].pos == A.start[c + i].pos; };
     float m = -INFINITY;
     for (uint32_t i = grp; i < np; i += kGroups)
-        if (!is_empty(i)) m = fmaxf(m, ml[place(i) * RP + r].x);
+        m = fmaxf(m, ml[place(i) * RP + r].x);
     red[0][grp][threadIdx.x % RW] = m;
     __syncthreads();
 #pragma unroll
@@ -966,8 +927,7 @@ __global__ void __launch_bounds__(256) k_attn_join(const __grid_constant__ attn_
         const uint32_t ni = min(32u, np - i0);
         __syncthreads();
         for (uint32_t i = grp; i < ni; i += kGroups) {
-            float2 q = make_float2(-INFINITY, 0.f);
-            if (!is_empty(i0 + i)) q = ml[place(i0 + i) * RP + r];
+            const float2 q = ml[place(i0 + i) * RP + r];
             const float f = q.x == -INFINITY ? 0.f : cr_exp2(q.x - m);
             wgt[i][threadIdx.x % RW] = f;
             l += q.y * f;
@@ -976,7 +936,7 @@ __global__ void __launch_bounds__(256) k_attn_join(const __grid_constant__ attn_
 #pragma unroll 4
         for (uint32_t i = 0; i < ni; ++i) {
             const float f = wgt[i][threadIdx.x % RW];
-            if (f == 0.f) continue;  // sees none of these keys, or no piece
+            if (f == 0.f) continue;  // sees none of these keys
 #pragma unroll
             for (int e = 0; e < kPer; ++e) {
                 const float4 v = part[(place(i0 + i) * (D / 4) + grp + e * kGroups) * RP + r];
@@ -1078,6 +1038,11 @@ __global__ void __launch_bounds__(kFewThreads, 2)
 #define QEMPTY (bar + 8u * (2 * cfg::kStages + 1))
 #define JOIN (bar + 8u * (2 * cfg::kStages + 2))
 
+    if (threadIdx.x == 32) {
+        cr_tma_prefetch_map(&map_q);
+        cr_tma_prefetch_map(&map_k);
+        cr_tma_prefetch_map(&map_v);
+    }
     if (threadIdx.x == 0) {
         gave_up = 0;
         for (int s = 0; s < cfg::kStages; ++s) {
@@ -1093,18 +1058,16 @@ __global__ void __launch_bounds__(kFewThreads, 2)
         asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(sq + 16 * i), "r"(0));
     cr_fence_async_smem();
     __syncthreads();
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    // After k_attn_rows of the same call this one needs nothing of it, and the list of work was there before that
+    // began: the wait comes at the end, so that whoever waits for this kernel waits for both.
+    if (!A.after_rows) cr_wait_previous();
+    cr_launch_next();
 
     walk w;
     w.begin(A.start, A.blk);
     uint32_t stage = 0, phase = 0, qphase = 0;
     if (warp == kFewWarps) {
         // ---- copies: a lane brings one box of one column block, keys and values ----
-        if (lane == 0) {
-            cr_tma_prefetch_map(&map_q);
-            cr_tma_prefetch_map(&map_k);
-            cr_tma_prefetch_map(&map_v);
-        }
         const uint32_t boxes = kFewTile >> A.box_log2;
         const uint32_t box = lane & (boxes - 1), ch = lane / boxes;
         while (w.next()) {
@@ -1252,7 +1215,10 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                 if (q4 == 0) join_ml[warp][r4 + 8 * r] = make_float2(m[r] == -INFINITY ? m[r] : m[r] * c, l[r]);
             }
             const int slot = w.slot();
-            const bool from_pfx = w.k.lo > 0 && w.t0 == 0;
+            // a whole block that a shared prefix still joins has a place of its own
+            const bool to_own = slot < 0 && w.k.lo > 0;
+            const uint64_t place = to_own ? (uint64_t)w.k.row0 * A.few_heads + w.h : (uint64_t)slot;
+            float *part = to_own ? A.own : A.part, *part_ml = to_own ? A.own_ml : A.part_ml;
 #pragma unroll
             for (int pass = 0; pass < (WIDE ? 2 : 1) * cfg::kChunks; ++pass) {
                 const int r = pass / cfg::kChunks, ch = pass % cfg::kChunks;
@@ -1267,11 +1233,6 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                     const uint64_t oh = (uint64_t)w.k.row0 * A.q_heads + h0 + row;
                     float mm = -INFINITY, ll = 0.f;
                     for (int v = 0; v < kFewWarps; ++v) mm = fmaxf(mm, join_ml[v][row].x);
-                    float px = -INFINITY;
-                    if (from_pfx) {
-                        px = A.pfx_lse[oh];
-                        mm = fmaxf(mm, px);
-                    }
                     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                     for (int v = 0; v < kFewWarps; ++v) {
@@ -1284,18 +1245,9 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                         s.z += x.z * f;
                         s.w += x.w * f;
                     }
-                    if (px != -INFINITY) {
-                        const float f = cr_exp2(px - mm);
-                        const float4 x = *reinterpret_cast<const float4 *>(A.pfx + oh * D + 4 * d4);
-                        ll += f;
-                        s.x += x.x * f;
-                        s.y += x.y * f;
-                        s.z += x.z * f;
-                        s.w += x.w * f;
-                    }
-                    if (slot >= 0) {
-                        reinterpret_cast<float4 *>(A.part)[((uint64_t)slot * (D / 4) + d4) * 16 + row] = s;
-                        if (d4 == 0) reinterpret_cast<float2 *>(A.part_ml)[(uint64_t)slot * 16 + row] = make_float2(mm, ll);
+                    if (slot >= 0 || to_own) {
+                        reinterpret_cast<float4 *>(part)[(place * (D / 4) + d4) * 16 + row] = s;
+                        if (d4 == 0) reinterpret_cast<float2 *>(part_ml)[place * 16 + row] = make_float2(mm, ll);
                     } else {
                         const float inv = ll == 0.f ? 0.f : 1.f / ll;
                         if (4 * d4 < A.head_dim)
@@ -1316,12 +1268,140 @@ out:
         if (lane == 0) atomicOr(A.status, CR_FLAG_TIMEOUT);
         for (int i = 0; i < 2000; ++i) __nanosleep(1000);
     }
-    asm volatile("griddepcontrol.launch_dependents;");
+    if (A.after_rows) cr_wait_previous();
 #undef FULL
 #undef EMPTY
 #undef QFULL
 #undef QEMPTY
 #undef JOIN
+}
+
+// Joins everything that a single token's heads have: the pieces of its own keys (or its place, where one CTA had them
+// all) and those of its group's shared prefix.  blockIdx: (entry, 16 rows of a key head).
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256)
+    k_attn_decode_join(const __grid_constant__ attn_in F, const __grid_constant__ attn_in R)
+{
+    constexpr int kGroups = 16, kPer = D / 4 / kGroups;
+    __shared__ float wgt[32][16];
+    __shared__ float red[2][kGroups][16];
+    __shared__ uint32_t range[2][2];
+    cr_launch_next();
+    cr_wait_previous();
+    const uint32_t e = blockIdx.x, h = blockIdx.y, kv = h / F.nsub, sub = h % F.nsub;
+    const int prefix = R.of_token[e];  // only entries with a shared prefix have one
+    const unsigned long long nf_all = F.start[0].N, nr_all = R.start[0].N;
+    const attn_blk kf = F.blk[e];
+    const bool shared = kf.lo > 0;
+    attn_blk kr = {};
+    if (shared) kr = R.blk[prefix];
+    // stretches that have a part of each list's block: one warp counts for each list
+    if (threadIdx.x < 64) {
+        const uint32_t which = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        const attn_in &A = which ? R : F;
+        if (!which || shared) {
+            const unsigned long long per = which ? nr_all / (F.few_heads / F.nsub) : nf_all / F.few_heads;
+            const attn_blk &k = which ? kr : kf;
+            const unsigned long long begin = per * (which ? kv : h) + k.at, end = begin + kExtra + (uint32_t)k.nt;
+            uint32_t a = 0, b = 0;
+            for (uint32_t c = 1 + lane; c < A.ncta; c += 32) {
+                const unsigned long long p = A.pos[c];
+                a += p <= begin;
+                b += p < end;
+            }
+            a = __reduce_add_sync(~0u, a);
+            b = __reduce_add_sync(~0u, b);
+            if (lane == 0) {
+                range[which][0] = a;
+                range[which][1] = b;
+            }
+        }
+    }
+    __syncthreads();
+    const uint32_t nf = range[0][1] - range[0][0] + 1, nr = shared ? range[1][1] - range[1][0] + 1 : 0;
+    if (nf == 1 && !shared) return;  // written already
+    const uint32_t r = threadIdx.x & 15, col = threadIdx.x & 15, grp = threadIdx.x >> 4;
+    const bool valid = sub * 16 + r < F.G;
+    const uint32_t head = kv * F.G + sub * 16 + r;
+    const uint64_t oh = (uint64_t)e * F.q_heads + head;
+    const uint32_t rt = (uint32_t)((int)e - kr.row0);  // token of the prefix' block
+    const uint32_t rr = shared ? rt / R.tq * kRowsTile + rt % R.tq * R.G + sub * 16 + r : 0;
+    const uint64_t own = (uint64_t)e * F.few_heads + h;
+    auto slot = [](uint32_t first, uint32_t i) { return (uint64_t)(i == 0 ? 2 * first + 1 : 2 * (first + i)); };
+    auto ml = [&](uint32_t i) {
+        if (!valid) return make_float2(-INFINITY, 0.f);
+        if (i < nf)
+            return nf == 1 ? reinterpret_cast<const float2 *>(F.own_ml)[own * 16 + r]
+                           : reinterpret_cast<const float2 *>(F.part_ml)[slot(range[0][0], i) * 16 + r];
+        return nr == 1 ? make_float2(F.pfx_lse[oh], 1.f)
+                       : reinterpret_cast<const float2 *>(R.part_ml)[slot(range[1][0], i - nf) * (2 * kRowsTile) + rr];
+    };
+    auto data = [&](uint32_t i, uint32_t d4) {
+        if (i < nf)
+            return nf == 1 ? reinterpret_cast<const float4 *>(F.own)[(own * (D / 4) + d4) * 16 + r]
+                           : reinterpret_cast<const float4 *>(F.part)[(slot(range[0][0], i) * (D / 4) + d4) * 16 + r];
+        return nr == 1 ? *reinterpret_cast<const float4 *>(F.pfx + oh * D + 4 * d4)
+                       : reinterpret_cast<const float4 *>(
+                             R.part)[(slot(range[1][0], i - nf) * (D / 4) + d4) * (2 * kRowsTile) + rr];
+    };
+    const uint32_t n = nf + nr;
+    float m = -INFINITY;
+    for (uint32_t i = grp; i < n; i += kGroups) m = fmaxf(m, ml(i).x);
+    red[0][grp][col] = m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kGroups; ++i) m = fmaxf(m, red[0][i][col]);
+    float l = 0.f;
+    float4 o[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (uint32_t i0 = 0; i0 < n; i0 += 32) {
+        const uint32_t ni = min(32u, n - i0);
+        __syncthreads();
+        for (uint32_t i = grp; i < ni; i += kGroups) {
+            const float2 q = ml(i0 + i);
+            const float f = q.x == -INFINITY ? 0.f : cr_exp2(q.x - m);
+            wgt[i][col] = f;
+            l += q.y * f;
+        }
+        __syncthreads();
+        for (uint32_t j = 0; j < ni; j += 8) {  // eight pieces' loads in flight
+            float4 v[8][kPer];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int x = 0; x < kPer; ++x) {
+                    v[i][x] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (j + i < ni && wgt[j + i][col] != 0.f) v[i][x] = data(i0 + j + i, grp + x * kGroups);
+                }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float f = j + i < ni ? wgt[j + i][col] : 0.f;
+#pragma unroll
+                for (int x = 0; x < kPer; ++x) {
+                    o[x].x += v[i][x].x * f;
+                    o[x].y += v[i][x].y * f;
+                    o[x].z += v[i][x].z * f;
+                    o[x].w += v[i][x].w * f;
+                }
+            }
+        }
+    }
+    red[1][grp][col] = l;
+    __syncthreads();
+    l = 0.f;
+#pragma unroll
+    for (int i = 0; i < kGroups; ++i) l += red[1][i][col];
+    if (!valid) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) {
+        const uint32_t d = 4 * (grp + x * kGroups);
+        if (d < F.head_dim)
+            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(F.o) + e * F.o_token + head * F.o_head + d) =
+                make_uint2(cr_pack16<BF16>(o[x].x * inv, o[x].y * inv), cr_pack16<BF16>(o[x].z * inv, o[x].w * inv));
+    }
+    if (grp == 0 && F.lse) F.lse[oh] = (l == 0.f ? -INFINITY : m + log2f(l)) * 0.693147180559945309f;
 }
 
 // ---- host -------------------------------------------------------------------------------------
@@ -1401,8 +1481,8 @@ uint32_t ilog2(uint32_t v)
 // Scratch of one list of work.
 struct plan_mem {
     size_t bytes;
-    size_t blk, cum, start, first;
-    plan_mem(uint32_t max_blk, uint32_t max_cta, uint32_t n)
+    size_t blk, cum, start, pos, first, of_token;
+    plan_mem(uint32_t max_blk, uint32_t max_cta, uint32_t n, uint32_t tokens)  // tokens: of groups
     {
         bytes = 0;
         auto take = [&](size_t b) {
@@ -1413,7 +1493,9 @@ struct plan_mem {
         blk = take(sizeof(attn_blk) * ((size_t)max_blk + 1));
         cum = take(max_blk > kPlanShared ? 8 * ((size_t)max_blk + 2) : 0);
         start = take(sizeof(attn_start) * ((size_t)max_cta + 2));
+        pos = take(8 * ((size_t)max_cta + 2));
         first = take(n > kPlanShared ? 4 * ((size_t)n + 1) : 0);
+        of_token = take(4 * (size_t)tokens);
     }
     void point(char *base, plan_in &p, attn_in &a) const
     {
@@ -1422,7 +1504,12 @@ struct plan_mem {
         p.start = reinterpret_cast<attn_start *>(base + start);
         p.first = reinterpret_cast<uint32_t *>(base + first);
         a.blk = p.blk;
+        p.pos = reinterpret_cast<unsigned long long *>(base + pos);
+        a.pos = p.pos;
+        p.of_token = reinterpret_cast<int32_t *>(base + of_token);
         a.start = p.start;
+        a.of_token = p.of_token;
+        a.ncta = p.max_cta;
     }
 };
 
@@ -1431,7 +1518,7 @@ bool aligned(const void *p, uint64_t a, uint64_t b) { return ((uintptr_t)p & 15)
 int check_heads(cr_ctx *ctx, const char *who, const cr_attn_args *a, uint32_t dtype, uint32_t kv_heads, uint32_t dim)
 {
     if (dtype > CR_DTYPE_FP16) return cr_fail(ctx, CR_EINVAL, "%s: dtype %u", who, dtype);
-    if (kv_heads == 0 || kv_heads > 65536 || a->q_heads == 0 || a->q_heads % kv_heads || a->q_heads / kv_heads > 128)
+    if (kv_heads == 0 || kv_heads > 4096 || a->q_heads == 0 || a->q_heads % kv_heads || a->q_heads / kv_heads > 128)
         return cr_fail(ctx, CR_EINVAL, "%s: %u query heads on %u key heads", who, a->q_heads, kv_heads);
     if (dim == 0 || dim > 128 || (dim & 7)) return cr_fail(ctx, CR_EINVAL, "%s: head_dim %u", who, dim);
     if (!(a->scale > 0.f) || isinf(a->scale)) return cr_fail(ctx, CR_EINVAL, "%s: scale must be finite and positive", who);
@@ -1466,26 +1553,6 @@ void fill_common(attn_in &A, cr_ctx *ctx, const cr_attn_args *a, const kv_desc &
     }
 }
 
-// Launches whose prologue may run before the kernel ahead of them on the stream has ended; they wait for its
-// end (griddepcontrol.wait) before they read anything of it.
-template <typename... P, typename... T>
-int launch_early(cr_ctx *ctx, const char *what, void (*kern)(P...), dim3 grid, uint32_t block, size_t smem, T... args)
-{
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(block);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = ctx->stream;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, kern, args...) != cudaSuccess) return cr_check_launch(ctx, what);
-    ctx->launches++;
-    return CR_OK;
-}
-
 int query_map(cr_ctx *ctx, CUtensorMap *map, const attn_in &A, const kv_desc &K, const cr_attn_args *a, uint32_t heads,
               uint32_t tokens)
 {
@@ -1497,20 +1564,16 @@ int query_map(cr_ctx *ctx, CUtensorMap *map, const attn_in &A, const kv_desc &K,
 template <int D, bool BF16>
 int launch_rows(cr_ctx *ctx, const attn_in &A, const kv_desc &K, const cr_attn_args *a, uint32_t ctas)
 {
-    CUtensorMap mq, mk, mv, mo;
+    CUtensorMap mq, mk, mv;
     CR_TRY(query_map(ctx, &mq, A, K, a, A.G, A.tq));
     CR_TRY(kv_map(ctx, &mk, K, false, A.box_rows));
     CR_TRY(kv_map(ctx, &mv, K, true, A.box_rows));
-    // outputs as the queries: same dims and boxes
-    const uint64_t dim[4] = {K.dim, A.G, K.heads, a->n_tokens}, st[3] = {a->o_head, a->o_head * A.G, a->o_token};
-    const uint32_t box[3] = {A.G, 1, A.tq};
-    CR_TRY(encode_map(ctx, &mo, BF16, a->d_o, dim, st, box, false));
     auto kern = k_attn_rows<D, BF16>;
     static const cudaError_t raised = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, rows_cfg<D>::kSmem);
     if (raised != cudaSuccess) return cr_fail(ctx, CR_ECUDA, "k_attn_rows: %s", cudaGetErrorString(raised));
-    CR_TRY(launch_early(ctx, "k_attn_rows", kern, dim3(ctas), kRowsThreads, rows_cfg<D>::kSmem, A, mq, mk, mv, mo));
-    if (ctas > 1)
-        CR_TRY(launch_early(ctx, "k_attn_join", k_attn_join<D, BF16, 2 * kRowsTile, 32>, dim3(ctas - 1, 8), 256, 0, A));
+    CR_TRY(cr_launch_early(ctx, "k_attn_rows", kern, dim3(ctas), kRowsThreads, rows_cfg<D>::kSmem, A, mq, mk, mv));
+    if (ctas > 1 && !A.to_pfx)
+        CR_TRY(cr_launch_early(ctx, "k_attn_join", k_attn_join<D, BF16, 2 * kRowsTile, 32>, dim3(ctas - 1, 8), 256, 0, A));
     return CR_OK;
 }
 
@@ -1521,7 +1584,7 @@ int rows(cr_ctx *ctx, const attn_in &A, const kv_desc &K, const cr_attn_args *a,
 }
 
 template <int D, bool BF16, bool WIDE>
-int launch_few(cr_ctx *ctx, const attn_in &A, const kv_desc &K, const cr_attn_args *a, uint32_t ctas)
+int launch_few(cr_ctx *ctx, const attn_in &A, const attn_in *R, const kv_desc &K, const cr_attn_args *a, uint32_t ctas)
 {
     CUtensorMap mq, mk, mv;
     CR_TRY(query_map(ctx, &mq, A, K, a, A.G < 16 ? A.G : 16, 1));
@@ -1530,21 +1593,23 @@ int launch_few(cr_ctx *ctx, const attn_in &A, const kv_desc &K, const cr_attn_ar
     auto kern = k_attn_few<D, BF16, WIDE>;
     static const cudaError_t raised = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, few_cfg<D>::kSmem);
     if (raised != cudaSuccess) return cr_fail(ctx, CR_ECUDA, "k_attn_few: %s", cudaGetErrorString(raised));
-    CR_TRY(launch_early(ctx, "k_attn_few", kern, dim3(ctas), kFewThreads, few_cfg<D>::kSmem, A, mq, mk, mv));
-    if (ctas > 1)
-        CR_TRY(launch_early(ctx, "k_attn_join", k_attn_join<D, BF16, 16, 16>, dim3(ctas - 1), 256, 0, A));
+    CR_TRY(cr_launch_early(ctx, "k_attn_few", kern, dim3(ctas), kFewThreads, few_cfg<D>::kSmem, A, mq, mk, mv));
+    if (R)
+        CR_TRY(cr_launch_early(ctx, "k_attn_decode_join", k_attn_decode_join<D, BF16>, dim3(a->n, A.few_heads), 256, 0, A, *R));
+    else if (ctas > 1)
+        CR_TRY(cr_launch_early(ctx, "k_attn_join", k_attn_join<D, BF16, 16, 16>, dim3(ctas - 1), 256, 0, A));
     return CR_OK;
 }
 
-int few(cr_ctx *ctx, const attn_in &A, const kv_desc &K, const cr_attn_args *a, uint32_t ctas)
+int few(cr_ctx *ctx, const attn_in &A, const attn_in *R, const kv_desc &K, const cr_attn_args *a, uint32_t ctas)
 {
     const bool wide = A.G > 8;
     if (K.dim <= 64) {
-        if (K.bf16) return wide ? launch_few<64, true, true>(ctx, A, K, a, ctas) : launch_few<64, true, false>(ctx, A, K, a, ctas);
-        return wide ? launch_few<64, false, true>(ctx, A, K, a, ctas) : launch_few<64, false, false>(ctx, A, K, a, ctas);
+        if (K.bf16) return wide ? launch_few<64, true, true>(ctx, A, R, K, a, ctas) : launch_few<64, true, false>(ctx, A, R, K, a, ctas);
+        return wide ? launch_few<64, false, true>(ctx, A, R, K, a, ctas) : launch_few<64, false, false>(ctx, A, R, K, a, ctas);
     }
-    if (K.bf16) return wide ? launch_few<128, true, true>(ctx, A, K, a, ctas) : launch_few<128, true, false>(ctx, A, K, a, ctas);
-    return wide ? launch_few<128, false, true>(ctx, A, K, a, ctas) : launch_few<128, false, false>(ctx, A, K, a, ctas);
+    if (K.bf16) return wide ? launch_few<128, true, true>(ctx, A, R, K, a, ctas) : launch_few<128, true, false>(ctx, A, R, K, a, ctas);
+    return wide ? launch_few<128, false, true>(ctx, A, R, K, a, ctas) : launch_few<128, false, false>(ctx, A, R, K, a, ctas);
 }
 
 // Pieces of a list of work: two per CTA at most.
@@ -1584,17 +1649,16 @@ int attn_many(cr_ctx *ctx, const cr_attn_args *a, const kv_desc &K)
         p.n_seqs = K.pg->n_seqs;
         p.max_len = K.pg->max_pages * K.pg->page;
     }
-    A.o_copy = 1;
-    p.max_cta = (uint32_t)ctx->num_sms;
-    const plan_mem mem(p.max_blk, p.max_cta, a->n);
+    p.max_cta = min((uint32_t)ctx->num_sms, kMaxCtas);
+    const plan_mem mem(p.max_blk, p.max_cta, a->n, 0);
     void *base;
     CR_TRY(cr_scratch(ctx, SCR_ATTN_PLAN, mem.bytes, &base));
     mem.point(static_cast<char *>(base), p, A);
     CR_TRY(part_mem(ctx, SCR_ATTN_PART, A, p.max_cta, 2 * kRowsTile, K.dim <= 64 ? 64 : 128));
     if (K.paged)
-        CR_LAUNCH(ctx, k_attn_plan<PLAN_PAGED>, 1, 1024, 0, p, p, ctx->d_status);
+        CR_TRY(cr_launch_early(ctx, "k_attn_plan", k_attn_plan<PLAN_PAGED>, dim3(1), 1024, 0, p, p, ctx->d_status));
     else
-        CR_LAUNCH(ctx, k_attn_plan<PLAN_PACKED>, 1, 1024, 0, p, p, ctx->d_status);
+        CR_TRY(cr_launch_early(ctx, "k_attn_plan", k_attn_plan<PLAN_PACKED>, dim3(1), 1024, 0, p, p, ctx->d_status));
     return rows(ctx, A, K, a, p.max_cta);
 }
 
@@ -1677,6 +1741,7 @@ extern "C" int cr_attn_decode(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t la
     if (n_groups && (!d_group_off || !d_shared)) return cr_fail(ctx, CR_EINVAL, "cr_attn_decode: NULL groups");
     if (n_groups > (1u << 24)) return cr_fail(ctx, CR_EINVAL, "cr_attn_decode: %u groups", n_groups);
     if (args->n == 0) return CR_OK;
+    if (args->n == 1) n_groups = 0;  // nobody to share with
 
     const uint32_t D = K.dim <= 64 ? 64 : 128;
     attn_in F = {}, R = {};
@@ -1699,18 +1764,18 @@ extern "C" int cr_attn_decode(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t la
     f.n_seqs = pages->n_seqs;
     f.n_groups = n_groups;
     f.max_len = pages->max_pages * pages->page;
-    f.heads = K.heads * F.nsub;
-    f.max_cta = 2 * (uint32_t)ctx->num_sms;
+    f.heads = F.few_heads = K.heads * F.nsub;
+    f.max_cta = min(2 * (uint32_t)ctx->num_sms, kMaxCtas);
     f.min_tiles = kFewMinTiles;
     plan_in g = f;
     g.cu_q = d_group_off;
     g.heads = K.heads;
     g.tok_blk = 2 * R.tq;
     g.max_blk = args->n / g.tok_blk + (n_groups < args->n ? n_groups : args->n);
-    g.max_cta = (uint32_t)ctx->num_sms;
+    g.max_cta = min((uint32_t)ctx->num_sms, kMaxCtas);
     g.min_tiles = kRowsMinTiles;
 
-    const plan_mem mf(f.max_blk, f.max_cta, f.n), mg(g.max_blk, g.max_cta, n_groups);
+    const plan_mem mf(f.max_blk, f.max_cta, f.n, 0), mg(g.max_blk, g.max_cta, n_groups, f.n);
     void *base;
     CR_TRY(cr_scratch(ctx, SCR_ATTN_PLAN, mf.bytes + mg.bytes, &base));
     mf.point(static_cast<char *>(base), f, F);
@@ -1718,16 +1783,19 @@ extern "C" int cr_attn_decode(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t la
     CR_TRY(part_mem(ctx, SCR_ATTN_FEW, F, f.max_cta, 16, D));
     if (n_groups) {
         CR_TRY(part_mem(ctx, SCR_ATTN_PART, R, g.max_cta, 2 * kRowsTile, D));
-        const size_t heads = (size_t)args->n * args->q_heads;
+        const size_t heads = (size_t)args->n * args->q_heads, own = (size_t)args->n * F.few_heads * 16;
         void *p;
-        CR_TRY(cr_scratch(ctx, SCR_ATTN_PFX, heads * (D + 1) * 4, &p));
+        CR_TRY(cr_scratch(ctx, SCR_ATTN_PFX, ((heads + own) * (D + 1) + own) * 4, &p));
         F.pfx = R.pfx = static_cast<float *>(p);
-        F.pfx_lse = R.pfx_lse = F.pfx + heads * D;
+        F.own = F.pfx + heads * D;
+        F.own_ml = F.own + own * D;
+        F.pfx_lse = R.pfx_lse = F.own_ml + 2 * own;
         R.to_pfx = 1;
-        CR_LAUNCH(ctx, k_attn_plan<PLAN_FEW>, 2, 1024, 0, f, g, ctx->d_status);
+        F.after_rows = 1;
+        CR_TRY(cr_launch_early(ctx, "k_attn_plan", k_attn_plan<PLAN_FEW>, dim3(2), 1024, 0, f, g, ctx->d_status));
         CR_TRY(rows(ctx, R, K, args, g.max_cta));
     } else {
-        CR_LAUNCH(ctx, k_attn_plan<PLAN_FEW>, 1, 1024, 0, f, f, ctx->d_status);
+        CR_TRY(cr_launch_early(ctx, "k_attn_plan", k_attn_plan<PLAN_FEW>, dim3(1), 1024, 0, f, f, ctx->d_status));
     }
-    return few(ctx, F, K, args, f.max_cta);
+    return few(ctx, F, n_groups ? &R : nullptr, K, args, f.max_cta);
 }

@@ -180,6 +180,31 @@ int cr_check_launch(cr_ctx *ctx, const char *what);
         CR_TRY(cr_check_launch((ctx), #kern));                             \
     } while (0)
 
+// Launches of kernels that may begin before the one ahead of them on the stream has ended: each waits for its end
+// (cr_wait_previous) before it touches memory, and lets the next begin (cr_launch_next), so that launch latencies
+// and prologues overlap (a chain of small kernels on the legacy stream: 3.1 us a launch, 1.7 us so).
+#ifdef __CUDACC__
+__device__ __forceinline__ void cr_wait_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void cr_launch_next() { asm volatile("griddepcontrol.launch_dependents;"); }
+#endif
+template <typename... P, typename... T>
+static inline int cr_launch_early(cr_ctx *ctx, const char *what, void (*kern)(P...), dim3 grid, uint32_t block, size_t smem, T... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = ctx->stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kern, args...) != cudaSuccess) return cr_check_launch(ctx, what);
+    ctx->launches++;
+    return CR_OK;
+}
+
 // Bracket work enqueued on `st` with a timed event pair when profiling is on;
 // returns the pair's index (or -1) for cr_prof_end.
 static inline int cr_prof_begin(cr_ctx *ctx, cudaStream_t st, int tag)

@@ -69,6 +69,8 @@ template <int KIND>
 __global__ void __launch_bounds__(1024) k_pages_scan(const __grid_constant__ pages_in P, const __grid_constant__ pages_scan S,
                                                      const int32_t *a, const int32_t *b, const int32_t *c, uint32_t n)
 {
+    cr_launch_next();
+    cr_wait_previous();
     if (KIND != SCAN_NONE && blockIdx.x == 0) {
         unsigned long long base = 0;
         for (uint32_t i0 = 0; i0 < n; i0 += 1024) {
@@ -228,6 +230,8 @@ __device__ __forceinline__ uint16_t *plane(const pages_in &P, uint32_t l2)
 __global__ void __launch_bounds__(128) k_pages_extend(const __grid_constant__ pages_in P, const __grid_constant__ pages_scan S,
                                                       uint32_t n)
 {
+    cr_launch_next();
+    cr_wait_previous();
     __shared__ uint32_t pre[kMaxChunks + 1];
     page_index I;
     I.build(S, pre);
@@ -252,6 +256,8 @@ __global__ void __launch_bounds__(128) k_pages_extend(const __grid_constant__ pa
 __global__ void __launch_bounds__(128) k_pages_fork(const __grid_constant__ pages_in P, const __grid_constant__ pages_scan S,
                                                     uint32_t n)
 {
+    cr_launch_next();
+    cr_wait_previous();
     __shared__ uint32_t pre[kMaxChunks + 1];
     page_index I;
     I.build(S, pre);
@@ -299,6 +305,8 @@ __global__ void __launch_bounds__(128) k_pages_fork(const __grid_constant__ page
 // A block per entry.
 __global__ void __launch_bounds__(128) k_pages_free(const __grid_constant__ pages_in P, const int32_t *seqs)
 {
+    cr_launch_next();
+    cr_wait_previous();
     __shared__ int len;
     const int row = seqs[blockIdx.x];
     if (row < 0 || (uint32_t)row >= P.n_seqs) {
@@ -327,6 +335,8 @@ __global__ void __launch_bounds__(256) k_pages_compact(const __grid_constant__ p
                                                        int32_t *ref_out, int32_t *table_out, int32_t *map, int32_t *live,
                                                        uint32_t b_pages, uint32_t b_table)
 {
+    cr_launch_next();
+    cr_wait_previous();
     __shared__ uint32_t pre[kMaxChunks + 1];
     page_index I;
     I.build(S, pre);
@@ -381,6 +391,8 @@ struct write_in {
 __global__ void __launch_bounds__(128) k_kv_write(const __grid_constant__ pages_in P, const __grid_constant__ write_in W,
                                                   uint32_t layer)
 {
+    cr_launch_next();
+    cr_wait_previous();
     const uint64_t warp = ((uint64_t)blockIdx.x * 128 + threadIdx.x) >> 5;
     const uint64_t t = warp >> W.wpt_log2;
     if (t >= W.n_tokens) return;
@@ -477,7 +489,7 @@ int cr_pages_check(cr_ctx *ctx, const char *who, const cr_kv_pages *pg)
         return cr_fail(ctx, CR_EINVAL, "%s: page of %u tokens: a power of two, 8..256", who, pg->page);
     if (pg->head_dim == 0 || pg->head_dim > 128 || (pg->head_dim & 7))
         return cr_fail(ctx, CR_EINVAL, "%s: head_dim %u: a multiple of 8, 8..128", who, pg->head_dim);
-    if (!pg->layers || pg->layers > 4096 || !pg->kv_heads || pg->kv_heads > 65536 || !pg->n_pages || !pg->n_seqs || !pg->max_pages)
+    if (!pg->layers || pg->layers > 4096 || !pg->kv_heads || pg->kv_heads > 4096 || !pg->n_pages || !pg->n_seqs || !pg->max_pages)
         return cr_fail(ctx, CR_EINVAL, "%s: empty pool (layers, heads, pages, sequences, pages per row)", who);
     if ((uint64_t)pg->n_pages * pg->page >= (1ull << 31) || (uint64_t)pg->max_pages * pg->page >= (1ull << 31) ||
         (uint64_t)pg->n_seqs * pg->max_pages >= (1ull << 40) || pg->n_seqs >= (1u << 31))
@@ -511,8 +523,8 @@ extern "C" int cr_pages_extend(cr_ctx *ctx, const cr_kv_pages *pages, const int3
     const pages_in P = input(ctx, pages);
     pages_scan S;
     CR_TRY(scan_mem(ctx, pages, n, S));
-    CR_LAUNCH(ctx, k_pages_scan<SCAN_EXTEND>, S.chunks + 1, 1024, 0, P, S, d_seqs, d_add, nullptr, n);
-    CR_LAUNCH(ctx, k_pages_extend, n, 128, 0, P, S, n);
+    CR_TRY(cr_launch_early(ctx, "k_pages_scan", k_pages_scan<SCAN_EXTEND>, dim3(S.chunks + 1), 1024, 0, P, S, d_seqs, d_add, d_add, n));
+    CR_TRY(cr_launch_early(ctx, "k_pages_extend", k_pages_extend, dim3(n), 128, 0, P, S, n));
     return CR_OK;
 }
 
@@ -527,8 +539,8 @@ extern "C" int cr_pages_fork(cr_ctx *ctx, const cr_kv_pages *pages, const int32_
     const pages_in P = input(ctx, pages);
     pages_scan S;
     CR_TRY(scan_mem(ctx, pages, n, S));
-    CR_LAUNCH(ctx, k_pages_scan<SCAN_FORK>, S.chunks + 1, 1024, 0, P, S, d_src, d_dst, d_keep, n);
-    CR_LAUNCH(ctx, k_pages_fork, dim3(n, pages->layers < 32 ? 2 * pages->layers : 64), 128, 0, P, S, n);
+    CR_TRY(cr_launch_early(ctx, "k_pages_scan", k_pages_scan<SCAN_FORK>, dim3(S.chunks + 1), 1024, 0, P, S, d_src, d_dst, d_keep, n));
+    CR_TRY(cr_launch_early(ctx, "k_pages_fork", k_pages_fork, dim3(n, pages->layers < 32 ? 2 * pages->layers : 64), 128, 0, P, S, n));
     return CR_OK;
 }
 
@@ -540,7 +552,7 @@ extern "C" int cr_pages_free(cr_ctx *ctx, const cr_kv_pages *pages, const int32_
     CR_TRY(list_check(ctx, "cr_pages_free", n, d_seqs, d_seqs, d_seqs));
     if (!n) return CR_OK;
     const pages_in P = input(ctx, pages);
-    CR_LAUNCH(ctx, k_pages_free, n, 128, 0, P, d_seqs);
+    CR_TRY(cr_launch_early(ctx, "k_pages_free", k_pages_free, dim3(n), 128, 0, P, d_seqs));
     return CR_OK;
 }
 
@@ -556,11 +568,12 @@ extern "C" int cr_pages_compact(cr_ctx *ctx, const cr_kv_pages *pages, int32_t *
     const pages_in P = input(ctx, pages);
     pages_scan S;
     CR_TRY(scan_mem(ctx, pages, 0, S));
-    CR_LAUNCH(ctx, k_pages_scan<SCAN_NONE>, S.chunks, 1024, 0, P, S, nullptr, nullptr, nullptr, 0);
+    const int32_t *none = nullptr;
+    CR_TRY(cr_launch_early(ctx, "k_pages_scan", k_pages_scan<SCAN_NONE>, dim3(S.chunks), 1024, 0, P, S, none, none, none, 0u));
     const uint32_t sms = (uint32_t)ctx->num_sms;
     const uint32_t b_pages = cr_blocks(pages->n_pages, 256, 2 * sms);
     const uint32_t b_table = b_pages + cr_blocks((uint64_t)pages->n_seqs * pages->max_pages, 1024, 2 * sms);
-    CR_LAUNCH(ctx, k_pages_compact, b_table + 8 * sms, 256, 0, P, S, d_ref_out, d_table_out, d_map, d_live, b_pages, b_table);
+    CR_TRY(cr_launch_early(ctx, "k_pages_compact", k_pages_compact, dim3(b_table + 8 * sms), 256, 0, P, S, d_ref_out, d_table_out, d_map, d_live, b_pages, b_table));
     return CR_OK;
 }
 
@@ -585,6 +598,6 @@ extern "C" int cr_kv_write(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t layer
            (32u << W.wpt_log2) < pages->kv_heads * (pages->head_dim / 8))
         ++W.wpt_log2;
     const uint64_t warps = (uint64_t)n_tokens << W.wpt_log2;
-    CR_LAUNCH(ctx, k_kv_write, (uint32_t)((warps + 3) / 4), 128, 0, P, W, layer);
+    CR_TRY(cr_launch_early(ctx, "k_kv_write", k_kv_write, dim3((uint32_t)((warps + 3) / 4)), 128, 0, P, W, layer));
     return CR_OK;
 }
