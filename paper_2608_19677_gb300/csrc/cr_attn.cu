@@ -36,7 +36,7 @@ struct __align__(16) attn_blk {
     int diag;   // keys before the one that its first query token sees last (causal)
     int lo;     // k_attn_few: keys below are already counted (the shared prefix)
     int nt;     // its key tiles
-    uint32_t at;  // place in a head's list
+    int pad;
 };
 // Where a CTA's stretch begins.
 struct __align__(16) attn_start {
@@ -61,13 +61,19 @@ struct plan_in {
     uint32_t min_tiles;    // key tiles that a CTA is worth
     attn_blk *blk;
     attn_start *start;        // [max_cta + 1]
-    unsigned long long *pos;  // [max_cta + 1] their places alone
+    uint32_t *joins;          // [max_cta + 1] number of blocks with several pieces, and their first stretches
     // of long lists only (the plan kernel's shared memory holds the others)
     unsigned long long *cum;  // [max_blk + 1] key tiles before each block
     uint32_t *first;          // [n + 1] first block of each entry
-    int32_t *of_token;        // groups: block of each query token
+    int32_t *of_token;        // groups: first token of each query token's block
 };
-constexpr uint32_t kPlanShared = 1024;
+constexpr uint32_t kPlanShared = 512;
+struct plan_shared {
+    unsigned long long cum[kPlanShared + 1], pos[kMaxCtas + 1];
+    uint32_t first[kPlanShared + 1], joins;
+    int goff[kPlanShared + 1], keys[kPlanShared];  // groups
+    attn_blk blk[kPlanShared];
+};
 
 enum { PLAN_PACKED, PLAN_PAGED, PLAN_GROUPS, PLAN_FEW };
 
@@ -113,41 +119,55 @@ __device__ __forceinline__ void q_range(const plan_in &A, uint32_t i, int &lo, i
     hi = clampi(A.cu_q[i + 1], lo, (int)A.n_tokens);
 }
 
-// A group's shared keys are read once for all where it has several members.
+// Row of the table of an entry, or -1; its keys.
+__device__ __forceinline__ int row_of(const plan_in &A, int e)
+{
+    const int row = A.seqs ? A.seqs[e] : e;
+    return row >= 0 && (uint32_t)row < A.n_seqs ? row : -1;
+}
+__device__ __forceinline__ int keys_of(const plan_in &A, int row)
+{
+    return row < 0 ? 0 : clampi(A.lens[row], 0, (int)A.max_len);
+}
+// Keys that a group's members share, where it has several: they are read once for all.  The first member's length
+// bounds them.
 __device__ __forceinline__ int group_keys(const plan_in &A, uint32_t g)
 {
-    return A.goff[g + 1] - A.goff[g] >= 2 ? clampi(A.shared[g], 0, (int)A.max_len) : 0;
+    const int lo = A.goff[g], hi = A.goff[g + 1];
+    const int keys = clampi(A.shared[g], 0, (int)A.max_len);
+    if (lo < 0 || lo >= (int)A.n) return 0;
+    const int have = keys_of(A, row_of(A, lo));
+    return hi - lo < 2 ? 0 : (keys < have ? keys : have);
 }
 
-__device__ __forceinline__ uint32_t upper(const unsigned long long *a, uint32_t n, unsigned long long v)
+// Last index of a[0 .. n] (ascending) at or below v; a[0] is.
+template <typename T>
+__device__ __forceinline__ uint32_t at_or_below(const T *a, uint32_t n, T v)
 {
-    uint32_t lo = 0, hi = n;  // first index with a[] > v
+    uint32_t lo = 0, hi = n;
     while (lo < hi) {
-        const uint32_t m = (lo + hi) >> 1;
+        const uint32_t m = (lo + hi + 1) >> 1;
         if (a[m] <= v)
-            lo = m + 1;
+            lo = m;
         else
-            hi = m;
+            hi = m - 1;
     }
     return lo;
 }
 
 template <int KIND>
-__device__ void plan_build(const plan_in &A, uint32_t *status)
+__device__ void plan_build(const plan_in &A, plan_shared &S, uint32_t *status)
 {
-    __shared__ unsigned long long cum_near[kPlanShared + 1];
-    __shared__ uint32_t first_near[kPlanShared + 1];
-    __shared__ unsigned long long pos_near[kMaxCtas + 1];
     const uint32_t tid = threadIdx.x;
     const uint32_t n = KIND == PLAN_GROUPS ? A.n_groups : A.n;
-    uint32_t *first = n <= kPlanShared ? first_near : A.first;
-    unsigned long long *cum = A.max_blk <= kPlanShared ? cum_near : A.cum;
+    uint32_t *first = n <= kPlanShared ? S.first : A.first;
+    const bool near = A.max_blk <= kPlanShared;
+    unsigned long long *cum = near ? S.cum : A.cum;
     unsigned long long total, base = 0;
+    if (tid == 0) S.joins = 0;
     // blocks of every entry
-    uint32_t nblk;
-    if (KIND == PLAN_FEW) {
-        nblk = n;
-    } else {
+    uint32_t nblk = n;
+    if (KIND != PLAN_FEW) {
         for (uint32_t i0 = 0; i0 < n; i0 += 1024) {
             const uint32_t i = i0 + tid;
             unsigned long long nb = 0;
@@ -167,6 +187,11 @@ __device__ void plan_build(const plan_in &A, uint32_t *status)
         nblk = (uint32_t)base;
         if (tid == 0) first[n] = nblk;
         __syncthreads();
+    } else if (A.n_groups && A.n_groups <= kPlanShared) {
+        if (tid < A.n_groups) S.keys[tid] = group_keys(A, tid);
+        if (tid <= A.n_groups) S.goff[tid] = A.goff[tid];
+        __syncthreads();
+        if (tid < A.n_groups && S.goff[tid] > S.goff[tid + 1]) atomicOr(status, CR_FLAG_BADPAGES);
     }
     // their keys
     uint32_t filled = 0;  // blocks that have any
@@ -174,26 +199,14 @@ __device__ void plan_build(const plan_in &A, uint32_t *status)
     for (uint32_t b0 = 0; b0 < nblk; b0 += 1024) {
         const uint32_t b = b0 + tid;
         unsigned long long nt = 0;
+        attn_blk k = {};
         if (b < nblk) {
-            uint32_t i = b;
-            if (KIND != PLAN_FEW) {
-                uint32_t l = 0, h = n;
-                while (l < h) {
-                    const uint32_t m = (l + h) >> 1;
-                    if (first[m] <= b)
-                        l = m + 1;
-                    else
-                        h = m;
-                }
-                i = l - 1;
-            }
-            attn_blk k = {};
+            const uint32_t i = KIND == PLAN_FEW ? b : at_or_below(first, n, b);
             int lo, hi;
             q_range(A, i, lo, hi);
-            if (KIND == PLAN_FEW) {
-                k.row0 = (int)i;
-                k.ntok = 1;
-            } else {
+            k.row0 = lo;
+            k.ntok = hi - lo;
+            if (KIND != PLAN_FEW) {
                 const int t0 = (int)((b - first[i]) * A.tok_blk);
                 k.row0 = lo + t0;
                 k.ntok = clampi(hi - lo - t0, 0, (int)A.tok_blk);
@@ -203,37 +216,18 @@ __device__ void plan_build(const plan_in &A, uint32_t *status)
                 k.kbase = klo;
                 k.klen = khi - klo;
             } else {
-                const uint32_t e = KIND == PLAN_GROUPS ? (uint32_t)lo : i;  // entry whose row is read
-                int row = -1;
-                if (e < A.n) row = A.seqs ? A.seqs[e] : (int)e;
-                if (row < 0 || (uint32_t)row >= A.n_seqs) {
-                    if (e < A.n) atomicOr(status, CR_FLAG_BADPAGES);
-                    row = -1;
-                }
+                const int e = KIND == PLAN_GROUPS ? lo : (int)i;  // entry whose row is read
+                const int row = e < (int)A.n ? row_of(A, e) : -1;
+                if (row < 0 && e < (int)A.n) atomicOr(status, CR_FLAG_BADPAGES);
                 k.kbase = row < 0 ? 0 : row;
-                k.klen = row < 0 ? 0 : clampi(A.lens[row], 0, (int)A.max_len);
-                if (KIND == PLAN_GROUPS) {
-                    const int s = group_keys(A, i);
-                    k.klen = s < k.klen ? s : k.klen;
-                }
+                k.klen = KIND == PLAN_GROUPS ? group_keys(A, i) : keys_of(A, row);
                 if (KIND == PLAN_FEW && A.n_groups) {
-                    uint32_t l = 0, h = A.n_groups;  // last group that begins at or before i
-                    while (l < h) {
-                        const uint32_t m = (l + h) >> 1;
-                        if (A.goff[m] <= (int)i)
-                            l = m + 1;
-                        else
-                            h = m;
-                    }
-                    if (l > 0 && (int)i < A.goff[l]) {
-                        // the first member's length bounds what the group's pass has read
-                        const uint32_t e0 = (uint32_t)clampi(A.goff[l - 1], 0, (int)A.n - 1);
-                        int row0 = A.seqs ? A.seqs[e0] : (int)e0;
-                        int s = group_keys(A, l - 1);
-                        const int k0 = row0 < 0 || (uint32_t)row0 >= A.n_seqs ? 0 : clampi(A.lens[row0], 0, (int)A.max_len);
-                        s = s < k0 ? s : k0;
-                        k.lo = s;
-                        if (s > k.klen) atomicOr(status, CR_FLAG_BADPAGES);
+                    const bool in_shared = A.n_groups <= kPlanShared;
+                    const int *goff = in_shared ? S.goff : A.goff;
+                    if (goff[0] <= (int)i) {
+                        const uint32_t g = at_or_below(goff, A.n_groups, (int)i);
+                        if (g < A.n_groups) k.lo = in_shared ? S.keys[g] : group_keys(A, g);
+                        if (k.lo > k.klen) atomicOr(status, CR_FLAG_BADPAGES);
                     }
                 }
             }
@@ -250,39 +244,40 @@ __device__ void plan_build(const plan_in &A, uint32_t *status)
                 if (nt == 0 && KIND != PLAN_GROUPS) nt = 1;  // rows without keys: zeros
             }
             k.nt = (int)nt;
-            A.blk[b] = k;
             if (KIND == PLAN_GROUPS)
-                for (int t = 0; t < k.ntok; ++t) A.of_token[k.row0 + t] = (int)b;
+                for (int t = 0; t < k.ntok; ++t) A.of_token[k.row0 + t] = k.row0;
         }
         filled += __syncthreads_count(nt > 0);
         const unsigned long long at = base + scan1024(nt ? nt + kExtra : 0, &total);
         if (b < nblk) {
             cum[b] = at;
-            A.blk[b].at = (uint32_t)at;
+            A.blk[b] = k;
+            if (near) S.blk[b] = k;
         }
         base += total;
     }
     if (tid == 0) cum[nblk] = base;
     __syncthreads();
     // stretches
-    const unsigned long long Nb = base, N = Nb * A.heads;
-    unsigned long long want = N / A.min_tiles;
+    const unsigned long long Nb = base, N = Nb * A.heads;  // N < 2^54, a stretch's number <= 512
+    const unsigned long long want = N / A.min_tiles;
     uint32_t ncta = want < 1 ? 1u : (want < A.max_cta ? (uint32_t)want : A.max_cta);
     // Few blocks: as many stretches for each, so that most of them are within one block and leave one piece instead
     // of two, where that makes them longer by less than a piece costs (its result's way to scratch and back).
     const unsigned long long blocks = (unsigned long long)filled * A.heads;
     if (blocks && blocks <= ncta) {
-        const uint32_t even = (uint32_t)(ncta / blocks * blocks);
+        const uint32_t even = ncta / (uint32_t)blocks * (uint32_t)blocks;
         if (N / even <= N / ncta + kPieceCost) ncta = even;
     }
     const unsigned long long snap = N / ncta / 8;  // a stretch ends with its block where that is near
-    for (uint32_t c = tid; c <= A.max_cta; c += 1024) {
-        attn_start s = {};
-        s.pos = c < ncta ? N * c / ncta : N;  // N < 2^54, c <= 512
+    const uint32_t c = tid;
+    attn_start s = {};
+    if (c <= A.max_cta) {
+        s.pos = c < ncta ? N * c / ncta : N;
         if (s.pos < N) {
             s.head = (uint32_t)(s.pos / Nb);
             const unsigned long long rem = s.pos - s.head * Nb;
-            s.blk = upper(cum, nblk + 1, rem) - 1;
+            s.blk = at_or_below(cum, nblk, rem);
             const unsigned long long t = rem - cum[s.blk], left = cum[s.blk + 1] - rem;
             s.tile = (uint32_t)(t - kExtra);
             if (t <= snap || t <= kExtra) {
@@ -305,38 +300,44 @@ __device__ void plan_build(const plan_in &A, uint32_t *status)
                     s.blk = 0;
                     ++s.head;
                 }
-            s.k = A.blk[s.blk];
+            s.k = near ? S.blk[s.blk] : A.blk[s.blk];
         }
-        A.start[c] = s;
-        pos_near[c] = A.pos[c] = s.pos;
+        S.pos[c] = s.pos;
     }
     __syncthreads();
-    for (uint32_t c = 1 + tid; c < ncta; c += 1024) {
-        const attn_start &s = A.start[c];
-        const unsigned long long begin = s.pos - s.tile - kExtra, end = begin + kExtra + (uint32_t)s.k.nt;
-        uint32_t n = 0;
-        if (s.tile && s.pos < N && pos_near[c - 1] <= begin) n = upper(pos_near, A.max_cta + 1, end - 1) - (c - 1);
-        A.start[c].pieces = n;
+    if (c <= A.max_cta) {
+        if (c && s.tile && s.pos < N) {
+            const unsigned long long begin = s.pos - s.tile - kExtra, end = begin + kExtra + (uint32_t)s.k.nt;
+            if (S.pos[c - 1] <= begin) {
+                s.pieces = at_or_below(S.pos, A.max_cta, end - 1) + 1 - (c - 1);
+                A.joins[1 + atomicAdd(&S.joins, 1)] = c;  // in any order
+            }
+        }
+        A.start[c] = s;
     }
+    __syncthreads();
+    if (tid == 0) A.joins[0] = S.joins;
 }
 
 template <int KIND>
 __global__ void __launch_bounds__(1024) k_attn_plan(const __grid_constant__ plan_in a, const __grid_constant__ plan_in b,
                                                     uint32_t *status)
 {
+    __shared__ plan_shared S;
     cr_launch_next();
     cr_wait_previous();
     if (blockIdx.x == 0)
-        plan_build<KIND>(a, status);
+        plan_build<KIND>(a, S, status);
     else
-        plan_build<PLAN_GROUPS>(b, status);
+        plan_build<PLAN_GROUPS>(b, S, status);
 }
 
 // What the attention kernels read.
 struct attn_in {
     const attn_blk *blk;
     const attn_start *start;
-    const unsigned long long *pos;
+    const uint32_t *joins;
+    int32_t *first_cta, *last_cta;  // single tokens: CTAs that begin and end each (block, head)
     const int32_t *table;  // paged
     uint32_t max_pages, page_log2, box_rows, box_log2;
     uint32_t paged, causal, G, nsub, tq, q_heads, head_dim;
@@ -347,8 +348,8 @@ struct attn_in {
     float *part, *part_ml; // pieces
     float *pfx, *pfx_lse;  // shared prefix: o and log2 of the sum, [token][head]
     float *own, *own_ml;   // k_attn_few: whole blocks that a shared prefix still joins
-    const int32_t *of_token;  // groups: block of each query token
-    uint32_t few_heads, ncta, after_rows;
+    const int32_t *of_token;  // groups: first token of each query token's block
+    uint32_t kv_heads, few_heads, after_rows, ncta;
     uint32_t to_pfx;       // k_attn_rows, its join: write those instead of o
     uint32_t o_wide;       // rows of o begin at multiples of 32 bytes
     uint32_t *status;
@@ -532,6 +533,11 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             }
             __syncwarp();
             if (!more) break;
+            if (A.to_pfx && lane == 0) {
+                const uint64_t at = (uint64_t)w.k.row0 * A.kv_heads + w.h;
+                if (w.t0 == 0) A.first_cta[at] = (int)blockIdx.x;
+                if (w.t1 == (uint32_t)w.k.nt) A.last_cta[at] = (int)blockIdx.x;
+            }
             const int two = w.k.ntok > (int)A.tq;
             if (!cr_bar_wait(BAR(B_QEMPTY), (pieces & 1) ^ 1, &gave_up)) goto out;
             ++pieces;
@@ -876,101 +882,180 @@ out:
 #undef BAR
 }
 
-// Joins the pieces of blocks that several CTAs worked on: blockIdx.x + 1 is the first stretch that begins
-// inside the block, blockIdx.y a share of its rows.  Pieces lie in scratch as [D / 4][rows][4] with (m, l) per
-// row; a thread joins four columns of a row, the pieces' weights are in shared memory, 32 pieces at a time.
-// RP rows of a piece, RW of them here.
-template <int D, bool BF16, int RP, int RW>
-__global__ void __launch_bounds__(256) k_attn_join(const __grid_constant__ attn_in A)
+// ---- joining pieces ---------------------------------------------------------------------------
+// 256 threads join 16 rows by D columns: thread (row threadIdx % 16, columns 4 (threadIdx / 16 + 16 x) ..) adds up n
+// pieces of its row, ml(i) the maximum and sum of piece i, data(i, column / 4) four columns of it.  The first pieces'
+// columns are on their way while the weights are made.
+struct join_shared {
+    float wgt[32][16], red[16][16];
+};
+template <int kPer, typename ML, typename DATA>
+__device__ __forceinline__ void join_pieces(uint32_t n, ML ml, DATA data, join_shared &S, float &m, float &l, float4 *o)
 {
-    constexpr int kGroups = 256 / RW, kPer = D / 4 / kGroups;  // threads of a row, columns / 4 of each
-    __shared__ float wgt[32][RW];
-    __shared__ float red[2][kGroups][RW];
-    cr_launch_next();
-    cr_wait_previous();
-    const uint32_t c = blockIdx.x + 1;
-    const uint32_t np = A.start[c].pieces;
-    if (np == 0) return;
-    const attn_start s = A.start[c];
-    // row of the piece
-    const uint32_t r = blockIdx.y * RW + threadIdx.x % RW, grp = threadIdx.x / RW;
-    bool valid;
-    uint32_t head;
-    uint64_t tk;
-    if (RP == 16) {
-        head = s.head / A.nsub * A.G + s.head % A.nsub * 16 + r;
-        valid = s.head % A.nsub * 16 + r < A.G;
-        tk = (uint64_t)s.k.row0;
-    } else {
-        const uint32_t x = r / kRowsTile, rr = r % kRowsTile;
-        const uint32_t tok = x * A.tq + rr / A.G;
-        valid = rr < A.G * A.tq && (int)tok < s.k.ntok;
-        head = s.head * A.G + rr % A.G;
-        tk = (uint64_t)s.k.row0 + tok;
-    }
-    if (blockIdx.y * RW / kRowsTile && !__syncthreads_or(valid)) return;  // the second tile is not in use
-    const float2 *ml = reinterpret_cast<const float2 *>(A.part_ml);
-    const float4 *part = reinterpret_cast<const float4 *>(A.part);
-    auto place = [&](uint32_t i) { return (uint64_t)(i == 0 ? 2 * c - 1 : 2 * (c - 1 + i)); };
-    float m = -INFINITY;
-    for (uint32_t i = grp; i < np; i += kGroups)
-        m = fmaxf(m, ml[place(i) * RP + r].x);
-    red[0][grp][threadIdx.x % RW] = m;
+    const uint32_t col = threadIdx.x & 15, grp = threadIdx.x >> 4;
+    float4 v[4][kPer];
+    auto load = [&](uint32_t i0) {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+            for (int x = 0; x < kPer; ++x)
+                v[i][x] = i0 + i < n ? data(i0 + i, grp + 16 * x) : make_float4(0.f, 0.f, 0.f, 0.f);
+    };
+    load(0);
+    float2 mine = make_float2(-INFINITY, 0.f);
+    if (grp < n) mine = ml(grp);
+    m = mine.x;
+    for (uint32_t i = grp + 16; i < n; i += 16) m = fmaxf(m, ml(i).x);
+    S.red[grp][col] = m;
     __syncthreads();
 #pragma unroll
-    for (int e = 0; e < kGroups; ++e) m = fmaxf(m, red[0][e][threadIdx.x % RW]);
-    float l = 0.f;
-    float4 o[kPer];
+    for (int e = 0; e < 16; ++e) m = fmaxf(m, S.red[e][col]);
+    l = 0.f;
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) o[e] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (uint32_t i0 = 0; i0 < np; i0 += 32) {
-        const uint32_t ni = min(32u, np - i0);
-        __syncthreads();
-        for (uint32_t i = grp; i < ni; i += kGroups) {
-            const float2 q = ml[place(i0 + i) * RP + r];
+    for (int x = 0; x < kPer; ++x) o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (uint32_t i0 = 0; i0 < n; i0 += 32) {
+        if (i0) __syncthreads();
+        for (uint32_t i = grp; i < 32; i += 16) {
+            const float2 q = i0 + i == grp ? mine : (i0 + i < n ? ml(i0 + i) : make_float2(-INFINITY, 0.f));
             const float f = q.x == -INFINITY ? 0.f : cr_exp2(q.x - m);
-            wgt[i][threadIdx.x % RW] = f;
+            S.wgt[i][col] = f;
             l += q.y * f;
         }
         __syncthreads();
-#pragma unroll 4
-        for (uint32_t i = 0; i < ni; ++i) {
-            const float f = wgt[i][threadIdx.x % RW];
-            if (f == 0.f) continue;  // sees none of these keys
+        const uint32_t ni = min(32u, n - i0);
+        for (uint32_t j = 0; j < ni; j += 4) {
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) {
-                const float4 v = part[(place(i0 + i) * (D / 4) + grp + e * kGroups) * RP + r];
-                o[e].x += v.x * f;
-                o[e].y += v.y * f;
-                o[e].z += v.z * f;
-                o[e].w += v.w * f;
+            for (uint32_t i = 0; i < 4; ++i) {
+                const float f = S.wgt[j + i][col];
+                if (f == 0.f) continue;  // sees none of these keys
+#pragma unroll
+                for (int x = 0; x < kPer; ++x) {
+                    o[x].x += v[i][x].x * f;
+                    o[x].y += v[i][x].y * f;
+                    o[x].z += v[i][x].z * f;
+                    o[x].w += v[i][x].w * f;
+                }
             }
+            load(i0 + j + 4);
         }
     }
-    red[1][grp][threadIdx.x % RW] = l;
+    __syncthreads();  // red may still be read
+    S.red[grp][col] = l;
     __syncthreads();
     l = 0.f;
 #pragma unroll
-    for (int e = 0; e < kGroups; ++e) l += red[1][e][threadIdx.x % RW];
-    if (!valid) return;
+    for (int e = 0; e < 16; ++e) l += S.red[e][col];
+    __syncthreads();
+}
+
+// Where the i-th piece of a block lies that CTA `first` began.
+__device__ __forceinline__ uint64_t piece_slot(uint32_t first, uint32_t i) { return i == 0 ? 2ull * first + 1 : 2ull * (first + i); }
+
+// A row's result.
+template <int kPer, bool BF16>
+__device__ __forceinline__ void join_write(const attn_in &A, uint64_t token, uint32_t head, float m, float l, const float4 *o)
+{
+    const uint32_t grp = threadIdx.x >> 4;
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-        const uint32_t d = 4 * (grp + e * kGroups);
-        const float4 v = make_float4(o[e].x * inv, o[e].y * inv, o[e].z * inv, o[e].w * inv);
-        if (A.to_pfx)
-            *reinterpret_cast<float4 *>(A.pfx + (tk * A.q_heads + head) * D + d) = v;
-        else if (d < A.head_dim)
-            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(A.o) + tk * A.o_token + head * A.o_head + d) =
-                make_uint2(cr_pack16<BF16>(v.x, v.y), cr_pack16<BF16>(v.z, v.w));
+    for (int x = 0; x < kPer; ++x) {
+        const uint32_t d = 4 * (grp + 16 * x);
+        if (d < A.head_dim)
+            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(A.o) + token * A.o_token + head * A.o_head + d) =
+                make_uint2(cr_pack16<BF16>(o[x].x * inv, o[x].y * inv), cr_pack16<BF16>(o[x].z * inv, o[x].w * inv));
     }
-    if (grp == 0) {
-        if (A.to_pfx)
-            A.pfx_lse[tk * A.q_heads + head] = lse2;
-        else if (A.lse)
-            A.lse[tk * A.q_heads + head] = lse2 * 0.693147180559945309f;
+    if (grp == 0 && A.lse)
+        A.lse[token * A.q_heads + head] = (l == 0.f ? -INFINITY : m + log2f(l)) * 0.693147180559945309f;
+}
+
+// Joins the blocks that several CTAs worked on, 16 rows of one at a time.  Pieces lie in scratch as [D / 4][RP rows][4].
+template <int D, bool BF16, int RP>
+__global__ void __launch_bounds__(256) k_attn_join(const __grid_constant__ attn_in A)
+{
+    __shared__ join_shared S;
+    cr_launch_next();
+    cr_wait_previous();
+    const uint32_t items = A.joins[0] * (RP / 16);
+    for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const uint32_t c = A.joins[1 + item / (RP / 16)], r = item % (RP / 16) * 16 + (threadIdx.x & 15);
+        const attn_start s = A.start[c];
+        bool valid;
+        uint32_t head;
+        uint64_t tk = (uint64_t)s.k.row0;
+        if (RP == 16) {
+            head = s.head / A.nsub * A.G + s.head % A.nsub * 16 + r;
+            valid = s.head % A.nsub * 16 + r < A.G;
+        } else {
+            const uint32_t x = r / kRowsTile, rr = r % kRowsTile, tok = x * A.tq + rr / A.G;
+            valid = rr < A.G * A.tq && (int)tok < s.k.ntok;
+            head = s.head * A.G + rr % A.G;
+            tk += tok;
+        }
+        if (!__syncthreads_or(valid)) continue;  // the second tile is not in use
+        float m, l;
+        float4 o[D / 64];
+        join_pieces<D / 64>(
+            s.pieces,
+            [&](uint32_t i) { return reinterpret_cast<const float2 *>(A.part_ml)[piece_slot(c - 1, i) * RP + r]; },
+            [&](uint32_t i, uint32_t d4) {
+                return reinterpret_cast<const float4 *>(A.part)[(piece_slot(c - 1, i) * (D / 4) + d4) * RP + r];
+            },
+            S, m, l, o);
+        if (valid) join_write<D / 64, BF16>(A, tk, head, m, l, o);
     }
+}
+
+// Joins everything that a single token's heads have: the pieces of its own keys (or its place, where one CTA had them
+// all) and those of its group's shared prefix.  blockIdx: (entry, 16 rows of a key head).
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256)
+    k_attn_decode_join(const __grid_constant__ attn_in F, const __grid_constant__ attn_in R)
+{
+    __shared__ join_shared S;
+    cr_launch_next();
+    cr_wait_previous();
+    const uint32_t e = blockIdx.x, h = blockIdx.y, kv = h / F.nsub, sub = h % F.nsub;
+    const uint64_t own = (uint64_t)e * F.few_heads + h;
+    // groups that are not ascending leave some of these unset: no index passes its array all the same
+    const int row0 = clampi(R.of_token[e], 0, (int)e), f0 = F.first_cta[own], f1 = F.last_cta[own];
+    const bool shared = F.blk[e].lo > 0;  // else row0 means nothing
+    if (f0 == f1 && !shared) return;      // written already
+    const uint32_t r = threadIdx.x & 15;
+    const bool valid = sub * 16 + r < F.G;
+    const uint32_t head = kv * F.G + sub * 16 + r;
+    const uint64_t oh = (uint64_t)e * F.q_heads + head;
+    uint32_t nf = (uint32_t)(f1 - f0) + 1, nr = 0, rr = 0;
+    int r0 = 0;
+    if (shared) {
+        const uint64_t at = (uint64_t)row0 * R.kv_heads + kv;
+        r0 = clampi(R.first_cta[at], 0, (int)R.ncta - 1);
+        nr = (uint32_t)(clampi(R.last_cta[at], r0, (int)R.ncta - 1) - r0) + 1;
+        const uint32_t t = min(e - (uint32_t)row0, 2 * R.tq - 1);  // token of the prefix' block
+        rr = t / R.tq * kRowsTile + t % R.tq * R.G + sub * 16 + r;
+    }
+    float m, l;
+    float4 o[D / 64];
+    join_pieces<D / 64>(
+        nf + nr,
+        [&](uint32_t i) {
+            if (!valid) return make_float2(-INFINITY, 0.f);
+            if (i < nf)
+                return nf == 1 ? reinterpret_cast<const float2 *>(F.own_ml)[own * 16 + r]
+                               : reinterpret_cast<const float2 *>(F.part_ml)[piece_slot(f0, i) * 16 + r];
+            return nr == 1 ? make_float2(F.pfx_lse[oh], 1.f)
+                           : reinterpret_cast<const float2 *>(R.part_ml)[piece_slot(r0, i - nf) * (2 * kRowsTile) + rr];
+        },
+        [&](uint32_t i, uint32_t d4) {
+            if (!valid) return make_float4(0.f, 0.f, 0.f, 0.f);
+            if (i < nf)
+                return nf == 1 ? reinterpret_cast<const float4 *>(F.own)[(own * (D / 4) + d4) * 16 + r]
+                               : reinterpret_cast<const float4 *>(F.part)[(piece_slot(f0, i) * (D / 4) + d4) * 16 + r];
+            return nr == 1 ? *reinterpret_cast<const float4 *>(F.pfx + oh * D + 4 * d4)
+                           : reinterpret_cast<const float4 *>(
+                                 R.part)[(piece_slot(r0, i - nf) * (D / 4) + d4) * (2 * kRowsTile) + rr];
+        },
+        S, m, l, o);
+    if (valid) join_write<D / 64, BF16>(F, e, head, m, l, o);
 }
 
 // ---- few rows ---------------------------------------------------------------------------------
@@ -1072,6 +1157,11 @@ __global__ void __launch_bounds__(kFewThreads, 2)
         const uint32_t box = lane & (boxes - 1), ch = lane / boxes;
         while (w.next()) {
             const int kv = (int)(w.h / A.nsub);
+            if (A.after_rows && lane == 0) {
+                const uint64_t at = (uint64_t)w.k.row0 * A.few_heads + w.h;
+                if (w.t0 == 0) A.first_cta[at] = (int)blockIdx.x;
+                if (w.t1 == (uint32_t)w.k.nt) A.last_cta[at] = (int)blockIdx.x;
+            }
             if (!cr_bar_wait(QEMPTY, qphase ^ 1, &gave_up)) goto out;
             qphase ^= 1;
             if (lane == 0) {
@@ -1276,134 +1366,6 @@ out:
 #undef JOIN
 }
 
-// Joins everything that a single token's heads have: the pieces of its own keys (or its place, where one CTA had them
-// all) and those of its group's shared prefix.  blockIdx: (entry, 16 rows of a key head).
-template <int D, bool BF16>
-__global__ void __launch_bounds__(256)
-    k_attn_decode_join(const __grid_constant__ attn_in F, const __grid_constant__ attn_in R)
-{
-    constexpr int kGroups = 16, kPer = D / 4 / kGroups;
-    __shared__ float wgt[32][16];
-    __shared__ float red[2][kGroups][16];
-    __shared__ uint32_t range[2][2];
-    cr_launch_next();
-    cr_wait_previous();
-    const uint32_t e = blockIdx.x, h = blockIdx.y, kv = h / F.nsub, sub = h % F.nsub;
-    const int prefix = R.of_token[e];  // only entries with a shared prefix have one
-    const unsigned long long nf_all = F.start[0].N, nr_all = R.start[0].N;
-    const attn_blk kf = F.blk[e];
-    const bool shared = kf.lo > 0;
-    attn_blk kr = {};
-    if (shared) kr = R.blk[prefix];
-    // stretches that have a part of each list's block: one warp counts for each list
-    if (threadIdx.x < 64) {
-        const uint32_t which = threadIdx.x >> 5, lane = threadIdx.x & 31;
-        const attn_in &A = which ? R : F;
-        if (!which || shared) {
-            const unsigned long long per = which ? nr_all / (F.few_heads / F.nsub) : nf_all / F.few_heads;
-            const attn_blk &k = which ? kr : kf;
-            const unsigned long long begin = per * (which ? kv : h) + k.at, end = begin + kExtra + (uint32_t)k.nt;
-            uint32_t a = 0, b = 0;
-            for (uint32_t c = 1 + lane; c < A.ncta; c += 32) {
-                const unsigned long long p = A.pos[c];
-                a += p <= begin;
-                b += p < end;
-            }
-            a = __reduce_add_sync(~0u, a);
-            b = __reduce_add_sync(~0u, b);
-            if (lane == 0) {
-                range[which][0] = a;
-                range[which][1] = b;
-            }
-        }
-    }
-    __syncthreads();
-    const uint32_t nf = range[0][1] - range[0][0] + 1, nr = shared ? range[1][1] - range[1][0] + 1 : 0;
-    if (nf == 1 && !shared) return;  // written already
-    const uint32_t r = threadIdx.x & 15, col = threadIdx.x & 15, grp = threadIdx.x >> 4;
-    const bool valid = sub * 16 + r < F.G;
-    const uint32_t head = kv * F.G + sub * 16 + r;
-    const uint64_t oh = (uint64_t)e * F.q_heads + head;
-    const uint32_t rt = (uint32_t)((int)e - kr.row0);  // token of the prefix' block
-    const uint32_t rr = shared ? rt / R.tq * kRowsTile + rt % R.tq * R.G + sub * 16 + r : 0;
-    const uint64_t own = (uint64_t)e * F.few_heads + h;
-    auto slot = [](uint32_t first, uint32_t i) { return (uint64_t)(i == 0 ? 2 * first + 1 : 2 * (first + i)); };
-    auto ml = [&](uint32_t i) {
-        if (!valid) return make_float2(-INFINITY, 0.f);
-        if (i < nf)
-            return nf == 1 ? reinterpret_cast<const float2 *>(F.own_ml)[own * 16 + r]
-                           : reinterpret_cast<const float2 *>(F.part_ml)[slot(range[0][0], i) * 16 + r];
-        return nr == 1 ? make_float2(F.pfx_lse[oh], 1.f)
-                       : reinterpret_cast<const float2 *>(R.part_ml)[slot(range[1][0], i - nf) * (2 * kRowsTile) + rr];
-    };
-    auto data = [&](uint32_t i, uint32_t d4) {
-        if (i < nf)
-            return nf == 1 ? reinterpret_cast<const float4 *>(F.own)[(own * (D / 4) + d4) * 16 + r]
-                           : reinterpret_cast<const float4 *>(F.part)[(slot(range[0][0], i) * (D / 4) + d4) * 16 + r];
-        return nr == 1 ? *reinterpret_cast<const float4 *>(F.pfx + oh * D + 4 * d4)
-                       : reinterpret_cast<const float4 *>(
-                             R.part)[(slot(range[1][0], i - nf) * (D / 4) + d4) * (2 * kRowsTile) + rr];
-    };
-    const uint32_t n = nf + nr;
-    float m = -INFINITY;
-    for (uint32_t i = grp; i < n; i += kGroups) m = fmaxf(m, ml(i).x);
-    red[0][grp][col] = m;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kGroups; ++i) m = fmaxf(m, red[0][i][col]);
-    float l = 0.f;
-    float4 o[kPer];
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (uint32_t i0 = 0; i0 < n; i0 += 32) {
-        const uint32_t ni = min(32u, n - i0);
-        __syncthreads();
-        for (uint32_t i = grp; i < ni; i += kGroups) {
-            const float2 q = ml(i0 + i);
-            const float f = q.x == -INFINITY ? 0.f : cr_exp2(q.x - m);
-            wgt[i][col] = f;
-            l += q.y * f;
-        }
-        __syncthreads();
-        for (uint32_t j = 0; j < ni; j += 8) {  // eight pieces' loads in flight
-            float4 v[8][kPer];
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-                for (int x = 0; x < kPer; ++x) {
-                    v[i][x] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (j + i < ni && wgt[j + i][col] != 0.f) v[i][x] = data(i0 + j + i, grp + x * kGroups);
-                }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float f = j + i < ni ? wgt[j + i][col] : 0.f;
-#pragma unroll
-                for (int x = 0; x < kPer; ++x) {
-                    o[x].x += v[i][x].x * f;
-                    o[x].y += v[i][x].y * f;
-                    o[x].z += v[i][x].z * f;
-                    o[x].w += v[i][x].w * f;
-                }
-            }
-        }
-    }
-    red[1][grp][col] = l;
-    __syncthreads();
-    l = 0.f;
-#pragma unroll
-    for (int i = 0; i < kGroups; ++i) l += red[1][i][col];
-    if (!valid) return;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-    for (int x = 0; x < kPer; ++x) {
-        const uint32_t d = 4 * (grp + x * kGroups);
-        if (d < F.head_dim)
-            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(F.o) + e * F.o_token + head * F.o_head + d) =
-                make_uint2(cr_pack16<BF16>(o[x].x * inv, o[x].y * inv), cr_pack16<BF16>(o[x].z * inv, o[x].w * inv));
-    }
-    if (grp == 0 && F.lse) F.lse[oh] = (l == 0.f ? -INFINITY : m + log2f(l)) * 0.693147180559945309f;
-}
-
 // ---- host -------------------------------------------------------------------------------------
 typedef CUresult (*encode_fn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                               const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -1481,10 +1443,13 @@ uint32_t ilog2(uint32_t v)
 // Scratch of one list of work.
 struct plan_mem {
     size_t bytes;
-    size_t blk, cum, start, pos, first, of_token;
-    plan_mem(uint32_t max_blk, uint32_t max_cta, uint32_t n, uint32_t tokens)  // tokens: of groups
+    size_t blk, cum, start, joins, ctas, first, of_token;
+    uint64_t n_marks;
+    // tokens: of groups; marks: (token, head) places of first_cta and last_cta
+    plan_mem(uint32_t max_blk, uint32_t max_cta, uint32_t n, uint32_t tokens, uint64_t marks)
     {
         bytes = 0;
+        n_marks = marks;
         auto take = [&](size_t b) {
             const size_t at = bytes;
             bytes += (b + 255) & ~(size_t)255;
@@ -1493,7 +1458,8 @@ struct plan_mem {
         blk = take(sizeof(attn_blk) * ((size_t)max_blk + 1));
         cum = take(max_blk > kPlanShared ? 8 * ((size_t)max_blk + 2) : 0);
         start = take(sizeof(attn_start) * ((size_t)max_cta + 2));
-        pos = take(8 * ((size_t)max_cta + 2));
+        joins = take(4 * ((size_t)max_cta + 2));
+        ctas = take(8 * (size_t)marks);
         first = take(n > kPlanShared ? 4 * ((size_t)n + 1) : 0);
         of_token = take(4 * (size_t)tokens);
     }
@@ -1504,12 +1470,14 @@ struct plan_mem {
         p.start = reinterpret_cast<attn_start *>(base + start);
         p.first = reinterpret_cast<uint32_t *>(base + first);
         a.blk = p.blk;
-        p.pos = reinterpret_cast<unsigned long long *>(base + pos);
-        a.pos = p.pos;
+        p.joins = reinterpret_cast<uint32_t *>(base + joins);
+        a.joins = p.joins;
+        a.first_cta = reinterpret_cast<int32_t *>(base + ctas);
+        a.last_cta = a.first_cta + n_marks;
         p.of_token = reinterpret_cast<int32_t *>(base + of_token);
         a.start = p.start;
-        a.of_token = p.of_token;
         a.ncta = p.max_cta;
+        a.of_token = p.of_token;
     }
 };
 
@@ -1537,6 +1505,7 @@ void fill_common(attn_in &A, cr_ctx *ctx, const cr_attn_args *a, const kv_desc &
     A.nsub = 1;
     A.tq = kRowsTile / A.G;
     A.q_heads = a->q_heads;
+    A.kv_heads = K.heads;
     A.head_dim = K.dim;
     A.c = a->scale * 1.44269504088896341f;
     A.causal = a->causal != 0;
@@ -1573,7 +1542,7 @@ int launch_rows(cr_ctx *ctx, const attn_in &A, const kv_desc &K, const cr_attn_a
     if (raised != cudaSuccess) return cr_fail(ctx, CR_ECUDA, "k_attn_rows: %s", cudaGetErrorString(raised));
     CR_TRY(cr_launch_early(ctx, "k_attn_rows", kern, dim3(ctas), kRowsThreads, rows_cfg<D>::kSmem, A, mq, mk, mv));
     if (ctas > 1 && !A.to_pfx)
-        CR_TRY(cr_launch_early(ctx, "k_attn_join", k_attn_join<D, BF16, 2 * kRowsTile, 32>, dim3(ctas - 1, 8), 256, 0, A));
+        CR_TRY(cr_launch_early(ctx, "k_attn_join", k_attn_join<D, BF16, 2 * kRowsTile>, dim3(4 * ctx->num_sms), 256, 0, A));
     return CR_OK;
 }
 
@@ -1597,7 +1566,7 @@ int launch_few(cr_ctx *ctx, const attn_in &A, const attn_in *R, const kv_desc &K
     if (R)
         CR_TRY(cr_launch_early(ctx, "k_attn_decode_join", k_attn_decode_join<D, BF16>, dim3(a->n, A.few_heads), 256, 0, A, *R));
     else if (ctas > 1)
-        CR_TRY(cr_launch_early(ctx, "k_attn_join", k_attn_join<D, BF16, 16, 16>, dim3(ctas - 1), 256, 0, A));
+        CR_TRY(cr_launch_early(ctx, "k_attn_join", k_attn_join<D, BF16, 16>, dim3(min(ctas - 1, 2 * (uint32_t)ctx->num_sms)), 256, 0, A));
     return CR_OK;
 }
 
@@ -1650,7 +1619,7 @@ int attn_many(cr_ctx *ctx, const cr_attn_args *a, const kv_desc &K)
         p.max_len = K.pg->max_pages * K.pg->page;
     }
     p.max_cta = min((uint32_t)ctx->num_sms, kMaxCtas);
-    const plan_mem mem(p.max_blk, p.max_cta, a->n, 0);
+    const plan_mem mem(p.max_blk, p.max_cta, a->n, 0, 0);
     void *base;
     CR_TRY(cr_scratch(ctx, SCR_ATTN_PLAN, mem.bytes, &base));
     mem.point(static_cast<char *>(base), p, A);
@@ -1775,7 +1744,9 @@ extern "C" int cr_attn_decode(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t la
     g.max_cta = min((uint32_t)ctx->num_sms, kMaxCtas);
     g.min_tiles = kRowsMinTiles;
 
-    const plan_mem mf(f.max_blk, f.max_cta, f.n, 0), mg(g.max_blk, g.max_cta, n_groups, f.n);
+    const bool grouped = n_groups > 0;
+    const plan_mem mf(f.max_blk, f.max_cta, f.n, 0, grouped ? (uint64_t)f.n * F.few_heads : 0),
+        mg(g.max_blk, g.max_cta, n_groups, grouped ? f.n : 0, grouped ? (uint64_t)f.n * K.heads : 0);
     void *base;
     CR_TRY(cr_scratch(ctx, SCR_ATTN_PLAN, mf.bytes + mg.bytes, &base));
     mf.point(static_cast<char *>(base), f, F);

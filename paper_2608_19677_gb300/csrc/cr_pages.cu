@@ -167,32 +167,10 @@ struct page_index {
         if (c >= S->chunks) return pre[S->chunks];
         return pre[c] + S->wpre[p >> 5] + __popc(S->bits[p >> 5] & ((1u << (p & 31)) - 1));
     }
-    // page of the k-th free page (LIVE: live page), which exists
-    template <bool LIVE>
-    __device__ uint32_t select(uint32_t k) const
+    // the k-th bit of a word
+    static __device__ __forceinline__ uint32_t bit_of(uint32_t word, uint32_t k)
     {
-        uint32_t lo = 0, hi = S->chunks;  // last chunk with at most k before it
-        while (hi - lo > 1) {
-            const uint32_t m = (lo + hi) >> 1;
-            if ((LIVE ? (m << S->chunk_log2) - pre[m] : pre[m]) <= k)
-                lo = m;
-            else
-                hi = m;
-        }
-        k -= LIVE ? (lo << S->chunk_log2) - pre[lo] : pre[lo];
-        const uint32_t w0 = lo << (S->chunk_log2 - 5);
-        uint32_t a = 0, b = 1u << (S->chunk_log2 - 5);
-        while (b - a > 1) {
-            const uint32_t m = (a + b) >> 1;
-            const uint32_t v = S->wpre[w0 + m];
-            if ((LIVE ? 32 * m - v : v) <= k)
-                a = m;
-            else
-                b = m;
-        }
-        const uint32_t v = S->wpre[w0 + a];
-        k -= LIVE ? 32 * a - v : v;
-        uint32_t word = LIVE ? ~S->bits[w0 + a] : S->bits[w0 + a], at = 0;
+        uint32_t at = 0;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
             const uint32_t low = __popc(word & ((1u << o) - 1));
@@ -202,7 +180,60 @@ struct page_index {
                 at += o;
             }
         }
-        return ((w0 + a) << 5) + at;
+        return at;
+    }
+    // last chunk with at most k free (LIVE: live) pages before it; k becomes the rank within it
+    template <bool LIVE>
+    __device__ __forceinline__ uint32_t chunk_of(uint32_t &k) const
+    {
+        uint32_t lo = 0, hi = S->chunks;
+        while (hi - lo > 1) {
+            const uint32_t m = (lo + hi) >> 1;
+            if ((LIVE ? (m << S->chunk_log2) - pre[m] : pre[m]) <= k)
+                lo = m;
+            else
+                hi = m;
+        }
+        k -= LIVE ? (lo << S->chunk_log2) - pre[lo] : pre[lo];
+        return lo;
+    }
+    // The k-th free (LIVE: live) page, which exists, found by one thread.
+    template <bool LIVE>
+    __device__ uint32_t select(uint32_t k) const
+    {
+        const uint32_t w0 = chunk_of<LIVE>(k) << (S->chunk_log2 - 5);
+        uint32_t a = 0, b = 1u << (S->chunk_log2 - 5);
+        while (b - a > 1) {
+            const uint32_t m = (a + b) >> 1;
+            const uint32_t v = S->wpre[w0 + m];
+            if ((LIVE ? 32 * m - v : v) <= k)
+                a = m;
+            else
+                b = m;
+        }
+        const uint32_t v = S->wpre[w0 + a], word = S->bits[w0 + a];
+        return ((w0 + a) << 5) + bit_of(LIVE ? ~word : word, k - (LIVE ? 32 * a - v : v));
+    }
+    // The same by a warp: 32 words at a look, one after the other only in pools of more than a million pages.
+    template <bool LIVE>
+    __device__ uint32_t select_warp(uint32_t k) const
+    {
+        const uint32_t lane = threadIdx.x & 31, w0 = chunk_of<LIVE>(k) << (S->chunk_log2 - 5);
+        uint32_t at = 0, v = 0;
+        for (uint32_t step = 1u << (S->chunk_log2 - 10);; step >>= 5) {
+            if (step == 0) step = 1;
+            const uint32_t m = at + lane * step, words = 1u << (S->chunk_log2 - 5);
+            const bool in = m < words;
+            v = in ? S->wpre[w0 + m] : 0;
+            const uint32_t word = in ? S->bits[w0 + m] : 0;
+            const uint32_t last = 31 - __clz(__ballot_sync(~0u, in && (LIVE ? 32 * m - v : v) <= k));
+            at = __shfl_sync(~0u, m, last);
+            if (step == 1) {
+                v = __shfl_sync(~0u, v, last);
+                const uint32_t w = __shfl_sync(~0u, word, last);
+                return ((w0 + at) << 5) + bit_of(LIVE ? ~w : w, k - (LIVE ? 32 * at - v : v));
+            }
+        }
     }
 };
 
@@ -226,7 +257,7 @@ __device__ __forceinline__ uint16_t *plane(const pages_in &P, uint32_t l2)
     return P.cache + (uint64_t)(l2 >> 1) * P.layer_stride + (uint64_t)(l2 & 1) * P.kv_stride;
 }
 
-// A block per entry: its pages, a thread each.
+// A block per entry: its pages, a warp each where they are few, else a thread.
 __global__ void __launch_bounds__(128) k_pages_extend(const __grid_constant__ pages_in P, const __grid_constant__ pages_scan S,
                                                       uint32_t n)
 {
@@ -244,8 +275,19 @@ __global__ void __launch_bounds__(128) k_pages_extend(const __grid_constant__ pa
     if (!ok) return;
     const uint32_t had = pages_of((uint32_t)e.y, P.page_log2), now = pages_of((uint32_t)(e.y + e.z), P.page_log2);
     int32_t *row = P.table + (uint64_t)e.x * P.max_pages;
+    const uint32_t first = S.base[blockIdx.x];
+    if (now - had <= 8) {  // a warp a page
+        for (uint32_t j = had + (threadIdx.x >> 5); j < now; j += blockDim.x >> 5) {
+            const uint32_t p = I.select_warp<false>(first + (j - had));
+            if ((threadIdx.x & 31) == 0) {
+                row[j] = (int32_t)p;
+                P.ref[p] = 1;
+            }
+        }
+        return;
+    }
     for (uint32_t j = had + threadIdx.x; j < now; j += blockDim.x) {
-        const uint32_t p = I.select<false>(S.base[blockIdx.x] + (j - had));
+        const uint32_t p = I.select<false>(first + (j - had));
         row[j] = (int32_t)p;
         P.ref[p] = 1;
     }
@@ -253,7 +295,7 @@ __global__ void __launch_bounds__(128) k_pages_extend(const __grid_constant__ pa
 
 // blockIdx.x: entry; blockIdx.y == 0 writes its row, and every blockIdx.y copies the tail in its share
 // of the layers' keys and values.
-__global__ void __launch_bounds__(128) k_pages_fork(const __grid_constant__ pages_in P, const __grid_constant__ pages_scan S,
+__global__ void __launch_bounds__(256) k_pages_fork(const __grid_constant__ pages_in P, const __grid_constant__ pages_scan S,
                                                     uint32_t n)
 {
     cr_launch_next();
@@ -281,7 +323,7 @@ __global__ void __launch_bounds__(128) k_pages_fork(const __grid_constant__ page
                 atomicOr(P.status, CR_FLAG_BADPAGES);
         }
     if (!tail) return;
-    const uint32_t to = I.select<false>(S.base[blockIdx.x]);
+    const uint32_t to = I.select_warp<false>(S.base[blockIdx.x]);
     const int from = src[full];
     if (first && threadIdx.x == 0) {
         dst[full] = (int32_t)to;
@@ -294,11 +336,23 @@ __global__ void __launch_bounds__(128) k_pages_fork(const __grid_constant__ page
     const bool by_token = P.token_stride >= P.head_stride;  // the page's tokens lie one after the other
     const uint32_t segs = by_token ? 1 : P.kv_heads;
     const uint32_t words = tail * P.head_dim / 8 * (by_token ? P.kv_heads : 1);
-    for (uint32_t l2 = blockIdx.y; l2 < 2 * P.layers; l2 += gridDim.y) {
-        uint16_t *base = plane(P, l2);
-        for (uint32_t g = 0; g < segs; ++g)
-            copy16(reinterpret_cast<uint4 *>(base + to * P.page_stride + g * P.head_stride),
-                   reinterpret_cast<const uint4 *>(base + (uint64_t)from * P.page_stride + g * P.head_stride), words);
+    // one warp copies a segment, or several where there are fewer segments than warps
+    const uint32_t nseg = (2 * P.layers - blockIdx.y + gridDim.y - 1) / gridDim.y * segs, nw = blockDim.x >> 5;
+    const uint32_t share = nseg < nw ? nw / nseg : 1, warp = threadIdx.x >> 5;
+    for (uint32_t g = warp / share; g < nseg; g += nw / share) {
+        uint16_t *base = plane(P, blockIdx.y + g / segs * gridDim.y) + g % segs * P.head_stride;
+        uint4 *out = reinterpret_cast<uint4 *>(base + to * P.page_stride);
+        const uint4 *in = reinterpret_cast<const uint4 *>(base + (uint64_t)from * P.page_stride);
+        const uint32_t step = 32 * share;
+        for (uint32_t i = warp % share * 32 + (threadIdx.x & 31); i < words; i += 4 * step) {  // four loads in flight
+            uint4 v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (i + e * step < words) v[e] = in[i + e * step];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (i + e * step < words) out[i + e * step] = v[e];
+        }
     }
 }
 
@@ -368,14 +422,25 @@ __global__ void __launch_bounds__(256) k_pages_compact(const __grid_constant__ p
             table_out[i] = to;
         }
     } else {
-        const uint32_t words = P.page * P.kv_heads * (P.head_dim / 8);
-        const uint64_t n = (uint64_t)(L - low) * 2 * P.layers;
-        for (uint64_t i = blockIdx.x - b_table; i < n; i += gridDim.x - b_table) {
-            const uint32_t k = (uint32_t)(i / (2 * P.layers));
-            uint16_t *base = plane(P, (uint32_t)(i % (2 * P.layers)));
-            const uint32_t from = I.select<true>(low + k), to = I.select<false>(k);
-            copy16(reinterpret_cast<uint4 *>(base + to * P.page_stride),
-                   reinterpret_cast<const uint4 *>(base + from * P.page_stride), words);
+        // an equal share of the (move, plane) pairs, in batches whose pages the threads look up together
+        __shared__ uint32_t from[256], to[256];
+        const uint32_t words = P.page * P.kv_heads * (P.head_dim / 8), planes = 2 * P.layers, nb = gridDim.x - b_table;
+        const uint64_t n = (uint64_t)(L - low) * planes, b = blockIdx.x - b_table;
+        for (uint64_t i = n * b / nb, end = n * (b + 1) / nb; i < end;) {
+            const uint32_t k0 = (uint32_t)(i / planes), k = k0 + threadIdx.x;
+            const uint64_t stop = min(end, ((uint64_t)k0 + 256) * planes);
+            __syncthreads();
+            if ((uint64_t)k * planes < stop) {
+                from[threadIdx.x] = I.select<true>(low + k);
+                to[threadIdx.x] = I.select<false>(k);
+            }
+            __syncthreads();
+            for (; i < stop; ++i) {
+                const uint32_t m = (uint32_t)(i / planes) - k0;
+                uint16_t *base = plane(P, (uint32_t)(i % planes));
+                copy16(reinterpret_cast<uint4 *>(base + to[m] * P.page_stride),
+                       reinterpret_cast<const uint4 *>(base + from[m] * P.page_stride), words);
+            }
         }
     }
 }
@@ -396,15 +461,18 @@ __global__ void __launch_bounds__(128) k_kv_write(const __grid_constant__ pages_
     const uint64_t warp = ((uint64_t)blockIdx.x * 128 + threadIdx.x) >> 5;
     const uint64_t t = warp >> W.wpt_log2;
     if (t >= W.n_tokens) return;
-    uint32_t lo = 0, hi = W.n + 1;  // entry: the last whose tokens begin at or before t
-    while (lo < hi) {
-        const uint32_t m = (lo + hi) >> 1;
-        if (W.cu[m] <= (int)t)
-            lo = m + 1;
-        else
-            hi = m;
+    // entry: the last whose tokens begin at or before t, 32 looks at a time
+    const uint32_t lane = threadIdx.x & 31;
+    uint32_t lo = 0, span = W.n + 1;
+    while (span > 1) {
+        const uint32_t step = (span + 31) / 32, i = lo + lane * step;
+        const bool in = lane * step < span && W.cu[i] <= (int)t;
+        const uint32_t some = __ballot_sync(~0u, in), last = some ? 31 - __clz(some) : 0;
+        lo += last * step;
+        span = min(step, span - last * step);
     }
-    bool ok = lo >= 1 && lo <= W.n;
+    bool ok = lo < W.n && W.cu[lo] <= (int)t && (int)t < W.cu[lo + 1];
+    ++lo;
     uint64_t dst = 0;
     if (ok) {
         const int row = W.seqs ? W.seqs[lo - 1] : (int)lo - 1;
@@ -540,7 +608,10 @@ extern "C" int cr_pages_fork(cr_ctx *ctx, const cr_kv_pages *pages, const int32_
     pages_scan S;
     CR_TRY(scan_mem(ctx, pages, n, S));
     CR_TRY(cr_launch_early(ctx, "k_pages_scan", k_pages_scan<SCAN_FORK>, dim3(S.chunks + 1), 1024, 0, P, S, d_src, d_dst, d_keep, n));
-    CR_TRY(cr_launch_early(ctx, "k_pages_fork", k_pages_fork, dim3(n, pages->layers < 32 ? 2 * pages->layers : 64), 128, 0, P, S, n));
+    // few entries: several blocks copy the layers of each (8 are resident on every SM)
+    uint32_t fork_split = 8 * (uint32_t)ctx->num_sms / n;
+    fork_split = fork_split < 1 ? 1 : (fork_split > 2 * pages->layers ? 2 * pages->layers : fork_split);
+    CR_TRY(cr_launch_early(ctx, "k_pages_fork", k_pages_fork, dim3(n, fork_split), 256, 0, P, S, n));
     return CR_OK;
 }
 
