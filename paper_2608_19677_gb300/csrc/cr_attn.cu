@@ -46,7 +46,7 @@ struct __align__(16) attn_start {
     // where the stretch is the first to begin inside that block: the block's pieces (from the stretch before on)
     uint32_t pieces, pad[3];
 };
-constexpr uint32_t kMaxCtas = 512;
+constexpr uint32_t kPlanThreads = 512, kMaxCtas = kPlanThreads - 1;
 
 // What the plan kernel reads.
 struct plan_in {
@@ -79,10 +79,10 @@ enum { PLAN_PACKED, PLAN_PAGED, PLAN_GROUPS, PLAN_FEW };
 
 __device__ __forceinline__ int clampi(int v, int lo, int hi) { return v < lo ? lo : (v > hi ? hi : v); }
 
-// Exclusive scan over the 1,024 threads of the CTA; *total receives the sum.
-__device__ unsigned long long scan1024(unsigned long long v, unsigned long long *total)
+// Exclusive scan over the kPlanThreads threads of the CTA; *total receives the sum.
+__device__ unsigned long long scan_cta(unsigned long long v, unsigned long long *total)
 {
-    __shared__ unsigned long long part[32];
+    __shared__ unsigned long long part[kPlanThreads / 32];
     const uint32_t lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     unsigned long long x = v;
 #pragma unroll
@@ -93,17 +93,17 @@ __device__ unsigned long long scan1024(unsigned long long v, unsigned long long 
     if (lane == 31) part[w] = x;
     __syncthreads();
     if (w == 0) {
-        unsigned long long p = part[lane], q = p;
+        unsigned long long q = lane < kPlanThreads / 32 ? part[lane] : 0;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const unsigned long long y = __shfl_up_sync(~0u, q, o);
             if (lane >= (uint32_t)o) q += y;
         }
-        part[lane] = q;
+        if (lane < kPlanThreads / 32) part[lane] = q;
     }
     __syncthreads();
     const unsigned long long before = w ? part[w - 1] : 0;
-    *total = part[31];
+    *total = part[kPlanThreads / 32 - 1];
     __syncthreads();
     return before + x - v;
 }
@@ -155,6 +155,12 @@ __device__ __forceinline__ uint32_t at_or_below(const T *a, uint32_t n, T v)
     return lo;
 }
 
+// Most lists are short: their divisions are done in 32 bits.
+__device__ __forceinline__ unsigned long long div_by(unsigned long long a, unsigned long long b)
+{
+    return a >> 32 || b >> 32 ? a / b : (uint32_t)a / (uint32_t)b;
+}
+
 template <int KIND>
 __device__ void plan_build(const plan_in &A, plan_shared &S, uint32_t *status)
 {
@@ -168,7 +174,7 @@ __device__ void plan_build(const plan_in &A, plan_shared &S, uint32_t *status)
     // blocks of every entry
     uint32_t nblk = n;
     if (KIND != PLAN_FEW) {
-        for (uint32_t i0 = 0; i0 < n; i0 += 1024) {
+        for (uint32_t i0 = 0; i0 < n; i0 += kPlanThreads) {
             const uint32_t i = i0 + tid;
             unsigned long long nb = 0;
             if (i < n) {
@@ -176,7 +182,7 @@ __device__ void plan_build(const plan_in &A, plan_shared &S, uint32_t *status)
                 q_range(A, i, lo, hi);
                 nb = ((uint32_t)(hi - lo) + A.tok_blk - 1) / A.tok_blk;
             }
-            const unsigned long long at = base + scan1024(nb, &total);
+            const unsigned long long at = base + scan_cta(nb, &total);
             if (i < n) first[i] = (uint32_t)(at < A.max_blk ? at : A.max_blk);
             base += total;
         }
@@ -188,15 +194,18 @@ __device__ void plan_build(const plan_in &A, plan_shared &S, uint32_t *status)
         if (tid == 0) first[n] = nblk;
         __syncthreads();
     } else if (A.n_groups && A.n_groups <= kPlanShared) {
-        if (tid < A.n_groups) S.keys[tid] = group_keys(A, tid);
-        if (tid <= A.n_groups) S.goff[tid] = A.goff[tid];
+        if (tid < A.n_groups) {
+            S.keys[tid] = group_keys(A, tid);
+            S.goff[tid] = A.goff[tid];
+            if (A.goff[tid] > A.goff[tid + 1]) atomicOr(status, CR_FLAG_BADPAGES);
+        }
+        if (tid == 0) S.goff[A.n_groups] = A.goff[A.n_groups];
         __syncthreads();
-        if (tid < A.n_groups && S.goff[tid] > S.goff[tid + 1]) atomicOr(status, CR_FLAG_BADPAGES);
     }
     // their keys
     uint32_t filled = 0;  // blocks that have any
     base = 0;
-    for (uint32_t b0 = 0; b0 < nblk; b0 += 1024) {
+    for (uint32_t b0 = 0; b0 < nblk; b0 += kPlanThreads) {
         const uint32_t b = b0 + tid;
         unsigned long long nt = 0;
         attn_blk k = {};
@@ -248,7 +257,7 @@ __device__ void plan_build(const plan_in &A, plan_shared &S, uint32_t *status)
                 for (int t = 0; t < k.ntok; ++t) A.of_token[k.row0 + t] = k.row0;
         }
         filled += __syncthreads_count(nt > 0);
-        const unsigned long long at = base + scan1024(nt ? nt + kExtra : 0, &total);
+        const unsigned long long at = base + scan_cta(nt ? nt + kExtra : 0, &total);
         if (b < nblk) {
             cum[b] = at;
             A.blk[b] = k;
@@ -259,23 +268,23 @@ __device__ void plan_build(const plan_in &A, plan_shared &S, uint32_t *status)
     if (tid == 0) cum[nblk] = base;
     __syncthreads();
     // stretches
-    const unsigned long long Nb = base, N = Nb * A.heads;  // N < 2^54, a stretch's number <= 512
-    const unsigned long long want = N / A.min_tiles;
+    const unsigned long long Nb = base, N = Nb * A.heads;  // N < 2^54
+    const unsigned long long want = div_by(N, A.min_tiles);
     uint32_t ncta = want < 1 ? 1u : (want < A.max_cta ? (uint32_t)want : A.max_cta);
     // Few blocks: as many stretches for each, so that most of them are within one block and leave one piece instead
     // of two, where that makes them longer by less than a piece costs (its result's way to scratch and back).
     const unsigned long long blocks = (unsigned long long)filled * A.heads;
     if (blocks && blocks <= ncta) {
         const uint32_t even = ncta / (uint32_t)blocks * (uint32_t)blocks;
-        if (N / even <= N / ncta + kPieceCost) ncta = even;
+        if (div_by(N, even) <= div_by(N, ncta) + kPieceCost) ncta = even;
     }
-    const unsigned long long snap = N / ncta / 8;  // a stretch ends with its block where that is near
+    const unsigned long long snap = div_by(N, ncta) / 8;  // a stretch ends with its block where that is near
     const uint32_t c = tid;
     attn_start s = {};
     if (c <= A.max_cta) {
-        s.pos = c < ncta ? N * c / ncta : N;
+        s.pos = c < ncta ? div_by(N * c, ncta) : N;
         if (s.pos < N) {
-            s.head = (uint32_t)(s.pos / Nb);
+            s.head = (uint32_t)div_by(s.pos, Nb);
             const unsigned long long rem = s.pos - s.head * Nb;
             s.blk = at_or_below(cum, nblk, rem);
             const unsigned long long t = rem - cum[s.blk], left = cum[s.blk + 1] - rem;
@@ -320,7 +329,7 @@ __device__ void plan_build(const plan_in &A, plan_shared &S, uint32_t *status)
 }
 
 template <int KIND>
-__global__ void __launch_bounds__(1024) k_attn_plan(const __grid_constant__ plan_in a, const __grid_constant__ plan_in b,
+__global__ void __launch_bounds__(kPlanThreads) k_attn_plan(const __grid_constant__ plan_in a, const __grid_constant__ plan_in b,
                                                     uint32_t *status)
 {
     __shared__ plan_shared S;
@@ -541,12 +550,12 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             const int two = w.k.ntok > (int)A.tq;
             if (!cr_bar_wait(BAR(B_QEMPTY), (pieces & 1) ^ 1, &gave_up)) goto out;
             ++pieces;
-            if (lane == 0) {
-                cr_bar_expect(BAR(B_QFULL), q_bytes * (1 + two));
-                for (int x = 0; x <= two; ++x)
-                    for (int ch = 0; ch < cfg::kChunks; ++ch)
-                        cr_tma_load(sq + x * cfg::kTile + ch * (kRowsTile * 128), &map_q, BAR(B_QFULL), ch * 64, 0,
-                                    (int)w.h, w.k.row0 + x * (int)A.tq);
+            if (lane == 0) cr_bar_expect(BAR(B_QFULL), q_bytes * (1 + two));
+            __syncwarp();
+            if ((int)lane < cfg::kChunks * (1 + two)) {
+                const int x = (int)lane / cfg::kChunks, ch = (int)lane % cfg::kChunks;
+                cr_tma_load(sq + x * cfg::kTile + ch * (kRowsTile * 128), &map_q, BAR(B_QFULL), ch * 64, 0, (int)w.h,
+                            w.k.row0 + x * (int)A.tq);
             }
             // lane: one box of one column block of a tile
             const uint32_t boxes = kRowsTile >> A.box_log2;
@@ -1625,9 +1634,9 @@ int attn_many(cr_ctx *ctx, const cr_attn_args *a, const kv_desc &K)
     mem.point(static_cast<char *>(base), p, A);
     CR_TRY(part_mem(ctx, SCR_ATTN_PART, A, p.max_cta, 2 * kRowsTile, K.dim <= 64 ? 64 : 128));
     if (K.paged)
-        CR_TRY(cr_launch_early(ctx, "k_attn_plan", k_attn_plan<PLAN_PAGED>, dim3(1), 1024, 0, p, p, ctx->d_status));
+        CR_TRY(cr_launch_early(ctx, "k_attn_plan", k_attn_plan<PLAN_PAGED>, dim3(1), kPlanThreads, 0, p, p, ctx->d_status));
     else
-        CR_TRY(cr_launch_early(ctx, "k_attn_plan", k_attn_plan<PLAN_PACKED>, dim3(1), 1024, 0, p, p, ctx->d_status));
+        CR_TRY(cr_launch_early(ctx, "k_attn_plan", k_attn_plan<PLAN_PACKED>, dim3(1), kPlanThreads, 0, p, p, ctx->d_status));
     return rows(ctx, A, K, a, p.max_cta);
 }
 
@@ -1763,10 +1772,10 @@ extern "C" int cr_attn_decode(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t la
         F.pfx_lse = R.pfx_lse = F.own_ml + 2 * own;
         R.to_pfx = 1;
         F.after_rows = 1;
-        CR_TRY(cr_launch_early(ctx, "k_attn_plan", k_attn_plan<PLAN_FEW>, dim3(2), 1024, 0, f, g, ctx->d_status));
+        CR_TRY(cr_launch_early(ctx, "k_attn_plan", k_attn_plan<PLAN_FEW>, dim3(2), kPlanThreads, 0, f, g, ctx->d_status));
         CR_TRY(rows(ctx, R, K, args, g.max_cta));
     } else {
-        CR_TRY(cr_launch_early(ctx, "k_attn_plan", k_attn_plan<PLAN_FEW>, dim3(1), 1024, 0, f, f, ctx->d_status));
+        CR_TRY(cr_launch_early(ctx, "k_attn_plan", k_attn_plan<PLAN_FEW>, dim3(1), kPlanThreads, 0, f, f, ctx->d_status));
     }
     return few(ctx, F, n_groups ? &R : nullptr, K, args, f.max_cta);
 }
