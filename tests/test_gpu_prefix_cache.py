@@ -586,3 +586,54 @@ def test_empty_calls(P, ctx):
     out, lse = P.attn_decode(ctx, one, pg, 0, lse=True)      # rows without tokens
     ctx.sync()
     assert (out == 0).all() and (lse == -math.inf).all()
+
+
+# ---- the calls together --------------------------------------------------------------------------------------------
+def test_example_serves_routed_requests():
+    """Router, pages, prompts and shared decoding together, against the model from scratch.  Two layers of about five
+    roundings to bfloat16 each (unit roundoff 2^-8, root mean square below 2^-9) stay below 2^-9 * sqrt(10) * 2."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "serve_prefixes.py")
+    spec = importlib.util.spec_from_file_location("serve_prefixes", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    said = []
+    assert m.main(48, 3, log=said.append) < 2.0 ** -9 * math.sqrt(10) * 2
+    assert len(said) == 2
+
+
+def test_destination_keeps_within_its_rows_and_pages(P, ctx):
+    """Idle prefixes leave, least recent first; a batch that does not fit changes nothing."""
+    from paper_2608_19677_gb300.destination import Destination
+
+    class Flat:
+        layers = 1
+
+        def embed(self, t):
+            return t[:, None].to(BF).expand(-1, 64)
+
+        def qkv(self, layer, x):
+            y = x[:, None, :].contiguous()
+            return y, y, y
+
+        def mix(self, layer, x, out):
+            return out
+
+    pg = P.KVPages.empty(12, 16, 5, 8, 1, 1, 64)
+    d = Destination(ctx, pg, Flat())
+    t = lambda n: torch.arange(n, device=DEV) % 7  # noqa: E731
+    rows, _ = d.admit([(1, t(40), 32)])
+    d.finish(rows)
+    rows, _ = d.admit([(2, t(20), 16)])
+    assert set(d.prefixes) == {1, 2}
+    with pytest.raises(RuntimeError):
+        d.admit([(3, t(300), 200)])
+    assert set(d.prefixes) == {1, 2} and d.order() == rows
+    more, out = d.admit([(3, t(70), 64), (2, t(18), 16)])     # prefix 1 leaves
+    assert set(d.prefixes) == {2, 3} and out.shape[0] == 8
+    d.step(t(3))
+    ctx.sync()
+    used = int((pg.ref > 0).sum())
+    assert used == pg.n_pages - d.free_pages
+    assert [int(pg.lens[r]) for r in d.order()] == [21, 19, 71]
