@@ -185,6 +185,8 @@ class Context:
         if st != CR_OK:
             raise CacheRouteError(st, "cr_create", lib().cr_last_error(None).decode())
         self._h = h
+        self._raw_stream = self._stream_obj.cuda_stream
+        _load_torch()
 
     @property
     def handle(self):
@@ -198,7 +200,7 @@ class Context:
         self.check(lib().cr_sync(self._h), "cr_sync")
 
     def set_stream(self, stream):
-        self._stream_obj = stream
+        self._stream_obj, self._raw_stream = stream, stream.cuda_stream
         self.check(lib().cr_set_stream(self._h, C.c_void_p(stream.cuda_stream)), "cr_set_stream")
 
     @property
@@ -544,48 +546,56 @@ def shadow_replay(ctx: Context, replay: Replay, keys, plen, slen, dest, ctr):
 
 
 # ---- what a destination does with the prefixes it holds ------------------------------------------------------------
-# These calls are made once per layer and step, so their checks take one look at each tensor.
-def _dtype_code(t) -> int:
-    import torch
-    if t.dtype == torch.bfloat16:
-        return 0
-    if t.dtype == torch.float16:
-        return 1
-    raise ValueError(f"keys, values and queries are bfloat16 or float16, got {t.dtype}")
+# These calls are made once per layer and step: their checks take one look at each tensor.
+_torch = None        # set by the first Context
+_codes = {}          # dtype -> CR_DTYPE_*
 
 
-def _out(ctx: Context, shape, like, dtype=None):
+def _load_torch():
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+        _codes.update({torch.bfloat16: 0, torch.float16: 1})
+    return _torch
+
+
+def _dtype_code(dtype) -> int:
+    _load_torch()
+    if dtype not in _codes:
+        raise ValueError(f"keys, values and queries are bfloat16 or float16, got {dtype}")
+    return _codes[dtype]
+
+
+def _out(ctx: Context, shape, like, dtype):
     """An output of a call: its memory is not handed out again before ctx's stream has written it."""
-    import torch
-    t = torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
-    if ctx._stream_obj.cuda_stream != torch._C._cuda_getCurrentRawStream(ctx.device):
+    t = _torch.empty(shape, dtype=dtype, device=like.device)
+    if ctx._raw_stream != _torch._C._cuda_getCurrentRawStream(ctx.device):
         t.record_stream(ctx._stream_obj)
     return t
 
 
 def _int32(name, t, n=None):
     """Address of a contiguous int32 CUDA tensor, of n elements."""
-    import torch
-    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous():
+    if t.dtype is not _torch.int32 or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 CUDA tensor")
     if n is not None and t.numel() != n:
         raise ValueError(f"{name} must have {n} elements, got {t.numel()}")
     return t.data_ptr()
 
 
-def _heads(name, t, dtype, want):
-    """(tokens, address, token stride, head stride) of a tensor [tokens, heads, head_dim], contiguous in head_dim;
-    ``want``: (tokens, heads, head_dim), None for any."""
-    shape = t.shape
-    if t.dtype != dtype or not t.is_cuda or len(shape) != 3:
+def _heads(name, t, dtype, shape, tokens, heads, dim):
+    """(address, token stride, head stride) of a tensor [tokens, heads, dim] of that shape, contiguous in its last
+    dimension; ``shape``: t.shape; None: any."""
+    if t.dtype is not dtype or not t.is_cuda or len(shape) != 3:
         raise ValueError(f"{name} must be a {dtype} CUDA tensor [tokens, heads, head_dim]")
-    if ((want[0] is not None and shape[0] != want[0]) or (want[1] is not None and shape[1] != want[1]) or
-            (want[2] is not None and shape[2] != want[2])):
-        raise ValueError(f"{name} must have shape {tuple(want)} (None: any), got {tuple(shape)}")
-    st = t.stride()
-    if st[2] != 1:
+    T, h, d = shape
+    if (tokens is not None and T != tokens) or (heads is not None and h != heads) or (dim is not None and d != dim):
+        raise ValueError(f"{name} must have shape {(tokens, heads, dim)} (None: any), got {tuple(shape)}")
+    st, sh, sd = t.stride()
+    if sd != 1:
         raise ValueError(f"{name} must be contiguous in head_dim")
-    return shape[0], t.data_ptr(), st[0], st[1]
+    return t.data_ptr(), st, sh
 
 
 class KVPages:
@@ -597,6 +607,7 @@ class KVPages:
     tokens.  ``KVPages.empty`` makes an empty pool."""
 
     def __init__(self, cache, ref, table, lens):
+        _load_torch()
         if cache.dim() != 6 or cache.shape[1] != 2 or not cache.is_cuda or cache.stride(5) != 1:
             raise ValueError("cache must be a CUDA tensor [layers, 2, n_pages, page, kv_heads, head_dim]")
         layers, _, n_pages, page, heads, dim = cache.shape
@@ -608,7 +619,7 @@ class KVPages:
         self.cache, self.ref, self.table, self.lens = cache, ref, table, lens
         self.layers, self.n_pages, self.page, self.kv_heads, self.head_dim = layers, n_pages, page, heads, dim
         self.dtype = cache.dtype
-        self._code = _dtype_code(cache)
+        self._code = _dtype_code(cache.dtype)
         self._bind()
 
     def _bind(self):
@@ -621,7 +632,7 @@ class KVPages:
     @classmethod
     def empty(cls, n_pages: int, page: int, n_seqs: int, max_pages: int, layers: int, kv_heads: int, head_dim: int,
               dtype=None, device="cuda"):
-        import torch
+        torch = _load_torch()
         cache = torch.zeros((layers, 2, n_pages, page, kv_heads, head_dim), dtype=dtype or torch.bfloat16,
                             device=device)
         return cls(cache, torch.zeros(n_pages, dtype=torch.int32, device=device),
@@ -640,25 +651,23 @@ class KVPages:
 
 def pages_extend(ctx: Context, pages: KVPages, seqs, add):
     """The sequences ``seqs`` get pages for ``add`` more tokens each (cr_pages_extend)."""
-    n = seqs.shape[0]
-    st = lib().cr_pages_extend(ctx._h, pages._addr, _int32("seqs", seqs, n), _int32("add", add, n), n)
+    n = seqs.numel()
+    st = lib().cr_pages_extend(ctx._h, pages._addr, _int32("seqs", seqs), _int32("add", add, n), n)
     if st:
         ctx.check(st, "cr_pages_extend")
 
 
 def pages_fork(ctx: Context, pages: KVPages, src, dst, keep):
     """The empty rows ``dst`` become the first ``keep`` tokens of the rows ``src`` (cr_pages_fork)."""
-    n = src.shape[0]
-    st = lib().cr_pages_fork(ctx._h, pages._addr, _int32("src", src, n), _int32("dst", dst, n),
-                             _int32("keep", keep, n), n)
+    n = src.numel()
+    st = lib().cr_pages_fork(ctx._h, pages._addr, _int32("src", src), _int32("dst", dst, n), _int32("keep", keep, n), n)
     if st:
         ctx.check(st, "cr_pages_fork")
 
 
 def pages_free(ctx: Context, pages: KVPages, seqs):
     """The rows ``seqs`` become empty (cr_pages_free)."""
-    n = seqs.shape[0]
-    st = lib().cr_pages_free(ctx._h, pages._addr, _int32("seqs", seqs, n), n)
+    st = lib().cr_pages_free(ctx._h, pages._addr, _int32("seqs", seqs), seqs.numel())
     if st:
         ctx.check(st, "cr_pages_free")
 
@@ -666,10 +675,11 @@ def pages_free(ctx: Context, pages: KVPages, seqs):
 def pages_compact(ctx: Context, pages: KVPages):
     """Move live pages to the front (cr_pages_compact): (ref, table, page_map, n_live), new tensors;
     ``pages.replace(ref, table)`` takes them."""
-    ref = _out(ctx, pages.ref.shape, pages.ref)
-    table = _out(ctx, pages.table.shape, pages.table)
-    page_map = _out(ctx, pages.ref.shape, pages.ref)
-    live = _out(ctx, (1,), pages.ref)
+    int32 = _torch.int32
+    ref = _out(ctx, pages.ref.shape, pages.ref, int32)
+    table = _out(ctx, pages.table.shape, pages.table, int32)
+    page_map = _out(ctx, pages.ref.shape, pages.ref, int32)
+    live = _out(ctx, (1,), pages.ref, int32)
     st = lib().cr_pages_compact(ctx._h, pages._addr, ref.data_ptr(), table.data_ptr(), page_map.data_ptr(),
                                 live.data_ptr())
     if st:
@@ -680,9 +690,11 @@ def pages_compact(ctx: Context, pages: KVPages):
 def kv_write(ctx: Context, pages: KVPages, layer: int, k, v, cu, seqs=None):
     """Write the keys and values [tokens, kv_heads, head_dim] of every sequence's last tokens into its pages:
     entry i's tokens are cu[i] .. cu[i+1]-1, its row seqs[i] (None: i) (cr_kv_write)."""
-    n = max(cu.shape[0] - 1, 0)
-    T, kp, kt, kh = _heads("k", k, pages.dtype, (None, pages.kv_heads, pages.head_dim))
-    _, vp, vt, vh = _heads("v", v, pages.dtype, (T, pages.kv_heads, pages.head_dim))
+    n = max(cu.numel() - 1, 0)
+    shape = k.shape
+    T = shape[0]
+    kp, kt, kh = _heads("k", k, pages.dtype, shape, None, pages.kv_heads, pages.head_dim)
+    vp, vt, vh = _heads("v", v, pages.dtype, v.shape, T, pages.kv_heads, pages.head_dim)
     st = lib().cr_kv_write(ctx._h, pages._addr, layer, kp, kt, kh, vp, vt, vh, _int32("cu", cu),
                            None if seqs is None else _int32("seqs", seqs, n), n, T)
     if st:
@@ -692,24 +704,26 @@ def kv_write(ctx: Context, pages: KVPages, layer: int, k, v, cu, seqs=None):
 _pack_attn = struct.Struct("@5P4IfI4Q").pack  # cr_attn_args
 
 
-def _attn_args(ctx: Context, q, dtype, dim, n, cu, seqs, causal, scale, out, lse):
-    """cr_attn_args as bytes, and the outputs."""
-    import torch
-    T, qp, qt, qh = _heads("q", q, dtype, (None, None, dim))
-    heads, dim = q.shape[1], q.shape[2]
+def _attn_args(ctx: Context, q, dtype, shape, dim, n, cu, seqs, causal, scale, out, lse):
+    """cr_attn_args as bytes, and the outputs; ``shape``: q.shape, ``cu``: address or 0."""
+    qp, qt, qh = _heads("q", q, dtype, shape, None, None, dim)
+    T, heads, dim = shape
     if out is None:
-        out = _out(ctx, (T, heads, dim), q)
-    _, op, ot, oh = _heads("out", out, dtype, (T, heads, dim))
-    if lse is True:
-        lse = _out(ctx, (T, heads), q, torch.float32)
-    elif lse is False:
-        lse = None
-    elif lse is not None:
-        _need_cuda("lse", lse, torch.float32)
+        out = _torch.empty_like(q, memory_format=_torch.contiguous_format)
+        if ctx._raw_stream != _torch._C._cuda_getCurrentRawStream(ctx.device):
+            out.record_stream(ctx._stream_obj)
+        op, ot, oh = out.data_ptr(), heads * dim, dim
+    else:
+        op, ot, oh = _heads("out", out, dtype, out.shape, T, heads, dim)
+    lp = 0
+    if lse is not None and lse is not False:
+        if lse is True:
+            lse = _out(ctx, (T, heads), q, _torch.float32)
+        _need_cuda("lse", lse, _torch.float32)
         if tuple(lse.shape) != (T, heads):
             raise ValueError(f"lse must have shape {(T, heads)}")
-    a = _pack_attn(qp, op, 0 if lse is None else lse.data_ptr(), 0 if cu is None else _int32("cu", cu),
-                   0 if seqs is None else _int32("seqs", seqs, n), n, T, heads, 1 if causal else 0,
+        lp = lse.data_ptr()
+    a = _pack_attn(qp, op, lp, cu, 0 if seqs is None else _int32("seqs", seqs, n), n, T, heads, 1 if causal else 0,
                    dim ** -0.5 if scale is None else scale, 0, qt, qh, ot, oh)
     return a, out, lse
 
@@ -719,30 +733,34 @@ def attn_packed(ctx: Context, q, k, v, cu, cu_k=None, causal: bool = True, scale
     """Attention over whole prompts packed back to back: q [tokens, heads, head_dim], k and v [tokens, kv_heads,
     head_dim]; sequence i's queries are cu[i] .. cu[i+1]-1, its keys cu_k[i] .. (None: the same) (cr_attn_packed).
     Returns the output, or (output, lse) with ``lse=True`` (or a tensor for it)."""
-    n = max(cu.shape[0] - 1, 0)
-    code = _dtype_code(q)
-    a, out, lse = _attn_args(ctx, q, q.dtype, None, n, cu, None, causal, scale, out, lse)
-    dim = q.shape[2]
-    S, kp, kt, kh = _heads("k", k, q.dtype, (None if cu_k is not None else q.shape[0], None, dim))
-    heads = k.shape[1]
-    _, vp, vt, vh = _heads("v", v, q.dtype, (S, heads, dim))
+    n = max(cu.numel() - 1, 0)
+    dtype, shape, kshape = q.dtype, q.shape, k.shape
+    code = _codes.get(dtype)
+    if code is None:
+        code = _dtype_code(dtype)
+    if len(shape) != 3 or len(kshape) != 3:
+        raise ValueError("q and k must be [tokens, heads, head_dim]")
+    S, heads, dim = kshape
+    kp, kt, kh = _heads("k", k, dtype, kshape, None if cu_k is not None else shape[0], None, shape[2])
+    vp, vt, vh = _heads("v", v, dtype, v.shape, S, heads, dim)
+    a, out, lse = _attn_args(ctx, q, dtype, shape, dim, n, _int32("cu", cu), None, causal, scale, out, lse)
     st = lib().cr_attn_packed(ctx._h, a, code, heads, dim, kp, kt, kh, vp, vt, vh,
                               None if cu_k is None else _int32("cu_k", cu_k, n + 1), S)
     if st:
         ctx.check(st, "cr_attn_packed")
-    return out if lse is None else (out, lse)
+    return (out, lse) if lse is not None and lse is not False else out
 
 
 def attn_paged(ctx: Context, q, pages: KVPages, layer: int, cu, seqs=None, causal: bool = True,
                scale: Optional[float] = None, out=None, lse=None):
     """Attention of every sequence's last tokens over its pages (cr_attn_paged): q [tokens, heads, head_dim], entry
     i's queries cu[i] .. cu[i+1]-1, its row seqs[i] (None: i).  Returns as ``attn_packed``."""
-    n = max(cu.shape[0] - 1, 0)
-    a, out, lse = _attn_args(ctx, q, pages.dtype, pages.head_dim, n, cu, seqs, causal, scale, out, lse)
+    a, out, lse = _attn_args(ctx, q, pages.dtype, q.shape, pages.head_dim, max(cu.numel() - 1, 0), _int32("cu", cu), seqs,
+                             causal, scale, out, lse)
     st = lib().cr_attn_paged(ctx._h, pages._addr, layer, a)
     if st:
         ctx.check(st, "cr_attn_paged")
-    return out if lse is None else (out, lse)
+    return (out, lse) if lse is not None and lse is not False else out
 
 
 def attn_decode(ctx: Context, q, pages: KVPages, layer: int, seqs=None, group_off=None, shared=None,
@@ -754,10 +772,11 @@ def attn_decode(ctx: Context, q, pages: KVPages, layer: int, seqs=None, group_of
     if group_off is not None:
         if shared is None:
             raise ValueError("group_off without shared")
-        ng = max(group_off.shape[0] - 1, 0)
+        ng = max(group_off.numel() - 1, 0)
         go, sh = _int32("group_off", group_off), _int32("shared", shared, ng)
-    a, out, lse = _attn_args(ctx, q, pages.dtype, pages.head_dim, q.shape[0], None, seqs, False, scale, out, lse)
+    shape = q.shape
+    a, out, lse = _attn_args(ctx, q, pages.dtype, shape, pages.head_dim, shape[0], 0, seqs, False, scale, out, lse)
     st = lib().cr_attn_decode(ctx._h, pages._addr, layer, a, go, sh, ng)
     if st:
         ctx.check(st, "cr_attn_decode")
-    return out if lse is None else (out, lse)
+    return (out, lse) if lse is not None and lse is not False else out

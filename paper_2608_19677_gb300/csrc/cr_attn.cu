@@ -25,7 +25,7 @@ namespace {
 constexpr int kRowsTile = 128;  // query rows of a tile, and keys of one
 constexpr int kFewTile = 64;    // keys of a tile of k_attn_few
 constexpr int kFewWarps = 4;
-constexpr uint32_t kExtra = 1, kPieceCost = 3;
+constexpr uint32_t kExtra = 1;
 
 // A block of query rows of one key head.
 struct __align__(16) attn_blk {
@@ -46,7 +46,7 @@ struct __align__(16) attn_start {
     // where the stretch is the first to begin inside that block: the block's pieces (from the stretch before on)
     uint32_t pieces, pad[3];
 };
-constexpr uint32_t kPlanThreads = 512, kMaxCtas = kPlanThreads - 1;
+constexpr uint32_t kMaxCtas = 511;
 
 // What the plan kernel reads.
 struct plan_in {
@@ -59,6 +59,7 @@ struct plan_in {
     uint32_t tok_blk;      // query tokens per block
     uint32_t max_len;      // paged: tokens that a row can hold
     uint32_t min_tiles;    // key tiles that a CTA is worth
+    uint32_t piece_cost;   // what a piece costs, in key tiles
     attn_blk *blk;
     attn_start *start;        // [max_cta + 1]
     uint32_t *joins;          // [max_cta + 1] number of blocks with several pieces, and their first stretches
@@ -70,7 +71,10 @@ struct plan_in {
 constexpr uint32_t kPlanShared = 512;
 struct plan_shared {
     unsigned long long cum[kPlanShared + 1], pos[kMaxCtas + 1];
-    uint32_t first[kPlanShared + 1], joins;
+    unsigned long long end[kMaxCtas + 1];  // of the block that a stretch begins inside, or 0
+    unsigned long long part[32];
+    uint32_t first_tile[kMaxCtas + 1];
+    uint32_t first[kPlanShared + 1], joins, longest;
     int goff[kPlanShared + 1], keys[kPlanShared];  // groups
     attn_blk blk[kPlanShared];
 };
@@ -79,10 +83,10 @@ enum { PLAN_PACKED, PLAN_PAGED, PLAN_GROUPS, PLAN_FEW };
 
 __device__ __forceinline__ int clampi(int v, int lo, int hi) { return v < lo ? lo : (v > hi ? hi : v); }
 
-// Exclusive scan over the kPlanThreads threads of the CTA; *total receives the sum.
-__device__ unsigned long long scan_cta(unsigned long long v, unsigned long long *total)
+// Exclusive scan over the CTA's NT threads; *total receives the sum.
+template <int NT>
+__device__ unsigned long long scan_cta(unsigned long long v, unsigned long long *part, unsigned long long *total)
 {
-    __shared__ unsigned long long part[kPlanThreads / 32];
     const uint32_t lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     unsigned long long x = v;
 #pragma unroll
@@ -92,18 +96,14 @@ __device__ unsigned long long scan_cta(unsigned long long v, unsigned long long 
     }
     if (lane == 31) part[w] = x;
     __syncthreads();
-    if (w == 0) {
-        unsigned long long q = lane < kPlanThreads / 32 ? part[lane] : 0;
+    unsigned long long before = 0, sum = 0;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const unsigned long long y = __shfl_up_sync(~0u, q, o);
-            if (lane >= (uint32_t)o) q += y;
-        }
-        if (lane < kPlanThreads / 32) part[lane] = q;
+    for (int i = 0; i < NT / 32; ++i) {
+        const unsigned long long y = part[i];
+        if (i < (int)w) before += y;
+        sum += y;
     }
-    __syncthreads();
-    const unsigned long long before = w ? part[w - 1] : 0;
-    *total = part[kPlanThreads / 32 - 1];
+    *total = sum;
     __syncthreads();
     return before + x - v;
 }
@@ -161,7 +161,7 @@ __device__ __forceinline__ unsigned long long div_by(unsigned long long a, unsig
     return a >> 32 || b >> 32 ? a / b : (uint32_t)a / (uint32_t)b;
 }
 
-template <int KIND>
+template <int KIND, int NT>
 __device__ void plan_build(const plan_in &A, plan_shared &S, uint32_t *status)
 {
     const uint32_t tid = threadIdx.x;
@@ -170,11 +170,11 @@ __device__ void plan_build(const plan_in &A, plan_shared &S, uint32_t *status)
     const bool near = A.max_blk <= kPlanShared;
     unsigned long long *cum = near ? S.cum : A.cum;
     unsigned long long total, base = 0;
-    if (tid == 0) S.joins = 0;
+    if (tid == 0) S.joins = S.longest = 0;
     // blocks of every entry
     uint32_t nblk = n;
     if (KIND != PLAN_FEW) {
-        for (uint32_t i0 = 0; i0 < n; i0 += kPlanThreads) {
+        for (uint32_t i0 = 0; i0 < n; i0 += NT) {
             const uint32_t i = i0 + tid;
             unsigned long long nb = 0;
             if (i < n) {
@@ -182,7 +182,7 @@ __device__ void plan_build(const plan_in &A, plan_shared &S, uint32_t *status)
                 q_range(A, i, lo, hi);
                 nb = ((uint32_t)(hi - lo) + A.tok_blk - 1) / A.tok_blk;
             }
-            const unsigned long long at = base + scan_cta(nb, &total);
+            const unsigned long long at = base + scan_cta<NT>(nb, S.part, &total);
             if (i < n) first[i] = (uint32_t)(at < A.max_blk ? at : A.max_blk);
             base += total;
         }
@@ -194,18 +194,19 @@ __device__ void plan_build(const plan_in &A, plan_shared &S, uint32_t *status)
         if (tid == 0) first[n] = nblk;
         __syncthreads();
     } else if (A.n_groups && A.n_groups <= kPlanShared) {
-        if (tid < A.n_groups) {
-            S.keys[tid] = group_keys(A, tid);
-            S.goff[tid] = A.goff[tid];
-            if (A.goff[tid] > A.goff[tid + 1]) atomicOr(status, CR_FLAG_BADPAGES);
+        for (uint32_t g = tid; g < A.n_groups; g += NT) {
+            S.keys[g] = group_keys(A, g);
+            S.goff[g] = A.goff[g];
+            if (A.goff[g] > A.goff[g + 1]) atomicOr(status, CR_FLAG_BADPAGES);
         }
         if (tid == 0) S.goff[A.n_groups] = A.goff[A.n_groups];
         __syncthreads();
     }
     // their keys
     uint32_t filled = 0;  // blocks that have any
+    unsigned long long most = 0;
     base = 0;
-    for (uint32_t b0 = 0; b0 < nblk; b0 += kPlanThreads) {
+    for (uint32_t b0 = 0; b0 < nblk; b0 += NT) {
         const uint32_t b = b0 + tid;
         unsigned long long nt = 0;
         attn_blk k = {};
@@ -257,33 +258,46 @@ __device__ void plan_build(const plan_in &A, plan_shared &S, uint32_t *status)
                 for (int t = 0; t < k.ntok; ++t) A.of_token[k.row0 + t] = k.row0;
         }
         filled += __syncthreads_count(nt > 0);
-        const unsigned long long at = base + scan_cta(nt ? nt + kExtra : 0, &total);
+        const unsigned long long at = base + scan_cta<NT>(nt ? nt + kExtra : 0, S.part, &total);
         if (b < nblk) {
             cum[b] = at;
             A.blk[b] = k;
             if (near) S.blk[b] = k;
+            if (nt > most) most = nt;
         }
         base += total;
     }
     if (tid == 0) cum[nblk] = base;
+    if (most) atomicMax(&S.longest, (uint32_t)most);
     __syncthreads();
     // stretches
     const unsigned long long Nb = base, N = Nb * A.heads;  // N < 2^54
     const unsigned long long want = div_by(N, A.min_tiles);
     uint32_t ncta = want < 1 ? 1u : (want < A.max_cta ? (uint32_t)want : A.max_cta);
-    // Few blocks: as many stretches for each, so that most of them are within one block and leave one piece instead
-    // of two, where that makes them longer by less than a piece costs (its result's way to scratch and back).
+    // Few blocks.  One stretch for each block leaves no pieces; where that is too long, as many for each, so that most
+    // stretches are within one block and leave one piece instead of two.  Both where they make the longest stretch
+    // longer by less than a piece costs (its result's way to scratch and back).
     const unsigned long long blocks = (unsigned long long)filled * A.heads;
-    if (blocks && blocks <= ncta) {
-        const uint32_t even = ncta / (uint32_t)blocks * (uint32_t)blocks;
-        if (div_by(N, even) <= div_by(N, ncta) + kPieceCost) ncta = even;
+    bool one_each = false;
+    if (blocks && blocks <= A.max_cta) {
+        const unsigned long long most_now = div_by(N, ncta) + A.piece_cost;
+        if (filled == nblk && S.longest + kExtra <= most_now) {
+            one_each = true;
+            ncta = (uint32_t)blocks;
+        } else if (blocks <= ncta) {
+            const uint32_t even = ncta / (uint32_t)blocks * (uint32_t)blocks;
+            if (div_by(N, even) <= most_now) ncta = even;
+        }
     }
     const unsigned long long snap = div_by(N, ncta) / 8;  // a stretch ends with its block where that is near
-    const uint32_t c = tid;
-    attn_start s = {};
-    if (c <= A.max_cta) {
+    for (uint32_t c = tid; c <= A.max_cta; c += NT) {
+        attn_start s = {};
         s.pos = c < ncta ? div_by(N * c, ncta) : N;
-        if (s.pos < N) {
+        if (one_each && c < ncta) {
+            s.head = c / nblk;
+            s.blk = c - s.head * nblk;
+            s.pos = s.head * Nb + cum[s.blk];
+        } else if (s.pos < N) {
             s.head = (uint32_t)div_by(s.pos, Nb);
             const unsigned long long rem = s.pos - s.head * Nb;
             s.blk = at_or_below(cum, nblk, rem);
@@ -311,34 +325,33 @@ __device__ void plan_build(const plan_in &A, plan_shared &S, uint32_t *status)
                 }
             s.k = near ? S.blk[s.blk] : A.blk[s.blk];
         }
+        A.start[c] = s;
         S.pos[c] = s.pos;
+        S.end[c] = s.tile && s.pos < N ? s.pos - s.tile + (uint32_t)s.k.nt : 0;
+        S.first_tile[c] = s.tile;
     }
     __syncthreads();
-    if (c <= A.max_cta) {
-        if (c && s.tile && s.pos < N) {
-            const unsigned long long begin = s.pos - s.tile - kExtra, end = begin + kExtra + (uint32_t)s.k.nt;
-            if (S.pos[c - 1] <= begin) {
-                s.pieces = at_or_below(S.pos, A.max_cta, end - 1) + 1 - (c - 1);
-                A.joins[1 + atomicAdd(&S.joins, 1)] = c;  // in any order
-            }
-        }
-        A.start[c] = s;
+    // the first stretch that begins inside a block joins its pieces
+    for (uint32_t c = 1 + tid; c < ncta; c += NT) {
+        if (S.end[c] == 0 || S.pos[c - 1] > S.pos[c] - S.first_tile[c] - kExtra) continue;
+        A.start[c].pieces = at_or_below(S.pos, A.max_cta, S.end[c] - 1) + 1 - (c - 1);
+        A.joins[1 + atomicAdd(&S.joins, 1)] = c;  // in any order
     }
     __syncthreads();
     if (tid == 0) A.joins[0] = S.joins;
 }
 
-template <int KIND>
-__global__ void __launch_bounds__(kPlanThreads) k_attn_plan(const __grid_constant__ plan_in a, const __grid_constant__ plan_in b,
-                                                    uint32_t *status)
+template <int KIND, int NT>
+__global__ void __launch_bounds__(NT) k_attn_plan(const __grid_constant__ plan_in a, const __grid_constant__ plan_in b,
+                                                  uint32_t *status)
 {
     __shared__ plan_shared S;
     cr_launch_next();
     cr_wait_previous();
     if (blockIdx.x == 0)
-        plan_build<KIND>(a, S, status);
+        plan_build<KIND, NT>(a, S, status);
     else
-        plan_build<PLAN_GROUPS>(b, S, status);
+        plan_build<PLAN_GROUPS, NT>(b, S, status);
 }
 
 // What the attention kernels read.
@@ -1590,6 +1603,16 @@ int few(cr_ctx *ctx, const attn_in &A, const attn_in *R, const kv_desc &K, const
     return wide ? launch_few<128, false, true>(ctx, A, R, K, a, ctas) : launch_few<128, false, false>(ctx, A, R, K, a, ctas);
 }
 
+// The list of work of a call, and that of its groups.  A short list for few CTAs is made by fewer threads, whose
+// barriers are cheaper (one prompt of 512 tokens: 7,600 cycles with 512 threads, 6,400 with 256).
+template <int KIND>
+int launch_plan(cr_ctx *ctx, const plan_in &a, const plan_in *b)
+{
+    if (a.n <= 256 && a.max_blk <= 256 && a.max_cta < 256)
+        return cr_launch_early(ctx, "k_attn_plan", k_attn_plan<KIND, 256>, dim3(b ? 2 : 1), 256, 0, a, b ? *b : a, ctx->d_status);
+    return cr_launch_early(ctx, "k_attn_plan", k_attn_plan<KIND, 512>, dim3(b ? 2 : 1), 512, 0, a, b ? *b : a, ctx->d_status);
+}
+
 // Pieces of a list of work: two per CTA at most.
 int part_mem(cr_ctx *ctx, int slot, attn_in &A, uint32_t ctas, uint32_t rows_per_piece, uint32_t D)
 {
@@ -1601,7 +1624,7 @@ int part_mem(cr_ctx *ctx, int slot, attn_in &A, uint32_t ctas, uint32_t rows_per
     return CR_OK;
 }
 
-constexpr uint32_t kRowsMinTiles = 4, kFewMinTiles = 4;
+constexpr uint32_t kRowsMinTiles = 4, kFewMinTiles = 4, kRowsPieceCost = 3, kFewPieceCost = 6;
 
 int attn_many(cr_ctx *ctx, const cr_attn_args *a, const kv_desc &K)
 {
@@ -1622,6 +1645,7 @@ int attn_many(cr_ctx *ctx, const cr_attn_args *a, const kv_desc &K)
     p.tok_blk = 2 * A.tq;
     p.max_blk = a->n_tokens / p.tok_blk + (a->n < a->n_tokens ? a->n : a->n_tokens);
     p.min_tiles = kRowsMinTiles;
+    p.piece_cost = kRowsPieceCost;
     if (K.paged) {
         p.lens = K.pg->d_lens;
         p.n_seqs = K.pg->n_seqs;
@@ -1634,9 +1658,9 @@ int attn_many(cr_ctx *ctx, const cr_attn_args *a, const kv_desc &K)
     mem.point(static_cast<char *>(base), p, A);
     CR_TRY(part_mem(ctx, SCR_ATTN_PART, A, p.max_cta, 2 * kRowsTile, K.dim <= 64 ? 64 : 128));
     if (K.paged)
-        CR_TRY(cr_launch_early(ctx, "k_attn_plan", k_attn_plan<PLAN_PAGED>, dim3(1), kPlanThreads, 0, p, p, ctx->d_status));
+        CR_TRY(launch_plan<PLAN_PAGED>(ctx, p, nullptr));
     else
-        CR_TRY(cr_launch_early(ctx, "k_attn_plan", k_attn_plan<PLAN_PACKED>, dim3(1), kPlanThreads, 0, p, p, ctx->d_status));
+        CR_TRY(launch_plan<PLAN_PACKED>(ctx, p, nullptr));
     return rows(ctx, A, K, a, p.max_cta);
 }
 
@@ -1745,6 +1769,7 @@ extern "C" int cr_attn_decode(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t la
     f.heads = F.few_heads = K.heads * F.nsub;
     f.max_cta = min(2 * (uint32_t)ctx->num_sms, kMaxCtas);
     f.min_tiles = kFewMinTiles;
+    f.piece_cost = kFewPieceCost;
     plan_in g = f;
     g.cu_q = d_group_off;
     g.heads = K.heads;
@@ -1752,6 +1777,7 @@ extern "C" int cr_attn_decode(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t la
     g.max_blk = args->n / g.tok_blk + (n_groups < args->n ? n_groups : args->n);
     g.max_cta = min((uint32_t)ctx->num_sms, kMaxCtas);
     g.min_tiles = kRowsMinTiles;
+    g.piece_cost = kRowsPieceCost;
 
     const bool grouped = n_groups > 0;
     const plan_mem mf(f.max_blk, f.max_cta, f.n, 0, grouped ? (uint64_t)f.n * F.few_heads : 0),
@@ -1772,10 +1798,10 @@ extern "C" int cr_attn_decode(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t la
         F.pfx_lse = R.pfx_lse = F.own_ml + 2 * own;
         R.to_pfx = 1;
         F.after_rows = 1;
-        CR_TRY(cr_launch_early(ctx, "k_attn_plan", k_attn_plan<PLAN_FEW>, dim3(2), kPlanThreads, 0, f, g, ctx->d_status));
+        CR_TRY(launch_plan<PLAN_FEW>(ctx, f, &g));
         CR_TRY(rows(ctx, R, K, args, g.max_cta));
     } else {
-        CR_TRY(cr_launch_early(ctx, "k_attn_plan", k_attn_plan<PLAN_FEW>, dim3(1), kPlanThreads, 0, f, f, ctx->d_status));
+        CR_TRY(launch_plan<PLAN_FEW>(ctx, f, nullptr));
     }
     return few(ctx, F, n_groups ? &R : nullptr, K, args, f.max_cta);
 }
