@@ -445,7 +445,7 @@ struct rows_cfg {
     static constexpr int kStages = D == 128 ? 5 : 10;    // of a tile's keys or values
     // after the tiles: a value per (tile, half, row), pieces, barriers, two words
     static constexpr int kXch = (2 + kStages) * kTile, kPieces = kXch + 4 * kRowsTile * 4, kBars = kPieces + 2 * 48;
-    static constexpr int kSmem = kBars + 8 * (18 + 2 * kStages) + 16;
+    static constexpr int kSmem = kBars + 8 * (26 + 2 * kStages) + 16;
     static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
 };
 // Warps 0-15: softmax (tile, half of the keys, 32 rows); 16: products; 17: copies; 18, 19 make the
@@ -453,7 +453,7 @@ struct rows_cfg {
 constexpr int kRowsThreads = 640;
 
 enum { B_QFULL, B_QEMPTY, B_DONE, B_SFULL, B_PREADY = B_SFULL + 2, B_OFULL = B_PREADY + 4, B_OEMPTY = B_OFULL + 2,
-       B_PFULL = B_OEMPTY + 2, B_PEMPTY = B_PFULL + 2, B_FULL = B_PEMPTY + 2 };
+       B_PFULL = B_OEMPTY + 2, B_PEMPTY = B_PFULL + 2, B_LREAD = B_PEMPTY + 2, B_FULL = B_LREAD + 8 };
 
 // What the copying warp tells the others of a piece (two of them are kept).
 struct rows_piece {
@@ -470,7 +470,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                 const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
 {
     using cfg = rows_cfg<D>;
-    static_assert(B_FULL <= 18, "barriers");
+    static_assert(B_FULL <= 26, "barriers");
     extern __shared__ __align__(1024) unsigned char dyn[];
     volatile rows_piece *piece = reinterpret_cast<volatile rows_piece *>(dyn + cfg::kPieces);
     float(*xch)[kRowsTile] = reinterpret_cast<float(*)[kRowsTile]>(dyn + cfg::kXch);
@@ -506,6 +506,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             cr_bar_init(BAR(B_PFULL + x), 1);
             cr_bar_init(BAR(B_PEMPTY + x), 17);
         }
+        for (int i = 0; i < 8; ++i) cr_bar_init(BAR(B_LREAD + i), 2);
         for (int s = 0; s < cfg::kStages; ++s) {
             cr_bar_init(FULL(s), 1);
             cr_bar_init(EMPTY(s), 1);
@@ -700,14 +701,16 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         const unsigned long long c2 = cr_pair(c, c);
         uint32_t sphase = 0;
         // The other half's value of this row.  The next value is written only after the other warp has read this
-        // one: the next scores come after both warps' weights, and a piece ends with another meeting.
+        // one: the next scores come after both warps' weights, and the last value of a piece has a barrier for it.
+        // Between two meetings there is always a wait with a limit, where a warp may leave (then it releases its
+        // partner once).
         auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(pair) : "memory"); };
         auto exchange = [&](float v) {
             xch[x * 2 + half][row] = v;
             meet();
             return xch[x * 2 + (half ^ 1)][row];
         };
-        for (uint32_t ophase = 0;; ++pieces) {
+        for (uint32_t ophase = 0, lphase = 0;; ++pieces) {
             if (!cr_bar_wait(BAR(B_PFULL + (pieces & 1)), (pieces >> 1) & 1, &gave_up)) goto left;
             const volatile rows_piece *p = piece + (pieces & 1);
             const int n = p->n;
@@ -813,7 +816,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             ophase ^= 1;
             cr_tc_after();
             const float l2 = exchange(l);
-            meet();
+            __syncwarp();
+            if (lane == 0) cr_bar_arrive(BAR(B_LREAD + pair - 1));
+            if (!cr_bar_wait(BAR(B_LREAD + pair - 1), lphase, &gave_up)) goto left;
+            lphase ^= 1;
             l = half ? l2 + l : l + l2;
             const int mine = x * (int)A.tq + (int)(row / A.G);  // token of the block
             const bool valid = row < A.G * A.tq && mine < p->ntok;
@@ -1544,6 +1550,17 @@ void fill_common(attn_in &A, cr_ctx *ctx, const cr_attn_args *a, const kv_desc &
     }
 }
 
+// Raises a kernel's limit of dynamic shared memory, once per device (bits of `done`).
+template <typename K>
+int raise_smem(cr_ctx *ctx, K kern, int bytes, unsigned long long &done)
+{
+    const unsigned long long bit = 1ull << (ctx->device & 63);
+    if (done & bit) return CR_OK;
+    CR_CUDA(ctx, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    done |= bit;
+    return CR_OK;
+}
+
 int query_map(cr_ctx *ctx, CUtensorMap *map, const attn_in &A, const kv_desc &K, const cr_attn_args *a, uint32_t heads,
               uint32_t tokens)
 {
@@ -1560,8 +1577,8 @@ int launch_rows(cr_ctx *ctx, const attn_in &A, const kv_desc &K, const cr_attn_a
     CR_TRY(kv_map(ctx, &mk, K, false, A.box_rows));
     CR_TRY(kv_map(ctx, &mv, K, true, A.box_rows));
     auto kern = k_attn_rows<D, BF16>;
-    static const cudaError_t raised = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, rows_cfg<D>::kSmem);
-    if (raised != cudaSuccess) return cr_fail(ctx, CR_ECUDA, "k_attn_rows: %s", cudaGetErrorString(raised));
+    static unsigned long long raised = 0;
+    CR_TRY(raise_smem(ctx, kern, rows_cfg<D>::kSmem, raised));
     CR_TRY(cr_launch_early(ctx, "k_attn_rows", kern, dim3(ctas), kRowsThreads, rows_cfg<D>::kSmem, A, mq, mk, mv));
     if (ctas > 1 && !A.to_pfx)
         CR_TRY(cr_launch_early(ctx, "k_attn_join", k_attn_join<D, BF16, 2 * kRowsTile>, dim3(4 * ctx->num_sms), 256, 0, A));
@@ -1582,8 +1599,8 @@ int launch_few(cr_ctx *ctx, const attn_in &A, const attn_in *R, const kv_desc &K
     CR_TRY(kv_map(ctx, &mk, K, false, A.box_rows));
     CR_TRY(kv_map(ctx, &mv, K, true, A.box_rows));
     auto kern = k_attn_few<D, BF16, WIDE>;
-    static const cudaError_t raised = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, few_cfg<D>::kSmem);
-    if (raised != cudaSuccess) return cr_fail(ctx, CR_ECUDA, "k_attn_few: %s", cudaGetErrorString(raised));
+    static unsigned long long raised = 0;
+    CR_TRY(raise_smem(ctx, kern, few_cfg<D>::kSmem, raised));
     CR_TRY(cr_launch_early(ctx, "k_attn_few", kern, dim3(ctas), kFewThreads, few_cfg<D>::kSmem, A, mq, mk, mv));
     if (R)
         CR_TRY(cr_launch_early(ctx, "k_attn_decode_join", k_attn_decode_join<D, BF16>, dim3(a->n, A.few_heads), 256, 0, A, *R));
@@ -1709,11 +1726,10 @@ extern "C" int cr_attn_packed(cr_ctx *ctx, const cr_attn_args *args, uint32_t dt
     K.v_head = v_head;
     K.n_kv = n_kv;
     K.cu_k = d_cu_k ? d_cu_k : args->d_cu_q;
-    if (n_kv == 0) {  // nothing to map: any 16-byte aligned memory stands for the empty tensors
+    if (n_kv == 0 && args->n_tokens) {  // nothing to map: the queries' first elements stand for the empty tensors
         K.k = K.v = args->d_q;
-        K.k_row = K.v_row = args->q_token;
-        K.k_head = K.v_head = 8;
-        K.heads = kv_heads;
+        K.k_row = K.v_row = K.k_head = K.v_head = 8;
+        K.n_kv = 1;
     }
     return attn_many(ctx, args, K);
 }

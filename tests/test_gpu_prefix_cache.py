@@ -139,6 +139,13 @@ def test_packed_other_key_lengths(P, ctx, m, n, causal):
           [0, m, m + 3])
 
 
+def test_packed_without_any_keys(P, ctx):
+    q, none = randn(gen(4), 6, 8, 64), torch.zeros((0, 2, 64), dtype=BF, device=DEV)
+    out, lse = P.attn_packed(ctx, q, none, none, ints([0, 4, 6]), cu_k=ints([0, 0, 0]), lse=True)
+    ctx.sync()
+    assert (out == 0).all() and (lse == -math.inf).all()
+
+
 def test_packed_neighbours_do_not_leak(P, ctx):
     """What stands behind a sequence's end is its neighbour's; not a number there stays there."""
     g = gen(5)
@@ -481,6 +488,23 @@ def test_decode(P, ctx, page, hkv, hq, d, dtype, order, shared, seqs):
     out, lse = P.attn_decode(ctx, q, pg, 0, seqs=ints(rows), lse=True)
     ctx.sync()
     check(out, lse, [reference(q[i:i + 1], *kv[rows[i]], False, d ** -0.5) for i in range(len(lens))], cu)
+
+
+def test_decode_with_groups_that_are_not_ascending_stays_in_bounds(P, ctx):
+    """Outputs mean nothing then; the call is reported and the next one is right."""
+    g = gen(15)
+    pg, kv = fill(P, ctx, g, 16, [200, 300, 40, 500], 2, 64, BF)
+    q = randn(g, 4, 8, 64)
+    for off, shared in (([0, 3, 1, 4], [64, 64, 32]), ([3, 2, 1, 0], [16, 16, 16]), ([2, 9, -5, 4], [600, -7, 48]),
+                        ([0, 4, 4, 4], [5000, 16, 16])):
+        P.attn_decode(ctx, q, pg, 0, group_off=ints(off), shared=ints(shared))
+        try:
+            ctx.sync()
+        except P.CacheRouteError as e:
+            assert e.code == P.CR_EINVAL
+    out, lse = P.attn_decode(ctx, q, pg, 0, lse=True)
+    ctx.sync()
+    check(out, lse, [reference(q[i:i + 1], *kv[i], False, 0.125) for i in range(4)], range(5))
 
 
 def test_decode_long_and_shared_not_whole_pages(P, ctx):
