@@ -704,9 +704,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         const uint32_t pair = 1 + x * 4 + (warp & 3);  // barrier of the two warps that share rows
         const float c = A.c;
         const unsigned long long c2 = cr_pair(c, c);
+        const int tok = x * (int)A.tq + (int)(row / A.G), hd = row < A.G * A.tq ? (int)(row % A.G) : -1;
         uint32_t sphase = 0;
         // The other half's value of this row.  The next value is written only after the other warp has read this
-        // one: the next scores come after both warps' weights, and the last value of a piece has a barrier for it.
+        // one: the next scores come after both warps' weights, and a piece's sums have B_LREAD before and after them.
         // Between two meetings there is always a wait with a limit, where a warp may leave (then it releases its
         // partner once).
         auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(pair) : "memory"); };
@@ -715,7 +716,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             meet();
             return xch[x * 2 + (half ^ 1)][row];
         };
-        for (uint32_t ophase = 0, lphase = 0;; ++pieces) {
+        for (uint32_t ophase = 0;; ++pieces) {
             if (!cr_bar_wait(BAR(B_PFULL + (pieces & 1)), (pieces >> 1) & 1, &gave_up)) goto left;
             const volatile rows_piece *p = piece + (pieces & 1);
             const int n = p->n;
@@ -728,7 +729,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             // keys that this row sees, from the first tile's on; the tile with the sequence's end
             int seen = p->klen - p->t0 * kRowsTile - half * 64;
             const int tail = x == 0 && half < cfg::kChunks ? (p->klen >> 7) - p->t0 : -1;
-            if (A.causal) seen = min(seen, p->diag + x * (int)A.tq + (int)(row / A.G) + 1 - p->t0 * kRowsTile - half * 64);
+            if (A.causal) seen = min(seen, p->diag + tok + 1 - p->t0 * kRowsTile - half * 64);
             float m = -INFINITY, l = 0.f;
             for (int j = 0; j < n; ++j, seen -= kRowsTile) {
                 if (!cr_bar_wait(BAR(B_SFULL + x), sphase, &gave_up)) goto left;
@@ -817,20 +818,23 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                 l += s0 + s1;
             }
             // ---- the piece's result ----
-            if (!cr_bar_wait(BAR(B_OFULL + x), ophase, &gave_up)) goto left;
-            ophase ^= 1;
-            cr_tc_after();
+            // While the last product is under way: the sums meet where the maxima did, once both warps have read those,
+            // and whatever else the result needs (0.5 to 1.5% of a call against doing it after that product).
+            __syncwarp();
+            if (lane == 0) cr_bar_arrive(BAR(B_LREAD + pair - 1));
+            if (!cr_bar_wait(BAR(B_LREAD + pair - 1), 0, &gave_up)) goto left;
             const float l2 = exchange(l);
             __syncwarp();
             if (lane == 0) cr_bar_arrive(BAR(B_LREAD + pair - 1));
-            if (!cr_bar_wait(BAR(B_LREAD + pair - 1), lphase, &gave_up)) goto left;
-            lphase ^= 1;
             l = half ? l2 + l : l + l2;
-            const int mine = x * (int)A.tq + (int)(row / A.G);  // token of the block
-            const bool valid = row < A.G * A.tq && mine < p->ntok;
+            const bool valid = hd >= 0 && tok < p->ntok;
             const int slot = p->slot;
-            const int head = p->h * (int)A.G + (int)(row % A.G);
-            const uint64_t tk = (uint64_t)(p->row0 + mine);
+            const int head = p->h * (int)A.G + hd;
+            const uint64_t tk = (uint64_t)(p->row0 + tok);
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            if (!cr_bar_wait(BAR(B_OFULL + x), ophase, &gave_up)) goto left;
+            ophase ^= 1;
+            cr_tc_after();
             if (slot >= 0) {
                 constexpr int RP = 2 * kRowsTile;  // rows of a piece
                 const uint32_t r = x * kRowsTile + row;
@@ -849,7 +853,6 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                     reinterpret_cast<float2 *>(A.part_ml)[(uint64_t)slot * RP + r] =
                         make_float2(m == -INFINITY ? m : m * c, l);
             } else {
-                const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll 1
                 for (int i = 0; i < D / 2; i += 16) {
                     uint32_t o[16];
@@ -886,6 +889,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                         A.lse[tk * A.q_heads + head] = lse2 * 0.693147180559945309f;
                 }
             }
+            if (!cr_bar_wait(BAR(B_LREAD + pair - 1), 1, &gave_up)) goto left;
             cr_tc_before();
             __syncwarp();
             if (lane == 0) {
