@@ -163,6 +163,89 @@ __device__ __forceinline__ unsigned long long div_by(unsigned long long a, unsig
     return a >> 32 || b >> 32 ? a / b : (uint32_t)a / (uint32_t)b;
 }
 
+// Key tiles of a single token's block; one at least, which writes zeros where there are no keys.
+__device__ __forceinline__ uint32_t few_tiles(int lo, int klen)
+{
+    const int t = (klen + kFewTile - 1) / kFewTile - lo / kFewTile;
+    return t > 1 ? t : 1;
+}
+
+// How the work is cut: N units in stretches of equal length, or one stretch for each block.
+struct plan_cut {
+    unsigned long long N, Nb, snap;
+    uint32_t nblk, ncta;
+    bool one_each;
+};
+// Nb: of a head; filled: blocks that have keys; longest: their most tiles.
+__device__ __forceinline__ plan_cut cut_work(const plan_in &A, unsigned long long Nb, uint32_t nblk, uint32_t filled,
+                                             uint32_t longest)
+{
+    plan_cut C;
+    C.Nb = Nb;
+    C.nblk = nblk;
+    C.N = Nb * A.heads;  // N < 2^54
+    const unsigned long long want = div_by(C.N, A.min_tiles);
+    C.ncta = want < 1 ? 1u : (want < A.max_cta ? (uint32_t)want : A.max_cta);
+    // Few blocks.  One stretch for each block leaves no pieces; where that is too long, as many for each, so that most
+    // stretches are within one block and leave one piece instead of two.  Both where they make the longest stretch
+    // longer by less than a piece costs (its result's way to scratch and back).
+    const unsigned long long blocks = (unsigned long long)filled * A.heads;
+    C.one_each = false;
+    if (blocks && blocks <= A.max_cta) {
+        const unsigned long long most_now = div_by(C.N, C.ncta) + A.piece_cost;
+        if (filled == nblk && longest + kExtra <= most_now) {
+            C.one_each = true;
+            C.ncta = (uint32_t)blocks;
+        } else if (blocks <= C.ncta) {
+            const uint32_t even = C.ncta / (uint32_t)blocks * (uint32_t)blocks;
+            if (div_by(C.N, even) <= most_now) C.ncta = even;
+        }
+    }
+    C.snap = div_by(C.N, C.ncta) / 8;  // a stretch ends with its block where that is near
+    return C;
+}
+
+// Where stretch c begins; cum: units before each block.
+__device__ __forceinline__ attn_start stretch(const plan_cut &C, const unsigned long long *cum, const attn_blk *blk,
+                                              uint32_t c)
+{
+    attn_start s = {};
+    s.pos = c < C.ncta ? div_by(C.N * c, C.ncta) : C.N;
+    if (C.one_each && c < C.ncta) {
+        s.head = c / C.nblk;
+        s.blk = c - s.head * C.nblk;
+        s.pos = s.head * C.Nb + cum[s.blk];
+    } else if (s.pos < C.N) {
+        s.head = (uint32_t)div_by(s.pos, C.Nb);
+        const unsigned long long rem = s.pos - s.head * C.Nb;
+        s.blk = at_or_below(cum, C.nblk, rem);
+        const unsigned long long t = rem - cum[s.blk], left = cum[s.blk + 1] - rem;
+        s.tile = (uint32_t)(t - kExtra);
+        if (t <= C.snap || t <= kExtra) {
+            s.pos -= t;
+            s.tile = 0;
+        } else if (left <= C.snap) {
+            s.pos += left;
+            s.tile = 0;
+            if (++s.blk == C.nblk) {
+                s.blk = 0;
+                ++s.head;
+            }
+        }
+    }
+    s.N = C.N;
+    s.nblk = C.nblk;
+    if (s.pos < C.N) {
+        while (cum[s.blk + 1] == cum[s.blk])  // blocks without keys
+            if (++s.blk == C.nblk) {
+                s.blk = 0;
+                ++s.head;
+            }
+        s.k = blk[s.blk];
+    }
+    return s;
+}
+
 template <int KIND, int NT>
 __device__ void plan_build(const plan_in &A, plan_shared &S, uint32_t *status)
 {
@@ -249,8 +332,7 @@ __device__ void plan_build(const plan_in &A, plan_shared &S, uint32_t *status)
                 if (A.causal) end = clampi(k.diag + k.ntok, 0, k.klen);
             }
             if (KIND == PLAN_FEW) {
-                const int t = (end + kFewTile - 1) / kFewTile - k.lo / kFewTile;
-                nt = t > 1 ? t : 1;
+                nt = few_tiles(k.lo, k.klen);
             } else {
                 nt = (uint32_t)((end + kRowsTile - 1) / kRowsTile);
                 if (nt == 0 && KIND != PLAN_GROUPS) nt = 1;  // rows without keys: zeros
@@ -273,68 +355,17 @@ __device__ void plan_build(const plan_in &A, plan_shared &S, uint32_t *status)
     if (most) atomicMax(&S.longest, (uint32_t)most);
     __syncthreads();
     // stretches
-    const unsigned long long Nb = base, N = Nb * A.heads;  // N < 2^54
-    const unsigned long long want = div_by(N, A.min_tiles);
-    uint32_t ncta = want < 1 ? 1u : (want < A.max_cta ? (uint32_t)want : A.max_cta);
-    // Few blocks.  One stretch for each block leaves no pieces; where that is too long, as many for each, so that most
-    // stretches are within one block and leave one piece instead of two.  Both where they make the longest stretch
-    // longer by less than a piece costs (its result's way to scratch and back).
-    const unsigned long long blocks = (unsigned long long)filled * A.heads;
-    bool one_each = false;
-    if (blocks && blocks <= A.max_cta) {
-        const unsigned long long most_now = div_by(N, ncta) + A.piece_cost;
-        if (filled == nblk && S.longest + kExtra <= most_now) {
-            one_each = true;
-            ncta = (uint32_t)blocks;
-        } else if (blocks <= ncta) {
-            const uint32_t even = ncta / (uint32_t)blocks * (uint32_t)blocks;
-            if (div_by(N, even) <= most_now) ncta = even;
-        }
-    }
-    const unsigned long long snap = div_by(N, ncta) / 8;  // a stretch ends with its block where that is near
+    const plan_cut C = cut_work(A, base, nblk, filled, S.longest);
     for (uint32_t c = tid; c <= A.max_cta; c += NT) {
-        attn_start s = {};
-        s.pos = c < ncta ? div_by(N * c, ncta) : N;
-        if (one_each && c < ncta) {
-            s.head = c / nblk;
-            s.blk = c - s.head * nblk;
-            s.pos = s.head * Nb + cum[s.blk];
-        } else if (s.pos < N) {
-            s.head = (uint32_t)div_by(s.pos, Nb);
-            const unsigned long long rem = s.pos - s.head * Nb;
-            s.blk = at_or_below(cum, nblk, rem);
-            const unsigned long long t = rem - cum[s.blk], left = cum[s.blk + 1] - rem;
-            s.tile = (uint32_t)(t - kExtra);
-            if (t <= snap || t <= kExtra) {
-                s.pos -= t;
-                s.tile = 0;
-            } else if (left <= snap) {
-                s.pos += left;
-                s.tile = 0;
-                if (++s.blk == nblk) {
-                    s.blk = 0;
-                    ++s.head;
-                }
-            }
-        }
-        s.N = N;
-        s.nblk = nblk;
-        if (s.pos < N) {
-            while (cum[s.blk + 1] == cum[s.blk])  // blocks without keys
-                if (++s.blk == nblk) {
-                    s.blk = 0;
-                    ++s.head;
-                }
-            s.k = near ? S.blk[s.blk] : A.blk[s.blk];
-        }
+        const attn_start s = stretch(C, cum, near ? S.blk : A.blk, c);
         A.start[c] = s;
         S.pos[c] = s.pos;
-        S.end[c] = s.tile && s.pos < N ? s.pos - s.tile + (uint32_t)s.k.nt : 0;
+        S.end[c] = s.tile && s.pos < C.N ? s.pos - s.tile + (uint32_t)s.k.nt : 0;
         S.first_tile[c] = s.tile;
     }
     __syncthreads();
     // the first stretch that begins inside a block joins its pieces
-    for (uint32_t c = 1 + tid; c < ncta; c += NT) {
+    for (uint32_t c = 1 + tid; c < C.ncta; c += NT) {
         if (S.end[c] == 0 || S.pos[c - 1] > S.pos[c] - S.first_tile[c] - kExtra) continue;
         A.start[c].pieces = at_or_below(S.pos, A.max_cta, S.end[c] - 1) + 1 - (c - 1);
         A.joins[1 + atomicAdd(&S.joins, 1)] = c;  // in any order
@@ -377,7 +408,68 @@ struct attn_in {
     uint32_t to_pfx;       // k_attn_rows, its join: write those instead of o
     uint32_t o_wide;       // rows of o begin at multiples of 32 bytes
     uint32_t *status;
+    uint32_t own_list;     // k_attn_few, its join: every CTA makes the list of work itself, from
+    plan_in plan;
 };
+
+// A short list of single tokens: a warp makes it in every CTA, a token a lane, which saves the plan kernel's launch and
+// its run before this one's (32/8 heads of 128, calls back to back: one sequence of 2,048 keys 15.0 us with that kernel
+// and 12.6 so, eight 20.9 and 18.3, 32 65.3 and 61.8).
+constexpr uint32_t kOwnList = 32;
+struct own_list {
+    attn_start start[2];        // this CTA's stretch and the next
+    unsigned long long before;  // where the one before begins
+    attn_blk blk[kOwnList];
+    unsigned long long cum[kOwnList + 1];
+};
+__device__ __forceinline__ plan_cut make_list(const plan_in &P, own_list *L, uint32_t *status)
+{
+    const uint32_t lane = threadIdx.x & 31;
+    attn_blk k = {};
+    unsigned long long at = 0;
+    if (lane < P.n) {
+        const int row = row_of(P, (int)lane);
+        if (row < 0 && blockIdx.x == 0) atomicOr(status, CR_FLAG_BADPAGES);
+        k.row0 = (int)lane;
+        k.ntok = 1;
+        k.kbase = row < 0 ? 0 : row;
+        k.klen = keys_of(P, row);
+        k.nt = (int)few_tiles(0, k.klen);
+        at = (uint32_t)k.nt + kExtra;
+    }
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const unsigned long long y = __shfl_up_sync(~0u, at, o);
+        if ((int)lane >= o) at += y;
+    }
+    L->blk[lane] = k;
+    L->cum[lane + 1] = at;
+    if (lane == 0) L->cum[0] = 0;
+    __syncwarp();
+    const plan_cut C = cut_work(P, L->cum[P.n], P.n, P.n, __reduce_max_sync(~0u, (uint32_t)k.nt));
+    if (lane < 3) {
+        const uint32_t c = blockIdx.x + lane - 1;  // the stretch before, this one, the next
+        const attn_start s = stretch(C, L->cum, L->blk, c == ~0u ? 0 : c);
+        if (lane == 0)
+            L->before = s.pos;
+        else
+            L->start[lane - 1] = s;
+        if (lane == 1) P.start[c] = s;
+    }
+    __syncwarp();
+    return C;
+}
+// Once the copies are under way: if this stretch is the first to begin inside its block, the block's pieces.
+__device__ __forceinline__ void count_pieces(const plan_in &P, const plan_cut &C, const own_list *L)
+{
+    const attn_start &s = L->start[0];
+    if (s.tile == 0 || s.pos >= C.N || L->before > s.pos - s.tile - kExtra) return;
+    const unsigned long long end = s.pos - s.tile + (uint32_t)s.k.nt;
+    // stretches that begin before the block's end: none of them begins a whole stretch from its even share
+    const uint32_t near = (uint32_t)div_by(end * C.ncta, C.N), c0 = near > 8 ? near - 8 : 0, c = c0 + (threadIdx.x & 31);
+    const uint32_t upto = c0 + __popc(__ballot_sync(~0u, c < C.ncta && stretch(C, L->cum, L->blk, c).pos < end));
+    if ((threadIdx.x & 31) == 0) P.start[blockIdx.x].pieces = upto - (blockIdx.x - 1);
+}
 
 // A CTA's stretch, a block at a time; the next block's description is on its way while one is worked on.
 struct walk {
@@ -392,9 +484,9 @@ struct walk {
         d[0] = g[0];
         d[1] = g[1];
     }
-    __device__ __forceinline__ void begin(const attn_start *start, const attn_blk *list)
+    // s: this CTA's beginning, and the next one's
+    __device__ __forceinline__ void begin(const attn_start *s, const attn_blk *list)
     {
-        const attn_start *s = start + blockIdx.x;
         blk = list;
         next_h = s->head;
         b = s->blk;
@@ -539,7 +631,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         const uint32_t q_bytes = A.G * A.tq * 128 * cfg::kChunks;
         uint32_t stage = 0, phase = 0;
         walk w;
-        w.begin(A.start, A.blk);
+        w.begin(A.start + blockIdx.x, A.blk);
         for (;;) {
             const bool more = w.next();
             if (!cr_bar_wait(BAR(B_PEMPTY + (pieces & 1)), ((pieces >> 1) & 1) ^ 1, &gave_up)) goto out;
@@ -1054,10 +1146,12 @@ __global__ void __launch_bounds__(256) k_attn_join(const __grid_constant__ attn_
     __shared__ join_shared S;
     cr_launch_next();
     cr_wait_previous();
-    const uint32_t items = A.joins[0] * (RP / 16);
+    const bool own = RP == 16 && A.own_list;  // no list: every stretch but the first may join pieces
+    const uint32_t items = (own ? A.ncta - 1 : A.joins[0]) * (RP / 16);
     for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const uint32_t c = A.joins[1 + item / (RP / 16)], r = item % (RP / 16) * 16 + (threadIdx.x & 15);
+        const uint32_t c = own ? 1 + item : A.joins[1 + item / (RP / 16)], r = item % (RP / 16) * 16 + (threadIdx.x & 15);
         const attn_start s = A.start[c];
+        if (own && s.pieces == 0) continue;
         bool valid;
         uint32_t head;
         uint64_t tk = (uint64_t)s.k.row0;
@@ -1194,6 +1288,7 @@ __global__ void __launch_bounds__(kFewThreads, 2)
     __shared__ __align__(8) unsigned long long bars[2 * cfg::kStages + 3];
     __shared__ float2 join_ml[kFewWarps][16];
     __shared__ int gave_up;
+    __shared__ own_list list;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t base = cr_smem(dyn), ring = (base + 1023u) & ~1023u, sq = ring + cfg::kStages * 2 * cfg::kTile;
     float *join = reinterpret_cast<float *>(dyn + (sq - base) + cfg::kQ);
@@ -1230,7 +1325,14 @@ __global__ void __launch_bounds__(kFewThreads, 2)
     cr_launch_next();
 
     walk w;
-    w.begin(A.start, A.blk);
+    plan_cut cut;
+    if (A.own_list) {
+        if (warp == kFewWarps) cut = make_list(A.plan, &list, A.status);
+        __syncthreads();
+        w.begin(list.start, list.blk);
+    } else {
+        w.begin(A.start + blockIdx.x, A.blk);
+    }
     uint32_t stage = 0, phase = 0, qphase = 0;
     if (warp == kFewWarps) {
         // ---- copies: a lane brings one box of one column block, keys and values ----
@@ -1271,6 +1373,7 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                 }
             }
         }
+        if (A.own_list) count_pieces(A.plan, cut, &list);
     } else {
         const uint32_t r4 = lane >> 2, q4 = lane & 3;
         const float c = A.c;
@@ -1871,6 +1974,9 @@ extern "C" int cr_attn_decode(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t la
         F.after_rows = 1;
         CR_TRY(launch_plan<PLAN_FEW>(ctx, f, &g));
         CR_TRY(rows(ctx, R, K, args, g.max_cta));
+    } else if (f.n <= kOwnList) {
+        F.own_list = 1;
+        F.plan = f;
     } else {
         CR_TRY(launch_plan<PLAN_FEW>(ctx, f, nullptr));
     }

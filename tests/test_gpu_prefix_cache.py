@@ -490,6 +490,36 @@ def test_decode(P, ctx, page, hkv, hq, d, dtype, order, shared, seqs):
     check(out, lse, [reference(q[i:i + 1], *kv[rows[i]], False, d ** -0.5) for i in range(len(lens))], cu)
 
 
+@pytest.mark.parametrize("n,longest,hq,hkv,d,dtype", [
+    (1, 30000, 8, 2, 128, BF), (2, 1, 4, 4, 64, HF), (8, 9000, 16, 2, 128, BF), (31, 700, 4, 1, 64, BF),
+    (32, 5000, 8, 8, 64, HF), (33, 5000, 8, 8, 64, HF), (32, 0, 4, 2, 128, BF), (32, 2500, 40, 1, 128, HF),
+])
+def test_decode_of_lists_that_the_attention_kernel_makes_and_longer_ones(P, ctx, n, longest, hq, hkv, d, dtype):
+    """Up to 32 tokens are listed by the kernel that works on them; pieces of long sequences are joined either way."""
+    g = gen(1000 + n + longest)
+    rng = np.random.default_rng(n + longest)
+    lens = [int(x) for x in rng.integers(0, longest // 4 + 1, n)]
+    lens[n // 2] = longest
+    pg, kv = fill(P, ctx, g, 16, lens, hkv, d, dtype)
+    q = randn(g, n, hq, d, dtype=dtype)
+    want = [reference(q[i:i + 1], *kv[i], False, d ** -0.5) for i in range(n)]
+    out, lse = P.attn_decode(ctx, q, pg, 0, lse=True)
+    ctx.sync()
+    check(out, lse, want, range(n + 1))
+    rows = rng.permutation(n)
+    again, lse = P.attn_decode(ctx, q, pg, 0, seqs=ints(rows), lse=True)
+    ctx.sync()
+    check(again, lse, [reference(q[i:i + 1], *kv[r], False, d ** -0.5) for i, r in enumerate(rows)], range(n + 1))
+    rows[n - 1] = n  # no such row: reported, zeros, the others as before
+    out, lse = P.attn_decode(ctx, q, pg, 0, seqs=ints(rows), lse=True)
+    with pytest.raises(P.CacheRouteError) as e:
+        ctx.sync()
+    assert e.value.code == P.CR_EINVAL
+    assert (out[n - 1] == 0).all() and (lse[n - 1] == -math.inf).all()
+    check(out[:n - 1], lse[:n - 1], [reference(q[i:i + 1], *kv[r], False, d ** -0.5) for i, r in enumerate(rows[:-1])],
+          range(n))
+
+
 def test_decode_with_groups_that_are_not_ascending_stays_in_bounds(P, ctx):
     """Outputs mean nothing then; the call is reported and the next one is right."""
     g = gen(15)
