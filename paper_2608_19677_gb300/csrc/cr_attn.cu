@@ -8,8 +8,9 @@
 // Work is therefore a list of (key head, block of query rows) with a number of key tiles each,
 // laid end to end; every CTA takes an equal stretch of it, wherever that begins or ends.  What a
 // CTA has of a block that it shares with others goes to scratch, and a second kernel joins the
-// pieces in order (k_attn_plan writes the list and the stretches, one CTA).  A block counts for its tiles
-// and for kExtra more: its queries, its first scores and its result, which no other work hides.
+// pieces in order (k_attn_plan, one CTA, writes the list and the stretches, but for a few single tokens,
+// whose list k_attn_few makes).  A block counts for its tiles and for kExtra more: its queries, its first
+// scores and its result, which no other work hides.
 //
 // Two kernels do the work:
 //   k_attn_rows  many query rows per key head: 256 rows (tokens x grouped heads) against tiles of
@@ -532,7 +533,7 @@ struct walk {
 // on the other's, so the softmax has to be as short as a tile's two products (1,024 cycles each way):
 // a row belongs to two threads, 64 keys each, which exchange their maxima through shared memory, and
 // the product with v begins when half of the weights are there.
-// Measured (one GB300, 32/8 heads of 128, causal): 8,192 tokens 368 us, 1,492 TFLOP/s, tensor cores at work
+// Measured (one GB300, 32/8 heads of 128, causal): 8,192 tokens 362 us, 1,519 TFLOP/s, tensor cores at work
 // in 71% of the cycles; about 2,650 cycles for a pair of tiles whose products take 2,048: scores to weights
 // 1,250 cycles (exponentials half of them), hand-overs the rest.  Calls of milliseconds meet the power limit.
 template <int D>
