@@ -30,6 +30,7 @@ class Destination:
         self.prefixes: "OrderedDict[int, Tuple[int, int]]" = OrderedDict()  # key -> (row, tokens), least recent first
         self.running: "OrderedDict[int, List[int]]" = OrderedDict()         # key -> rows of its running requests
         self.own: Dict[int, Tuple[int, int]] = {}                           # row -> (tokens, pages that are its alone)
+        self.kept: Dict[int, int] = {}                                      # running row -> tokens of its key's prefix
 
     def _ints(self, values):
         import torch
@@ -82,6 +83,7 @@ class Destination:
         pages_free(self.ctx, self.pages, self._ints(rows))
         for row in rows:
             self.free_pages += self.own.pop(row)[1]
+            self.kept.pop(row, None)
         self.free_rows.extend(rows)
 
     def admit(self, requests: Sequence[Tuple[int, object, int]]):
@@ -109,9 +111,10 @@ class Destination:
             pages_extend(self.ctx, self.pages, rows, self._ints(lens))
             self._forward(torch.cat(list(new.values())), self._cu(lens), rows)
         rows = [self._take(n, p) for n, p in zip(whole, alone)]
-        for (key, _, _), row in zip(requests, rows):
+        for (key, _, plen), row in zip(requests, rows):
             self.prefixes.move_to_end(key)
             self.running.setdefault(key, []).append(row)
+            self.kept[row] = plen
         dst, lens = self._ints(rows), [int(t.shape[0]) for t in own]
         pages_fork(self.ctx, self.pages, self._ints(self.prefixes[key][0] for key, _, _ in requests), dst,
                    self._ints(plen for _, _, plen in requests))
@@ -134,7 +137,8 @@ class Destination:
         for key, mine in self.running.items():
             if mine:
                 off.append(off[-1] + len(mine))
-                shared.append(self.prefixes[key][1] // page * page)
+                # whole pages that all of them kept: behind the shortest they are each request's own
+                shared.append(min(self.kept[row] for row in mine) // page * page)
         r = self._ints(rows)
         pages_extend(self.ctx, self.pages, r, self._ints([1] * len(rows)))
         return self._forward(tokens, self._ints(range(len(rows) + 1)), r, (self._ints(off), self._ints(shared)))

@@ -1,0 +1,140 @@
+"""The bookkeeping of a destination's server, on the host: the library's calls are replaced by a model of the pages that
+keeps, for every row, which request's text stands at each of its tokens."""
+from types import SimpleNamespace
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+
+class Pool:
+    """Pages, tables and lengths as the calls leave them; ``text``: what was written at each place of each page."""
+
+    def __init__(self, n_pages, page, n_seqs, max_pages):
+        self.page, self.n_pages, self.layers = page, n_pages, 1
+        self.table = torch.full((n_seqs, max_pages), -1, dtype=torch.int32)
+        self.lens = torch.zeros(n_seqs, dtype=torch.int32)
+        self.ref = torch.zeros(n_pages, dtype=torch.int32)
+        self.text = torch.full((n_pages, page), -1, dtype=torch.int64)
+        self.calls = []
+
+    def _take(self):
+        p = int((self.ref == 0).nonzero()[0])
+        self.ref[p] = 1
+        return p
+
+    def extend(self, ctx, pages, seqs, add):
+        self.calls.append(("extend", seqs.tolist(), add.tolist()))
+        for s, a in zip(seqs.tolist(), add.tolist()):
+            n = int(self.lens[s])
+            assert n + a <= self.table.shape[1] * self.page, "the row cannot hold it"
+            for j in range(-(-n // self.page), -(-(n + a) // self.page)):
+                self.table[s, j] = self._take()
+            self.lens[s] = n + a
+
+    def fork(self, ctx, pages, src, dst, keep):
+        self.calls.append(("fork", src.tolist(), dst.tolist(), keep.tolist()))
+        for s, d, n in zip(src.tolist(), dst.tolist(), keep.tolist()):
+            assert self.lens[d] == 0 and 1 <= n <= self.lens[s], "a fork the pages refuse"
+            full, tail = divmod(n, self.page)
+            self.table[d, :full] = self.table[s, :full]
+            self.ref[self.table[s, :full].long()] += 1
+            if tail:
+                p = self._take()
+                self.table[d, full] = p
+                self.text[p, :tail] = self.text[self.table[s, full], :tail]
+            self.lens[d] = n
+
+    def free(self, ctx, pages, seqs):
+        self.calls.append(("free", seqs.tolist()))
+        for s in seqs.tolist():
+            used = self.table[s, :-(-int(self.lens[s]) // self.page)].long()
+            assert (self.ref[used] > 0).all()
+            self.ref[used] -= 1
+            self.table[s], self.lens[s] = -1, 0
+
+    def at(self, row, pos):
+        return int(self.table[row, pos // self.page]), pos % self.page
+
+    def write(self, ctx, pages, layer, k, v, cu, seqs=None):
+        cu = cu.tolist()
+        assert cu[-1] == k.shape[0]
+        for i, row in enumerate(seqs.tolist()):
+            for t in range(cu[i], cu[i + 1]):
+                p, r = self.at(row, int(self.lens[row]) - (cu[i + 1] - t))
+                assert self.ref[p] == 1, "a page that other rows read"
+                self.text[p, r] = int(k[t, 0, 0])
+
+    def read(self, row, n):
+        return [int(self.text[self.at(row, j)]) for j in range(n)]
+
+    def paged(self, ctx, q, pages, layer, cu, seqs=None, **kw):
+        return q
+
+    def decode(self, ctx, q, pages, layer, seqs=None, group_off=None, shared=None, **kw):
+        """What each query reads: its group's first row's shared tokens, then its own."""
+        rows, off, shared = seqs.tolist(), group_off.tolist(), shared.tolist()
+        self.seen = {}
+        for g, n in enumerate(shared):
+            for row in rows[off[g]:off[g + 1]]:
+                mine = self.read(row, int(self.lens[row]))
+                self.seen[row] = self.read(rows[off[g]], n) + mine[n:]
+        return q
+
+
+class Model:
+    """Keys are the tokens themselves."""
+    layers = 1
+
+    def embed(self, tokens):
+        return tokens
+
+    def qkv(self, layer, x):
+        y = x.to(torch.int64)[:, None, None]
+        return y, y, y
+
+    def mix(self, layer, x, out):
+        return x
+
+
+@pytest.fixture
+def serve(monkeypatch):
+    from paper_2608_19677_gb300 import destination as D
+
+    def make(n_pages=64, page=16, n_seqs=8, max_pages=8):
+        pool = Pool(n_pages, page, n_seqs, max_pages)
+        for name in ("extend", "fork", "free"):
+            monkeypatch.setattr(D, f"pages_{name}", getattr(pool, name))
+        monkeypatch.setattr(D, "kv_write", pool.write)
+        monkeypatch.setattr(D, "attn_paged", pool.paged)
+        monkeypatch.setattr(D, "attn_decode", pool.decode)
+        return D.Destination(SimpleNamespace(), pool, Model()), pool
+
+    return make
+
+
+def text(seed, n):
+    return torch.arange(n, dtype=torch.int64) + 1000 * seed
+
+
+def prompt(seed, prefix, plen, own):
+    return torch.cat([prefix[:plen], text(seed, own)])
+
+
+@pytest.mark.parametrize("kept", [(32, 16), (16, 32), (48, 33), (47, 15), (48, 48)])
+def test_requests_that_keep_different_parts_of_a_prefix_read_their_own_tokens(serve, kept):
+    d, pool = serve()
+    prefix = text(1, 48)
+    rows, _ = d.admit([(5, prompt(2, prefix, 48, 3), 48)])
+    said = {rows[0]: prompt(2, prefix, 48, 3).tolist()}
+    for i, n in enumerate(kept):
+        (row,), _ = d.admit([(5, prompt(3 + i, prefix, n, 20 + i), n)])
+        said[row] = prompt(3 + i, prefix, n, 20 + i).tolist()
+    d.finish(rows)
+    del said[rows[0]]
+    for step in range(3):
+        new = text(9 + step, len(said))
+        for row, t in zip(d.order(), new.tolist()):
+            said[row].append(t)
+        d.step(new)
+        assert pool.seen == said
