@@ -87,15 +87,21 @@ class Destination:
         self.free_rows.extend(rows)
 
     def admit(self, requests: Sequence[Tuple[int, object, int]]):
-        """requests: (key, tokens, prefix length).  Returns each request's row and the model's output for its own
-        tokens, back to back."""
+        """requests: (key, tokens, prefix length).  Requests of a key may keep less of its prefix than is held (a prefix
+        that is not held is read as far as the longest of the call keeps it), not more.  Returns each request's row and
+        the model's output for its own tokens, back to back."""
         import torch
         page = self.pages.page
         if not requests:
             raise ValueError("no requests")
         new: Dict[int, object] = {}
         for key, tokens, plen in requests:
-            if key not in self.prefixes and key not in new:
+            if not 1 <= plen <= int(tokens.shape[0]):
+                raise ValueError(f"a prefix of {plen} tokens in a prompt of {int(tokens.shape[0])}")
+            if key in self.prefixes:
+                if plen > self.prefixes[key][1]:
+                    raise ValueError(f"key {key} is held with a prefix of {self.prefixes[key][1]} tokens, not {plen}")
+            elif key not in new or plen > new[key].shape[0]:
                 new[key] = tokens[:plen]
         own = [tokens[plen:] for _, tokens, plen in requests]
         whole = [int(tokens.shape[0]) for _, tokens, _ in requests]

@@ -138,3 +138,28 @@ def test_requests_that_keep_different_parts_of_a_prefix_read_their_own_tokens(se
             said[row].append(t)
         d.step(new)
         assert pool.seen == said
+
+
+def state(d, pool):
+    return (list(d.free_rows), d.free_pages, dict(d.prefixes), {k: list(v) for k, v in d.running.items()}, dict(d.own),
+            dict(d.kept), pool.table.tolist(), pool.lens.tolist(), pool.ref.tolist(), list(pool.calls))
+
+
+@pytest.mark.parametrize("plen,whole", [(0, 40), (-3, 40), (41, 40), (33, 60), (48, 48)])
+def test_prefix_lengths_that_cannot_be_are_refused_before_anything_changes(serve, plen, whole):
+    """None, more than the prompt, and more than is held of the key."""
+    d, pool = serve()
+    d.admit([(5, text(1, 40), 32)])
+    before = state(d, pool)
+    with pytest.raises(ValueError):
+        d.admit([(6, text(2, 20), 16), (5, text(1, whole), plen)])
+    assert state(d, pool) == before
+
+
+def test_a_new_prefix_is_read_as_far_as_the_longest_request_of_the_call_keeps_it(serve):
+    d, pool = serve()
+    prefix = text(1, 48)
+    asked = [(5, prompt(2 + i, prefix, n, 4), n) for i, n in enumerate((16, 48, 20))]
+    rows, _ = d.admit(asked)
+    assert d.prefixes[5][1] == 48 and pool.read(d.prefixes[5][0], 48) == prefix.tolist()
+    assert [pool.read(r, int(pool.lens[r])) for r in rows] == [t.tolist() for _, t, _ in asked]
