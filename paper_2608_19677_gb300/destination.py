@@ -42,6 +42,12 @@ class Destination:
             at.append(at[-1] + n)
         return self._ints(at)
 
+    def _check_width(self, tokens: int) -> None:
+        """A row that cannot hold its tokens is not grown by the library, and what is then written goes to other places."""
+        width = self.pages.table.shape[1] * self.pages.page
+        if tokens > width:
+            raise RuntimeError(f"a row of {width} tokens has no room for {tokens}")
+
     def _pages(self, tokens: int) -> int:
         return -(-tokens // self.pages.page)
 
@@ -105,6 +111,7 @@ class Destination:
                 new[key] = tokens[:plen]
         own = [tokens[plen:] for _, tokens, plen in requests]
         whole = [int(tokens.shape[0]) for _, tokens, _ in requests]
+        self._check_width(max(whole))
         alone = [self._pages(n) - plen // page for n, (_, _, plen) in zip(whole, requests)]
         self._make_room(len(new) + len(requests),
                         sum(self._pages(int(t.shape[0])) for t in new.values()) + sum(alone),
@@ -134,6 +141,7 @@ class Destination:
     def step(self, tokens):
         """One more token for every running request, in ``order()``: the model's output [requests, ...]."""
         rows, page = self.order(), self.pages.page
+        self._check_width(max((self.own[row][0] + 1 for row in rows), default=0))
         grown = {row: (self.own[row][0] + 1, self.own[row][1] + (self.own[row][0] % page == 0)) for row in rows}
         more = sum(p - self.own[row][1] for row, (_, p) in grown.items())
         self._make_room(0, more, ())

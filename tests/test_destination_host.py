@@ -163,3 +163,20 @@ def test_a_new_prefix_is_read_as_far_as_the_longest_request_of_the_call_keeps_it
     rows, _ = d.admit(asked)
     assert d.prefixes[5][1] == 48 and pool.read(d.prefixes[5][0], 48) == prefix.tolist()
     assert [pool.read(r, int(pool.lens[r])) for r in rows] == [t.tolist() for _, t, _ in asked]
+
+
+def test_requests_and_steps_that_a_row_cannot_hold_are_refused_before_anything_changes(serve):
+    """Rows of four pages of 16 tokens, whose pool has many more."""
+    d, pool = serve(max_pages=4)
+    rows, _ = d.admit([(5, text(1, 63), 32)])
+    before = state(d, pool)
+    for asked in ([(5, text(1, 65), 32)], [(6, text(2, 20), 16), (7, text(3, 130), 64)]):
+        with pytest.raises(RuntimeError):
+            d.admit(asked)
+        assert state(d, pool) == before
+    d.step(text(2, 1))
+    assert int(pool.lens[rows[0]]) == 64
+    before = state(d, pool)
+    with pytest.raises(RuntimeError):
+        d.step(text(3, 1))
+    assert state(d, pool) == before
