@@ -483,7 +483,9 @@ __global__ void __launch_bounds__(128) k_kv_write(const __grid_constant__ pages_
             ok = pos >= 0 && ((uint32_t)pos >> P.page_log2) < P.max_pages;
             if (ok) {
                 const int p = P.table[(uint64_t)row * P.max_pages + ((uint32_t)pos >> P.page_log2)];
-                ok = p >= 0 && (uint32_t)p < P.n_pages;
+                // pages that other rows name are not this row's to write: a row that was not grown (too wide, too few
+                // pages) would put its tokens there
+                ok = p >= 0 && (uint32_t)p < P.n_pages && P.ref[p] <= 1;
                 dst = (uint64_t)(uint32_t)p * P.page_stride + ((uint32_t)pos & (P.page - 1)) * P.token_stride;
             }
         }

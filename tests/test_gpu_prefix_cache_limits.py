@@ -1,0 +1,43 @@
+"""Pages and attention at the limits of their use: rows that were not grown, long lists, streams, graphs.  Bounds of the
+attention tests are those derived in test_gpu_prefix_cache.py."""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytestmark = [pytest.mark.gpu, pytest.mark.skip(reason="needs a CUDA GPU")]
+else:
+    pytestmark = pytest.mark.gpu
+
+from test_gpu_prefix_cache import BF, DEV, HF, P, check, ctx, fill, gen, ints, randn, reference  # noqa: E402, F401
+
+
+def raises_at_sync(P, ctx, code):
+    with pytest.raises(P.CacheRouteError) as e:
+        ctx.sync()
+    assert e.value.code == code
+
+
+@pytest.mark.parametrize("add,pages,code", [(70, 64, "CR_EINVAL"), (30, 4, "CR_EOVERFLOW")])
+@pytest.mark.parametrize("keep", [32, 40])
+def test_a_row_that_was_not_grown_does_not_write_into_shared_pages(P, ctx, add, pages, code, keep):
+    """A fork of 32 tokens (or 40: two shared pages and one of its own) whose extension the row's width, or the pool,
+    does not allow: its new tokens would fall on the prefix' last ones."""
+    g = gen(keep + add)
+    pg = P.KVPages.empty(pages, 16, 3, 6, 2, 2, 64)
+    pg.cache.copy_(randn(g, *pg.cache.shape))
+    P.pages_extend(ctx, pg, ints([0]), ints([48]))
+    P.pages_fork(ctx, pg, ints([0]), ints([1]), ints([keep]))
+    ctx.sync()
+    P.pages_extend(ctx, pg, ints([1]), ints([add]))
+    raises_at_sync(P, ctx, getattr(P, code))
+    assert int(pg.lens[1]) == keep
+    before = pg.cache.clone()
+    k, v = randn(g, 20, 2, 64), randn(g, 20, 2, 64)
+    P.kv_write(ctx, pg, 1, k, v, ints([0, 20]), seqs=ints([1]))
+    raises_at_sync(P, ctx, P.CR_EINVAL)
+    if keep == 40:      # the row's own page holds its last 8 tokens
+        before[1, 0, int(pg.table[1, 2]), :8], before[1, 1, int(pg.table[1, 2]), :8] = k[12:], v[12:]
+    assert torch.equal(pg.cache, before)
