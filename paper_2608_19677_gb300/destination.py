@@ -160,6 +160,10 @@ class Destination:
     def finish(self, rows: Sequence[int]) -> None:
         """Rows of requests that have ended become empty; their keys' prefixes stay."""
         gone = set(rows)
+        if len(gone) != len(rows) or not gone.issubset(self.kept):
+            raise ValueError(f"rows {list(rows)}: a running request's each, once")
+        if not gone:
+            return
         self._free(list(rows))
         for key in list(self.running):
             self.running[key] = [row for row in self.running[key] if row not in gone]

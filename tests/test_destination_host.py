@@ -180,3 +180,18 @@ def test_requests_and_steps_that_a_row_cannot_hold_are_refused_before_anything_c
     with pytest.raises(RuntimeError):
         d.step(text(3, 1))
     assert state(d, pool) == before
+
+
+def test_only_running_requests_are_finished_each_once(serve):
+    """Not a prefix' row, an empty one, or one twice."""
+    d, pool = serve()
+    rows, _ = d.admit([(5, text(1, 40), 32), (5, text(1, 36), 32)])
+    before = state(d, pool)
+    for asked in ([d.prefixes[5][0]], [rows[0], rows[0]], [rows[1], d.free_rows[0]], [rows[0], 99], [-1]):
+        with pytest.raises(ValueError):
+            d.finish(asked)
+        assert state(d, pool) == before
+    d.finish([])
+    assert state(d, pool) == before
+    d.finish(rows)
+    assert not d.running and not d.kept and int(pool.ref.sum()) == 2
