@@ -95,7 +95,8 @@ class Destination:
     def admit(self, requests: Sequence[Tuple[int, object, int]]):
         """requests: (key, tokens, prefix length).  Requests of a key may keep less of its prefix than is held (a prefix
         that is not held is read as far as the longest of the call keeps it), not more.  Returns each request's row and
-        the model's output for its own tokens, back to back."""
+        the model's output for its own tokens, back to back.  If the model or a call fails, the call's requests and the
+        prefixes that it was to read are given up."""
         import torch
         page = self.pages.page
         if not requests:
@@ -116,31 +117,56 @@ class Destination:
         self._make_room(len(new) + len(requests),
                         sum(self._pages(int(t.shape[0])) for t in new.values()) + sum(alone),
                         {key for key, _, _ in requests})
-        if new:
-            lens = [int(t.shape[0]) for t in new.values()]
-            for key, n in zip(new, lens):
-                self.prefixes[key] = (self._take(n, self._pages(n)), n)
-            rows = self._ints(self.prefixes[key][0] for key in new)
-            pages_extend(self.ctx, self.pages, rows, self._ints(lens))
-            self._forward(torch.cat(list(new.values())), self._cu(lens), rows)
-        rows = [self._take(n, p) for n, p in zip(whole, alone)]
-        for (key, _, plen), row in zip(requests, rows):
-            self.prefixes.move_to_end(key)
-            self.running.setdefault(key, []).append(row)
-            self.kept[row] = plen
-        dst, lens = self._ints(rows), [int(t.shape[0]) for t in own]
-        pages_fork(self.ctx, self.pages, self._ints(self.prefixes[key][0] for key, _, _ in requests), dst,
-                   self._ints(plen for _, _, plen in requests))
-        pages_extend(self.ctx, self.pages, dst, self._ints(lens))
-        return rows, self._forward(torch.cat(own), self._cu(lens), dst)
+        taken: List[int] = []
+        try:
+            if new:
+                lens = [int(t.shape[0]) for t in new.values()]
+                for key, n in zip(new, lens):
+                    taken.append(self._take(n, self._pages(n)))
+                    self.prefixes[key] = (taken[-1], n)
+                rows = self._ints(taken)
+                pages_extend(self.ctx, self.pages, rows, self._ints(lens))
+                self._forward(torch.cat(list(new.values())), self._cu(lens), rows)
+            rows = [self._take(n, p) for n, p in zip(whole, alone)]
+            taken += rows
+            for (key, _, plen), row in zip(requests, rows):
+                self.prefixes.move_to_end(key)
+                self.running.setdefault(key, []).append(row)
+                self.kept[row] = plen
+            dst, lens = self._ints(rows), [int(t.shape[0]) for t in own]
+            pages_fork(self.ctx, self.pages, self._ints(self.prefixes[key][0] for key, _, _ in requests), dst,
+                       self._ints(plen for _, _, plen in requests))
+            pages_extend(self.ctx, self.pages, dst, self._ints(lens))
+            return rows, self._forward(torch.cat(own), self._cu(lens), dst)
+        except BaseException:
+            self._give_up(taken)
+            raise
+
+    def _give_up(self, rows: Sequence[int]) -> None:
+        """Rows whose keys and values were not all written leave, prefixes among them."""
+        gone = set(rows)
+        for key in [key for key, (row, _) in self.prefixes.items() if row in gone]:
+            del self.prefixes[key]
+        self._leave(gone)
+        if gone:
+            self._free(list(rows))
+
+    def _leave(self, gone) -> None:
+        for key in list(self.running):
+            self.running[key] = [row for row in self.running[key] if row not in gone]
+            if not self.running[key]:
+                del self.running[key]
 
     def order(self) -> List[int]:
         """Rows of the running requests as ``step`` takes them."""
         return [row for rows in self.running.values() for row in rows]
 
     def step(self, tokens):
-        """One more token for every running request, in ``order()``: the model's output [requests, ...]."""
+        """One more token for every running request, in ``order()``: the model's output [requests, ...].  If the model or
+        a call fails, the running requests are given up: their last token's keys and values are not in every layer."""
         rows, page = self.order(), self.pages.page
+        if len(tokens) != len(rows):
+            raise ValueError(f"{len(tokens)} tokens for {len(rows)} running requests")
         self._check_width(max((self.own[row][0] + 1 for row in rows), default=0))
         grown = {row: (self.own[row][0] + 1, self.own[row][1] + (self.own[row][0] % page == 0)) for row in rows}
         more = sum(p - self.own[row][1] for row, (_, p) in grown.items())
@@ -153,9 +179,13 @@ class Destination:
                 off.append(off[-1] + len(mine))
                 # whole pages that all of them kept: behind the shortest they are each request's own
                 shared.append(min(self.kept[row] for row in mine) // page * page)
-        r = self._ints(rows)
-        pages_extend(self.ctx, self.pages, r, self._ints([1] * len(rows)))
-        return self._forward(tokens, self._ints(range(len(rows) + 1)), r, (self._ints(off), self._ints(shared)))
+        try:
+            r = self._ints(rows)
+            pages_extend(self.ctx, self.pages, r, self._ints([1] * len(rows)))
+            return self._forward(tokens, self._ints(range(len(rows) + 1)), r, (self._ints(off), self._ints(shared)))
+        except BaseException:
+            self._give_up(rows)
+            raise
 
     def finish(self, rows: Sequence[int]) -> None:
         """Rows of requests that have ended become empty; their keys' prefixes stay."""
@@ -165,10 +195,7 @@ class Destination:
         if not gone:
             return
         self._free(list(rows))
-        for key in list(self.running):
-            self.running[key] = [row for row in self.running[key] if row not in gone]
-            if not self.running[key]:
-                del self.running[key]
+        self._leave(gone)
 
     def compact(self):
         """Live pages to the front of the pool; their number (on the device)."""

@@ -195,3 +195,47 @@ def test_only_running_requests_are_finished_each_once(serve):
     assert state(d, pool) == before
     d.finish(rows)
     assert not d.running and not d.kept and int(pool.ref.sum()) == 2
+
+
+class Failing(Model):
+    """Raises at its n-th pass."""
+
+    def __init__(self):
+        self.left = -1
+
+    def mix(self, layer, x, out):
+        self.left -= 1
+        if self.left == 0:
+            raise ArithmeticError
+        return x
+
+
+@pytest.mark.parametrize("at", [1, 2])
+def test_a_call_that_fails_leaves_nothing_half_read(serve, at):
+    """While a prefix is read, and while the requests' own tokens are: neither may be found there later."""
+    d, pool = serve()
+    d.model = Failing()
+    d.admit([(4, text(1, 30), 20)])
+    ref, lens, held = pool.ref.clone(), pool.lens.clone(), dict(d.prefixes)
+    d.model.left = at
+    with pytest.raises(ArithmeticError):
+        d.admit([(5, text(2, 40), 32), (4, text(1, 25), 20)])
+    assert torch.equal(pool.ref, ref) and torch.equal(pool.lens, lens) and d.prefixes == held
+    assert d.free_pages == int((pool.ref == 0).sum()) and len(d.free_rows) == 6 and list(d.running) == [4]
+    (row,), _ = d.admit([(5, text(2, 40), 32)])
+    assert pool.read(row, 40) == text(2, 40).tolist()
+
+
+def test_a_step_that_fails_gives_its_requests_up(serve):
+    d, pool = serve()
+    d.model = Failing()
+    d.admit([(4, text(1, 30), 20), (5, text(2, 32), 32)])
+    before = state(d, pool)
+    with pytest.raises(ValueError):
+        d.step(text(3, 3))
+    assert state(d, pool) == before
+    d.model.left = 1
+    with pytest.raises(ArithmeticError):
+        d.step(text(3, 2))
+    assert not d.running and not d.kept and set(d.prefixes) == {4, 5} and len(d.free_rows) == 6
+    assert d.free_pages == int((pool.ref == 0).sum()) == 64 - 4
