@@ -192,6 +192,11 @@ class Context:
     def handle(self):
         return self._h
 
+    @property
+    def stream(self):
+        """The torch stream that the library's work runs on."""
+        return self._stream_obj
+
     def check(self, st: int, where: str):
         if st != CR_OK:
             raise CacheRouteError(st, where, lib().cr_last_error(self._h).decode())

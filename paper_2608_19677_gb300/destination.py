@@ -12,14 +12,50 @@ those prefixes in pages of a key/value cache, one table row each:
 
 The model is the caller's: ``layers``, ``embed(tokens) -> x``, ``qkv(layer, x) -> q, k, v`` ([tokens, heads, head_dim])
 and ``mix(layer, x, out) -> x``.  Bookkeeping of rows is on the host; nothing here waits for the GPU.
+
+Every call runs on the context's stream, the model's passes among it: after what torch's current stream has when the
+call is made, and before what that stream gets next.
 """
 from __future__ import annotations
 
+import functools
 from collections import OrderedDict
 from typing import Dict, List, Sequence, Tuple
 
 from . import (Context, KVPages, attn_decode, attn_paged, kv_write, pages_compact, pages_extend, pages_fork,
                pages_free)
+
+
+def _on_context_stream(call):
+    """The call's work on the context's stream, in the current stream's order.  Lists and results are allocated there: a
+    list that is dropped is not handed out again before the kernels that read it."""
+    @functools.wraps(call)
+    def ordered(self, *args):
+        if not self.pages.lens.is_cuda:
+            return call(self, *args)
+        import torch
+        mine, here = self.ctx.stream, torch.cuda.current_stream(self.pages.lens.device)
+        if mine.cuda_stream == here.cuda_stream:
+            return call(self, *args)
+        mine.wait_stream(here)
+        _used_on(args, mine)
+        try:
+            with torch.cuda.stream(mine):
+                result = call(self, *args)
+            _used_on((result, self.pages.ref, self.pages.table), here)
+            return result
+        finally:
+            here.wait_stream(mine)
+    return ordered
+
+
+def _used_on(values, stream):
+    """Tensors among the values are not handed out again before ``stream`` has passed their last use."""
+    for v in values:
+        if isinstance(v, (tuple, list)):
+            _used_on(v, stream)
+        elif getattr(v, "is_cuda", False):
+            v.record_stream(stream)
 
 
 class Destination:
@@ -92,6 +128,7 @@ class Destination:
             self.kept.pop(row, None)
         self.free_rows.extend(rows)
 
+    @_on_context_stream
     def admit(self, requests: Sequence[Tuple[int, object, int]]):
         """requests: (key, tokens, prefix length).  Requests of a key may keep less of its prefix than is held (a prefix
         that is not held is read as far as the longest of the call keeps it), not more.  Returns each request's row and
@@ -161,6 +198,7 @@ class Destination:
         """Rows of the running requests as ``step`` takes them."""
         return [row for rows in self.running.values() for row in rows]
 
+    @_on_context_stream
     def step(self, tokens):
         """One more token for every running request, in ``order()``: the model's output [requests, ...].  If the model or
         a call fails, the running requests are given up: their last token's keys and values are not in every layer."""
@@ -187,6 +225,7 @@ class Destination:
             self._give_up(rows)
             raise
 
+    @_on_context_stream
     def finish(self, rows: Sequence[int]) -> None:
         """Rows of requests that have ended become empty; their keys' prefixes stay."""
         gone = set(rows)
@@ -197,6 +236,7 @@ class Destination:
         self._free(list(rows))
         self._leave(gone)
 
+    @_on_context_stream
     def compact(self):
         """Live pages to the front of the pool; their number (on the device)."""
         ref, table, _, live = pages_compact(self.ctx, self.pages)
