@@ -70,7 +70,11 @@ class Destination:
 
     def _ints(self, values):
         import torch
-        return torch.tensor(list(values), dtype=torch.int32, device=self.pages.lens.device)
+        lens = self.pages.lens
+        if not lens.is_cuda:
+            return torch.tensor(list(values), dtype=torch.int32)
+        # from pinned memory, which torch keeps until the copy has passed: one from pageable memory waits for the stream
+        return torch.tensor(list(values), dtype=torch.int32, pin_memory=True).to(lens.device, non_blocking=True)
 
     def _cu(self, lens):
         at = [0]

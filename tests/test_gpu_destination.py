@@ -93,3 +93,31 @@ def test_a_context_with_a_stream_of_its_own(P):
 
         assert serve(P, ctx, model(), 2, busy) < BOUND
         ctx.close()
+
+
+@pytest.mark.parametrize("own_stream", [False, True])
+def test_calls_return_while_the_gpu_is_still_busy(P, own_stream):
+    from paper_2608_19677_gb300.destination import Destination
+    stream = torch.cuda.Stream() if own_stream else torch.cuda.current_stream()
+    ctx, m = P.Context(0, stream=stream), model()
+    d = Destination(ctx, P.KVPages.empty(256, 16, 16, 16, m.layers, m.kv_heads, m.dim), m)
+    t = torch.arange(100, device=DEV)
+
+    def pass_():
+        rows, _ = d.admit([(1, t[:40], 32), (2, t[3:60], 20), (1, t[:50], 32)])
+        d.step(t[:3])
+        d.finish(rows)
+        d.compact()
+
+    for _ in range(3):      # memory, libraries and kernels are there
+        pass_()
+    ctx.sync()
+    end = torch.cuda.Event()
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(50 * LONG)
+        end.record()
+    pass_()
+    waited = end.query()
+    ctx.sync()
+    ctx.close()
+    assert not waited
