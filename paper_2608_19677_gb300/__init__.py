@@ -573,10 +573,13 @@ def _dtype_code(dtype) -> int:
 
 
 def _out(ctx: Context, shape, like, dtype):
-    """An output of a call: its memory is not handed out again before ctx's stream has written it."""
-    t = _torch.empty(shape, dtype=dtype, device=like.device)
-    if ctx._raw_stream != _torch._C._cuda_getCurrentRawStream(ctx.device):
-        t.record_stream(ctx._stream_obj)
+    """An output of a call, in memory that ctx's stream has done with: on another stream's memory, that stream's earlier
+    work might still read what is written here.  It is not handed out again before the current stream has passed it."""
+    if ctx._raw_stream == _torch._C._cuda_getCurrentRawStream(ctx.device):
+        return _torch.empty(shape, dtype=dtype, device=like.device)
+    with _torch.cuda.stream(ctx._stream_obj):
+        t = _torch.empty(shape, dtype=dtype, device=like.device)
+    t.record_stream(_torch.cuda.current_stream(ctx.device))
     return t
 
 
@@ -645,7 +648,8 @@ class KVPages:
                    torch.zeros(n_seqs, dtype=torch.int32, device=device))
 
     def replace(self, ref, table):
-        """Take the counts and tables that ``pages_compact`` gave (the cache's pages have moved already)."""
+        """Take the counts and tables that ``pages_compact`` gave (the cache's pages have moved already).  The old ones
+        are let go: where the context has a stream of its own, after that stream's work."""
         _int32("ref", ref, self.n_pages)
         _int32("table", table)
         if table.shape != self.table.shape:
@@ -714,9 +718,10 @@ def _attn_args(ctx: Context, q, dtype, shape, dim, n, cu, seqs, causal, scale, o
     qp, qt, qh = _heads("q", q, dtype, shape, None, None, dim)
     T, heads, dim = shape
     if out is None:
-        out = _torch.empty_like(q, memory_format=_torch.contiguous_format)
-        if ctx._raw_stream != _torch._C._cuda_getCurrentRawStream(ctx.device):
-            out.record_stream(ctx._stream_obj)
+        if ctx._raw_stream == _torch._C._cuda_getCurrentRawStream(ctx.device):
+            out = _torch.empty_like(q, memory_format=_torch.contiguous_format)
+        else:
+            out = _out(ctx, shape, q, dtype)
         op, ot, oh = out.data_ptr(), heads * dim, dim
     else:
         op, ot, oh = _heads("out", out, dtype, out.shape, T, heads, dim)

@@ -41,3 +41,32 @@ def test_a_row_that_was_not_grown_does_not_write_into_shared_pages(P, ctx, add, 
     if keep == 40:      # the row's own page holds its last 8 tokens
         before[1, 0, int(pg.table[1, 2]), :8], before[1, 1, int(pg.table[1, 2]), :8] = k[12:], v[12:]
     assert torch.equal(pg.cache, before)
+
+
+@pytest.mark.parametrize("call", ["packed", "paged", "decode", "compact"])
+def test_outputs_leave_memory_alone_that_the_current_stream_still_reads(P, call):
+    """A context with a stream of its own makes an output while the current stream has not yet read a tensor of that
+    shape that the program has already let go."""
+    g = gen(31)
+    stream = torch.cuda.Stream()
+    c = P.Context(0, stream=stream)
+    pg, _ = fill(P, c, g, 16, [700] * 300, 2, 64, BF)
+    q, k = randn(g, 300, 8, 64), randn(g, 300, 2, 64)
+    cu = ints(range(301))
+    run = {"packed": lambda: [P.attn_packed(c, q, k, k, cu, lse=True)[0]],
+           "paged": lambda: [P.attn_paged(c, q, pg, 0, cu)],
+           "decode": lambda: [P.attn_decode(c, q, pg, 0)],
+           "compact": lambda: list(P.pages_compact(c, pg)[:3])}[call]
+    torch.cuda.synchronize()
+    like = [(t.shape, t.dtype) for t in run()]
+    c.sync()
+    for _ in range(4):
+        x = [torch.full(s, 3, dtype=d, device=DEV) for s, d in like]
+        torch.cuda._sleep(20_000_000)
+        y = [t + 1 for t in x]
+        x = None
+        out = run()
+        torch.cuda.synchronize()
+        assert all((t == 4).all() for t in y)
+        y = out = None
+    c.close()
