@@ -35,29 +35,30 @@ struct pages_in {
     uint32_t *status;
 };
 
-__device__ uint32_t block_scan(uint32_t v, uint32_t *total)  // exclusive, blockDim.x <= 1024
+template <typename T>
+__device__ T block_scan(T v, T *total)  // exclusive, blockDim.x <= 1024
 {
-    __shared__ uint32_t part[32];
+    __shared__ T part[32];
     const uint32_t lane = threadIdx.x & 31, w = threadIdx.x >> 5, nw = (blockDim.x + 31) >> 5;
-    uint32_t x = v;
+    T x = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t y = __shfl_up_sync(~0u, x, o);
+        const T y = __shfl_up_sync(~0u, x, o);
         if (lane >= (uint32_t)o) x += y;
     }
     if (lane == 31) part[w] = x;
     __syncthreads();
     if (w == 0) {
-        uint32_t p = lane < nw ? part[lane] : 0;
+        T p = lane < nw ? part[lane] : 0;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t y = __shfl_up_sync(~0u, p, o);
+            const T y = __shfl_up_sync(~0u, p, o);
             if (lane >= (uint32_t)o) p += y;
         }
         part[lane] = p;
     }
     __syncthreads();
-    const uint32_t before = w ? part[w - 1] : 0;
+    const T before = w ? part[w - 1] : 0;
     *total = part[31];
     __syncthreads();
     return before + x - v;
@@ -104,8 +105,9 @@ __global__ void __launch_bounds__(1024) k_pages_scan(const __grid_constant__ pag
                 }
                 if (!ok) atomicOr(P.status, CR_FLAG_BADPAGES);
             }
-            uint32_t total;
-            const unsigned long long at = base + block_scan(need, &total);
+            // in 64 bits: a row may ask for 2^28 pages, and 1,024 of them are summed here
+            unsigned long long total;
+            const unsigned long long at = base + block_scan((unsigned long long)need, &total);
             if (i < n) {
                 S.entry[i] = e;
                 S.base[i] = at < 0xffffffffull ? (uint32_t)at : 0xffffffffu;

@@ -70,3 +70,19 @@ def test_outputs_leave_memory_alone_that_the_current_stream_still_reads(P, call)
         assert all((t == 4).all() for t in y)
         y = out = None
     c.close()
+
+
+@pytest.mark.parametrize("adds", [[1 << 25] * 1024, [1 << 25] * 1023 + [(1 << 25) - 8], [1 << 25] * 512 + [8]])
+def test_needs_that_pass_32_bits_change_nothing(P, ctx, adds):
+    """1,024 rows that ask for 2^22 pages of 8 tokens each: 2^32 pages, of the 64 that there are."""
+    n = len(adds)
+    z = P.KVPages.empty(64, 8, 1, 1, 1, 1, 8)
+    pg = P.KVPages(z.cache, z.ref, torch.full((n, 1 << 22), -1, dtype=torch.int32, device=DEV),
+                   torch.zeros(n, dtype=torch.int32, device=DEV))
+    assert sum(-(-a // 8) for a in adds) >= 1 << 31
+    P.pages_extend(ctx, pg, ints(range(n)), ints(adds))
+    raises_at_sync(P, ctx, P.CR_EOVERFLOW)
+    assert not pg.lens.any() and not pg.ref.any() and int(pg.table.amax()) == -1
+    P.pages_extend(ctx, pg, ints([5, 3]), ints([100, 408]))      # 13 and 51: all of them
+    ctx.sync()
+    assert pg.ref.all() and pg.table[5, :13].tolist() == list(range(13)) and pg.table[3, :51].tolist() == list(range(13, 64))
