@@ -524,14 +524,16 @@ typedef struct {
 } cr_kv_pages;
 
 /* The rows d_seqs[n] get pages for d_add[i] (>= 0) more tokens each, and are that
- * much longer.  A row that stands in the list twice is extended once (CR_EINVAL).
+ * much longer.  A row that stands in the list twice is extended once, by the first
+ * of its entries that can be carried out (CR_EINVAL for the others).
  * Errors: CR_EINVAL (pool out of limits, n >= 2^24), CR_ENOMEM, CR_ECUDA. */
 CR_API int cr_pages_extend(cr_ctx *ctx, const cr_kv_pages *pages, const int32_t *d_seqs, const int32_t *d_add,
                            uint32_t n);
 /* The empty rows d_dst[i] become the first d_keep[i] tokens of rows d_src[i]: the
  * pages that are full of them are shared, the tokens that are left are copied, in
- * every layer, into a page of the row's own.  No row may stand in d_dst twice, nor
- * in both lists.  Errors as cr_pages_extend. */
+ * every layer, into a page of the row's own.  No row may stand in both lists; one
+ * that stands in d_dst twice is forked by the first of its entries that can be
+ * carried out (CR_EINVAL for the others).  Errors as cr_pages_extend. */
 CR_API int cr_pages_fork(cr_ctx *ctx, const cr_kv_pages *pages, const int32_t *d_src, const int32_t *d_dst,
                          const int32_t *d_keep, uint32_t n);
 /* The rows d_seqs[n] become empty; pages that no row names any more are free.  An

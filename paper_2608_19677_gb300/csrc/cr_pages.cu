@@ -74,40 +74,53 @@ __global__ void __launch_bounds__(1024) k_pages_scan(const __grid_constant__ pag
     cr_launch_next();
     cr_wait_previous();
     if (KIND != SCAN_NONE && blockIdx.x == 0) {
+        __shared__ int rows[1024];
         unsigned long long base = 0;
         for (uint32_t i0 = 0; i0 < n; i0 += 1024) {
             const uint32_t i = i0 + threadIdx.x;
             int4 e = make_int4(-1, 0, 0, 0);
             uint32_t need = 0;
+            int row = -1, len = 0;  // an entry that can be carried out: its row, which has len tokens
             if (i < n) {
-                bool ok = false;
                 if (KIND == SCAN_EXTEND) {
-                    const int row = a[i], add = b[i];
-                    if (row >= 0 && (uint32_t)row < P.n_seqs && add >= 0) {
-                        const int len = P.lens[row];
-                        // a row is claimed (its length stands as -1 - len) by the entry that extends it
-                        if (len >= 0 && (long long)len + add <= ((long long)P.max_pages << P.page_log2) &&
-                            atomicCAS(P.lens + row, len, -1 - len) == len) {
-                            ok = true;
-                            e = make_int4(row, len, add, 0);
+                    const int r = a[i], add = b[i];
+                    if (r >= 0 && (uint32_t)r < P.n_seqs && add >= 0) {
+                        len = __ldcg(P.lens + r);
+                        if (len >= 0 && (long long)len + add <= ((long long)P.max_pages << P.page_log2)) {
+                            row = r;
+                            e = make_int4(r, len, add, 0);
                             need = pages_of((uint32_t)len + (uint32_t)add, P.page_log2) - pages_of((uint32_t)len, P.page_log2);
                         }
                     }
                 } else {
                     const int src = a[i], dst = b[i], keep = c[i];
                     if (src >= 0 && (uint32_t)src < P.n_seqs && dst >= 0 && (uint32_t)dst < P.n_seqs && keep >= 1 &&
-                        keep <= P.lens[src] && pages_of((uint32_t)keep, P.page_log2) <= P.max_pages &&
-                        atomicCAS(P.lens + dst, 0, -1) == 0) {
-                        ok = true;
+                        keep <= __ldcg(P.lens + src) && pages_of((uint32_t)keep, P.page_log2) <= P.max_pages &&
+                        __ldcg(P.lens + dst) == 0) {
+                        row = dst;
                         e = make_int4(dst, src, keep, 0);
                         need = (keep & (int)(P.page - 1)) != 0;
                     }
                 }
-                if (!ok) atomicOr(P.status, CR_FLAG_BADPAGES);
             }
-            // in 64 bits: a row may ask for 2^28 pages, and 1,024 of them are summed here
-            unsigned long long total;
-            const unsigned long long at = base + block_scan((unsigned long long)need, &total);
+            __syncthreads();  // lengths are read before any is marked
+            // A row is claimed (its length stands as -1 - len) by the entry that changes it: of several, the first in the
+            // list.  Those of this round meet here; later ones find the mark.  The needs are summed while the claims are on
+            // their way, in 64 bits: a row may ask for 2^28 pages.
+            const int was = row >= 0 ? atomicCAS(P.lens + row, len, -1 - len) : len;
+            unsigned long long total, at = block_scan((unsigned long long)need, &total);
+            bool ok = row >= 0;
+            if (__syncthreads_or(was != len)) {
+                rows[threadIdx.x] = row;
+                __syncthreads();
+                for (uint32_t j = 0; ok && j < threadIdx.x; ++j) ok = rows[j] != row;
+                at = block_scan(ok ? (unsigned long long)need : 0ull, &total);
+            }
+            at += base;
+            if (!ok) {
+                e.x = -1;
+                if (i < n) atomicOr(P.status, CR_FLAG_BADPAGES);
+            }
             if (i < n) {
                 S.entry[i] = e;
                 S.base[i] = at < 0xffffffffull ? (uint32_t)at : 0xffffffffu;

@@ -11,7 +11,7 @@ if not torch.cuda.is_available():
 else:
     pytestmark = pytest.mark.gpu
 
-from test_gpu_prefix_cache import BF, DEV, HF, P, check, ctx, fill, gen, ints, randn, reference  # noqa: E402, F401
+from test_gpu_prefix_cache import BF, DEV, HF, Model, P, check, ctx, fill, gen, ints, randn, reference  # noqa: E402, F401
 
 
 def raises_at_sync(P, ctx, code):
@@ -86,3 +86,39 @@ def test_needs_that_pass_32_bits_change_nothing(P, ctx, adds):
     P.pages_extend(ctx, pg, ints([5, 3]), ints([100, 408]))      # 13 and 51: all of them
     ctx.sync()
     assert pg.ref.all() and pg.table[5, :13].tolist() == list(range(13)) and pg.table[3, :51].tolist() == list(range(13, 64))
+
+
+def test_of_entries_that_name_a_row_twice_the_first_is_carried_out(P, ctx):
+    """Within a round of 1,024 entries and across rounds, each entry with a need of its own; the first of a row may be
+    one that cannot be carried out."""
+    r = np.random.default_rng(8)
+    n_seqs, width, n = 600, 40, 3000
+    for trial in range(12):
+        seqs, add = r.integers(0, n_seqs, n), r.integers(0, 300, n)
+        add[r.random(n) < 0.05] = width * 16 + 1
+        add[r.random(n) < 0.05] = -1
+        m = Model(20000, 16, n_seqs, width)
+        first = {}
+        for i, (s, a) in enumerate(zip(seqs, add)):
+            if s not in first and 0 <= a <= width * 16:
+                first[s] = i
+        m.extend(seqs[list(first.values())], add[list(first.values())])
+        pg = P.KVPages.empty(20000, 16, n_seqs, width, 1, 1, 8)
+        P.pages_extend(ctx, pg, ints(seqs), ints(add))
+        raises_at_sync(P, ctx, P.CR_EINVAL)
+        m.same(pg)
+        # forks into rows that stand twice: each from a parent, and of a length, of its own
+        some = [s for s in first if m.lens[s]]
+        empty = np.nonzero(m.lens == 0)[0]
+        src, dst = r.choice(some, 2000), r.choice(empty, 2000)
+        keep = np.array([r.integers(1, m.lens[s] + 1) for s in src])
+        keep[::37] = 0
+        taken = {}
+        for i, d in enumerate(dst):
+            if d not in taken and keep[i] > 0:
+                taken[d] = i
+        taken = list(taken.values())
+        m.fork(src[taken], dst[taken], keep[taken])
+        P.pages_fork(ctx, pg, ints(src), ints(dst), ints(keep))
+        raises_at_sync(P, ctx, P.CR_EINVAL)
+        m.same(pg)
