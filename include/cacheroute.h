@@ -48,7 +48,10 @@
  *   - A call whose scratch buffers are already large enough allocates
  *     nothing and does not synchronise, so a sequence of non-blocking calls
  *     can be captured into a CUDA graph after one pass over the same sizes
- *     (stream capture on a stream other than the legacy default one).
+ *     (stream capture on a stream other than the legacy default one).  Scratch
+ *     that a captured call works in stays until cr_destroy, whatever larger
+ *     calls come later; arrays of a plan, replay or replay input that a later,
+ *     larger build or partition replaces do not: capture again after one.
  */
 #ifndef CACHEROUTE_H
 #define CACHEROUTE_H
@@ -112,7 +115,8 @@ typedef struct cr_replay_input cr_replay_input;
  * CR_ECUDA, CR_ENOMEM. */
 CR_API int cr_create(cr_ctx **out, int device, void *cuda_stream);
 
-/* Destroy a context after waiting for its stream.  NULL is accepted. */
+/* Destroy a context after waiting for its stream; graphs captured from its calls
+ * may not be launched any more.  NULL is accepted. */
 CR_API int cr_destroy(cr_ctx *ctx);
 
 /* Switch the stream later calls enqueue on. */

@@ -26,11 +26,32 @@ int cr_check_launch(cr_ctx *ctx, const char *what)
     return CR_OK;
 }
 
+// The legacy default stream cannot be captured (and asking it is an error while another stream is).
+static bool capturing(cudaStream_t stream)
+{
+    if (stream == NULL || stream == cudaStreamLegacy) return false;
+    cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(stream, &st) != cudaSuccess) {
+        cudaGetLastError();
+        return false;
+    }
+    return st != cudaStreamCaptureStatusNone;
+}
+
 int cr_scratch(cr_ctx *ctx, int slot, size_t bytes, void **out)
 {
     if (bytes == 0) bytes = 16;
     if (ctx->scratch_bytes[slot] < bytes) {
-        if (ctx->scratch[slot]) {
+        if (ctx->scratch[slot] && ctx->scratch_in_graph[slot]) {
+            // a graph that is replayed later still works in the old buffer
+            void **list = (void **)realloc(ctx->outgrown, (ctx->n_outgrown + 1) * sizeof(void *));
+            if (!list) return cr_fail(ctx, CR_ENOMEM, "scratch slot %d: host allocation failed", slot);
+            ctx->outgrown = list;
+            list[ctx->n_outgrown++] = ctx->scratch[slot];
+            ctx->scratch[slot] = NULL;
+            ctx->scratch_bytes[slot] = 0;
+            ctx->scratch_in_graph[slot] = 0;
+        } else if (ctx->scratch[slot]) {
             // the old buffer may still be read by enqueued work
             cudaError_t e = cudaStreamSynchronize(ctx->stream);
             if (e != cudaSuccess) return cr_fail(ctx, CR_ECUDA, "scratch sync: %s", cudaGetErrorString(e));
@@ -48,6 +69,7 @@ int cr_scratch(cr_ctx *ctx, int slot, size_t bytes, void **out)
         ctx->scratch[slot] = p;
         ctx->scratch_bytes[slot] = grow;
     }
+    if (capturing(ctx->stream)) ctx->scratch_in_graph[slot] = 1;
     *out = ctx->scratch[slot];
     return CR_OK;
 }
@@ -154,6 +176,8 @@ extern "C" int cr_destroy(cr_ctx *ctx)
     if (ctx->ev_resolve) cudaEventDestroy(ctx->ev_resolve);
     for (int i = 0; i < SCR_NUM; ++i)
         if (ctx->scratch[i]) cudaFree(ctx->scratch[i]);
+    for (uint32_t i = 0; i < ctx->n_outgrown; ++i) cudaFree(ctx->outgrown[i]);
+    free(ctx->outgrown);
     cudaFree(ctx->d_status);
     free(ctx);
     return CR_OK;

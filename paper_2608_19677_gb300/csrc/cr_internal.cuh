@@ -75,6 +75,9 @@ struct cr_ctx {
     uint64_t launches;
     void *scratch[SCR_NUM];
     size_t scratch_bytes[SCR_NUM];
+    uint8_t scratch_in_graph[SCR_NUM];  // a captured graph has the buffer's address: it outlives its replacement
+    void **outgrown;                    // such buffers, freed with the context
+    uint32_t n_outgrown;
     char msg[320];
     // routing split over two streams (cr_set_resolve_stream): the load-dependent
     // resolution runs on resolve_stream, after ev_cand; ev_resolve marks its end

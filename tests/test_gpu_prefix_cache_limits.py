@@ -122,3 +122,52 @@ def test_of_entries_that_name_a_row_twice_the_first_is_carried_out(P, ctx):
         P.pages_fork(ctx, pg, ints(src), ints(dst), ints(keep))
         raises_at_sync(P, ctx, P.CR_EINVAL)
         m.same(pg)
+
+
+def test_a_graph_stays_right_after_larger_calls(P):
+    """Larger lists of work, pieces and page calls replace the scratch that the captured calls work in."""
+    g = gen(41)
+    stream = torch.cuda.Stream()
+    c = P.Context(0, stream=stream)
+    lens, group = [900, 33, 917, 500], [0, 1, 0, 2]
+    order = [0, 2, 1, 3]
+    pg, kv = fill(P, c, g, 16, [lens[i] for i in order], 2, 128, BF, shared=[896, 0, 0], group=[group[i] for i in order])
+    big, _ = fill(P, c, g, 16, [3000] * 700, 2, 128, BF)
+    q, out, prompt = randn(g, 4, 16, 128), torch.empty(4, 16, 128, dtype=BF, device=DEV), randn(g, 300, 4, 128)
+    whole = torch.empty_like(prompt)
+    off, shared, cu = ints([0, 2, 3, 4]), ints([896, 0, 0]), ints([0, 300])
+    rows = P.KVPages.empty(100, 16, 8, 16, 1, 1, 64)
+    row, tokens = ints([3]), ints([40])
+    torch.cuda.synchronize()
+
+    def step():
+        P.attn_decode(c, q, pg, 0, group_off=off, shared=shared, out=out)
+        P.attn_packed(c, prompt, prompt, prompt, cu, out=whole)
+        P.pages_extend(c, rows, row, tokens)
+        P.pages_free(c, rows, row)
+
+    with torch.cuda.stream(stream):
+        step()
+        c.sync()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            step()
+        many = randn(g, 700, 32, 128)
+        for _ in range(2):
+            P.attn_decode(c, many, big, 0, group_off=ints(range(0, 701, 350)), shared=ints([0, 0]))
+            P.attn_decode(c, many, big, 0)
+            P.attn_packed(c, many, many, many, ints([0, 1, 700]))
+            z = P.KVPages.empty(4_000_000, 8, 4, 4, 1, 1, 8)
+            P.pages_extend(c, z, ints([0]), ints([8]))
+            c.sync()
+            q.copy_(randn(g, 4, 16, 128))
+            prompt.copy_(randn(g, 300, 4, 128))
+            graph.replay()
+            c.sync()
+            for i in range(4):
+                o, _, bo, _ = reference(q[i:i + 1], *kv[i], False, 128 ** -0.5)
+                assert ((out[i:i + 1].double() - o).abs() <= bo).all()
+            o, _, bo, _ = reference(prompt, prompt, prompt, True, 128 ** -0.5)
+            assert ((whole.double() - o).abs() <= bo).all()
+            assert not rows.ref.any()
+    c.close()
