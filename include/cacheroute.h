@@ -119,7 +119,11 @@ CR_API int cr_create(cr_ctx **out, int device, void *cuda_stream);
  * may not be launched any more.  NULL is accepted. */
 CR_API int cr_destroy(cr_ctx *ctx);
 
-/* Switch the stream later calls enqueue on. */
+/* Switch the stream later calls enqueue on; they run after what the context has
+ * enqueued so far, since they work in the same scratch.  The stream before must
+ * still exist.  A switch to or from a stream under capture orders nothing: a graph's
+ * launches and other calls of the context must not run at the same time.
+ * Errors: CR_EINVAL (ctx NULL), CR_ECUDA. */
 CR_API int cr_set_stream(cr_ctx *ctx, void *cuda_stream);
 
 /* Routing split over two streams: with a non-NULL stream, cr_route_batch runs

@@ -205,8 +205,9 @@ class Context:
         self.check(lib().cr_sync(self._h), "cr_sync")
 
     def set_stream(self, stream):
-        self._stream_obj, self._raw_stream = stream, stream.cuda_stream
+        """Later calls run on ``stream``, after what the context has enqueued so far."""
         self.check(lib().cr_set_stream(self._h, C.c_void_p(stream.cuda_stream)), "cr_set_stream")
+        self._stream_obj, self._raw_stream = stream, stream.cuda_stream
 
     @property
     def launches(self) -> int:

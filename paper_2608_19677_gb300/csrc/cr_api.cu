@@ -172,6 +172,7 @@ extern "C" int cr_destroy(cr_ctx *ctx)
     prof_free(ctx);
     cr_replay_input_destroy(nullptr, ctx->replay_in);
     if (ctx->resolve_stream) cudaStreamSynchronize(ctx->resolve_stream);
+    if (ctx->ev_switch) cudaEventDestroy(ctx->ev_switch);
     if (ctx->ev_cand) cudaEventDestroy(ctx->ev_cand);
     if (ctx->ev_resolve) cudaEventDestroy(ctx->ev_resolve);
     for (int i = 0; i < SCR_NUM; ++i)
@@ -186,7 +187,21 @@ extern "C" int cr_destroy(cr_ctx *ctx)
 extern "C" int cr_set_stream(cr_ctx *ctx, void *cuda_stream)
 {
     if (!ctx) return CR_EINVAL;
-    ctx->stream = (cudaStream_t)cuda_stream;
+    const cudaStream_t next = (cudaStream_t)cuda_stream;
+    if (next == ctx->stream) return CR_OK;
+    // The calls of both streams work in the same scratch.  A stream under capture takes part in no such order (and
+    // recording on the legacy stream would break another's capture): asking that one is an error then.
+    cudaStreamCaptureStatus a = cudaStreamCaptureStatusNone, b = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(next, &a) != cudaSuccess || cudaStreamIsCapturing(ctx->stream, &b) != cudaSuccess) {
+        cudaGetLastError();
+        a = cudaStreamCaptureStatusActive;
+    }
+    if (a == cudaStreamCaptureStatusNone && b == cudaStreamCaptureStatusNone) {
+        if (!ctx->ev_switch) CR_CUDA(ctx, cudaEventCreateWithFlags(&ctx->ev_switch, cudaEventDisableTiming));
+        CR_CUDA(ctx, cudaEventRecord(ctx->ev_switch, ctx->stream));
+        CR_CUDA(ctx, cudaStreamWaitEvent(next, ctx->ev_switch, 0));
+    }
+    ctx->stream = next;
     return CR_OK;
 }
 

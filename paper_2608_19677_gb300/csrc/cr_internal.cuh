@@ -71,6 +71,7 @@ struct cr_ctx {
     int device;
     int num_sms;
     cudaStream_t stream;
+    cudaEvent_t ev_switch;       // end of the work on the stream before (cr_set_stream)
     uint32_t *d_status;          // CR_FLAG_* bits
     uint64_t launches;
     void *scratch[SCR_NUM];

@@ -171,3 +171,56 @@ def test_a_graph_stays_right_after_larger_calls(P):
             assert ((whole.double() - o).abs() <= bo).all()
             assert not rows.ref.any()
     c.close()
+
+
+@pytest.mark.parametrize("way", ["default to own", "own to own", "own to default"])
+def test_calls_after_a_switch_of_streams_wait_for_those_before(P, way):
+    """Both work in the context's scratch."""
+    g = gen(51)
+    own = [torch.cuda.Stream(), torch.cuda.Stream()]
+    old = torch.cuda.current_stream() if way.startswith("default") else own[0]
+    new = torch.cuda.current_stream() if way.endswith("default") else own[1]
+    c = P.Context(0, stream=old)
+    pg, kv = fill(P, c, g, 16, [3000, 40], 2, 128, BF)
+    q = randn(g, 2, 8, 128)
+    torch.cuda.synchronize()
+    P.attn_decode(c, q, pg, 0)
+    c.sync()
+    ended = torch.cuda.Event()
+    with torch.cuda.stream(old):
+        torch.cuda._sleep(100_000_000)
+        ended.record()
+    c.set_stream(new)
+    assert c.stream.cuda_stream == new.cuda_stream
+    out, lse = P.attn_decode(c, q, pg, 0, lse=True)
+    new.synchronize()
+    waited = ended.query()
+    c.sync()
+    check(out, lse, [reference(q[i:i + 1], *kv[i], False, 128 ** -0.5) for i in range(2)], range(3))
+    c.close()
+    assert waited
+
+
+def test_a_switch_to_a_stream_under_capture_leaves_the_capture_alone(P):
+    g = gen(52)
+    c = P.Context(0)
+    pg, kv = fill(P, c, g, 16, [300, 40], 2, 128, BF)
+    q = randn(g, 2, 8, 128)
+    out = torch.empty_like(q)
+    P.attn_decode(c, q, pg, 0, out=out)
+    c.sync()
+    out.zero_()
+    stream, home = torch.cuda.Stream(), c.stream
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        c.set_stream(torch.cuda.current_stream())
+        P.attn_decode(c, q, pg, 0, out=out)
+        c.set_stream(home)
+    torch.cuda.synchronize()
+    assert not out.any()
+    graph.replay()
+    torch.cuda.synchronize()
+    for i in range(2):
+        o, _, bo, _ = reference(q[i:i + 1], *kv[i], False, 128 ** -0.5)
+        assert ((out[i:i + 1].double() - o).abs() <= bo).all()
+    c.close()
