@@ -622,7 +622,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     cr_tc_after();
     const uint32_t tmem = tmem_at;
     cr_wait_previous();
-    if (A.to_pfx) cr_launch_next();  // k_attn_few of the same call takes the SMs as they come free
+    if (A.to_pfx) cr_launch_next();  // k_attn_few of the same call gets ready on the SMs that come free
 
     uint32_t pieces = 0;  // their number so far; they take two places in turn
 
@@ -1320,9 +1320,9 @@ __global__ void __launch_bounds__(kFewThreads, 2)
         asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(sq + 16 * i), "r"(0));
     cr_fence_async_smem();
     __syncthreads();
-    // After k_attn_rows of the same call this one needs nothing of it, and the list of work was there before that
-    // began: the wait comes at the end, so that whoever waits for this kernel waits for both.
-    if (!A.after_rows) cr_wait_previous();
+    // After k_attn_rows of the same call this one needs nothing of it, but it does read what was written before that
+    // began (the list of work, tables, pages), and only the wait makes any of it visible here.
+    cr_wait_previous();
     cr_launch_next();
 
     walk w;
@@ -1543,7 +1543,6 @@ out:
         if (lane == 0) atomicOr(A.status, CR_FLAG_TIMEOUT);
         for (int i = 0; i < 2000; ++i) __nanosleep(1000);
     }
-    if (A.after_rows) cr_wait_previous();
 #undef FULL
 #undef EMPTY
 #undef QFULL

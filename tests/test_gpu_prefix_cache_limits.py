@@ -224,3 +224,51 @@ def test_a_switch_to_a_stream_under_capture_leaves_the_capture_alone(P):
         o, _, bo, _ = reference(q[i:i + 1], *kv[i], False, 128 ** -0.5)
         assert ((out[i:i + 1].double() - o).abs() <= bo).all()
     c.close()
+
+
+@pytest.mark.parametrize("hq,hkv,d,n", [(8, 2, 128, 40), (16, 1, 64, 150)])
+def test_steps_queued_one_after_the_other_see_each_others_tables_and_pages(P, ctx, hq, hkv, d, n):
+    """Rows are freed, forked, grown and written again and again without a wait between, each step's tables and values
+    unlike the last one's, and every step's grouped decoding is right."""
+    g, r = gen(n), np.random.default_rng(n)
+    page, pre, keys = 16, 900, 3
+    pg = P.KVPages.empty(keys * 57 + n * 10 + 40, page, keys + n, 70, 1, hkv, d)
+    own = list(range(keys, keys + n))
+    m = Model(pg.n_pages, page, keys + n, 70)
+    heads = [ints(range(keys)), ints([pre] * keys), ints(np.arange(keys + 1) * pre)]
+    k0, v0 = randn(g, keys * pre, hkv, d, spread=2.0), randn(g, keys * pre, hkv, d)
+    group = np.sort(r.integers(0, keys, n))
+    off, dst = np.searchsorted(group, np.arange(keys + 1)), ints(own)
+    steps = []
+    for step in range(6):
+        keep, add = r.integers(1, pre + 1, n), r.integers(1, 100, n)
+        keep[r.random(n) < 0.7] = pre
+        least = [min([pre] + [int(x) for x in keep[off[i]:off[i + 1]]]) // page * page for i in range(keys)]
+        T = int(add.sum())
+        steps.append((keep, add, [ints(group), ints(keep), ints(add), ints(np.concatenate([[0], np.cumsum(add)])), ints(off),
+                                  ints(least)], randn(g, T, hkv, d, spread=2.0), randn(g, T, hkv, d), randn(g, n, hq, d)))
+    torch.cuda.synchronize()
+    P.pages_extend(ctx, pg, heads[0], heads[1])
+    P.kv_write(ctx, pg, 0, k0, v0, heads[2], seqs=heads[0])
+    m.extend(range(keys), [pre] * keys)
+    got = []
+    for keep, add, (src, kp, ad, cu, go, sh), k, v, q in steps:
+        P.pages_free(ctx, pg, dst)
+        P.pages_fork(ctx, pg, src, dst, kp)
+        P.pages_extend(ctx, pg, dst, ad)
+        P.kv_write(ctx, pg, 0, k, v, cu, seqs=dst)
+        got.append(P.attn_decode(ctx, q, pg, 0, seqs=dst, group_off=go, shared=sh, lse=True))
+    ctx.sync()
+    for (keep, add, _, k, v, q), (out, lse) in zip(steps, got):
+        m.free(own)
+        m.fork(group, own, keep)
+        m.extend(own, add)
+        at = np.concatenate([[0], np.cumsum(add)])
+        want = []
+        for i in range(n):
+            a = int(group[i]) * pre
+            kk = torch.cat([k0[a:a + keep[i]], k[at[i]:at[i + 1]]])
+            vv = torch.cat([v0[a:a + keep[i]], v[at[i]:at[i + 1]]])
+            want.append(reference(q[i:i + 1], kk, vv, False, d ** -0.5))
+        check(out, lse, want, range(n + 1))
+    m.same(pg)
