@@ -18,6 +18,7 @@
 //   k_attn_few   at most 16 rows per key head (one token's grouped heads): tiles of 64 keys.
 #include <math.h>
 
+#include "cr_attn_index.cuh"
 #include "cr_internal.cuh"
 #include "cr_tensor.cuh"
 
@@ -1190,20 +1191,23 @@ __global__ void __launch_bounds__(256)
     cr_wait_previous();
     const uint32_t e = blockIdx.x, h = blockIdx.y, kv = h / F.nsub, sub = h % F.nsub;
     const uint64_t own = (uint64_t)e * F.few_heads + h;
-    // groups that are not ascending leave some of these unset: no index passes its array all the same
-    const int row0 = clampi(R.of_token[e], 0, (int)e), f0 = F.first_cta[own], f1 = F.last_cta[own];
-    const bool shared = F.blk[e].lo > 0;  // else row0 means nothing
-    if (f0 == f1 && !shared) return;      // written already
+    // groups that are not ascending, and waits that have given up, leave some of these unset: no index passes its array
+    // all the same
+    const int row0 = clampi(R.of_token[e], 0, (int)e);
+    const cr_cta_span of_own = cr_marked_ctas(F.first_cta[own], F.last_cta[own], (int)F.ncta);
+    const bool shared = F.blk[e].lo > 0;   // else row0 means nothing
+    if (of_own.n == 1 && !shared) return;  // written already
     const uint32_t r = threadIdx.x & 15;
     const bool valid = sub * 16 + r < F.G;
     const uint32_t head = kv * F.G + sub * 16 + r;
     const uint64_t oh = (uint64_t)e * F.q_heads + head;
-    uint32_t nf = (uint32_t)(f1 - f0) + 1, nr = 0, rr = 0;
-    int r0 = 0;
+    const uint32_t f0 = (uint32_t)of_own.first, nf = of_own.n;
+    uint32_t r0 = 0, nr = 0, rr = 0;
     if (shared) {
         const uint64_t at = (uint64_t)row0 * R.kv_heads + kv;
-        r0 = clampi(R.first_cta[at], 0, (int)R.ncta - 1);
-        nr = (uint32_t)(clampi(R.last_cta[at], r0, (int)R.ncta - 1) - r0) + 1;
+        const cr_cta_span of_prefix = cr_marked_ctas(R.first_cta[at], R.last_cta[at], (int)R.ncta);
+        r0 = (uint32_t)of_prefix.first;
+        nr = of_prefix.n;
         const uint32_t t = min(e - (uint32_t)row0, 2 * R.tq - 1);  // token of the prefix' block
         rr = t / R.tq * kRowsTile + t % R.tq * R.G + sub * 16 + r;
     }

@@ -1,0 +1,39 @@
+"""Index arithmetic of the attention kernels, compiled for the host and tried at its edges."""
+import os
+import subprocess
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2608_19677_gb300", "csrc")
+
+
+def run(tmp_path, body):
+    src, exe = tmp_path / "t.cpp", tmp_path / "t"
+    src.write_text('#include <limits.h>\n#include <stdio.h>\n#include <stdint.h>\n#include "cr_attn_index.cuh"\n'
+                   "int main()\n{\n" + body + "\nreturn 0;\n}\n")
+    subprocess.run(["g++", "-std=c++17", "-fsanitize=undefined", "-fno-sanitize-recover", "-I", CSRC, str(src), "-o",
+                    str(exe)], check=True)
+    return subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()
+
+
+def test_marks_that_nobody_set_stay_within_the_ctas(tmp_path):
+    """What memory may hold where a CTA gave up before it set its marks."""
+    run(tmp_path, r"""
+    const int some[] = {INT_MIN, INT_MIN + 1, -1000000, -2, -1, 0, 1, 2, 150, 151, 152, 303, 304, 511, 1 << 20, INT_MAX - 1,
+                        INT_MAX};
+    const int ctas[] = {1, 2, 152, 304, 511};
+    for (int n : ctas)
+        for (int a : some)
+            for (int b : some) {
+                const cr_cta_span s = cr_marked_ctas(a, b, n);
+                if (s.first < 0 || s.n < 1 || s.n > (unsigned)n || s.first + (long long)s.n > n) return 1;
+                if (0 <= a && a <= b && b < n && (s.first != a || s.n != (unsigned)(b - a + 1))) return 2;
+            }
+    """)
+
+
+def test_the_join_takes_no_mark_as_it_finds_it():
+    """Every use of the marks goes through the function above."""
+    text = open(os.path.join(CSRC, "cr_attn.cu")).read()
+    uses = [line for line in text.splitlines() if "first_cta[" in line or "last_cta[" in line]
+    reads = [line for line in uses if "] = (int)blockIdx.x" not in line]
+    assert len(reads) == 2 and all("cr_marked_ctas(" in line for line in reads)
