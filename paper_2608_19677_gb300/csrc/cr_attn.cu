@@ -681,7 +681,9 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                 const bool on = lane < boxes * cfg::kChunks && (!A.paged || key < w.k.klen);
                 int y = w.k.kbase + key, pg = 0;
                 if (A.paged) {
-                    if (on) pg = __ldg(row + ((uint32_t)key >> A.page_log2));
+                    // an ordinary load: k_pages_extend and others of the same chain may still write tables while this
+                    // kernel is resident, which only ordinary loads behind the wait above are ordered with
+                    if (on) pg = row[(uint32_t)key >> A.page_log2];
                     y = key & ((1 << A.page_log2) - 1);
                 }
                 const uint32_t bytes = __popc(__ballot_sync(~0u, on)) * A.box_rows * 128;
@@ -1362,7 +1364,8 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                 const bool on = lane < boxes * cfg::kChunks && key < w.k.klen;
                 const uint32_t bytes = 2 * __popc(__ballot_sync(~0u, on)) * A.box_rows * 128;
                 int pg = 0;
-                if (on) pg = __ldg(A.table + (uint64_t)w.k.kbase * A.max_pages + ((uint32_t)key >> A.page_log2));
+                // an ordinary load, as in k_attn_rows
+                if (on) pg = A.table[(uint64_t)w.k.kbase * A.max_pages + ((uint32_t)key >> A.page_log2)];
                 const int y = key & ((1 << A.page_log2) - 1);
                 if (!cr_bar_wait(EMPTY(stage), phase ^ 1, &gave_up)) goto out;
                 if (lane == 0) cr_bar_expect(FULL(stage), bytes);

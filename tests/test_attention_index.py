@@ -37,3 +37,11 @@ def test_the_join_takes_no_mark_as_it_finds_it():
     uses = [line for line in text.splitlines() if "first_cta[" in line or "last_cta[" in line]
     reads = [line for line in uses if "] = (int)blockIdx.x" not in line]
     assert len(reads) == 2 and all("cr_marked_ctas(" in line for line in reads)
+
+
+def test_no_load_takes_the_path_for_data_that_nothing_writes():
+    """Kernels of these files are resident while the one before them may still write what they read: only ordinary loads
+    are ordered by their wait for it."""
+    for name in ("cr_attn.cu", "cr_pages.cu", "cr_tensor.cuh"):
+        text = open(os.path.join(CSRC, name)).read()
+        assert not [w for w in ("__ldg(", "ld.global.nc", "__restrict__") if w in text], name
