@@ -165,13 +165,6 @@ __device__ __forceinline__ unsigned long long div_by(unsigned long long a, unsig
     return a >> 32 || b >> 32 ? a / b : (uint32_t)a / (uint32_t)b;
 }
 
-// Key tiles of a single token's block; one at least, which writes zeros where there are no keys.
-__device__ __forceinline__ uint32_t few_tiles(int lo, int klen)
-{
-    const int t = (klen + kFewTile - 1) / kFewTile - lo / kFewTile;
-    return t > 1 ? t : 1;
-}
-
 // How the work is cut: N units in stretches of equal length, or one stretch for each block.
 struct plan_cut {
     unsigned long long N, Nb, snap;
@@ -334,9 +327,9 @@ __device__ void plan_build(const plan_in &A, plan_shared &S, uint32_t *status)
                 if (A.causal) end = clampi(k.diag + k.ntok, 0, k.klen);
             }
             if (KIND == PLAN_FEW) {
-                nt = few_tiles(k.lo, k.klen);
+                nt = cr_few_tiles(k.lo, k.klen, kFewTile);
             } else {
-                nt = (uint32_t)((end + kRowsTile - 1) / kRowsTile);
+                nt = cr_key_tiles(end, kRowsTile);
                 if (nt == 0 && KIND != PLAN_GROUPS) nt = 1;  // rows without keys: zeros
             }
             k.nt = (int)nt;
@@ -436,7 +429,7 @@ __device__ __forceinline__ plan_cut make_list(const plan_in &P, own_list *L, uin
         k.ntok = 1;
         k.kbase = row < 0 ? 0 : row;
         k.klen = keys_of(P, row);
-        k.nt = (int)few_tiles(0, k.klen);
+        k.nt = (int)cr_few_tiles(0, k.klen, kFewTile);
         at = (uint32_t)k.nt + kExtra;
     }
 #pragma unroll
@@ -679,8 +672,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                 const int key = (int)(t * kRowsTile + (box << A.box_log2));
                 // packed keys come as one box; its rows behind the sequence are never used
                 const bool on = lane < boxes * cfg::kChunks && (!A.paged || key < w.k.klen);
-                int y = w.k.kbase + key, pg = 0;
-                if (A.paged) {
+                int y, pg = 0;
+                if (!A.paged) {
+                    y = w.k.kbase + key;
+                } else {
                     // an ordinary load: k_pages_extend and others of the same chain may still write tables while this
                     // kernel is resident, which only ordinary loads behind the wait above are ordered with
                     if (on) pg = row[(uint32_t)key >> A.page_log2];
@@ -825,7 +820,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             // keys that this row sees, from the first tile's on; the tile with the sequence's end
             int seen = p->klen - p->t0 * kRowsTile - half * 64;
             const int tail = x == 0 && half < cfg::kChunks ? (p->klen >> 7) - p->t0 : -1;
-            if (A.causal) seen = min(seen, p->diag + tok + 1 - p->t0 * kRowsTile - half * 64);
+            if (A.causal) seen = min(seen, p->diag - p->t0 * kRowsTile - half * 64 + tok + 1);
             float m = -INFINITY, l = 0.f;
             for (int j = 0; j < n; ++j, seen -= kRowsTile) {
                 if (!cr_bar_wait(BAR(B_SFULL + x), sphase, &gave_up)) goto left;
@@ -1420,7 +1415,8 @@ __global__ void __launch_bounds__(kFewThreads, 2)
             for (uint32_t t = w.t0; t < w.t1; ++t) {
                 if (!cr_bar_wait(FULL(stage), phase, &gave_up)) goto out;
                 const int key = (int)((w.k.lo / kFewTile + t) * kFewTile + warp * 16);  // this warp's first key
-                if (key < w.k.klen && key + 16 > w.k.lo) {
+                const cr_keys16 see = cr_seen16(key, w.k.lo, w.k.klen);
+                if (see.any()) {
                     const uint32_t kt = ring + stage * 2 * cfg::kTile, vt = kt + cfg::kTile;
                     float s[2][4] = {};
                     const uint32_t kr = warp * 16 + (lane & 7) + ((lane >> 4) << 3);
@@ -1434,13 +1430,12 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                         mma16816<BF16>(s[1], qa[i], b[2], b[3]);
                     }
                     uint32_t keep[2] = {~0u, ~0u};  // halves of v's registers that are seen
-                    if (key + 16 > w.k.klen || key < w.k.lo) {
+                    if (!see.all()) {
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
-                                const int j = key + i * 8 + (int)q4 * 2 + e;
-                                if (j < w.k.lo || j >= w.k.klen) {
+                                if (!see.sees(i * 8 + (int)q4 * 2 + e)) {
                                     s[i][e] = s[i][2 + e] = -INFINITY;
                                     keep[i] &= e ? 0x0000ffffu : 0xffff0000u;
                                 }

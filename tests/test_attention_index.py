@@ -45,3 +45,33 @@ def test_no_load_takes_the_path_for_data_that_nothing_writes():
     for name in ("cr_attn.cu", "cr_pages.cu", "cr_tensor.cuh"):
         text = open(os.path.join(CSRC, name)).read()
         assert not [w for w in ("__ldg(", "ld.global.nc", "__restrict__") if w in text], name
+
+
+def test_tiles_and_masks_of_the_longest_sequences(tmp_path):
+    """Against 64-bit arithmetic, up to the 2^31 - 8 tokens that a row can have; no signed sum passes 32 bits."""
+    run(tmp_path, r"""
+    const long long top = (1ll << 31) - 8;
+    const long long at[] = {0, 1, 2, 63, 64, 65, 127, 128, 129, 1000, 1 << 30, top - 129, top - 128, top - 65, top - 64,
+                            top - 17, top - 16, top - 9, top - 8, top - 1, top};
+    for (long long n : at) {
+        if (cr_key_tiles((int)n, 128) != (n + 127) / 128) return 1;
+        for (long long lo : at) {
+            const long long t = (n + 63) / 64 - lo / 64;
+            if (cr_few_tiles((int)lo, (int)n, 64) != (t > 1 ? t : 1)) return 2;
+            for (long long base : at)
+                for (int d = -32; d <= 32; d += 16) {
+                    const long long key = base / 16 * 16 + d;
+                    if (key < 0 || key > (1ll << 31) - 16) continue;
+                    const cr_keys16 s = cr_seen16((int)key, (int)lo, (int)n);
+                    int seen = 0;
+                    for (int j = 0; j < 16; ++j) {
+                        const bool want = key + j >= lo && key + j < n;
+                        if (s.sees(j) != want) return 3;
+                        seen += want;
+                    }
+                    if (s.all() != (seen == 16)) return 4;
+                    if (seen && !s.any()) return 5;
+                }
+        }
+    }
+    """)

@@ -272,3 +272,37 @@ def test_steps_queued_one_after_the_other_see_each_others_tables_and_pages(P, ct
             want.append(reference(q[i:i + 1], kk, vv, False, d ** -0.5))
         check(out, lse, want, range(n + 1))
     m.same(pg)
+
+
+def test_the_longest_row(P, ctx):
+    """2^31 - 8 tokens, 64 GB of keys and values.  Keys are zeros but for the last 24, values too: the sums are known.
+    Beside the bounds of the other tests, the sum of 2^31 weights in up to 304 pieces: 2^-15 of it."""
+    n, page, d, hq = (1 << 31) - 8, 8, 8, 4
+    if torch.cuda.mem_get_info()[0] < 90 << 30:
+        pytest.skip("needs 90 GB")
+    g = gen(61)
+    pages = n // page
+    cache = torch.zeros((1, 2, pages, page, 1, d), dtype=BF, device=DEV)
+    k, v = randn(g, 24, 1, d), randn(g, 24, 1, d)
+    k[:, :, 0] = torch.linspace(3, 4.5, 24, device=DEV).to(BF)[:, None]
+    cache[0, 0].view(-1, 1, d)[n - 24:], cache[0, 1].view(-1, 1, d)[n - 24:] = k, v
+    pg = P.KVPages(cache, torch.ones(pages, dtype=torch.int32, device=DEV),
+                   torch.arange(pages, dtype=torch.int32, device=DEV)[None], ints([n]))
+    q = randn(g, 20, hq, d)
+    q[..., 0] = 6.0
+    outs = [(P.attn_decode(ctx, q[19:], pg, 0, scale=1.0, lse=True), 19),
+            (P.attn_paged(ctx, q, pg, 0, ints([0, 20]), scale=1.0, lse=True), 0)]
+    ctx.sync()
+    for (out, lse), first in outs:
+        for i in range(first, 20):
+            sees = n - 20 + 1 + i
+            few = sees - (n - 24)                                    # of the last 24 keys
+            s = torch.einsum("hd,jd->hj", q[i].double(), k[:few, 0].double())
+            z = torch.logsumexp(torch.cat([s, torch.full((hq, 1), math.log(n - 24), device=DEV, dtype=torch.float64)], 1), 1)
+            p = torch.exp(s - z[:, None])
+            o, a = p @ v[:few, 0].double(), p @ v[:few, 0].double().abs()
+            e = torch.einsum("hd,jd->hj", q[i].double().abs(), k[:few, 0].double().abs()).amax() * 2.0 ** -18
+            bound = 2.0 ** -8 * (o.abs() + a) * 1.01 + (4 * e + 2.0 ** -19 + 2.0 ** -15) * a
+            got, gl = out[i - first].double(), lse[i - first].double()
+            assert ((got - o).abs() <= bound).all(), (first, i)
+            assert ((gl - z).abs() <= 2 * e + 2.0 ** -20 * z.abs() + 2.0 ** -18 + 2.0 ** -15).all(), (first, i)
