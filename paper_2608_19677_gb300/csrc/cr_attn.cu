@@ -1612,8 +1612,10 @@ int kv_map(cr_ctx *ctx, CUtensorMap *map, const kv_desc &K, bool value, uint32_t
         dim[1] = K.pg->page;
         dim[3] = K.pg->n_pages;
         st[2] = K.pg->page_stride;
-    } else {
+    } else if (K.n_kv) {
         dim[1] = K.n_kv;
+    } else {
+        dim[1] = dim[2] = 1;  // one row stands for no keys at all (cr_attn_packed)
     }
     const uint32_t box[3] = {box_rows, 1, 1};
     return encode_map(ctx, map, K.bf16, value ? K.v : K.k, dim, st, box, K.paged);
@@ -1886,11 +1888,7 @@ extern "C" int cr_attn_packed(cr_ctx *ctx, const cr_attn_args *args, uint32_t dt
     K.v_head = v_head;
     K.n_kv = n_kv;
     K.cu_k = d_cu_k ? d_cu_k : args->d_cu_q;
-    if (n_kv == 0 && args->n_tokens) {  // nothing to map: the queries' first elements stand for the empty tensors
-        K.k = K.v = args->d_q;
-        K.k_row = K.v_row = K.k_head = K.v_head = 8;
-        K.n_kv = 1;
-    }
+    if (n_kv == 0) K.k = K.v = args->d_q;  // nothing to map: a query's row is copied, which no query sees
     return attn_many(ctx, args, K);
 }
 

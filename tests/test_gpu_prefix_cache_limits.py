@@ -306,3 +306,12 @@ def test_the_longest_row(P, ctx):
             got, gl = out[i - first].double(), lse[i - first].double()
             assert ((got - o).abs() <= bound).all(), (first, i)
             assert ((gl - z).abs() <= 2 * e + 2.0 ** -20 * z.abs() + 2.0 ** -18 + 2.0 ** -15).all(), (first, i)
+
+
+@pytest.mark.parametrize("cu_k", [[0, 0, 0], [0, 1, 2], [0, 0, 1 << 30], [1, 1, 1]])
+@pytest.mark.parametrize("causal", [True, False])
+def test_no_keys_at_all_whatever_the_offsets_say(P, ctx, cu_k, causal):
+    q, none = randn(gen(71), 6, 8, 64), torch.zeros((0, 2, 64), dtype=BF, device=DEV)
+    out, lse = P.attn_packed(ctx, q, none, none, ints([0, 4, 6]), cu_k=ints(cu_k), causal=causal, lse=True)
+    ctx.sync()
+    assert (out == 0).all() and (lse == -math.inf).all()
