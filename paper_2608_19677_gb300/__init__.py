@@ -552,7 +552,8 @@ def shadow_replay(ctx: Context, replay: Replay, keys, plen, slen, dest, ctr):
 
 
 # ---- what a destination does with the prefixes it holds ------------------------------------------------------------
-# These calls are made once per layer and step: their checks take one look at each tensor.
+# These calls are made once per layer and step: their checks take one look at each tensor.  They have no gradient, and
+# refuse tensors that want one where gradients are recorded.
 _torch = None        # set by the first Context
 _codes = {}          # dtype -> CR_DTYPE_*
 
@@ -605,6 +606,14 @@ def _heads(name, t, dtype, shape, tokens, heads, dim):
     if sd != 1:
         raise ValueError(f"{name} must be contiguous in head_dim")
     return t.data_ptr(), st, sh
+
+
+def _no_gradient(*tensors):
+    """These calls are for serving: a gradient that is asked for would be lost without a word."""
+    for t in tensors:
+        if t.requires_grad and _torch.is_grad_enabled():
+            raise ValueError("the attention and cache calls have no gradient: call them under torch.no_grad(), or on "
+                             "detached tensors")
 
 
 class KVPages:
@@ -701,6 +710,8 @@ def kv_write(ctx: Context, pages: KVPages, layer: int, k, v, cu, seqs=None):
     """Write the keys and values [tokens, kv_heads, head_dim] of every sequence's last tokens into its pages:
     entry i's tokens are cu[i] .. cu[i+1]-1, its row seqs[i] (None: i) (cr_kv_write)."""
     n = max(cu.numel() - 1, 0)
+    if k.requires_grad or v.requires_grad:
+        _no_gradient(k, v)
     shape = k.shape
     T = shape[0]
     kp, kt, kh = _heads("k", k, pages.dtype, shape, None, pages.kv_heads, pages.head_dim)
@@ -716,6 +727,8 @@ _pack_attn = struct.Struct("@5P4IfI4Q").pack  # cr_attn_args
 
 def _attn_args(ctx: Context, q, dtype, shape, dim, n, cu, seqs, causal, scale, out, lse):
     """cr_attn_args as bytes, and the outputs; ``shape``: q.shape, ``cu``: address or 0."""
+    if q.requires_grad:
+        _no_gradient(q)
     qp, qt, qh = _heads("q", q, dtype, shape, None, None, dim)
     T, heads, dim = shape
     if out is None:
@@ -751,6 +764,8 @@ def attn_packed(ctx: Context, q, k, v, cu, cu_k=None, causal: bool = True, scale
         code = _dtype_code(dtype)
     if len(shape) != 3 or len(kshape) != 3:
         raise ValueError("q and k must be [tokens, heads, head_dim]")
+    if k.requires_grad or v.requires_grad:
+        _no_gradient(k, v)
     S, heads, dim = kshape
     kp, kt, kh = _heads("k", k, dtype, kshape, None if cu_k is not None else shape[0], None, shape[2])
     vp, vt, vh = _heads("v", v, dtype, v.shape, S, heads, dim)

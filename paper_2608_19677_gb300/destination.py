@@ -92,17 +92,19 @@ class Destination:
         return -(-tokens // self.pages.page)
 
     def _forward(self, tokens, cu, rows, groups=None):
-        """One pass of the model over new tokens that the rows' lengths already count."""
-        x = self.model.embed(tokens)
-        for layer in range(self.model.layers):
-            q, k, v = self.model.qkv(layer, x)
-            kv_write(self.ctx, self.pages, layer, k, v, cu, seqs=rows)
-            if groups is None:
-                out = attn_paged(self.ctx, q, self.pages, layer, cu, seqs=rows)
-            else:
-                out = attn_decode(self.ctx, q, self.pages, layer, seqs=rows, group_off=groups[0], shared=groups[1])
-            x = self.model.mix(layer, x, out)
-        return x
+        """One pass of the model, without gradients, over new tokens that the rows' lengths already count."""
+        import torch
+        with torch.no_grad():
+            x = self.model.embed(tokens)
+            for layer in range(self.model.layers):
+                q, k, v = self.model.qkv(layer, x)
+                kv_write(self.ctx, self.pages, layer, k, v, cu, seqs=rows)
+                if groups is None:
+                    out = attn_paged(self.ctx, q, self.pages, layer, cu, seqs=rows)
+                else:
+                    out = attn_decode(self.ctx, q, self.pages, layer, seqs=rows, group_off=groups[0], shared=groups[1])
+                x = self.model.mix(layer, x, out)
+            return x
 
     def _make_room(self, rows: int, pages: int, keep) -> None:
         """Idle prefixes leave, least recent first, until rows and pages are free; nothing changes if that is too few."""

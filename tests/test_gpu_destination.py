@@ -121,3 +121,13 @@ def test_calls_return_while_the_gpu_is_still_busy(P, own_stream):
     ctx.sync()
     ctx.close()
     assert not waited
+
+
+def test_a_model_whose_weights_want_gradients_is_served_without_them(P):
+    ctx, m = P.Context(0), model()
+    for w in (m.wq, m.wk, m.wv, m.wo):
+        for i in range(len(w)):
+            w[i] = torch.nn.Parameter(w[i])
+    m.exact = torch.no_grad()(m.exact)
+    assert serve(P, ctx, m, 3) < BOUND
+    ctx.close()

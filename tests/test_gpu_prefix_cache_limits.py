@@ -315,3 +315,27 @@ def test_no_keys_at_all_whatever_the_offsets_say(P, ctx, cu_k, causal):
     out, lse = P.attn_packed(ctx, q, none, none, ints([0, 4, 6]), cu_k=ints(cu_k), causal=causal, lse=True)
     ctx.sync()
     assert (out == 0).all() and (lse == -math.inf).all()
+
+
+def test_tensors_that_want_a_gradient_are_refused_where_gradients_are_recorded(P, ctx):
+    g = gen(81)
+    pg, _ = fill(P, ctx, g, 16, [20, 30], 2, 64, BF)
+    q, k, v = randn(g, 2, 8, 64), randn(g, 2, 2, 64), randn(g, 2, 2, 64)
+    cu = ints([0, 1, 2])
+    calls = [("q", lambda t: P.attn_packed(ctx, t, k, v, cu)), ("k", lambda t: P.attn_packed(ctx, q, t, v, cu)),
+             ("v", lambda t: P.attn_packed(ctx, q, k, t, cu)), ("q", lambda t: P.attn_paged(ctx, t, pg, 0, cu)),
+             ("q", lambda t: P.attn_decode(ctx, t, pg, 0)), ("k", lambda t: P.kv_write(ctx, pg, 0, t, v, cu)),
+             ("v", lambda t: P.kv_write(ctx, pg, 0, k, t, cu))]
+    for name, call in calls:
+        t = {"q": q, "k": k, "v": v}[name]
+        want = call(t)
+        asks = t.clone().requires_grad_()
+        before = ctx.launches
+        with pytest.raises(ValueError, match="gradient"):
+            call(asks)
+        assert ctx.launches == before
+        with torch.no_grad():
+            got = call(asks)
+        also = call(asks.detach())
+        ctx.sync()
+        assert want is None or (torch.equal(got, want) and torch.equal(also, want))
