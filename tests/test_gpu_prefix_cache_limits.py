@@ -339,3 +339,61 @@ def test_tensors_that_want_a_gradient_are_refused_where_gradients_are_recorded(P
         also = call(asks.detach())
         ctx.sync()
         assert want is None or (torch.equal(got, want) and torch.equal(also, want))
+
+
+# ---- lists of work that are longer than the plan kernel's shared memory (512 entries, blocks or groups) ----------------
+@pytest.mark.parametrize("hq,hkv,d,dtype,lens", [
+    (128, 1, 64, BF, [1203, 5]),                 # two tokens a block: 605 blocks of two entries
+    (16, 1, 128, HF, [9001]),                    # 563 blocks of one entry
+    (8, 2, 64, BF, None),                        # 1,500 entries
+    (28, 4, 128, HF, None),
+])
+@pytest.mark.parametrize("causal", [True, False])
+def test_long_lists_of_prompts(P, ctx, hq, hkv, d, dtype, lens, causal):
+    r = np.random.default_rng(hq)
+    lens = lens or [int(x) for x in r.integers(0, 40, 1500)]
+    g, cu = gen(hq + d), np.concatenate([[0], np.cumsum(lens)])
+    q, k, v = (randn(g, int(cu[-1]), h, d, dtype=dtype) for h in (hq, hkv, hkv))
+    out, lse = P.attn_packed(ctx, q, k, v, ints(cu), causal=causal, lse=True)
+    again = P.attn_packed(ctx, q, k, v, ints(cu), causal=causal)
+    ctx.sync()
+    assert torch.equal(out, again)
+    if len(lens) == 1:      # the first and the last rows, and some between
+        rows = [0, 1, 2, 3000, 3001, 8998, 8999, 9000]
+        for i in rows:
+            sees = i + 1 if causal else lens[0]
+            o, l, bo, bl = reference(q[i:i + 1], k[:sees], v[:sees], False, d ** -0.5)
+            assert ((out[i:i + 1].double() - o).abs() <= bo).all() and ((lse[i:i + 1].double() - l).abs() <= bl).all(), i
+        return
+    check(out, lse, [reference(q[a:b], k[a:b], v[a:b], causal, d ** -0.5) for a, b in zip(cu[:-1], cu[1:])], cu)
+
+
+def test_long_lists_of_suffixes(P, ctx):
+    r, g = np.random.default_rng(2), gen(91)
+    new = [int(x) for x in r.integers(0, 30, 900)]
+    lens = [n + int(x) for n, x in zip(new, r.integers(0, 200, 900))]
+    pg, kv = fill(P, ctx, g, 16, lens, 2, 64, BF)
+    rows = r.permutation(900)
+    cu = np.concatenate([[0], np.cumsum([new[i] for i in rows])])
+    q = randn(g, int(cu[-1]), 8, 64)
+    out, lse = P.attn_paged(ctx, q, pg, 0, ints(cu), seqs=ints(rows), lse=True)
+    ctx.sync()
+    check(out, lse, [reference(q[a:b], *kv[i], True, 0.125) for i, a, b in zip(rows, cu[:-1], cu[1:])], cu)
+
+
+@pytest.mark.parametrize("n,groups", [(1200, 0), (1200, 40), (1200, 512), (1300, 700), (700, 699)])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 64), (20, 1, 128)])
+def test_long_lists_of_single_tokens(P, ctx, n, groups, hq, hkv, d):
+    """Entries, and groups of none to many of them, on both sides of what the plan kernel keeps."""
+    r, g = np.random.default_rng(n + groups), gen(n + groups + d)
+    group = np.sort(r.integers(0, groups, n)) if groups else np.arange(n)
+    shared = [16 * int(x) for x in r.integers(0, 20, max(groups, 1))] if groups else [0] * n
+    lens = [shared[a] + int(x) for a, x in zip(group, r.integers(0, 150, n))]
+    pg, kv = fill(P, ctx, g, 16, lens, hkv, d, BF, shared=shared, group=list(group))
+    q = randn(g, n, hq, d)
+    kw = dict(group_off=ints(np.searchsorted(group, np.arange(groups + 1))), shared=ints(shared)) if groups else {}
+    out, lse = P.attn_decode(ctx, q, pg, 0, lse=True, **kw)
+    again = P.attn_decode(ctx, q, pg, 0, **kw)
+    ctx.sync()
+    assert torch.equal(out, again)
+    check(out, lse, [reference(q[i:i + 1], *kv[i], False, d ** -0.5) for i in range(n)], range(n + 1))
