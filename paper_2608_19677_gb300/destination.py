@@ -30,18 +30,18 @@ def _on_context_stream(call):
     """The call's work on the context's stream, in the current stream's order.  Lists and results are allocated there: a
     list that is dropped is not handed out again before the kernels that read it."""
     @functools.wraps(call)
-    def ordered(self, *args):
+    def ordered(self, *args, **kw):
         if not self.pages.lens.is_cuda:
-            return call(self, *args)
+            return call(self, *args, **kw)
         import torch
         mine, here = self.ctx.stream, torch.cuda.current_stream(self.pages.lens.device)
         if mine.cuda_stream == here.cuda_stream:
-            return call(self, *args)
+            return call(self, *args, **kw)
         mine.wait_stream(here)
-        _used_on(args, mine)
+        _used_on((args, list(kw.values())), mine)
         try:
             with torch.cuda.stream(mine):
-                result = call(self, *args)
+                result = call(self, *args, **kw)
             _used_on((result, self.pages.ref, self.pages.table), here)
             return result
         finally:

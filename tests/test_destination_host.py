@@ -239,3 +239,11 @@ def test_a_step_that_fails_gives_its_requests_up(serve):
         d.step(text(3, 2))
     assert not d.running and not d.kept and set(d.prefixes) == {4, 5} and len(d.free_rows) == 6
     assert d.free_pages == int((pool.ref == 0).sum()) == 64 - 4
+
+
+def test_arguments_may_be_named(serve):
+    d, _ = serve()
+    rows, _ = d.admit(requests=[(5, text(1, 40), 32)])
+    d.step(tokens=text(2, 1))
+    d.finish(rows=rows)
+    assert not d.running
