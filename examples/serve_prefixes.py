@@ -41,7 +41,7 @@ class TinyAttention:
                 (x @ self.wv[layer]).view(T, self.kv_heads, self.dim))
 
     def mix(self, layer, x, out):
-        return x + out.reshape(x.shape[0], -1) @ self.wo[layer]
+        return x + out.reshape(x.shape[0], self.heads * self.dim) @ self.wo[layer]
 
     def exact(self, tokens):
         """The whole sequence at once, in 64 bits."""

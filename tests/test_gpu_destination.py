@@ -131,3 +131,23 @@ def test_a_model_whose_weights_want_gradients_is_served_without_them(P):
     m.exact = torch.no_grad()(m.exact)
     assert serve(P, ctx, m, 3) < BOUND
     ctx.close()
+
+
+@pytest.mark.parametrize("own_stream", [False, True])
+def test_requests_without_tokens_of_their_own_and_steps_without_requests(P, own_stream):
+    from paper_2608_19677_gb300.destination import Destination
+    stream = torch.cuda.Stream() if own_stream else torch.cuda.current_stream()
+    ctx, m, g = P.Context(0, stream=stream), model(), gen(7)
+    d = Destination(ctx, P.KVPages.empty(64, 16, 8, 16, m.layers, m.kv_heads, m.dim), m)
+    t = torch.randint(0, 4096, (40,), generator=g, device=DEV)
+    rows, out = d.admit(requests=[(1, t, 40), (1, t[:33], 33)])
+    assert out.shape[0] == 0
+    new = torch.randint(0, 4096, (2,), generator=g, device=DEV)
+    out = d.step(tokens=new)
+    ctx.sync()
+    assert worst(out, m, [(torch.cat([t, new[:1]]), 1), (torch.cat([t[:33], new[1:]]), 1)]) < BOUND
+    d.finish(rows=rows)
+    assert d.step(new[:0]).shape[0] == 0
+    ctx.sync()
+    assert int((d.pages.ref > 0).sum()) == 3 == 64 - d.free_pages
+    ctx.close()
