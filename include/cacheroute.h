@@ -566,7 +566,8 @@ CR_API int cr_pages_compact(cr_ctx *ctx, const cr_kv_pages *pages, int32_t *d_re
  * h*k_head (d_v alike), strides multiples of 8, pointers 16-byte aligned.  Tokens
  * that fall outside their row, or into a page that other rows name too (as those of
  * a forked row do that could not be extended), are skipped and reported as CR_EINVAL
- * by the next blocking call.  Errors: CR_EINVAL, CR_ECUDA. */
+ * by the next blocking call: a row's tokens are written before it is forked, in
+ * every layer.  Errors: CR_EINVAL, CR_ECUDA. */
 CR_API int cr_kv_write(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t layer, const void *d_k, uint64_t k_token,
                        uint64_t k_head, const void *d_v, uint64_t v_token, uint64_t v_head, const int32_t *d_cu,
                        const int32_t *d_seqs, uint32_t n, uint32_t n_tokens);

@@ -708,7 +708,8 @@ def pages_compact(ctx: Context, pages: KVPages):
 
 def kv_write(ctx: Context, pages: KVPages, layer: int, k, v, cu, seqs=None):
     """Write the keys and values [tokens, kv_heads, head_dim] of every sequence's last tokens into its pages:
-    entry i's tokens are cu[i] .. cu[i+1]-1, its row seqs[i] (None: i) (cr_kv_write)."""
+    entry i's tokens are cu[i] .. cu[i+1]-1, its row seqs[i] (None: i) (cr_kv_write).  Pages that other rows name are
+    left alone: a row's tokens are written before it is forked."""
     n = max(cu.numel() - 1, 0)
     if k.requires_grad or v.requires_grad:
         _no_gradient(k, v)
