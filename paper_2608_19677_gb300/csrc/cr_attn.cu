@@ -527,8 +527,8 @@ struct walk {
 // on the other's, so the softmax has to be as short as a tile's two products (1,024 cycles each way):
 // a row belongs to two threads, 64 keys each, which exchange their maxima through shared memory, and
 // the product with v begins when half of the weights are there.
-// Measured (one GB300, 32/8 heads of 128, causal): 8,192 tokens 362 us, 1,519 TFLOP/s, tensor cores at work
-// in 71% of the cycles; about 2,650 cycles for a pair of tiles whose products take 2,048: scores to weights
+// Measured (one GB300, 32/8 heads of 128, causal): 8,192 tokens 366 us, 1,504 TFLOP/s, tensor cores at work
+// in 72% of the cycles; about 2,650 cycles for a pair of tiles whose products take 2,048: scores to weights
 // 1,250 cycles (exponentials half of them), hand-overs the rest.  Calls of milliseconds meet the power limit.
 template <int D>
 struct rows_cfg {
@@ -1239,7 +1239,7 @@ __global__ void __launch_bounds__(256)
 // 16 keys each of a tile of 64 that a fifth warp's copies bring, with the softmax state of the
 // rows in every warp, joined at the piece's end.  The next piece's queries are copied meanwhile.
 // Two CTAs an SM with 96 KB of copies in flight each; measured: 128 contexts of 4,160 tokens, 64/8 heads of
-// 128, pages of 16 tokens: 349 us, 6.1 TB/s (a copy runs at 6.8); pages of 64 tokens 2% less.
+// 128, pages of 16 tokens: 357 us a call, 6.1 TB/s (a copy runs at 6.8); pages of 64 tokens 2% less.
 template <int D>
 struct few_cfg {
     static constexpr int kChunks = D / 64;

@@ -7,7 +7,7 @@
 // (in shared memory) and of the chunk's words.  Both kernels read the counts of every page once
 // (4 bytes a page) and are bound by their launches until the pool has millions of pages; copies of
 // page data are 16 bytes a thread with four loads in flight, bound by memory (664 MB of pages moved in
-// 224 us, 6.0 TB/s; a thousand forks with tails of 8 tokens on average, 4 planes: 10 us).
+// 226 us, 6.0 TB/s; a thousand forks with tails of 8 tokens on average, 4 planes: 14 us with cold caches).
 #include "cr_internal.cuh"
 
 namespace {
