@@ -572,6 +572,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     const uint32_t sq = cr_smem(dyn), ring = sq + 2 * cfg::kTile;
     const uint32_t bar = sq + cfg::kBars;
     if (sq & 1023u) {  // the swizzled tiles begin at multiples of 1,024 bytes
+        cr_wait_previous();  // who waits for this kernel waits for those before it
         if (threadIdx.x == 0) atomicOr(A.status, CR_FLAG_INTERNAL);
         return;
     }

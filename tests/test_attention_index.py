@@ -75,3 +75,15 @@ def test_tiles_and_masks_of_the_longest_sequences(tmp_path):
         }
     }
     """)
+
+
+def test_no_kernel_returns_before_it_has_waited_for_the_one_before():
+    """A kernel's end stands for the end of all before it: whoever waits for it counts on that."""
+    for name in ("cr_attn.cu", "cr_pages.cu"):
+        text = open(os.path.join(CSRC, name)).read()
+        kernels = text.split("__global__ ")[1:]
+        assert len(kernels) >= 5
+        for k in kernels:
+            head, body = k.split("{", 1)
+            before = body.split("cr_wait_previous();", 1)
+            assert len(before) == 2 and "return" not in before[0], head
