@@ -519,9 +519,27 @@ CR_API int cr_replay_import_state(cr_ctx *ctx, cr_replay *rp, uint32_t rep, uint
  * heads are dense in either order (token_stride = kv_heads*head_dim and
  * head_stride = head_dim, or head_stride = page*head_dim and token_stride =
  * head_dim).  n_pages * page < 2^31, n_seqs * max_pages < 2^40.
+ *
+ * A pool in 8 bits (CR_DTYPE_*_E4M3): keys, values and queries of the calls have
+ * the 16-bit type, the cache holds them as e4m3 numbers (1 byte an element) with
+ * one power of two for every `block` tokens of a page and head, which multiplies
+ * them:
+ *   d_scale  float[layers][2][n_pages][kv_heads][page/block], dense (keys: 0, values: 1)
+ * cr_kv_write and cr_kv_append choose the power: the smallest 2^e for which
+ * 448 * 2^e reaches the block's largest magnitude, e in -100..120 for bfloat16 and
+ * -15..8 for half, so that every number times its power is one of the 16-bit type
+ * (at the largest e numbers stay within 240).  Tokens that are added to a block may raise its
+ * power; the tokens before them in the block are then rounded again, which changes
+ * only those that become subnormal.  It is never lowered while the block is in use;
+ * the call that writes a block's first token chooses it anew.  An infinity, or what
+ * would be one in the 16-bit type, is held as not-a-number and does not count for
+ * the power.  head_dim a multiple of 16, 16..128, strides multiples of 16 elements;
+ * block a power of two, 8..page.
  */
 #define CR_DTYPE_BF16 0 /* bfloat16 */
 #define CR_DTYPE_FP16 1 /* IEEE half */
+#define CR_DTYPE_BF16_E4M3 2 /* bfloat16, held in 8 bits */
+#define CR_DTYPE_FP16_E4M3 3 /* half, held in 8 bits */
 
 typedef struct {
     void *d_cache;
@@ -529,6 +547,9 @@ typedef struct {
     uint32_t dtype; /* CR_DTYPE_* */
     uint32_t layers, n_pages, page, kv_heads, head_dim, n_seqs, max_pages;
     uint64_t layer_stride, kv_stride, page_stride, token_stride, head_stride; /* elements */
+    /* read for CR_DTYPE_*_E4M3 only */
+    float *d_scale;
+    uint32_t block, reserved; /* reserved: 0 */
 } cr_kv_pages;
 
 /* The rows d_seqs[n] get pages for d_add[i] (>= 0) more tokens each, and are that
@@ -571,6 +592,67 @@ CR_API int cr_pages_compact(cr_ctx *ctx, const cr_kv_pages *pages, int32_t *d_re
 CR_API int cr_kv_write(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t layer, const void *d_k, uint64_t k_token,
                        uint64_t k_head, const void *d_v, uint64_t v_token, uint64_t v_head, const int32_t *d_cu,
                        const int32_t *d_seqs, uint32_t n, uint32_t n_tokens);
+
+/* ==== rotary positions ================================================== */
+/*
+ * Pair i of the first 2*pairs elements of a head, at position p, turns by the angle
+ * p * f_i:   a' = s (a cos - b sin),   b' = s (b cos + a sin);
+ * the elements behind are left as they are.
+ *   d_turn   uint64[pairs] (device): f_i as the share of a full turn, times 2^64 and
+ *            rounded (f_i / 2 pi * 2^64 mod 2^64).  p * d_turn[i] mod 2^64 is then
+ *            the angle, exact to p * 2^-65 turns however far p is; its top 32 bits
+ *            are used.
+ *   layout   CR_ROTARY_HALF: a, b = x[i], x[pairs + i]
+ *            CR_ROTARY_PAIRS: a, b = x[2i], x[2i + 1]
+ *   inverse  != 0: turn by -p f_i (times s): the gradient of the forward call
+ *   scale    s, finite
+ * Computed in 32 bits, rounded once.  pairs a multiple of 4, 2*pairs <= head_dim.
+ */
+#define CR_ROTARY_HALF 0
+#define CR_ROTARY_PAIRS 1
+
+typedef struct {
+    const uint64_t *d_turn;
+    uint32_t pairs, layout, inverse;
+    float scale;
+} cr_rotary;
+
+/* Rotates packed tokens: token t, head a of d_x at element t*x_token + a*x_head (d_out
+ * alike; 16-byte aligned, strides multiples of 8), head_dim a multiple of 8, 8..128.
+ * d_out may be d_x with the same strides; else they do not overlap.
+ *   d_pos   int32[n_tokens]: position of each token (may be negative)
+ * Errors: CR_EINVAL, CR_ECUDA. */
+CR_API int cr_rope(cr_ctx *ctx, const cr_rotary *rotary, uint32_t dtype, const void *d_x, uint64_t x_token, uint64_t x_head,
+                   void *d_out, uint64_t o_token, uint64_t o_head, uint32_t n_tokens, uint32_t heads, uint32_t head_dim,
+                   const int32_t *d_pos);
+
+/* cr_kv_write with the new tokens' queries and keys rotated to their positions in
+ * their rows (the first token of a row is at 0): keys go rotated into the pages
+ * (rounded once, to the pool's numbers), queries [n_tokens][q_heads] to d_q_out
+ * (strides as cr_rope's; it may be d_q).  q_heads = 0: no queries.  Tokens whose page
+ * other rows name have their queries rotated all the same; queries of tokens that
+ * fall outside their row become zeros.  A row that stands in the list twice is
+ * written by the first of its entries (CR_EINVAL by the next blocking call; its
+ * queries are rotated in every entry).  Errors: CR_EINVAL, CR_ENOMEM, CR_ECUDA. */
+typedef struct {
+    const void *d_q;
+    void *d_q_out;
+    const void *d_k, *d_v;
+    uint64_t q_token, q_head, o_token, o_head, k_token, k_head, v_token, v_head; /* elements */
+    const int32_t *d_cu, *d_seqs; /* as cr_kv_write's */
+    uint32_t n, n_tokens, q_heads, reserved; /* reserved: 0 */
+} cr_append_args;
+CR_API int cr_kv_append(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t layer, const cr_rotary *rotary,
+                        const cr_append_args *args);
+
+/* Tokens of cached rows back, in the 16-bit type: those of entry i are tokens d_cu[i] ..
+ * d_cu[i+1]-1 of d_k and d_v (strides as cr_kv_write's), and tokens d_start[i] .. of row
+ * d_seqs[i] (NULL: of row i); d_start NULL: the row's last ones.  Tokens that fall
+ * outside their row become zeros (CR_EINVAL by the next blocking call).  Keys come as
+ * they are held: rotated, where they were written so.  Errors: CR_EINVAL, CR_ECUDA. */
+CR_API int cr_kv_read(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t layer, void *d_k, uint64_t k_token, uint64_t k_head,
+                      void *d_v, uint64_t v_token, uint64_t v_head, const int32_t *d_cu, const int32_t *d_seqs,
+                      const int32_t *d_start, uint32_t n, uint32_t n_tokens);
 
 /* ==== attention ======================================================== */
 /*

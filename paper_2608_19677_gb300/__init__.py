@@ -17,7 +17,10 @@ fails loudly otherwise.
 What a destination does with the prefixes it holds:
 
   KVPages         pages of a key/value cache, and pages_extend, pages_fork, pages_free, pages_compact
+  Rotary, rope    rotary positions of queries and keys          (cr_rope)
   kv_write        keys and values of new tokens -> pages        (cr_kv_write)
+  kv_append       the same, queries and keys rotated            (cr_kv_append)
+  kv_read         pages -> keys and values                      (cr_kv_read)
   attn_packed     attention over whole prompts                  (cr_attn_packed)
   attn_paged      attention over cached pages                   (cr_attn_paged)
   attn_decode     of single tokens that share prefixes          (cr_attn_decode)
@@ -25,6 +28,7 @@ What a destination does with the prefixes it holds:
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 import struct
 from typing import List, Optional, Sequence
@@ -53,7 +57,7 @@ EXPORTS = ("cr_create", "cr_destroy", "cr_set_stream", "cr_sync", "cr_last_error
            "cr_profile_enable", "cr_profile_read", "cr_plan_import", "cr_replay_import_state",
            "cr_replay_input_create", "cr_replay_input_destroy", "cr_replay_partition", "cr_replay_simulate",
            "cr_pages_extend", "cr_pages_fork", "cr_pages_free", "cr_pages_compact", "cr_kv_write",
-           "cr_attn_packed", "cr_attn_paged", "cr_attn_decode")
+           "cr_attn_packed", "cr_attn_paged", "cr_attn_decode", "cr_rope", "cr_kv_append", "cr_kv_read")
 PROF = {"hash": 0, "plan": 1, "route_cand": 2, "route_resolve": 3, "partition": 4, "replay": 5}
 CR_NOALLOC_MAX_KEYS = 65536
 
@@ -85,7 +89,13 @@ class KVPagesDesc(C.Structure):
     _fields_ = ([(f, C.c_void_p) for f in ("d_cache", "d_ref", "d_table", "d_lens")] +
                 [(f, C.c_uint32) for f in ("dtype", "layers", "n_pages", "page", "kv_heads", "head_dim", "n_seqs",
                                            "max_pages")] +
-                [(f, C.c_uint64) for f in ("layer_stride", "kv_stride", "page_stride", "token_stride", "head_stride")])
+                [(f, C.c_uint64) for f in ("layer_stride", "kv_stride", "page_stride", "token_stride", "head_stride")] +
+                [("d_scale", C.c_void_p), ("block", C.c_uint32), ("reserved", C.c_uint32)])
+
+
+class RotaryDesc(C.Structure):
+    _fields_ = [("d_turn", C.c_void_p), ("pairs", C.c_uint32), ("layout", C.c_uint32), ("inverse", C.c_uint32),
+                ("scale", C.c_float)]
 
 
 class Replica(C.Structure):
@@ -153,6 +163,9 @@ def lib() -> C.CDLL:
         "cr_pages_free": ([vp, vp, vp, u32], i32),
         "cr_pages_compact": ([vp, vp, vp, vp, vp, vp], i32),
         "cr_kv_write": ([vp, vp, u32, vp, u64, u64, vp, u64, u64, vp, vp, u32, u32], i32),
+        "cr_rope": ([vp, vp, u32, vp, u64, u64, vp, u64, u64, u32, u32, u32, vp], i32),
+        "cr_kv_append": ([vp, vp, u32, vp, vp], i32),
+        "cr_kv_read": ([vp, vp, u32, vp, u64, u64, vp, u64, u64, vp, vp, vp, u32, u32], i32),
         "cr_attn_packed": ([vp, vp, u32, u32, u32, vp, u64, u64, vp, u64, u64, vp, u32], i32),
         "cr_attn_paged": ([vp, vp, u32, vp], i32),
         "cr_attn_decode": ([vp, vp, u32, vp, vp, vp, u32], i32),
@@ -622,9 +635,13 @@ class KVPages:
     ``cache`` [layers, 2, n_pages, page, kv_heads, head_dim] (keys, values; bfloat16 or float16; a page's tokens and
     heads may be stored in either order), ``ref`` int32[n_pages] counts the table entries that name a page (0: free),
     ``table`` int32[n_seqs, max_pages] lists each sequence's pages (-1 behind them), ``lens`` int32[n_seqs] its
-    tokens.  ``KVPages.empty`` makes an empty pool."""
+    tokens.  ``KVPages.empty`` makes an empty pool.
 
-    def __init__(self, cache, ref, table, lens):
+    In 8 bits ``cache`` is float8_e4m3fn, ``scale`` float32 [layers, 2, n_pages, kv_heads, page / block] holds the power
+    of two of every block of tokens and head, and ``dtype`` (bfloat16 unless given) is the type of the keys, values and
+    queries of the calls."""
+
+    def __init__(self, cache, ref, table, lens, scale=None, dtype=None):
         _load_torch()
         if cache.dim() != 6 or cache.shape[1] != 2 or not cache.is_cuda or cache.stride(5) != 1:
             raise ValueError("cache must be a CUDA tensor [layers, 2, n_pages, page, kv_heads, head_dim]")
@@ -634,28 +651,49 @@ class KVPages:
         if table.dim() != 2:
             raise ValueError("table must have two dimensions")
         _int32("lens", lens, table.shape[0])
-        self.cache, self.ref, self.table, self.lens = cache, ref, table, lens
+        self.block = 0
+        if cache.dtype is _torch.float8_e4m3fn:
+            if scale is None:
+                raise ValueError("a cache in 8 bits needs its blocks' scales")
+            _need_cuda("scale", scale, _torch.float32)
+            blocks = scale.shape[-1] if scale.dim() == 5 else 0
+            if not blocks or page % blocks or tuple(scale.shape[:4]) != (layers, 2, n_pages, heads):
+                raise ValueError(f"scale must have shape {(layers, 2, n_pages, heads)} and page / block, got {tuple(scale.shape)}")
+            self.block = page // blocks
+            dtype = dtype or _torch.bfloat16
+        elif scale is not None or (dtype is not None and dtype is not cache.dtype):
+            raise ValueError("scale, and a type of its own, are a cache's in 8 bits (float8_e4m3fn)")
+        self.cache, self.ref, self.table, self.lens, self.scale = cache, ref, table, lens, scale
         self.layers, self.n_pages, self.page, self.kv_heads, self.head_dim = layers, n_pages, page, heads, dim
-        self.dtype = cache.dtype
-        self._code = _dtype_code(cache.dtype)
+        self.dtype = dtype or cache.dtype
+        self._code = _dtype_code(self.dtype) + (2 if self.block else 0)
         self._bind()
 
     def _bind(self):
         st = self.cache.stride()
         d = KVPagesDesc(_ptr(self.cache), _ptr(self.ref), _ptr(self.table), _ptr(self.lens), self._code, self.layers,
                         self.n_pages, self.page, self.kv_heads, self.head_dim, self.table.shape[0],
-                        self.table.shape[1], st[0], st[1], st[2], st[3], st[4])
+                        self.table.shape[1], st[0], st[1], st[2], st[3], st[4], _ptr(self.scale), self.block, 0)
         self._desc, self._addr = d, C.addressof(d)
 
     @classmethod
     def empty(cls, n_pages: int, page: int, n_seqs: int, max_pages: int, layers: int, kv_heads: int, head_dim: int,
-              dtype=None, device="cuda"):
+              dtype=None, device="cuda", bits: int = 16, block: Optional[int] = None):
+        """``bits``: 16, or 8: then with a scale for every ``block`` tokens (16 or the page, whichever is less) and head."""
         torch = _load_torch()
-        cache = torch.zeros((layers, 2, n_pages, page, kv_heads, head_dim), dtype=dtype or torch.bfloat16,
-                            device=device)
+        if bits not in (8, 16) or (block is not None and bits != 8):
+            raise ValueError("bits is 16 or 8; only a cache in 8 bits has blocks")
+        cache = torch.zeros((layers, 2, n_pages, page, kv_heads, head_dim), device=device,
+                            dtype=torch.float8_e4m3fn if bits == 8 else dtype or torch.bfloat16)
+        scale = None
+        if bits == 8:
+            block = block or min(16, page)
+            if not 8 <= block <= page or page % block:
+                raise ValueError(f"blocks of {block} tokens in pages of {page}: a power of two, 8 to the page")
+            scale = torch.ones((layers, 2, n_pages, kv_heads, page // block), dtype=torch.float32, device=device)
         return cls(cache, torch.zeros(n_pages, dtype=torch.int32, device=device),
                    torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device),
-                   torch.zeros(n_seqs, dtype=torch.int32, device=device))
+                   torch.zeros(n_seqs, dtype=torch.int32, device=device), scale=scale, dtype=dtype)
 
     def replace(self, ref, table):
         """Take the counts and tables that ``pages_compact`` gave (the cache's pages have moved already).  The old ones
@@ -721,6 +759,141 @@ def kv_write(ctx: Context, pages: KVPages, layer: int, k, v, cu, seqs=None):
                            None if seqs is None else _int32("seqs", seqs, n), n, T)
     if st:
         ctx.check(st, "cr_kv_write")
+
+
+class Rotary:
+    """Rotary positions: pair i of the first ``dims`` elements of a head turns by position * f_i, f_i = base^(-2i/dims).
+
+    ``layout``: "half" (pairs x[i], x[dims/2 + i]) or "interleaved" (x[2i], x[2i + 1]).  ``scaling`` stretches the
+    positions ``factor`` times: "linear" divides every f_i; "ntk" takes the base times factor^(dims/(dims - 2)); "ramp"
+    leaves pairs that turn more than ``fast`` times within ``original`` tokens, divides those that turn less than ``slow``
+    times, and goes from one to the other linearly in the turns, and multiplies the rotated elements by
+    0.1 ln(factor) + 1 (Peng et al., arXiv 2309.00071).  ``scale`` gives that multiplier instead.  ``frequencies`` gives
+    the f_i (radians a token, ``dims`` / 2 of them) instead of the base.  ``inverse()`` turns back."""
+
+    def __init__(self, dims: int, base: float = 10000.0, layout: str = "half", scaling: Optional[str] = None,
+                 factor: float = 1.0, original: int = 0, slow: float = 1.0, fast: float = 32.0,
+                 scale: Optional[float] = None, frequencies: Optional[Sequence[float]] = None, device="cuda"):
+        torch = _load_torch()
+        if dims < 8 or dims % 8 or dims > 128:
+            raise ValueError(f"{dims} rotated elements: a multiple of 8, 8..128")
+        if layout not in ("half", "interleaved"):
+            raise ValueError(f"layout {layout!r}: half or interleaved")
+        if scaling not in (None, "linear", "ntk", "ramp"):
+            raise ValueError(f"scaling {scaling!r}: linear, ntk or ramp")
+        if not (base > 0 and factor > 0) or not (math.isfinite(base) and math.isfinite(factor)):
+            raise ValueError("base and factor must be positive")
+        if frequencies is None:
+            if scaling == "ntk":
+                base *= factor ** (dims / (dims - 2))
+            f = [base ** (-2.0 * i / dims) for i in range(dims // 2)]
+        else:
+            f = [float(x) for x in frequencies]
+            if scaling == "ntk":
+                raise ValueError("ntk scaling changes the base: give frequencies or that")
+            if len(f) != dims // 2 or not all(map(math.isfinite, f)):
+                raise ValueError(f"{len(f)} frequencies for {dims // 2} pairs")
+        if scaling == "linear":
+            f = [x / factor for x in f]
+        elif scaling == "ramp":
+            if original <= 0 or not fast > slow:
+                raise ValueError("a ramp needs the original length, and fast > slow")
+            keep = [min(1.0, max(0.0, (original * abs(x) / (2 * math.pi) - slow) / (fast - slow))) for x in f]
+            f = [x * k + x / factor * (1.0 - k) for x, k in zip(f, keep)]
+            if scale is None:
+                scale = 0.1 * math.log(factor) + 1.0 if factor > 1.0 else 1.0
+        scale = 1.0 if scale is None else float(scale)
+        if not abs(scale) <= 3.4028234663852886e38:
+            raise ValueError("scale must be finite")
+        self.dims, self.layout, self.scale, self.frequencies = dims, layout, scale, f
+        # shares of a full turn, times 2^64; position times share drops whole turns by itself
+        turn = [round(x / (2 * math.pi) * 2.0 ** 64) % 2 ** 64 for x in f]
+        self.turn = torch.tensor([t - 2 ** 64 if t >= 2 ** 63 else t for t in turn], dtype=torch.int64, device=device)
+        self._bind(0)
+
+    def _bind(self, inverse: int):
+        d = RotaryDesc(_ptr(self.turn), self.dims // 2, 0 if self.layout == "half" else 1, inverse, self.scale)
+        self._desc, self._addr, self._inverse = d, C.addressof(d), inverse
+
+    def inverse(self) -> "Rotary":
+        """Turns by the opposite angles (and multiplies by the same scale): the gradient of the rotation."""
+        r = object.__new__(Rotary)
+        r.dims, r.layout, r.scale, r.frequencies, r.turn = self.dims, self.layout, self.scale, self.frequencies, self.turn
+        r._bind(1 - self._inverse)
+        return r
+
+
+def rope(ctx: Context, x, rotary: Rotary, pos, out=None):
+    """Rotate tokens x [tokens, heads, head_dim] (bfloat16 or float16) to positions ``pos`` int32[tokens] (cr_rope).
+    ``out`` may be ``x``."""
+    dtype, shape = x.dtype, x.shape
+    code = _dtype_code(dtype)
+    if x.requires_grad or (out is not None and out.requires_grad):
+        _no_gradient(x, *(() if out is None else (out,)))
+    xp, xt, xh = _heads("x", x, dtype, shape, None, None, None)
+    T, heads, dim = shape
+    if out is None:
+        out = _out(ctx, shape, x, dtype)
+    op, ot, oh = _heads("out", out, dtype, out.shape, T, heads, dim)
+    st = lib().cr_rope(ctx._h, rotary._addr, code, xp, xt, xh, op, ot, oh, T, heads, dim, _int32("pos", pos, T))
+    if st:
+        ctx.check(st, "cr_rope")
+    return out
+
+
+_pack_append = struct.Struct("@4P8Q2P4I").pack  # cr_append_args
+
+
+def kv_append(ctx: Context, pages: KVPages, layer: int, q, k, v, rotary: Rotary, cu, seqs=None, out=None):
+    """``kv_write`` with queries and keys rotated to the tokens' positions in their rows (cr_kv_append): returns the
+    rotated queries [tokens, heads, head_dim] (``out`` may be ``q``; ``q`` None: keys and values only)."""
+    n = max(cu.numel() - 1, 0)
+    if k.requires_grad or v.requires_grad or (q is not None and q.requires_grad):
+        _no_gradient(k, v, *(() if q is None else (q,)))
+    dtype, dim = pages.dtype, pages.head_dim
+    shape = k.shape
+    T = shape[0]
+    kp, kt, kh = _heads("k", k, dtype, shape, None, pages.kv_heads, dim)
+    vp, vt, vh = _heads("v", v, dtype, v.shape, T, pages.kv_heads, dim)
+    qp = qt = qh = op = ot = oh = heads = 0
+    if q is not None:
+        qp, qt, qh = _heads("q", q, dtype, q.shape, T, None, dim)
+        heads = q.shape[1]
+        if out is None:
+            out = _out(ctx, q.shape, q, dtype)
+        op, ot, oh = _heads("out", out, dtype, out.shape, T, heads, dim)
+    elif out is not None:
+        raise ValueError("out without queries")
+    a = _pack_append(qp, op, kp, vp, qt, qh, ot, oh, kt, kh, vt, vh, _int32("cu", cu),
+                     0 if seqs is None else _int32("seqs", seqs, n), n, T, heads, 0)
+    st = lib().cr_kv_append(ctx._h, pages._addr, layer, rotary._addr, a)
+    if st:
+        ctx.check(st, "cr_kv_append")
+    return out
+
+
+def kv_read(ctx: Context, pages: KVPages, layer: int, cu, seqs=None, start=None, tokens: Optional[int] = None, out=None):
+    """Keys and values of cached tokens, [tokens, kv_heads, head_dim] each (cr_kv_read): entry i's are cu[i] .. cu[i+1]-1
+    of them, and tokens start[i] .. of row seqs[i] (None: the row's last ones; row i).  ``tokens``: cu's last value, which
+    is read from the GPU where neither it nor ``out`` (a pair of tensors) is given."""
+    n = max(cu.numel() - 1, 0)
+    if out is None:
+        if tokens is None:
+            tokens = int(cu[-1]) if n else 0
+        shape = (tokens, pages.kv_heads, pages.head_dim)
+        out = _out(ctx, shape, pages.cache, pages.dtype), _out(ctx, shape, pages.cache, pages.dtype)
+    k, v = out
+    if k.requires_grad or v.requires_grad:
+        _no_gradient(k, v)
+    kp, kt, kh = _heads("k", k, pages.dtype, k.shape, tokens, pages.kv_heads, pages.head_dim)
+    T = k.shape[0]
+    vp, vt, vh = _heads("v", v, pages.dtype, v.shape, T, pages.kv_heads, pages.head_dim)
+    st = lib().cr_kv_read(ctx._h, pages._addr, layer, kp, kt, kh, vp, vt, vh, _int32("cu", cu),
+                          None if seqs is None else _int32("seqs", seqs, n),
+                          None if start is None else _int32("start", start, n), n, T)
+    if st:
+        ctx.check(st, "cr_kv_read")
+    return k, v
 
 
 _pack_attn = struct.Struct("@5P4IfI4Q").pack  # cr_attn_args

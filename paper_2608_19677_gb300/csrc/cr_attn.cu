@@ -19,7 +19,7 @@
 #include <math.h>
 
 #include "cr_attn_index.cuh"
-#include "cr_internal.cuh"
+#include "cr_pages.cuh"
 #include "cr_tensor.cuh"
 
 namespace {
@@ -405,6 +405,9 @@ struct attn_in {
     uint32_t *status;
     uint32_t own_list;     // k_attn_few, its join: every CTA makes the list of work itself, from
     plan_in plan;
+    // keys and values in 8 bits: their blocks' scales in this layer, [n_pages][kv_heads][1 << nb_log2]
+    const float *k_scale, *v_scale;
+    uint32_t block_log2, nb_log2, n_pages;
 };
 
 // A short list of single tokens: a warp makes it in every CTA, a token a lane, which saves the plan kernel's launch and
@@ -530,19 +533,26 @@ struct walk {
 // Measured (one GB300, 32/8 heads of 128, causal): 8,192 tokens 366 us, 1,504 TFLOP/s, tensor cores at work
 // in 72% of the cycles; about 2,650 cycles for a pair of tiles whose products take 2,048: scores to weights
 // 1,250 cycles (exponentials half of them), hand-overs the rest.  Calls of milliseconds meet the power limit.
-template <int D>
+template <int D, bool E8>
 struct rows_cfg {
     static constexpr int kChunks = D / 64;               // 64 elements: a 128-byte row
     static constexpr int kTile = kRowsTile * D * 2;      // bytes of 128 rows
-    static constexpr int kStages = D == 128 ? 5 : 10;    // of a tile's keys or values
-    // after the tiles: a value per (tile, half, row), pieces, barriers, two words
-    static constexpr int kXch = (2 + kStages) * kTile, kPieces = kXch + 4 * kRowsTile * 4, kBars = kPieces + 2 * 48;
-    static constexpr int kSmem = kBars + 8 * (26 + 2 * kStages) + 16;
+    static constexpr int kStages = (D == 128 ? 5 : 10) - (E8 ? D == 128 ? 1 : 2 : 0);  // of a tile's keys or values
+    static constexpr int kCodes = E8 ? (D == 128 ? 2 : 6) : 0;  // tiles as they come, in 8 bits
+    static constexpr int kCodeTile = kRowsTile * D;
+    // after the tiles: a value per (tile, half, row), pieces, barriers, scales of 16 groups of eight keys, two words
+    static constexpr int kCode0 = (2 + kStages) * kTile, kXch = kCode0 + kCodes * kCodeTile;
+    static constexpr int kPieces = kXch + 4 * kRowsTile * 4, kBars = kPieces + 2 * 48;
+    static constexpr int kScales = kBars + 8 * (26 + 2 * kStages + 2 * kCodes);
+    static constexpr int kSmem = kScales + 64 * kCodes + 16;
     static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
 };
 // Warps 0-15: softmax (tile, half of the keys, 32 rows); 16: products; 17: copies; 18, 19 make the
 // warpgroup whole, whose registers go to the softmax threads: 512 x 104 + 128 x 64 = 640 x 96.
 constexpr int kRowsThreads = 640;
+// Keys and values in 8 bits: warps 18 and 19 make 16-bit tiles of them, times their blocks' powers of two (exact in
+// the 16-bit type), and zeros of what is behind the sequence; the rest is the same.
+constexpr int kRowsWiden = 2;
 
 enum { B_QFULL, B_QEMPTY, B_DONE, B_SFULL, B_PREADY = B_SFULL + 2, B_OFULL = B_PREADY + 4, B_OEMPTY = B_OFULL + 2,
        B_PFULL = B_OEMPTY + 2, B_PEMPTY = B_PFULL + 2, B_LREAD = B_PEMPTY + 2, B_FULL = B_LREAD + 8 };
@@ -556,12 +566,12 @@ struct rows_piece {
 };
 static_assert(sizeof(rows_piece) == 48, "shared memory of the pieces");
 
-template <int D, bool BF16>
+template <int D, bool BF16, bool E8>
 __global__ void __launch_bounds__(kRowsThreads, 1)
     k_attn_rows(const __grid_constant__ attn_in A, const __grid_constant__ CUtensorMap map_q,
                 const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
 {
-    using cfg = rows_cfg<D>;
+    using cfg = rows_cfg<D, E8>;
     static_assert(B_FULL <= 26, "barriers");
     extern __shared__ __align__(1024) unsigned char dyn[];
     volatile rows_piece *piece = reinterpret_cast<volatile rows_piece *>(dyn + cfg::kPieces);
@@ -579,6 +589,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
 #define BAR(i) (bar + 8u * (uint32_t)(i))
 #define FULL(s) BAR(B_FULL + (s))
 #define EMPTY(s) BAR(B_FULL + cfg::kStages + (s))
+#define CODES(s) BAR(B_FULL + 2 * cfg::kStages + (s))
+#define TAKEN(s) BAR(B_FULL + 2 * cfg::kStages + cfg::kCodes + (s))
 
     if (threadIdx.x == 32) {
         cr_tma_prefetch_map(&map_q);
@@ -597,12 +609,16 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             cr_bar_init(BAR(B_OFULL + x), 1);
             cr_bar_init(BAR(B_OEMPTY + x), 8);
             cr_bar_init(BAR(B_PFULL + x), 1);
-            cr_bar_init(BAR(B_PEMPTY + x), 17);
+            cr_bar_init(BAR(B_PEMPTY + x), E8 ? 17 + kRowsWiden : 17);
         }
         for (int i = 0; i < 8; ++i) cr_bar_init(BAR(B_LREAD + i), 2);
         for (int s = 0; s < cfg::kStages; ++s) {
-            cr_bar_init(FULL(s), 1);
+            cr_bar_init(FULL(s), E8 ? kRowsWiden : 1);
             cr_bar_init(EMPTY(s), 1);
+        }
+        for (int s = 0; E8 && s < cfg::kCodes; ++s) {
+            cr_bar_init(CODES(s), 1 + 16);  // the copies of the tile, and of its 16 scales
+            cr_bar_init(TAKEN(s), kRowsWiden);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -669,6 +685,38 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             const uint32_t box = lane & (boxes - 1), ch = lane / boxes;
             const uint32_t at = ch * (kRowsTile * 128) + ((box << A.box_log2) * 128);
             const int32_t *row = A.paged ? A.table + (uint64_t)w.k.kbase * A.max_pages : nullptr;
+            if constexpr (E8) {
+                // lane: group of eight keys, whose scale it brings; lanes at a box' first group bring the box
+                const uint32_t group = lane & 15;
+                auto page_of = [&](uint32_t t) {  // n_pages: none
+                    const uint32_t at = t * kRowsTile + group * 8;
+                    return t < w.t1 && (int)at < w.k.klen ? (uint32_t)row[at >> A.page_log2] : A.n_pages;
+                };
+                uint32_t next = page_of(w.t0);
+                for (uint32_t t = w.t0; t < w.t1; ++t) {
+                    const uint32_t key = t * kRowsTile + group * 8, in_page = key & ((1u << A.page_log2) - 1);
+                    const uint32_t page = next;
+                    next = page_of(t + 1);
+                    const bool on = lane < 16 && page < A.n_pages, brings = on && (group * 8 & (A.box_rows - 1)) == 0;
+                    const uint32_t bytes = __popc(__ballot_sync(~0u, brings)) * A.box_rows * D;
+                    const uint64_t scale = on ? (((uint64_t)page * A.kv_heads + w.h) << A.nb_log2) + (in_page >> A.block_log2) : 0;
+#pragma unroll
+                    for (int v = 0; v < 2; ++v) {
+                        if (!cr_bar_wait(TAKEN(stage), phase ^ 1, &gave_up)) goto out;
+                        if (lane == 0) cr_bar_expect(CODES(stage), bytes);
+                        __syncwarp();
+                        if (brings)
+                            cr_tma_load(sq + cfg::kCode0 + stage * cfg::kCodeTile + group * 8 * D, v ? &map_v : &map_k, CODES(stage), 0,
+                                        (int)in_page, (int)w.h, (int)page);
+                        if (lane < 16)
+                            cr_copy_word(sq + cfg::kScales + stage * 64 + group * 4, (v ? A.v_scale : A.k_scale) + scale, on, CODES(stage));
+                        if (++stage == cfg::kCodes) {
+                            stage = 0;
+                            phase ^= 1;
+                        }
+                    }
+                }
+            } else
             for (uint32_t t = w.t0; t < w.t1; ++t) {
                 const int key = (int)(t * kRowsTile + (box << A.box_log2));
                 // packed keys come as one box; its rows behind the sequence are never used
@@ -785,6 +833,65 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         }
         cr_tc_commit(BAR(B_DONE), me);  // the shared memory is in use until the last product has ended
         cr_bar_wait(BAR(B_DONE), 0, &gave_up);
+    } else if (E8 && warp >= 18) {
+        // ---- 16-bit tiles ----
+        uint32_t stage = 0, phase = 0, code = 0, cphase = 0;
+        for (;; ++pieces) {
+            if (!cr_bar_wait(BAR(B_PFULL + (pieces & 1)), (pieces >> 1) & 1, &gave_up)) goto out;
+            const volatile rows_piece *p = piece + (pieces & 1);
+            const int n = p->n;
+            int left = p->klen - p->t0 * kRowsTile;  // keys from the tile's first on
+            __syncwarp();
+            if (lane == 0) cr_bar_arrive(BAR(B_PEMPTY + (pieces & 1)));
+            if (n == 0) break;
+            for (int j = 0; j < 2 * n; ++j) {
+                if (!cr_bar_wait(CODES(code), cphase, &gave_up)) goto out;
+                if (!cr_bar_wait(EMPTY(stage), phase ^ 1, &gave_up)) goto out;
+#pragma unroll 1
+                for (uint32_t r = (warp - 18) * 32 + lane; r < (uint32_t)kRowsTile; r += 32 * kRowsWiden) {
+                    float scale;  // 0: no page
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(scale) : "r"(sq + cfg::kScales + code * 64 + (r >> 3) * 4));
+                    const bool live = (int)r < left && scale != 0.f;
+                    const uint32_t src = sq + cfg::kCode0 + code * cfg::kCodeTile + r * D, turn = D == 128 ? r & 7 : (r >> 1) & 3;
+                    const uint32_t dst = ring + stage * cfg::kTile + r * 128;
+#pragma unroll
+                    for (uint32_t c = 0; c < D / 16; ++c) {
+                        uint32_t q[4], o[8];
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                     : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3])
+                                     : "r"(src + ((c ^ turn) << 4)));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) cr_widen4<BF16>(q[e], scale, o[2 * e], o[2 * e + 1]);
+                        if (!live) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) o[e] = 0;
+                        }
+                        const uint32_t to = dst + (c >> 2) * (kRowsTile * 128), u = (c & 3) * 2;
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((u ^ (r & 7)) << 4)), "r"(o[0]),
+                                     "r"(o[1]), "r"(o[2]), "r"(o[3])
+                                     : "memory");
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((u + 1) ^ (r & 7)) << 4)), "r"(o[4]),
+                                     "r"(o[5]), "r"(o[6]), "r"(o[7])
+                                     : "memory");
+                    }
+                }
+                cr_fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    cr_bar_arrive(FULL(stage));
+                    cr_bar_arrive(TAKEN(code));
+                }
+                if (++stage == cfg::kStages) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+                if (++code == cfg::kCodes) {
+                    code = 0;
+                    cphase ^= 1;
+                }
+                if (j & 1) left -= kRowsTile;
+            }
+        }
     } else if (warp < 16) {
         // ---- softmax: two threads a row ----
         asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
@@ -820,7 +927,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             }
             // keys that this row sees, from the first tile's on; the tile with the sequence's end
             int seen = p->klen - p->t0 * kRowsTile - half * 64;
-            const int tail = x == 0 && half < cfg::kChunks ? (p->klen >> 7) - p->t0 : -1;
+            const int tail = !E8 && x == 0 && half < cfg::kChunks ? (p->klen >> 7) - p->t0 : -1;
             if (A.causal) seen = min(seen, p->diag - p->t0 * kRowsTile - half * 64 + tok + 1);
             float m = -INFINITY, l = 0.f;
             for (int j = 0; j < n; ++j, seen -= kRowsTile) {
@@ -1049,6 +1156,8 @@ out:
     }
 #undef FULL
 #undef EMPTY
+#undef CODES
+#undef TAKEN
 #undef BAR
 }
 
@@ -1553,6 +1662,372 @@ out:
 #undef JOIN
 }
 
+// ---- few rows over 8 bits -----------------------------------------------------------------------
+// As k_attn_few with half of the bytes.  Numbers are widened to half precision in registers (exact), and the rest of
+// a product's arithmetic is arranged so that halves are enough:
+//   a row of bfloat16 queries is first multiplied by a power of two that brings its largest element to 2^14 .. 2^15
+//   (elements 2^28 below it are still exact); scores are 32-bit sums, times that power's inverse and the key block's;
+//   weights are multiplied by their value block's power over the largest, E, that the warp has met, and by 2^15: they
+//   are rounded to 11 bits as long as a block's power is above 2^-29 E, and are off by less than 2^-40 E otherwise.
+// The contraction's order is free, so a lane takes what lies together: for scores D/4 consecutive elements of a key, for
+// values 16 (8) consecutive elements of four keys, whose bytes it pairs up.
+template <int D>
+struct few8_cfg {
+    static constexpr int kTile = kFewTile * D;            // bytes of 64 keys
+    static constexpr int kStages = D == 128 ? 6 : 12;
+    static constexpr int kQ = 16 * D * 2;
+    static constexpr int kJoin = kFewWarps * 8 * 64 * 4;
+    static constexpr int kSmem = kStages * 2 * kTile + kQ + kJoin + 1024;
+};
+
+template <int D, bool BF16, bool WIDE>
+__global__ void __launch_bounds__(kFewThreads, 2)
+    k_attn_few8(const __grid_constant__ attn_in A, const __grid_constant__ CUtensorMap map_q,
+                const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
+{
+    using cfg = few8_cfg<D>;
+    constexpr int kDims = D / 4;      // elements of a key that a lane takes
+    constexpr int kRun = D / 8;       // elements of a value that a lane takes
+    constexpr uint32_t kR = WIDE ? 2 : 1;
+    extern __shared__ unsigned char dyn[];
+    __shared__ __align__(8) unsigned long long bars[2 * cfg::kStages + 3];
+    __shared__ float scales[cfg::kStages][16];  // of eight groups of eight keys, and values
+    __shared__ float2 join_ml[kFewWarps][16];
+    __shared__ int gave_up;
+    __shared__ own_list list;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t base = cr_smem(dyn), ring = (base + 1023u) & ~1023u, sq = ring + cfg::kStages * 2 * cfg::kTile;
+    float *join = reinterpret_cast<float *>(dyn + (sq - base) + cfg::kQ);
+    const uint32_t bar = cr_smem(bars);
+#define FULL(s) (bar + 8u * (s))
+#define EMPTY(s) (bar + 8u * (cfg::kStages + (s)))
+#define QFULL (bar + 8u * (2 * cfg::kStages))
+#define QEMPTY (bar + 8u * (2 * cfg::kStages + 1))
+#define JOIN (bar + 8u * (2 * cfg::kStages + 2))
+
+    if (threadIdx.x == 32) {
+        cr_tma_prefetch_map(&map_q);
+        cr_tma_prefetch_map(&map_k);
+        cr_tma_prefetch_map(&map_v);
+    }
+    if (threadIdx.x == 0) {
+        gave_up = 0;
+        for (int s = 0; s < cfg::kStages; ++s) {
+            cr_bar_init(FULL(s), 1 + 16);  // the tile's copies, and those of its scales
+            cr_bar_init(EMPTY(s), kFewWarps);
+        }
+        cr_bar_init(QFULL, 1);
+        cr_bar_init(QEMPTY, kFewWarps);
+        cr_bar_init(JOIN, kFewWarps);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    for (uint32_t i = threadIdx.x; i < cfg::kQ / 16; i += kFewThreads)  // rows that no copy writes
+        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(sq + 16 * i), "r"(0));
+    cr_fence_async_smem();
+    __syncthreads();
+    cr_wait_previous();  // as k_attn_few
+    cr_launch_next();
+
+    walk w;
+    plan_cut cut;
+    if (A.own_list) {
+        if (warp == kFewWarps) cut = make_list(A.plan, &list, A.status);
+        __syncthreads();
+        w.begin(list.start, list.blk);
+    } else {
+        w.begin(A.start + blockIdx.x, A.blk);
+    }
+    uint32_t stage = 0, phase = 0, qphase = 0;
+    if (warp == kFewWarps) {
+        // ---- copies: a lane has one group of eight keys; its scale, and the box that begins there ----
+        const uint32_t group = lane & 7;
+        while (w.next()) {
+            const int kv = (int)(w.h / A.nsub);
+            if (A.after_rows && lane == 0) {
+                const uint64_t at = (uint64_t)w.k.row0 * A.few_heads + w.h;
+                if (w.t0 == 0) A.first_cta[at] = (int)blockIdx.x;
+                if (w.t1 == (uint32_t)w.k.nt) A.last_cta[at] = (int)blockIdx.x;
+            }
+            if (!cr_bar_wait(QEMPTY, qphase ^ 1, &gave_up)) goto out;
+            qphase ^= 1;
+            if (lane == 0) {
+                cr_bar_expect(QFULL, min(16u, A.G) * 128 * (D / 64));
+                for (int c = 0; c < D / 64; ++c)
+                    cr_tma_load(sq + c * 16 * 128, &map_q, QFULL, c * 64, (int)(w.h % A.nsub) * 16, kv, w.k.row0);
+            }
+            const int32_t *row = A.table + (uint64_t)w.k.kbase * A.max_pages;
+            const uint32_t tile0 = (uint32_t)w.k.lo / kFewTile;
+            auto page_of = [&](uint32_t t) {  // n_pages: none
+                const uint32_t at = (tile0 + t) * kFewTile + group * 8;
+                return t < w.t1 && (int)at < w.k.klen ? (uint32_t)row[at >> A.page_log2] : A.n_pages;
+            };
+            uint32_t next = page_of(w.t0);
+            for (uint32_t t = w.t0; t < w.t1; ++t) {
+                const uint32_t in_page = ((tile0 + t) * kFewTile + group * 8) & ((1u << A.page_log2) - 1);
+                const uint32_t page = next;
+                next = page_of(t + 1);  // on its way while this tile waits for its place
+                const bool on = page < A.n_pages, brings = lane < 8 && on && (group * 8 & (A.box_rows - 1)) == 0;
+                const uint32_t bytes = 2 * __popc(__ballot_sync(~0u, brings)) * A.box_rows * D;
+                const uint64_t scale = on ? (((uint64_t)page * A.kv_heads + kv) << A.nb_log2) + (in_page >> A.block_log2) : 0;
+                if (!cr_bar_wait(EMPTY(stage), phase ^ 1, &gave_up)) goto out;
+                if (lane == 0) cr_bar_expect(FULL(stage), bytes);
+                __syncwarp();
+                if (brings) {
+                    const uint32_t dst = ring + stage * 2 * cfg::kTile + group * 8 * D;
+                    cr_tma_load(dst, &map_k, FULL(stage), 0, (int)in_page, kv, (int)page);
+                    cr_tma_load(dst + cfg::kTile, &map_v, FULL(stage), 0, (int)in_page, kv, (int)page);
+                }
+                if (lane < 16) cr_copy_word(cr_smem(&scales[stage][lane]), (lane < 8 ? A.k_scale : A.v_scale) + scale, on, FULL(stage));
+                if (++stage == cfg::kStages) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+            }
+        }
+        if (A.own_list) count_pieces(A.plan, cut, &list);
+    } else {
+        const uint32_t r4 = lane >> 2, q4 = lane & 3;
+        uint32_t jphase = 0;
+        auto meet = [&]() {  // of the four warps
+            __syncwarp();
+            if (lane == 0) cr_bar_arrive(JOIN);
+            const bool ok = cr_bar_wait(JOIN, jphase, &gave_up);
+            jphase ^= 1;
+            return ok;
+        };
+        while (w.next()) {
+            const uint32_t sub = w.h % A.nsub;
+            const uint32_t h0 = w.h / A.nsub * A.G + sub * 16;  // first query head of the rows
+            const uint32_t rows = min(16u, A.G - sub * 16);
+            uint32_t qa[D / 16][4];
+            float cr[kR];  // what makes scores of sums
+            if (!cr_bar_wait(QFULL, qphase, &gave_up)) goto out;
+            qphase ^= 1;
+            if (!WIDE) {
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) qa[i][1] = qa[i][3] = 0;
+            }
+#pragma unroll
+            for (uint32_t r = 0; r < kR; ++r) {
+                const uint32_t row = r4 + 8 * r;
+                uint32_t x[kDims / 2];
+#pragma unroll
+                for (int k = 0; k < kDims / 8; ++k) {
+                    const uint32_t u = q4 * (kDims / 8) + k;
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                 : "=r"(x[4 * k]), "=r"(x[4 * k + 1]), "=r"(x[4 * k + 2]), "=r"(x[4 * k + 3])
+                                 : "r"(sq + (u >> 3) * (16 * 128) + row * 128 + (((u & 7) ^ (row & 7)) << 4)));
+                }
+                cr[r] = A.c;
+                if (BF16) {
+                    uint32_t top = 0;  // the largest magnitude's bits
+#pragma unroll
+                    for (int k = 0; k < kDims / 2; ++k) top = max(top, max(x[k] << 16 & 0x7fffffffu, x[k] & 0x7fff0000u));
+                    top = max(top, __shfl_xor_sync(~0u, top, 1));
+                    top = max(top, __shfl_xor_sync(~0u, top, 2));
+                    const int up = max(-113, min(113, 14 + 127 - (int)(top >> 23)));
+                    const float f = __uint_as_float((uint32_t)(127 + up) << 23);
+                    cr[r] *= __uint_as_float((uint32_t)(127 - up) << 23);
+#pragma unroll
+                    for (int k = 0; k < kDims / 2; ++k)
+                        x[k] = cr_pack16<false>(__uint_as_float(x[k] << 16) * f, __uint_as_float(x[k] & 0xffff0000u) * f);
+                }
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    qa[i][r] = x[2 * i];
+                    qa[i][2 + r] = x[2 * i + 1];
+                }
+            }
+            __syncwarp();
+            if (lane == 0) cr_bar_arrive(QEMPTY);
+            // o[t]: elements (2 q4) kRun + t and (2 q4 + 1) kRun + t of rows r4 and r4 + 8, in units of 2^-15 E
+            float o[D / 8][4];
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
+            float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+            float E = 0.f, per_E = 0.f;  // per_E: 2^15 / E
+            for (uint32_t t = w.t0; t < w.t1; ++t) {
+                if (!cr_bar_wait(FULL(stage), phase, &gave_up)) goto out;
+                const int key = (int)((w.k.lo / kFewTile + t) * kFewTile + warp * 16);  // this warp's first key
+                const cr_keys16 see = cr_seen16(key, w.k.lo, w.k.klen);
+                if (see.any()) {
+                    const uint32_t kt = ring + stage * 2 * cfg::kTile, vt = kt + cfg::kTile;
+                    const float2 ks = *reinterpret_cast<const float2 *>(&scales[stage][2 * warp]);
+                    const float2 vs = *reinterpret_cast<const float2 *>(&scales[stage][8 + 2 * warp]);
+                    float s[2][4] = {};
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        const uint32_t kr = warp * 16 + g * 8 + r4, turn = D == 128 ? kr & 7 : (kr >> 1) & 3;
+#pragma unroll
+                        for (int k = 0; k < kDims / 16; ++k) {
+                            uint32_t c4[4];
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                         : "=r"(c4[0]), "=r"(c4[1]), "=r"(c4[2]), "=r"(c4[3])
+                                         : "r"(kt + kr * D + (((q4 * (kDims / 16) + k) ^ turn) << 4)));
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                mma16816<false>(s[g], qa[4 * k + i], cr_e4m3_pair(c4[i]), cr_e4m3_pair(c4[i] >> 16));
+                        }
+                    }
+                    uint32_t keep[2] = {~0u, ~0u};  // halves of v's registers that are seen
+                    if (!see.all()) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                if (!see.sees(i * 8 + (int)q4 * 2 + e)) {
+                                    s[i][e] = s[i][2 + e] = -INFINITY;
+                                    keep[i] &= e ? 0x0000ffffu : 0xffff0000u;
+                                }
+                            }
+                        }
+                    }
+                    float grown = 1.f;  // of E
+                    const float most = fmaxf(vs.x, vs.y);
+                    if (most > E) {
+                        grown = E / most;
+                        E = most;
+                        per_E = 32768.f / E;
+                    }
+                    const float by[2] = {vs.x * per_E, vs.y * per_E};
+                    uint32_t pa[4];
+#pragma unroll
+                    for (uint32_t r = 0; r < kR; ++r) {
+                        const float f0 = cr[r] * ks.x, f1 = cr[r] * ks.y;
+                        float x[4] = {s[0][2 * r], s[0][2 * r + 1], s[1][2 * r], s[1][2 * r + 1]};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (x[i] != -INFINITY) x[i] *= i < 2 ? f0 : f1;
+                        float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+                        top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
+                        top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
+                        const float m_new = fmaxf(m[r], top);
+                        if (__any_sync(~0u, m_new != m[r] || grown != 1.f)) {
+                            float f = m_new == m[r] ? 1.f : cr_exp2(m[r] - m_new);
+                            l[r] *= f;
+                            f *= grown;
+#pragma unroll
+                            for (int i = 0; i < D / 8; ++i) {
+                                o[i][2 * r] *= f;
+                                o[i][2 * r + 1] *= f;
+                            }
+                            m[r] = m_new;
+                        }
+                        const float off = m[r] == -INFINITY ? 0.f : m[r];
+                        float p[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) p[i] = cr_exp2(x[i] - off);
+                        l[r] += (p[0] + p[1]) + (p[2] + p[3]);
+                        pa[r] = cr_pack16<false>(p[0] * by[0], p[1] * by[0]);
+                        pa[2 + r] = cr_pack16<false>(p[2] * by[1], p[3] * by[1]);
+                    }
+                    if (!WIDE) pa[1] = pa[3] = 0;
+                    // four keys' runs; words of four elements
+                    uint32_t v[4][kRun / 4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t vr = warp * 16 + (e >> 1) * 8 + 2 * q4 + (e & 1);
+                        if (D == 128) {
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                         : "=r"(v[e][0]), "=r"(v[e][1]), "=r"(v[e][kRun / 4 - 2]), "=r"(v[e][kRun / 4 - 1])
+                                         : "r"(vt + vr * D + ((r4 ^ (vr & 7)) << 4)));
+                        } else {
+                            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];"
+                                         : "=r"(v[e][0]), "=r"(v[e][1])
+                                         : "r"(vt + vr * D + (((r4 >> 1) ^ ((vr >> 1) & 3)) << 4) + (r4 & 1) * 8));
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < kRun / 4; ++i) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {  // elements 4 i + 2 h and the next: bytes of two keys side by side
+                            const uint32_t a = __byte_perm(v[0][i], v[1][i], h ? 0x7362 : 0x5140);
+                            const uint32_t b = __byte_perm(v[2][i], v[3][i], h ? 0x7362 : 0x5140);
+                            mma16816<false>(o[4 * i + 2 * h], pa, cr_e4m3_pair(a) & keep[0], cr_e4m3_pair(b) & keep[1]);
+                            mma16816<false>(o[4 * i + 2 * h + 1], pa, cr_e4m3_pair(a >> 16) & keep[0], cr_e4m3_pair(b >> 16) & keep[1]);
+                        }
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) cr_bar_arrive(EMPTY(stage));
+                if (++stage == cfg::kStages) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+            }
+            // ---- the four warps' states join: eight rows and 64 columns at a time, four columns a thread ----
+            const float unit = E * 0x1p-15f;
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                l[r] += __shfl_xor_sync(~0u, l[r], 1);
+                l[r] += __shfl_xor_sync(~0u, l[r], 2);
+                if (q4 == 0) join_ml[warp][r4 + 8 * r] = make_float2(m[r], l[r]);
+            }
+            const int slot = w.slot();
+            // a whole block that a shared prefix still joins has a place of its own
+            const bool to_own = slot < 0 && w.k.lo > 0;
+            const uint64_t place = to_own ? (uint64_t)w.k.row0 * A.few_heads + w.h : (uint64_t)slot;
+            float *part = to_own ? A.own : A.part, *part_ml = to_own ? A.own_ml : A.part_ml;
+#pragma unroll
+            for (int pass = 0; pass < (int)kR * (D / 64); ++pass) {
+                const int r = pass / (D / 64), ch = pass % (D / 64);
+                if (rows <= 8u * r) break;
+                // place (i, run): element run * kRun + ch * 8 + i
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    *reinterpret_cast<float2 *>(join + (warp * 8 + r4) * 64 + i * 8 + q4 * 2) =
+                        make_float2(o[ch * 8 + i][2 * r] * unit, o[ch * 8 + i][2 * r + 1] * unit);
+                if (!meet()) goto out;
+                const uint32_t rr = threadIdx.x >> 4, col = threadIdx.x & 15, i0 = (col & 1) * 4, run = col >> 1, row = 8 * r + rr;
+                const uint32_t d4 = (run * kRun + ch * 8 + i0) / 4;
+                if (row < rows) {
+                    const uint64_t oh = (uint64_t)w.k.row0 * A.q_heads + h0 + row;
+                    float mm = -INFINITY, ll = 0.f;
+                    for (int v = 0; v < kFewWarps; ++v) mm = fmaxf(mm, join_ml[v][row].x);
+                    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int v = 0; v < kFewWarps; ++v) {
+                        const float2 ml = join_ml[v][row];
+                        const float f = ml.x == -INFINITY ? 0.f : cr_exp2(ml.x - mm);
+                        const float *x = join + (v * 8 + rr) * 64 + i0 * 8 + run;
+                        ll += ml.y * f;
+                        s.x += x[0] * f;
+                        s.y += x[8] * f;
+                        s.z += x[16] * f;
+                        s.w += x[24] * f;
+                    }
+                    if (slot >= 0 || to_own) {
+                        reinterpret_cast<float4 *>(part)[(place * (D / 4) + d4) * 16 + row] = s;
+                        if (d4 == 0) reinterpret_cast<float2 *>(part_ml)[place * 16 + row] = make_float2(mm, ll);
+                    } else {
+                        const float inv = ll == 0.f ? 0.f : 1.f / ll;
+                        if (4 * d4 < A.head_dim)
+                            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(A.o) + (uint64_t)w.k.row0 * A.o_token +
+                                                       (uint64_t)(h0 + row) * A.o_head + 4 * d4) =
+                                make_uint2(cr_pack16<BF16>(s.x * inv, s.y * inv), cr_pack16<BF16>(s.z * inv, s.w * inv));
+                        if (d4 == 0 && A.lse)
+                            A.lse[oh] = (ll == 0.f ? -INFINITY : mm + log2f(ll)) * 0.693147180559945309f;
+                    }
+                }
+                if (!meet()) goto out;
+            }
+        }
+    }
+out:
+    __syncwarp();
+    if (gave_up) {
+        if (lane == 0) atomicOr(A.status, CR_FLAG_TIMEOUT);
+        for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+    }
+#undef FULL
+#undef EMPTY
+#undef QFULL
+#undef QEMPTY
+#undef JOIN
+}
+
 // ---- host -------------------------------------------------------------------------------------
 typedef CUresult (*encode_fn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                               const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -1574,19 +2049,20 @@ encode_fn encoder()
 }
 
 // A 4-D map of 16-bit elements: dims and strides (elements) from the second dimension on, boxes of
-// 64 elements of the first.
+// 64 elements of the first.  bytes != 0: of 8-bit elements, so many in a box.
 int encode_map(cr_ctx *ctx, CUtensorMap *map, bool bf16, const void *base, const uint64_t dim[4], const uint64_t stride[3],
-               const uint32_t box[3], bool stream_once)
+               const uint32_t box[3], bool stream_once, uint32_t bytes = 0)
 {
     encode_fn fn = encoder();
     if (!fn) return cr_fail(ctx, CR_ECUDA, "cuTensorMapEncodeTiled is not available from this driver");
     cuuint64_t st[3];
-    for (int i = 0; i < 3; ++i) st[i] = dim[i + 1] == 1 ? 16 : stride[i] * 2;  // never stepped over
-    const cuuint32_t bx[4] = {64, box[0], box[1], box[2]}, es[4] = {1, 1, 1, 1};
+    for (int i = 0; i < 3; ++i) st[i] = dim[i + 1] == 1 ? 16 : stride[i] * (bytes ? 1 : 2);  // 1: never stepped over
+    const cuuint32_t bx[4] = {bytes ? bytes : 64, box[0], box[1], box[2]}, es[4] = {1, 1, 1, 1};
     const cuuint64_t dm[4] = {dim[0], dim[1], dim[2], dim[3]};
-    const CUresult r = fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
-                          const_cast<void *>(base), dm, st, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                          CU_TENSOR_MAP_SWIZZLE_128B,
+    const CUtensorMapDataType type = bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                           : (bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16);
+    const CUresult r = fn(map, type, 4, const_cast<void *>(base), dm, st, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
                           stream_once ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return cr_fail(ctx, CR_EINVAL, "tensor map rejected (%d): check pointers and strides", (int)r);
@@ -1595,7 +2071,7 @@ int encode_map(cr_ctx *ctx, CUtensorMap *map, bool bf16, const void *base, const
 
 // Keys and values of a call.
 struct kv_desc {
-    bool paged, bf16;
+    bool paged, bf16, e4m3;
     uint32_t heads, dim;
     const void *k, *v;
     uint64_t k_row, k_head, v_row, v_head;  // elements between tokens, heads
@@ -1604,6 +2080,7 @@ struct kv_desc {
     const int32_t *cu_k;
     // paged
     const cr_kv_pages *pg;
+    const float *k_scale, *v_scale;  // 8 bits
 };
 
 int kv_map(cr_ctx *ctx, CUtensorMap *map, const kv_desc &K, bool value, uint32_t box_rows)
@@ -1619,7 +2096,7 @@ int kv_map(cr_ctx *ctx, CUtensorMap *map, const kv_desc &K, bool value, uint32_t
         dim[1] = dim[2] = 1;  // one row stands for no keys at all (cr_attn_packed)
     }
     const uint32_t box[3] = {box_rows, 1, 1};
-    return encode_map(ctx, map, K.bf16, value ? K.v : K.k, dim, st, box, K.paged);
+    return encode_map(ctx, map, K.bf16, value ? K.v : K.k, dim, st, box, K.paged, K.e4m3 ? (K.dim <= 64 ? 64 : 128) : 0);
 }
 
 uint32_t ilog2(uint32_t v)
@@ -1708,6 +2185,13 @@ void fill_common(attn_in &A, cr_ctx *ctx, const cr_attn_args *a, const kv_desc &
         A.table = K.pg->d_table;
         A.max_pages = K.pg->max_pages;
         A.page_log2 = ilog2(K.pg->page);
+        A.n_pages = K.pg->n_pages;
+        A.k_scale = K.k_scale;
+        A.v_scale = K.v_scale;
+        if (K.e4m3) {
+            A.block_log2 = ilog2(K.pg->block);
+            A.nb_log2 = A.page_log2 - A.block_log2;
+        }
     }
 }
 
@@ -1730,29 +2214,34 @@ int query_map(cr_ctx *ctx, CUtensorMap *map, const attn_in &A, const kv_desc &K,
     return encode_map(ctx, map, K.bf16, a->d_q, dim, st, box, false);
 }
 
-template <int D, bool BF16>
+template <int D, bool BF16, bool E8>
 int launch_rows(cr_ctx *ctx, const attn_in &A, const kv_desc &K, const cr_attn_args *a, uint32_t ctas)
 {
     CUtensorMap mq, mk, mv;
     CR_TRY(query_map(ctx, &mq, A, K, a, A.G, A.tq));
     CR_TRY(kv_map(ctx, &mk, K, false, A.box_rows));
     CR_TRY(kv_map(ctx, &mv, K, true, A.box_rows));
-    auto kern = k_attn_rows<D, BF16>;
+    auto kern = k_attn_rows<D, BF16, E8>;
     static unsigned long long raised = 0;
-    CR_TRY(raise_smem(ctx, kern, rows_cfg<D>::kSmem, raised));
-    CR_TRY(cr_launch_early(ctx, "k_attn_rows", kern, dim3(ctas), kRowsThreads, rows_cfg<D>::kSmem, A, mq, mk, mv));
+    CR_TRY(raise_smem(ctx, kern, rows_cfg<D, E8>::kSmem, raised));
+    CR_TRY(cr_launch_early(ctx, "k_attn_rows", kern, dim3(ctas), kRowsThreads, rows_cfg<D, E8>::kSmem, A, mq, mk, mv));
     if (ctas > 1 && !A.to_pfx)
         CR_TRY(cr_launch_early(ctx, "k_attn_join", k_attn_join<D, BF16, 2 * kRowsTile>, dim3(4 * ctx->num_sms), 256, 0, A));
     return CR_OK;
 }
 
+template <bool E8>
+int rows_of(cr_ctx *ctx, const attn_in &A, const kv_desc &K, const cr_attn_args *a, uint32_t ctas)
+{
+    if (K.dim <= 64) return K.bf16 ? launch_rows<64, true, E8>(ctx, A, K, a, ctas) : launch_rows<64, false, E8>(ctx, A, K, a, ctas);
+    return K.bf16 ? launch_rows<128, true, E8>(ctx, A, K, a, ctas) : launch_rows<128, false, E8>(ctx, A, K, a, ctas);
+}
 int rows(cr_ctx *ctx, const attn_in &A, const kv_desc &K, const cr_attn_args *a, uint32_t ctas)
 {
-    if (K.dim <= 64) return K.bf16 ? launch_rows<64, true>(ctx, A, K, a, ctas) : launch_rows<64, false>(ctx, A, K, a, ctas);
-    return K.bf16 ? launch_rows<128, true>(ctx, A, K, a, ctas) : launch_rows<128, false>(ctx, A, K, a, ctas);
+    return K.e4m3 ? rows_of<true>(ctx, A, K, a, ctas) : rows_of<false>(ctx, A, K, a, ctas);
 }
 
-template <int D, bool BF16, bool WIDE>
+template <int D, bool BF16, bool WIDE, bool E8>
 int launch_few(cr_ctx *ctx, const attn_in &A, const attn_in *R, const kv_desc &K, const cr_attn_args *a, uint32_t ctas)
 {
     CUtensorMap mq, mk, mv;
@@ -1760,9 +2249,14 @@ int launch_few(cr_ctx *ctx, const attn_in &A, const attn_in *R, const kv_desc &K
     CR_TRY(kv_map(ctx, &mk, K, false, A.box_rows));
     CR_TRY(kv_map(ctx, &mv, K, true, A.box_rows));
     auto kern = k_attn_few<D, BF16, WIDE>;
+    int smem = few_cfg<D>::kSmem;
+    if (E8) {
+        kern = k_attn_few8<D, BF16, WIDE>;
+        smem = few8_cfg<D>::kSmem;
+    }
     static unsigned long long raised = 0;
-    CR_TRY(raise_smem(ctx, kern, few_cfg<D>::kSmem, raised));
-    CR_TRY(cr_launch_early(ctx, "k_attn_few", kern, dim3(ctas), kFewThreads, few_cfg<D>::kSmem, A, mq, mk, mv));
+    CR_TRY(raise_smem(ctx, kern, smem, raised));
+    CR_TRY(cr_launch_early(ctx, "k_attn_few", kern, dim3(ctas), kFewThreads, smem, A, mq, mk, mv));
     if (R)
         CR_TRY(cr_launch_early(ctx, "k_attn_decode_join", k_attn_decode_join<D, BF16>, dim3(a->n, A.few_heads), 256, 0, A, *R));
     else if (ctas > 1)
@@ -1770,15 +2264,18 @@ int launch_few(cr_ctx *ctx, const attn_in &A, const attn_in *R, const kv_desc &K
     return CR_OK;
 }
 
-int few(cr_ctx *ctx, const attn_in &A, const attn_in *R, const kv_desc &K, const cr_attn_args *a, uint32_t ctas)
+template <int D, bool BF16>
+int few_of(cr_ctx *ctx, const attn_in &A, const attn_in *R, const kv_desc &K, const cr_attn_args *a, uint32_t ctas)
 {
     const bool wide = A.G > 8;
-    if (K.dim <= 64) {
-        if (K.bf16) return wide ? launch_few<64, true, true>(ctx, A, R, K, a, ctas) : launch_few<64, true, false>(ctx, A, R, K, a, ctas);
-        return wide ? launch_few<64, false, true>(ctx, A, R, K, a, ctas) : launch_few<64, false, false>(ctx, A, R, K, a, ctas);
-    }
-    if (K.bf16) return wide ? launch_few<128, true, true>(ctx, A, R, K, a, ctas) : launch_few<128, true, false>(ctx, A, R, K, a, ctas);
-    return wide ? launch_few<128, false, true>(ctx, A, R, K, a, ctas) : launch_few<128, false, false>(ctx, A, R, K, a, ctas);
+    if (K.e4m3)
+        return wide ? launch_few<D, BF16, true, true>(ctx, A, R, K, a, ctas) : launch_few<D, BF16, false, true>(ctx, A, R, K, a, ctas);
+    return wide ? launch_few<D, BF16, true, false>(ctx, A, R, K, a, ctas) : launch_few<D, BF16, false, false>(ctx, A, R, K, a, ctas);
+}
+int few(cr_ctx *ctx, const attn_in &A, const attn_in *R, const kv_desc &K, const cr_attn_args *a, uint32_t ctas)
+{
+    if (K.dim <= 64) return K.bf16 ? few_of<64, true>(ctx, A, R, K, a, ctas) : few_of<64, false>(ctx, A, R, K, a, ctas);
+    return K.bf16 ? few_of<128, true>(ctx, A, R, K, a, ctas) : few_of<128, false>(ctx, A, R, K, a, ctas);
 }
 
 // The list of work of a call, and that of its groups.  A short list for few CTAs is made by fewer threads, whose
@@ -1846,20 +2343,23 @@ int attn_many(cr_ctx *ctx, const cr_attn_args *a, const kv_desc &K)
 
 }  // namespace
 
-// Limits of a pool of pages (cr_pages.cu).
-int cr_pages_check(cr_ctx *ctx, const char *who, const cr_kv_pages *pg);
-
 static int paged_desc(cr_ctx *ctx, const char *who, const cr_kv_pages *pg, uint32_t layer, kv_desc &K)
 {
     CR_TRY(cr_pages_check(ctx, who, pg));
     if (layer >= pg->layers) return cr_fail(ctx, CR_EINVAL, "%s: layer %u of %u", who, layer, pg->layers);
     K = kv_desc{};
     K.paged = true;
-    K.bf16 = pg->dtype == CR_DTYPE_BF16;
+    K.bf16 = cr_is_bf16(pg->dtype);
+    K.e4m3 = cr_in_8bit(pg->dtype);
     K.heads = pg->kv_heads;
     K.dim = pg->head_dim;
-    K.k = static_cast<const uint16_t *>(pg->d_cache) + layer * pg->layer_stride;
-    K.v = static_cast<const uint16_t *>(K.k) + pg->kv_stride;
+    K.k = static_cast<const uint8_t *>(pg->d_cache) + (K.e4m3 ? 1 : 2) * (layer * pg->layer_stride);
+    K.v = static_cast<const uint8_t *>(K.k) + (K.e4m3 ? 1 : 2) * pg->kv_stride;
+    if (K.e4m3) {
+        const uint64_t plane = ((uint64_t)pg->n_pages * pg->kv_heads) * (pg->page / pg->block);
+        K.k_scale = pg->d_scale + 2 * layer * plane;
+        K.v_scale = K.k_scale + plane;
+    }
     K.k_row = K.v_row = pg->token_stride;
     K.k_head = K.v_head = pg->head_stride;
     K.pg = pg;
@@ -1900,7 +2400,7 @@ extern "C" int cr_attn_paged(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t lay
     if (!args) return cr_fail(ctx, CR_EINVAL, "cr_attn_paged: args is NULL");
     kv_desc K;
     CR_TRY(paged_desc(ctx, "cr_attn_paged", pages, layer, K));
-    CR_TRY(check_heads(ctx, "cr_attn_paged", args, pages->dtype, pages->kv_heads, pages->head_dim));
+    CR_TRY(check_heads(ctx, "cr_attn_paged", args, cr_is_bf16(pages->dtype) ? CR_DTYPE_BF16 : CR_DTYPE_FP16, pages->kv_heads, pages->head_dim));
     if (args->n && !args->d_cu_q) return cr_fail(ctx, CR_EINVAL, "cr_attn_paged: d_cu_q is NULL");
     return attn_many(ctx, args, K);
 }
@@ -1913,7 +2413,7 @@ extern "C" int cr_attn_decode(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t la
     if (!args) return cr_fail(ctx, CR_EINVAL, "cr_attn_decode: args is NULL");
     kv_desc K;
     CR_TRY(paged_desc(ctx, "cr_attn_decode", pages, layer, K));
-    CR_TRY(check_heads(ctx, "cr_attn_decode", args, pages->dtype, pages->kv_heads, pages->head_dim));
+    CR_TRY(check_heads(ctx, "cr_attn_decode", args, cr_is_bf16(pages->dtype) ? CR_DTYPE_BF16 : CR_DTYPE_FP16, pages->kv_heads, pages->head_dim));
     if (args->n_tokens != args->n) return cr_fail(ctx, CR_EINVAL, "cr_attn_decode: one query token per entry");
     if (n_groups && (!d_group_off || !d_shared)) return cr_fail(ctx, CR_EINVAL, "cr_attn_decode: NULL groups");
     if (n_groups > (1u << 24)) return cr_fail(ctx, CR_EINVAL, "cr_attn_decode: %u groups", n_groups);

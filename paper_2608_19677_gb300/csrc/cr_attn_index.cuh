@@ -1,4 +1,4 @@
-// Index arithmetic of the attention kernels that the host's compiler can check too.
+// Index arithmetic of the attention and writing kernels that the host's compiler can check too.
 #pragma once
 
 #ifdef __CUDACC__
@@ -40,3 +40,18 @@ struct cr_keys16 {
     CR_HD_MEMBER bool sees(int j) const { return j >= first && j < end; }
 };
 CR_HD cr_keys16 cr_seen16(int key, int lo, int klen) { return {lo - key, klen - key}; }
+
+// Writing: steps of 2^log2 positions that rows are worked on in.  Entry i, whose tokens begin at cu, has the slots from
+// cr_slot_of(cu, i) on: its m tokens touch at most m / 2^log2 + 2 steps, which the next entry's first slot leaves it.
+CR_HD unsigned long long cr_slot_of(int cu, unsigned i, unsigned log2) { return ((unsigned)cu >> log2) + 2ull * i; }
+// Positions [begin, end) of the k-th step that the last m of a row's len tokens touch; none where begin >= end.
+// Positions may be negative (more tokens than the row has), but not on both sides of 0 in a step.
+struct cr_positions {
+    long long begin, end;
+};
+CR_HD cr_positions cr_slot_positions(long long len, int m, unsigned long long k, unsigned log2)
+{
+    const long long size = 1ll << log2, first = len - m, step = (first >> log2) + (long long)k;
+    const long long begin = step * size, end = begin + size;
+    return {begin < first ? first : begin, end > len ? len : end};
+}

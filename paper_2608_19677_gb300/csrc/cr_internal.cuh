@@ -55,6 +55,7 @@ enum cr_scratch_slot {
     SCR_ATTN_PART,     // attention: pieces of blocks that several CTAs share
     SCR_ATTN_FEW,      //   of single tokens
     SCR_ATTN_PFX,      // attention: results over shared prefixes
+    SCR_KV_CLAIM,      // long lists of rows that are written: the first entry of each row
     SCR_NUM
 };
 
@@ -149,6 +150,10 @@ struct cr_replay {
 // Dynamic shared memory that a launch may take without raising the kernel's limit: 48 KB
 // hold the static part as well (at most 2 KB in the kernels here).
 constexpr size_t kDefaultSmem = 46 * 1024;
+
+// Types that hold keys and values in 8 bits, and the 16-bit type of a CR_DTYPE_*.
+static inline bool cr_in_8bit(uint32_t dtype) { return dtype == CR_DTYPE_BF16_E4M3 || dtype == CR_DTYPE_FP16_E4M3; }
+static inline bool cr_is_bf16(uint32_t dtype) { return dtype == CR_DTYPE_BF16 || dtype == CR_DTYPE_BF16_E4M3; }
 
 // ---- host helpers (cr_api.cu) ----------------------------------------------
 int cr_fail(cr_ctx *ctx, int code, const char *fmt, ...);

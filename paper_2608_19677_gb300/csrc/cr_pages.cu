@@ -1,6 +1,9 @@
 // Pages of a destination's key/value cache (include/cacheroute.h): extend, fork, free, compact, and
 // writing new tokens' keys and values.
 //
+// Pages hold 16-bit elements, or 8-bit ones with a scale for every block of tokens and head, which go where
+// the page's data goes.
+//
 // A call that takes pages needs the k-th free page for many k at once.  k_pages_scan writes the free
 // pages as a bitmap with counts per 32-page word (within its chunk) and per chunk; any thread of the
 // next kernel then finds the page of a rank, or the rank of a page, by a search of the chunk counts
@@ -8,7 +11,7 @@
 // (4 bytes a page) and are bound by their launches until the pool has millions of pages; copies of
 // page data are 16 bytes a thread with four loads in flight, bound by memory (664 MB of pages moved in
 // 226 us, 6.0 TB/s; a thousand forks with tails of 8 tokens on average, 4 planes: 14 us with cold caches).
-#include "cr_internal.cuh"
+#include "cr_pages.cuh"
 
 namespace {
 
@@ -26,14 +29,6 @@ struct pages_scan {
 };
 
 enum { SCAN_NONE, SCAN_EXTEND, SCAN_FORK };
-
-struct pages_in {
-    uint16_t *cache;
-    int32_t *ref, *table, *lens;
-    uint32_t layers, n_pages, page, page_log2, kv_heads, head_dim, n_seqs, max_pages;
-    uint64_t layer_stride, kv_stride, page_stride, token_stride, head_stride;
-    uint32_t *status;
-};
 
 template <typename T>
 __device__ T block_scan(T v, T *total)  // exclusive, blockDim.x <= 1024
@@ -268,11 +263,6 @@ __device__ __forceinline__ void copy16(uint4 *dst, const uint4 *src, uint32_t wo
     for (; i < words; i += blockDim.x) dst[i] = src[i];
 }
 
-__device__ __forceinline__ uint16_t *plane(const pages_in &P, uint32_t l2)
-{
-    return P.cache + (uint64_t)(l2 >> 1) * P.layer_stride + (uint64_t)(l2 & 1) * P.kv_stride;
-}
-
 // A block per entry: its pages, a warp each where they are few, else a thread.
 __global__ void __launch_bounds__(128) k_pages_extend(const __grid_constant__ pages_in P, const __grid_constant__ pages_scan S,
                                                       uint32_t n)
@@ -351,14 +341,14 @@ __global__ void __launch_bounds__(256) k_pages_fork(const __grid_constant__ page
     }
     const bool by_token = P.token_stride >= P.head_stride;  // the page's tokens lie one after the other
     const uint32_t segs = by_token ? 1 : P.kv_heads;
-    const uint32_t words = tail * P.head_dim / 8 * (by_token ? P.kv_heads : 1);
+    const uint32_t words = (tail * P.head_dim << P.size_log2) / 16 * (by_token ? P.kv_heads : 1);
     // one warp copies a segment, or several where there are fewer segments than warps
     const uint32_t nseg = (2 * P.layers - blockIdx.y + gridDim.y - 1) / gridDim.y * segs, nw = blockDim.x >> 5;
     const uint32_t share = nseg < nw ? nw / nseg : 1, warp = threadIdx.x >> 5;
     for (uint32_t g = warp / share; g < nseg; g += nw / share) {
-        uint16_t *base = plane(P, blockIdx.y + g / segs * gridDim.y) + g % segs * P.head_stride;
-        uint4 *out = reinterpret_cast<uint4 *>(base + to * P.page_stride);
-        const uint4 *in = reinterpret_cast<const uint4 *>(base + (uint64_t)from * P.page_stride);
+        uint8_t *base = P.plane(blockIdx.y + g / segs * gridDim.y) + (g % segs * P.head_stride << P.size_log2);
+        uint4 *out = reinterpret_cast<uint4 *>(base + (to * P.page_stride << P.size_log2));
+        const uint4 *in = reinterpret_cast<const uint4 *>(base + ((uint64_t)from * P.page_stride << P.size_log2));
         const uint32_t step = 32 * share;
         for (uint32_t i = warp % share * 32 + (threadIdx.x & 31); i < words; i += 4 * step) {  // four loads in flight
             uint4 v[4];
@@ -370,6 +360,11 @@ __global__ void __launch_bounds__(256) k_pages_fork(const __grid_constant__ page
                 if (i + e * step < words) out[i + e * step] = v[e];
         }
     }
+    if (!P.scale) return;  // the blocks that hold the tail, the last of them perhaps in part
+    const uint32_t nb = 1u << (P.page_log2 - P.block_log2), used = ((tail - 1) >> P.block_log2) + 1;
+    for (uint32_t l2 = blockIdx.y; l2 < 2 * P.layers; l2 += gridDim.y)
+        for (uint32_t i = threadIdx.x; i < P.kv_heads * nb; i += blockDim.x)
+            if ((i & (nb - 1)) < used) P.scales(l2, to)[i] = P.scales(l2, (uint32_t)from)[i];
 }
 
 // A block per entry.
@@ -440,7 +435,8 @@ __global__ void __launch_bounds__(256) k_pages_compact(const __grid_constant__ p
     } else {
         // an equal share of the (move, plane) pairs, in batches whose pages the threads look up together
         __shared__ uint32_t from[256], to[256];
-        const uint32_t words = P.page * P.kv_heads * (P.head_dim / 8), planes = 2 * P.layers, nb = gridDim.x - b_table;
+        const uint32_t words = (P.page * P.kv_heads * P.head_dim << P.size_log2) / 16, planes = 2 * P.layers,
+                       nb = gridDim.x - b_table;
         const uint64_t n = (uint64_t)(L - low) * planes, b = blockIdx.x - b_table;
         for (uint64_t i = n * b / nb, end = n * (b + 1) / nb; i < end;) {
             const uint32_t k0 = (uint32_t)(i / planes), k = k0 + threadIdx.x;
@@ -453,9 +449,13 @@ __global__ void __launch_bounds__(256) k_pages_compact(const __grid_constant__ p
             __syncthreads();
             for (; i < stop; ++i) {
                 const uint32_t m = (uint32_t)(i / planes) - k0;
-                uint16_t *base = plane(P, (uint32_t)(i % planes));
-                copy16(reinterpret_cast<uint4 *>(base + to[m] * P.page_stride),
-                       reinterpret_cast<const uint4 *>(base + from[m] * P.page_stride), words);
+                const uint32_t l2 = (uint32_t)(i % planes);
+                uint8_t *base = P.plane(l2);
+                copy16(reinterpret_cast<uint4 *>(base + (to[m] * P.page_stride << P.size_log2)),
+                       reinterpret_cast<const uint4 *>(base + (from[m] * P.page_stride << P.size_log2)), words);
+                if (P.scale)
+                    for (uint32_t j = threadIdx.x; j < P.kv_heads << (P.page_log2 - P.block_log2); j += blockDim.x)
+                        P.scales(l2, to[m])[j] = P.scales(l2, from[m])[j];
             }
         }
     }
@@ -510,7 +510,8 @@ __global__ void __launch_bounds__(128) k_kv_write(const __grid_constant__ pages_
         return;
     }
     const uint32_t per = P.head_dim / 8, words = P.kv_heads * per, step = 32u << W.wpt_log2;
-    uint16_t *kd = plane(P, 2 * layer) + dst, *vd = plane(P, 2 * layer + 1) + dst;
+    uint16_t *kd = reinterpret_cast<uint16_t *>(P.plane(2 * layer)) + dst;
+    uint16_t *vd = reinterpret_cast<uint16_t *>(P.plane(2 * layer + 1)) + dst;
     const uint16_t *ks = W.k + t * W.k_token, *vs = W.v + t * W.v_token;
     for (uint32_t i = (threadIdx.x & 31) + 32 * (uint32_t)(warp & ((1u << W.wpt_log2) - 1)); i < words; i += step) {
         const uint32_t h = i / per, d = (i - h * per) * 8;
@@ -519,30 +520,6 @@ __global__ void __launch_bounds__(128) k_kv_write(const __grid_constant__ pages_
         *reinterpret_cast<uint4 *>(kd + h * P.head_stride + d) = a;
         *reinterpret_cast<uint4 *>(vd + h * P.head_stride + d) = b;
     }
-}
-
-pages_in input(cr_ctx *ctx, const cr_kv_pages *pg)
-{
-    pages_in P = {};
-    P.cache = static_cast<uint16_t *>(pg->d_cache);
-    P.ref = pg->d_ref;
-    P.table = pg->d_table;
-    P.lens = pg->d_lens;
-    P.layers = pg->layers;
-    P.n_pages = pg->n_pages;
-    P.page = pg->page;
-    while ((1u << P.page_log2) < pg->page) ++P.page_log2;
-    P.kv_heads = pg->kv_heads;
-    P.head_dim = pg->head_dim;
-    P.n_seqs = pg->n_seqs;
-    P.max_pages = pg->max_pages;
-    P.layer_stride = pg->layer_stride;
-    P.kv_stride = pg->kv_stride;
-    P.page_stride = pg->page_stride;
-    P.token_stride = pg->token_stride;
-    P.head_stride = pg->head_stride;
-    P.status = ctx->d_status;
-    return P;
 }
 
 int scan_mem(cr_ctx *ctx, const cr_kv_pages *pg, uint32_t n, pages_scan &S)
@@ -570,7 +547,7 @@ int cr_pages_check(cr_ctx *ctx, const char *who, const cr_kv_pages *pg)
 {
     if (!pg) return cr_fail(ctx, CR_EINVAL, "%s: pages is NULL", who);
     if (!pg->d_cache || !pg->d_ref || !pg->d_table || !pg->d_lens) return cr_fail(ctx, CR_EINVAL, "%s: NULL pointer in pages", who);
-    if (pg->dtype > CR_DTYPE_FP16) return cr_fail(ctx, CR_EINVAL, "%s: dtype %u", who, pg->dtype);
+    if (pg->dtype > CR_DTYPE_FP16_E4M3) return cr_fail(ctx, CR_EINVAL, "%s: dtype %u", who, pg->dtype);
     if (pg->page < 8 || pg->page > 256 || (pg->page & (pg->page - 1)))
         return cr_fail(ctx, CR_EINVAL, "%s: page of %u tokens: a power of two, 8..256", who, pg->page);
     if (pg->head_dim == 0 || pg->head_dim > 128 || (pg->head_dim & 7))
@@ -589,6 +566,15 @@ int cr_pages_check(cr_ctx *ctx, const char *who, const cr_kv_pages *pg)
         return cr_fail(ctx, CR_EINVAL, "%s: the cache must be 16-byte aligned, its strides multiples of 8", who);
     if (pg->page_stride >= (1ull << 38))
         return cr_fail(ctx, CR_EINVAL, "%s: page stride too large", who);
+    if (cr_in_8bit(pg->dtype)) {
+        if (!pg->d_scale || ((uintptr_t)pg->d_scale & 3)) return cr_fail(ctx, CR_EINVAL, "%s: d_scale must hold the blocks' scales", who);
+        if (pg->head_dim & 15) return cr_fail(ctx, CR_EINVAL, "%s: head_dim %u: a multiple of 16 in 8 bits", who, pg->head_dim);
+        if (pg->block < 8 || pg->block > pg->page || (pg->block & (pg->block - 1)))
+            return cr_fail(ctx, CR_EINVAL, "%s: blocks of %u tokens: a power of two, 8..page", who, pg->block);
+        if ((pg->layer_stride | pg->kv_stride | pg->page_stride) & 15)
+            return cr_fail(ctx, CR_EINVAL, "%s: strides of a cache in 8 bits must be multiples of 16", who);
+        if (pg->reserved) return cr_fail(ctx, CR_EINVAL, "%s: reserved must be 0", who);
+    }
     return CR_OK;
 }
 
@@ -606,7 +592,7 @@ extern "C" int cr_pages_extend(cr_ctx *ctx, const cr_kv_pages *pages, const int3
     CR_TRY(cr_pages_check(ctx, "cr_pages_extend", pages));
     CR_TRY(list_check(ctx, "cr_pages_extend", n, d_seqs, d_add, d_add));
     if (!n) return CR_OK;
-    const pages_in P = input(ctx, pages);
+    const pages_in P = cr_pages_input(ctx, pages);
     pages_scan S;
     CR_TRY(scan_mem(ctx, pages, n, S));
     CR_TRY(cr_launch_early(ctx, "k_pages_scan", k_pages_scan<SCAN_EXTEND>, dim3(S.chunks + 1), 1024, 0, P, S, d_seqs, d_add, d_add, n));
@@ -622,7 +608,7 @@ extern "C" int cr_pages_fork(cr_ctx *ctx, const cr_kv_pages *pages, const int32_
     CR_TRY(cr_pages_check(ctx, "cr_pages_fork", pages));
     CR_TRY(list_check(ctx, "cr_pages_fork", n, d_src, d_dst, d_keep));
     if (!n) return CR_OK;
-    const pages_in P = input(ctx, pages);
+    const pages_in P = cr_pages_input(ctx, pages);
     pages_scan S;
     CR_TRY(scan_mem(ctx, pages, n, S));
     CR_TRY(cr_launch_early(ctx, "k_pages_scan", k_pages_scan<SCAN_FORK>, dim3(S.chunks + 1), 1024, 0, P, S, d_src, d_dst, d_keep, n));
@@ -640,7 +626,7 @@ extern "C" int cr_pages_free(cr_ctx *ctx, const cr_kv_pages *pages, const int32_
     CR_TRY(cr_pages_check(ctx, "cr_pages_free", pages));
     CR_TRY(list_check(ctx, "cr_pages_free", n, d_seqs, d_seqs, d_seqs));
     if (!n) return CR_OK;
-    const pages_in P = input(ctx, pages);
+    const pages_in P = cr_pages_input(ctx, pages);
     CR_TRY(cr_launch_early(ctx, "k_pages_free", k_pages_free, dim3(n), 128, 0, P, d_seqs));
     return CR_OK;
 }
@@ -654,7 +640,7 @@ extern "C" int cr_pages_compact(cr_ctx *ctx, const cr_kv_pages *pages, int32_t *
     if (!d_ref_out || !d_table_out || !d_map || !d_live) return cr_fail(ctx, CR_EINVAL, "cr_pages_compact: NULL output");
     if (d_ref_out == pages->d_ref || d_table_out == pages->d_table)
         return cr_fail(ctx, CR_EINVAL, "cr_pages_compact: the outputs must be arrays of their own");
-    const pages_in P = input(ctx, pages);
+    const pages_in P = cr_pages_input(ctx, pages);
     pages_scan S;
     CR_TRY(scan_mem(ctx, pages, 0, S));
     const int32_t *none = nullptr;
@@ -677,9 +663,23 @@ extern "C" int cr_kv_write(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t layer
     if (n > (1u << 24) || n_tokens > (1u << 30)) return cr_fail(ctx, CR_EINVAL, "cr_kv_write: too many entries or tokens");
     if (!n || !n_tokens) return CR_OK;
     if (!d_k || !d_v || !d_cu) return cr_fail(ctx, CR_EINVAL, "cr_kv_write: NULL pointer");
+    if (cr_in_8bit(pages->dtype)) {
+        cr_append_args A = {};
+        A.d_k = d_k;
+        A.d_v = d_v;
+        A.k_token = k_token;
+        A.k_head = k_head;
+        A.v_token = v_token;
+        A.v_head = v_head;
+        A.d_cu = d_cu;
+        A.d_seqs = d_seqs;
+        A.n = n;
+        A.n_tokens = n_tokens;
+        return cr_append(ctx, "cr_kv_write", pages, layer, nullptr, &A);
+    }
     if (((uintptr_t)d_k & 15) || ((uintptr_t)d_v & 15) || ((k_token | k_head | v_token | v_head) & 7))
         return cr_fail(ctx, CR_EINVAL, "cr_kv_write: keys and values must be 16-byte aligned, strides multiples of 8");
-    const pages_in P = input(ctx, pages);
+    const pages_in P = cr_pages_input(ctx, pages);
     write_in W = {static_cast<const uint16_t *>(d_k), static_cast<const uint16_t *>(d_v), k_token, k_head, v_token, v_head,
                   d_cu, d_seqs, n, n_tokens, 0};
     // few tokens: more warps on each, as long as they have words to move
