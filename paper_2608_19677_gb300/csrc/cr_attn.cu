@@ -544,25 +544,34 @@ struct rows_cfg {
     static constexpr int kCode0 = (2 + kStages) * kTile, kXch = kCode0 + kCodes * kCodeTile;
     static constexpr int kPieces = kXch + 4 * kRowsTile * 4, kBars = kPieces + 2 * 48;
     static constexpr int kScales = kBars + 8 * (26 + 2 * kStages + 2 * kCodes);
-    static constexpr int kSmem = kScales + 64 * kCodes + 16;
+    static constexpr int kRefs = kScales + 64 * kCodes;  // of eight tiles, keys and values
+    static constexpr int kSmem = kRefs + (E8 ? 64 : 0) + 16;
     static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
 };
 // Warps 0-15: softmax (tile, half of the keys, 32 rows); 16: products; 17: copies; 18, 19 make the
 // warpgroup whole, whose registers go to the softmax threads: 512 x 104 + 128 x 64 = 640 x 96.
 constexpr int kRowsThreads = 640;
-// Keys and values in 8 bits: warps 18 and 19 make 16-bit tiles of them, times their blocks' powers of two (exact in
-// the 16-bit type), and zeros of what is behind the sequence; the rest is the same.
+// Keys and values in 8 bits: warps 18 and 19 make tiles of halves of them, and zeros of what is behind the sequence; the
+// products are of halves whatever the queries' type.  So that these are enough, each tile's largest power of two R
+// becomes 2^7 in the tile: the others are exact while they are above 2^-22 R, and off by less than 2^-31 R otherwise.
+// The softmax threads multiply scores by R of the keys' tile; values' R is the largest of the piece so far, and as it grows
+// the accumulator is scaled.  They also bring each row of bfloat16 queries to 2^14 .. 2^15 by a power of two (k_attn_few8),
+// and hold weights 2^6 times larger, so that those below the row's largest by 2^20 are still rounded to 11 bits.
+// (Tiles of bfloat16, exact without R: twice the instructions, two warps could not keep up: 40 suffixes of 1 to 128
+// tokens over prefixes to 16,384, 32/4 heads of 128: 249 us.)
 constexpr int kRowsWiden = 2;
+constexpr float kLift = 6.f;  // of the weights' logarithms
 
 enum { B_QFULL, B_QEMPTY, B_DONE, B_SFULL, B_PREADY = B_SFULL + 2, B_OFULL = B_PREADY + 4, B_OEMPTY = B_OFULL + 2,
-       B_PFULL = B_OEMPTY + 2, B_PEMPTY = B_PFULL + 2, B_LREAD = B_PEMPTY + 2, B_FULL = B_LREAD + 8 };
+       B_PFULL = B_OEMPTY + 2, B_PEMPTY = B_PFULL + 2, B_LREAD = B_PEMPTY + 2, B_QREADY = B_LREAD + 8, B_FULL };
 
 // What the copying warp tells the others of a piece (two of them are kept).
 struct rows_piece {
     int row0, ntok, klen, diag;
     int h, t0, n, slot;  // n: key tiles, 0: no more pieces
     int stage, phase;    // of the ring, at its first keys
-    int pad[2];
+    int tiles;           // of pieces before
+    int pad;
 };
 static_assert(sizeof(rows_piece) == 48, "shared memory of the pieces");
 
@@ -612,6 +621,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             cr_bar_init(BAR(B_PEMPTY + x), E8 ? 17 + kRowsWiden : 17);
         }
         for (int i = 0; i < 8; ++i) cr_bar_init(BAR(B_LREAD + i), 2);
+        cr_bar_init(BAR(B_QREADY), 16);
         for (int s = 0; s < cfg::kStages; ++s) {
             cr_bar_init(FULL(s), E8 ? kRowsWiden : 1);
             cr_bar_init(EMPTY(s), 1);
@@ -641,7 +651,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     if (warp == 17) {
         // ---- copies ----
         const uint32_t q_bytes = A.G * A.tq * 128 * cfg::kChunks;
-        uint32_t stage = 0, phase = 0;
+        uint32_t stage = 0, phase = 0, tiles = 0;
         walk w;
         w.begin(A.start + blockIdx.x, A.blk);
         for (;;) {
@@ -660,11 +670,13 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                     p->slot = w.slot();
                     p->stage = (int)stage;
                     p->phase = (int)phase;
+                    if (E8) p->tiles = (int)tiles;
                 }
                 cr_bar_arrive(BAR(B_PFULL + (pieces & 1)));
             }
             __syncwarp();
             if (!more) break;
+            tiles += w.t1 - w.t0;
             if (A.to_pfx && lane == 0) {
                 const uint64_t at = (uint64_t)w.k.row0 * A.kv_heads + w.h;
                 if (w.t0 == 0) A.first_cta[at] = (int)blockIdx.x;
@@ -749,7 +761,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     } else if (warp == 16) {
         // ---- products ----
         const uint32_t me = cr_elect();
-        const uint32_t id_s = cr_idesc(BF16, 128, 128, false), id_o = cr_idesc(BF16, 128, D, true);
+        const uint32_t id_s = cr_idesc(BF16 && !E8, 128, 128, false), id_o = cr_idesc(BF16 && !E8, 128, D, true);
         uint32_t stage = 0, phase = 0, pphase[2] = {0, 0}, ophase[2] = {0, 0};
         auto scores = [&](int x, uint32_t st) {
             const uint32_t a = sq + x * cfg::kTile, b = ring + st * cfg::kTile;
@@ -803,7 +815,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             const bool two = __shfl_sync(~0u, p->ntok, 0) > (int)A.tq;
             if (lane == 0) cr_bar_arrive(BAR(B_PEMPTY + (pieces & 1)));
             if (n == 0) break;
-            if (!cr_bar_wait(BAR(B_QFULL), pieces & 1, &gave_up)) goto out;
+            if (!cr_bar_wait(BAR(E8 && BF16 ? B_QREADY : B_QFULL), pieces & 1, &gave_up)) goto out;
             if (!cr_bar_wait(FULL(stage), phase, &gave_up)) goto out;
             cr_tc_after();
             scores(0, stage);
@@ -834,8 +846,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         cr_tc_commit(BAR(B_DONE), me);  // the shared memory is in use until the last product has ended
         cr_bar_wait(BAR(B_DONE), 0, &gave_up);
     } else if (E8 && warp >= 18) {
-        // ---- 16-bit tiles ----
-        uint32_t stage = 0, phase = 0, code = 0, cphase = 0;
+        // ---- tiles of halves: a lane widens rows of its own ----
+        uint32_t stage = 0, phase = 0, code = 0, cphase = 0, tile = 0;
         for (;; ++pieces) {
             if (!cr_bar_wait(BAR(B_PFULL + (pieces & 1)), (pieces >> 1) & 1, &gave_up)) goto out;
             const volatile rows_piece *p = piece + (pieces & 1);
@@ -844,33 +856,48 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             __syncwarp();
             if (lane == 0) cr_bar_arrive(BAR(B_PEMPTY + (pieces & 1)));
             if (n == 0) break;
+            float top = 0.f;  // values' largest power so far
             for (int j = 0; j < 2 * n; ++j) {
                 if (!cr_bar_wait(CODES(code), cphase, &gave_up)) goto out;
+                const uint32_t sc = sq + cfg::kScales + code * 64;
+                uint32_t r;
+                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r) : "r"(sc + (lane & 15) * 4));
+                float ref = __uint_as_float(__reduce_max_sync(~0u, r));
+                if (j & 1) ref = top = fmaxf(top, ref);
+                if (ref == 0.f) ref = 1.f;  // no keys
+                const float per = 128.f / ref;
                 if (!cr_bar_wait(EMPTY(stage), phase ^ 1, &gave_up)) goto out;
+                if (warp == 18 && lane == 0)
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(sq + cfg::kRefs + (j & 1) * 32 + (tile & 7) * 4), "f"(ref * 0x1p-7f)
+                                 : "memory");
 #pragma unroll 1
-                for (uint32_t r = (warp - 18) * 32 + lane; r < (uint32_t)kRowsTile; r += 32 * kRowsWiden) {
+                for (uint32_t row = (warp - 18) * 32 + lane; row < (uint32_t)kRowsTile; row += 32 * kRowsWiden) {
                     float scale;  // 0: no page
-                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(scale) : "r"(sq + cfg::kScales + code * 64 + (r >> 3) * 4));
-                    const bool live = (int)r < left && scale != 0.f;
-                    const uint32_t src = sq + cfg::kCode0 + code * cfg::kCodeTile + r * D, turn = D == 128 ? r & 7 : (r >> 1) & 3;
-                    const uint32_t dst = ring + stage * cfg::kTile + r * 128;
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(scale) : "r"(sc + (row >> 3) * 4));
+                    const bool live = (int)row < left && scale != 0.f;
+                    const __half2 f = __float2half2_rn(scale * per);
+                    const uint32_t src = sq + cfg::kCode0 + code * cfg::kCodeTile + row * D, turn = D == 128 ? row & 7 : (row >> 1) & 3;
+                    const uint32_t dst = ring + stage * cfg::kTile + row * 128;
+                    uint32_t q[D / 16][4];
 #pragma unroll
-                    for (uint32_t c = 0; c < D / 16; ++c) {
-                        uint32_t q[4], o[8];
+                    for (uint32_t c = 0; c < D / 16; ++c)
                         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                                     : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3])
+                                     : "=r"(q[c][0]), "=r"(q[c][1]), "=r"(q[c][2]), "=r"(q[c][3])
                                      : "r"(src + ((c ^ turn) << 4)));
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) cr_widen4<BF16>(q[e], scale, o[2 * e], o[2 * e + 1]);
-                        if (!live) {
+                    for (uint32_t c = 0; c < D / 16; ++c) {
+                        uint32_t o[8];
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) o[e] = 0;
+                        for (int e = 0; e < 8; ++e) {
+                            const uint32_t h = cr_e4m3_pair(e & 1 ? q[c][e / 2] >> 16 : q[c][e / 2]);
+                            const __half2 y = __hmul2(*reinterpret_cast<const __half2 *>(&h), f);
+                            o[e] = live ? *reinterpret_cast<const uint32_t *>(&y) : 0u;
                         }
                         const uint32_t to = dst + (c >> 2) * (kRowsTile * 128), u = (c & 3) * 2;
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((u ^ (r & 7)) << 4)), "r"(o[0]),
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((u ^ (row & 7)) << 4)), "r"(o[0]),
                                      "r"(o[1]), "r"(o[2]), "r"(o[3])
                                      : "memory");
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((u + 1) ^ (r & 7)) << 4)), "r"(o[4]),
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((u + 1) ^ (row & 7)) << 4)), "r"(o[4]),
                                      "r"(o[5]), "r"(o[6]), "r"(o[7])
                                      : "memory");
                     }
@@ -889,7 +916,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                     code = 0;
                     cphase ^= 1;
                 }
-                if (j & 1) left -= kRowsTile;
+                if (j & 1) {
+                    left -= kRowsTile;
+                    ++tile;
+                }
             }
         }
     } else if (warp < 16) {
@@ -901,8 +931,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         const uint32_t ts = tmem + ((warp & 3) << 21) + x * 128 + half * 64;
         const uint32_t to = tmem + ((warp & 3) << 21) + 256 + x * D + half * (D / 2);
         const uint32_t pair = 1 + x * 4 + (warp & 3);  // barrier of the two warps that share rows
-        const float c = A.c;
-        const unsigned long long c2 = cr_pair(c, c);
+        const float c = E8 ? 1.f : A.c;  // 8 bits: scores are scaled as they come, m is a base-2 logarithm
         const int tok = x * (int)A.tq + (int)(row / A.G), hd = row < A.G * A.tq ? (int)(row % A.G) : -1;
         uint32_t sphase = 0;
         // The other half's value of this row.  The next value is written only after the other warp has read this
@@ -922,9 +951,45 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             if (n == 0) break;
             if (x == 1 && p->ntok <= (int)A.tq) {
                 __syncwarp();
-                if (lane == 0) cr_bar_arrive(BAR(B_PEMPTY + (pieces & 1)));
+                if (lane == 0) {
+                    cr_bar_arrive(BAR(B_PEMPTY + (pieces & 1)));
+                    if (E8 && BF16) cr_bar_arrive(BAR(B_QREADY));
+                }
                 continue;
             }
+            float cq = A.c;
+            if constexpr (E8 && BF16) {
+                if (!cr_bar_wait(BAR(B_QFULL), pieces & 1, &gave_up)) goto left;
+                constexpr int kC = D / 16;  // chunks of eight elements
+                const uint32_t at = sq + x * cfg::kTile + (D == 128 ? half * (kRowsTile * 128) : half * 64) + row * 128;
+                const uint32_t turn = row & (D == 128 ? 7 : 3);
+                uint32_t q[kC][4], most = 0;
+#pragma unroll
+                for (uint32_t k = 0; k < kC; ++k) {
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                 : "=r"(q[k][0]), "=r"(q[k][1]), "=r"(q[k][2]), "=r"(q[k][3])
+                                 : "r"(at + ((k ^ turn) << 4)));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) most = max(most, max(q[k][e] << 16 & 0x7fffffffu, q[k][e] & 0x7fff0000u));
+                }
+                most = max(most, __float_as_uint(exchange(__uint_as_float(most))));
+                const int up = max(-113, min(113, 14 + 127 - (int)(most >> 23)));
+                const float f = __uint_as_float((uint32_t)(127 + up) << 23);
+                cq *= __uint_as_float((uint32_t)(127 - up) << 23);
+#pragma unroll
+                for (uint32_t k = 0; k < kC; ++k) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        q[k][e] = cr_pack16<false>(__uint_as_float(q[k][e] << 16) * f, __uint_as_float(q[k][e] & 0xffff0000u) * f);
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + ((k ^ turn) << 4)), "r"(q[k][0]), "r"(q[k][1]),
+                                 "r"(q[k][2]), "r"(q[k][3])
+                                 : "memory");
+                }
+                cr_fence_async_smem();
+                __syncwarp();
+                if (lane == 0) cr_bar_arrive(BAR(B_QREADY));
+            }
+            float unit = 0.f;  // of the accumulator
             // keys that this row sees, from the first tile's on; the tile with the sequence's end
             int seen = p->klen - p->t0 * kRowsTile - half * 64;
             const int tail = !E8 && x == 0 && half < cfg::kChunks ? (p->klen >> 7) - p->t0 : -1;
@@ -953,6 +1018,14 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                 }
                 float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                 top = fmaxf(top, exchange(top));
+                unsigned long long c2 = cr_pair(c, c);
+                if (E8) {
+                    float ct;
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ct) : "r"(sq + cfg::kRefs + ((p->tiles + j) & 7) * 4));
+                    ct *= cq;
+                    top *= ct;
+                    c2 = cr_pair(ct, ct);
+                }
                 // The maximum may lag by 2^8: weights stay below 2^8, sums below 2^31, and the
                 // accumulator is scaled a few times per row instead of at every tile.
                 const bool grow = j == 0 || !((top - m) * c <= 8.f || top == m);
@@ -990,7 +1063,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                     }
                     cr_fence_async_smem();
                 }
-                const float off = m == -INFINITY ? 0.f : -m * c;
+                float off = m == -INFINITY ? 0.f : -m * c;
+                if (E8) off += kLift;
                 const unsigned long long off2 = cr_pair(off, off);
                 unsigned long long sum[2] = {0ull, 0ull};
 #pragma unroll
@@ -1004,9 +1078,28 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                         a = cr_exp2(a);
                         b = cr_exp2(b);
                         sum[e & 1] = cr_add2(sum[e & 1], cr_pair(a, b));
-                        w[e] = cr_pack16<BF16>(a, b);
+                        w[e] = cr_pack16<BF16 && !E8>(a, b);
                     }
                     cr_tmem_st16(ts + part * 16, w);
+                    if (E8 && part == 0) {
+                        const uint32_t tile = (uint32_t)p->tiles + j, at = 2 * tile + 1;
+                        if (!cr_bar_wait(FULL(at % cfg::kStages), (at / cfg::kStages) & 1, &gave_up)) goto left;
+                        float now;
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(now) : "r"(sq + cfg::kRefs + 32 + (tile & 7) * 4));
+                        if (now != unit && j > 0) {
+                            const float f = unit / now;
+#pragma unroll 1
+                            for (int i = 0; i < D / 2; i += 16) {
+                                uint32_t o[16];
+                                cr_tmem_ld16(to + i, o);
+                                cr_tmem_ld_wait();
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                                cr_tmem_st16(to + i, o);
+                            }
+                        }
+                        unit = now;
+                    }
                     cr_tmem_st_wait();
                     cr_tc_before();
                     __syncwarp();
@@ -1030,7 +1123,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             const int slot = p->slot;
             const int head = p->h * (int)A.G + hd;
             const uint64_t tk = (uint64_t)(p->row0 + tok);
-            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const float inv = l == 0.f ? 0.f : E8 ? unit / l : 1.f / l;
             if (!cr_bar_wait(BAR(B_OFULL + x), ophase, &gave_up)) goto left;
             ophase ^= 1;
             cr_tc_after();
@@ -1043,6 +1136,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                     uint32_t o[16];
                     cr_tmem_ld16(to + i, o);
                     cr_tmem_ld_wait();
+                    if (E8) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * unit);
+                    }
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         dst[(i / 4 + e) * RP] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]),
@@ -1050,7 +1147,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                 }
                 if (half == 0)
                     reinterpret_cast<float2 *>(A.part_ml)[(uint64_t)slot * RP + r] =
-                        make_float2(m == -INFINITY ? m : m * c, l);
+                        make_float2(m == -INFINITY ? m : (E8 ? m - kLift : m * c), l);
             } else {
                 if (!A.to_pfx && A.o_wide && A.head_dim == D) {
                     // Lanes of a group of C hold C chunks of 32 bytes of a row each; the chunks change places, so that a
@@ -1122,7 +1219,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                     }
                 }
                 if (valid && half == 0) {
-                    const float lse2 = l == 0.f ? -INFINITY : m * c + log2f(l);
+                    const float lse2 = l == 0.f ? -INFINITY : (E8 ? m - kLift : m * c) + log2f(l);
                     if (A.to_pfx)
                         A.pfx_lse[tk * A.q_heads + head] = lse2;
                     else if (A.lse)
@@ -1665,18 +1762,23 @@ out:
 // ---- few rows over 8 bits -----------------------------------------------------------------------
 // As k_attn_few with half of the bytes.  Numbers are widened to half precision in registers (exact), and the rest of
 // a product's arithmetic is arranged so that halves are enough:
-//   a row of bfloat16 queries is first multiplied by a power of two that brings its largest element to 2^14 .. 2^15
+//   a head's bfloat16 query is first multiplied by a power of two that brings its largest element to 2^14 .. 2^15
 //   (elements 2^28 below it are still exact); scores are 32-bit sums, times that power's inverse and the key block's;
-//   weights are multiplied by their value block's power over the largest, E, that the warp has met, and by 2^15: they
-//   are rounded to 11 bits as long as a block's power is above 2^-29 E, and are off by less than 2^-40 E otherwise.
-// The contraction's order is free, so a lane takes what lies together: for scores D/4 consecutive elements of a key, for
-// values 16 (8) consecutive elements of four keys, whose bytes it pairs up.
+//   weights (at most 2^8, see below) are multiplied by their value block's power over the largest, E, that the warp has
+//   met, and by 2^7: they are rounded to 11 bits as long as that is above 2^-14, and are off by less than 2^-31 E
+//   otherwise.
+// Keys and values are the products' 16-row operand and heads the 8-column one, so that up to eight heads waste nothing
+// (scores come out key by head, weights go back in head by key: movmatrix turns them).  The contraction's order is free,
+// and so is that of the rows: a lane takes what lies together, for scores D/4 consecutive elements of two keys, for
+// values D/8 consecutive elements of four keys, whose bytes it pairs up.
+// A head's maximum may lag by 2^8: then a step needs no exchange between lanes but one vote.
 template <int D>
 struct few8_cfg {
     static constexpr int kTile = kFewTile * D;            // bytes of 64 keys
     static constexpr int kStages = D == 128 ? 6 : 12;
     static constexpr int kQ = 16 * D * 2;
-    static constexpr int kJoin = kFewWarps * 8 * 64 * 4;
+    static constexpr int kJoinRow = 68;                   // floats
+    static constexpr int kJoin = kFewWarps * 8 * kJoinRow * 4;
     static constexpr int kSmem = kStages * 2 * kTile + kQ + kJoin + 1024;
 };
 
@@ -1688,10 +1790,10 @@ __global__ void __launch_bounds__(kFewThreads, 2)
     using cfg = few8_cfg<D>;
     constexpr int kDims = D / 4;      // elements of a key that a lane takes
     constexpr int kRun = D / 8;       // elements of a value that a lane takes
-    constexpr uint32_t kR = WIDE ? 2 : 1;
+    constexpr int kN = WIDE ? 2 : 1;  // groups of eight heads
     extern __shared__ unsigned char dyn[];
     __shared__ __align__(8) unsigned long long bars[2 * cfg::kStages + 3];
-    __shared__ float scales[cfg::kStages][16];  // of eight groups of eight keys, and values
+    __shared__ __align__(16) float scales[cfg::kStages][16];  // of eight groups of eight keys, and values
     __shared__ float2 join_ml[kFewWarps][16];
     __shared__ int gave_up;
     __shared__ own_list list;
@@ -1799,17 +1901,13 @@ __global__ void __launch_bounds__(kFewThreads, 2)
             const uint32_t sub = w.h % A.nsub;
             const uint32_t h0 = w.h / A.nsub * A.G + sub * 16;  // first query head of the rows
             const uint32_t rows = min(16u, A.G - sub * 16);
-            uint32_t qa[D / 16][4];
-            float cr[kR];  // what makes scores of sums
+            uint32_t qb[kN][D / 16][2];  // head 8 n + r4
+            float cs[kN][2];             // what makes scores of sums: heads 8 n + 2 q4 and the next
             if (!cr_bar_wait(QFULL, qphase, &gave_up)) goto out;
             qphase ^= 1;
-            if (!WIDE) {
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i) qa[i][1] = qa[i][3] = 0;
-            }
-#pragma unroll
-            for (uint32_t r = 0; r < kR; ++r) {
-                const uint32_t row = r4 + 8 * r;
+            for (int n = 0; n < kN; ++n) {
+                const uint32_t row = r4 + 8 * n;
                 uint32_t x[kDims / 2];
 #pragma unroll
                 for (int k = 0; k < kDims / 8; ++k) {
@@ -1818,7 +1916,7 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                                  : "=r"(x[4 * k]), "=r"(x[4 * k + 1]), "=r"(x[4 * k + 2]), "=r"(x[4 * k + 3])
                                  : "r"(sq + (u >> 3) * (16 * 128) + row * 128 + (((u & 7) ^ (row & 7)) << 4)));
                 }
-                cr[r] = A.c;
+                float c = A.c;
                 if (BF16) {
                     uint32_t top = 0;  // the largest magnitude's bits
 #pragma unroll
@@ -1827,27 +1925,35 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                     top = max(top, __shfl_xor_sync(~0u, top, 2));
                     const int up = max(-113, min(113, 14 + 127 - (int)(top >> 23)));
                     const float f = __uint_as_float((uint32_t)(127 + up) << 23);
-                    cr[r] *= __uint_as_float((uint32_t)(127 - up) << 23);
+                    c *= __uint_as_float((uint32_t)(127 - up) << 23);
 #pragma unroll
                     for (int k = 0; k < kDims / 2; ++k)
                         x[k] = cr_pack16<false>(__uint_as_float(x[k] << 16) * f, __uint_as_float(x[k] & 0xffff0000u) * f);
                 }
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) {
-                    qa[i][r] = x[2 * i];
-                    qa[i][2 + r] = x[2 * i + 1];
+                    qb[n][i][0] = x[2 * i];
+                    qb[n][i][1] = x[2 * i + 1];
                 }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) cs[n][e] = __shfl_sync(~0u, c, (2 * q4 + e) * 4);
             }
             __syncwarp();
             if (lane == 0) cr_bar_arrive(QEMPTY);
-            // o[t]: elements (2 q4) kRun + t and (2 q4 + 1) kRun + t of rows r4 and r4 + 8, in units of 2^-15 E
-            float o[D / 8][4];
+            // o[n][t]: elements r4 kRun + 2 t (0, 1) and the next (2, 3) of heads 8 n + 2 q4 (0, 2) and the next (1, 3),
+            // in units of 2^-7 E
+            float o[kN][D / 16][4];
+            float m[kN][2], l[kN][2];
 #pragma unroll
-            for (int i = 0; i < D / 8; ++i)
+            for (int n = 0; n < kN; ++n) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
-            float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-            float E = 0.f, per_E = 0.f;  // per_E: 2^15 / E
+                for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[n][i][e] = 0.f;
+                m[n][0] = m[n][1] = -1e30f;  // below every score: the first that is seen is above it by more than may be
+                l[n][0] = l[n][1] = 0.f;
+            }
+            float E = 0.f, per_E = 0.f;  // per_E: 2^7 / E
             for (uint32_t t = w.t0; t < w.t1; ++t) {
                 if (!cr_bar_wait(FULL(stage), phase, &gave_up)) goto out;
                 const int key = (int)((w.k.lo / kFewTile + t) * kFewTile + warp * 16);  // this warp's first key
@@ -1856,97 +1962,121 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                     const uint32_t kt = ring + stage * 2 * cfg::kTile, vt = kt + cfg::kTile;
                     const float2 ks = *reinterpret_cast<const float2 *>(&scales[stage][2 * warp]);
                     const float2 vs = *reinterpret_cast<const float2 *>(&scales[stage][8 + 2 * warp]);
-                    float s[2][4] = {};
+                    // keys warp 16 + r4 and 8 more
+                    uint32_t c4[2][kDims / 4];
 #pragma unroll
                     for (int g = 0; g < 2; ++g) {
                         const uint32_t kr = warp * 16 + g * 8 + r4, turn = D == 128 ? kr & 7 : (kr >> 1) & 3;
 #pragma unroll
-                        for (int k = 0; k < kDims / 16; ++k) {
-                            uint32_t c4[4];
+                        for (int k = 0; k < kDims / 16; ++k)
                             asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                                         : "=r"(c4[0]), "=r"(c4[1]), "=r"(c4[2]), "=r"(c4[3])
+                                         : "=r"(c4[g][4 * k]), "=r"(c4[g][4 * k + 1]), "=r"(c4[g][4 * k + 2]), "=r"(c4[g][4 * k + 3])
                                          : "r"(kt + kr * D + (((q4 * (kDims / 16) + k) ^ turn) << 4)));
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                mma16816<false>(s[g], qa[4 * k + i], cr_e4m3_pair(c4[i]), cr_e4m3_pair(c4[i] >> 16));
-                        }
                     }
-                    uint32_t keep[2] = {~0u, ~0u};  // halves of v's registers that are seen
+                    // four keys' runs; words of four elements
+                    uint32_t v[4][kRun / 4];
+                    auto load_values = [&]() {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t vr = warp * 16 + (e >> 1) * 8 + 2 * q4 + (e & 1);
+                            if (D == 128) {
+                                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                             : "=r"(v[e][0]), "=r"(v[e][1]), "=r"(v[e][kRun / 4 - 2]), "=r"(v[e][kRun / 4 - 1])
+                                             : "r"(vt + vr * D + ((r4 ^ (vr & 7)) << 4)));
+                            } else {
+                                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];"
+                                             : "=r"(v[e][0]), "=r"(v[e][1])
+                                             : "r"(vt + vr * D + (((r4 >> 1) ^ ((vr >> 1) & 3)) << 4) + (r4 & 1) * 8));
+                            }
+                        }
+                    };
+                    if (!WIDE) load_values();  // sixteen heads leave no registers for them yet
+                    float s[kN][2][4] = {};  // two sums, so that a product does not wait for the one before
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) {
+                        const uint32_t a[4] = {cr_e4m3_pair(c4[0][i]), cr_e4m3_pair(c4[1][i]), cr_e4m3_pair(c4[0][i] >> 16),
+                                               cr_e4m3_pair(c4[1][i] >> 16)};
+#pragma unroll
+                        for (int n = 0; n < kN; ++n) mma16816<false>(s[n][i & 1], a, qb[n][i][0], qb[n][i][1]);
+                    }
+                    float x[kN][4];  // base-2 logarithms
+                    bool over = false;
+#pragma unroll
+                    for (int n = 0; n < kN; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[n][e] = (s[n][0][e] + s[n][1][e]) * (cs[n][e & 1] * (e < 2 ? ks.x : ks.y));
                     if (!see.all()) {
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
+                        for (int e = 0; e < 4; ++e)
+                            if (!see.sees((e >> 1) * 8 + (int)r4))
+#pragma unroll
+                                for (int n = 0; n < kN; ++n) x[n][e] = -INFINITY;
+                    }
+#pragma unroll
+                    for (int n = 0; n < kN; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) over |= x[n][e] - m[n][e & 1] > 8.f;
+                    const float most = fmaxf(vs.x, vs.y);
+                    if (__any_sync(~0u, over) || most > E) {
+                        float grown = 1.f;  // of E
+                        if (most > E) {
+                            grown = E / most;
+                            E = most;
+                            per_E = 128.f / E;
+                        }
+#pragma unroll
+                        for (int n = 0; n < kN; ++n) {
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
-                                if (!see.sees(i * 8 + (int)q4 * 2 + e)) {
-                                    s[i][e] = s[i][2 + e] = -INFINITY;
-                                    keep[i] &= e ? 0x0000ffffu : 0xffff0000u;
+                                float top = fmaxf(x[n][e], x[n][2 + e]);
+                                top = fmaxf(top, __shfl_xor_sync(~0u, top, 4));
+                                top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
+                                top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
+                                const float m_new = fmaxf(m[n][e], top);
+                                float r = m_new == m[n][e] ? 1.f : cr_exp2(m[n][e] - m_new);
+                                m[n][e] = m_new;
+                                l[n][e] *= r;
+                                r *= grown;
+#pragma unroll
+                                for (int i = 0; i < D / 16; ++i) {
+                                    o[n][i][e] *= r;
+                                    o[n][i][2 + e] *= r;
                                 }
                             }
                         }
                     }
-                    float grown = 1.f;  // of E
-                    const float most = fmaxf(vs.x, vs.y);
-                    if (most > E) {
-                        grown = E / most;
-                        E = most;
-                        per_E = 32768.f / E;
-                    }
                     const float by[2] = {vs.x * per_E, vs.y * per_E};
-                    uint32_t pa[4];
+                    uint32_t pb[kN][2];
 #pragma unroll
-                    for (uint32_t r = 0; r < kR; ++r) {
-                        const float f0 = cr[r] * ks.x, f1 = cr[r] * ks.y;
-                        float x[4] = {s[0][2 * r], s[0][2 * r + 1], s[1][2 * r], s[1][2 * r + 1]};
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (x[i] != -INFINITY) x[i] *= i < 2 ? f0 : f1;
-                        float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-                        top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
-                        top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
-                        const float m_new = fmaxf(m[r], top);
-                        if (__any_sync(~0u, m_new != m[r] || grown != 1.f)) {
-                            float f = m_new == m[r] ? 1.f : cr_exp2(m[r] - m_new);
-                            l[r] *= f;
-                            f *= grown;
-#pragma unroll
-                            for (int i = 0; i < D / 8; ++i) {
-                                o[i][2 * r] *= f;
-                                o[i][2 * r + 1] *= f;
-                            }
-                            m[r] = m_new;
-                        }
-                        const float off = m[r] == -INFINITY ? 0.f : m[r];
+                    for (int n = 0; n < kN; ++n) {
                         float p[4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) p[i] = cr_exp2(x[i] - off);
-                        l[r] += (p[0] + p[1]) + (p[2] + p[3]);
-                        pa[r] = cr_pack16<false>(p[0] * by[0], p[1] * by[0]);
-                        pa[2 + r] = cr_pack16<false>(p[2] * by[1], p[3] * by[1]);
-                    }
-                    if (!WIDE) pa[1] = pa[3] = 0;
-                    // four keys' runs; words of four elements
-                    uint32_t v[4][kRun / 4];
+                        for (int e = 0; e < 4; ++e) p[e] = cr_exp2(x[n][e] - m[n][e & 1]);
+                        l[n][0] += p[0] + p[2];
+                        l[n][1] += p[1] + p[3];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t vr = warp * 16 + (e >> 1) * 8 + 2 * q4 + (e & 1);
-                        if (D == 128) {
-                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                                         : "=r"(v[e][0]), "=r"(v[e][1]), "=r"(v[e][kRun / 4 - 2]), "=r"(v[e][kRun / 4 - 1])
-                                         : "r"(vt + vr * D + ((r4 ^ (vr & 7)) << 4)));
-                        } else {
-                            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];"
-                                         : "=r"(v[e][0]), "=r"(v[e][1])
-                                         : "r"(vt + vr * D + (((r4 >> 1) ^ ((vr >> 1) & 3)) << 4) + (r4 & 1) * 8));
-                        }
+                        for (int g = 0; g < 2; ++g)
+                            asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;"
+                                         : "=r"(pb[n][g])
+                                         : "r"(cr_pack16<false>(p[2 * g] * by[g], p[2 * g + 1] * by[g])));
+                    }
+                    if (WIDE) load_values();
+                    if (!see.all()) {  // what is not seen may be no number
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!see.sees((e >> 1) * 8 + (int)q4 * 2 + (e & 1)))
+#pragma unroll
+                                for (int i = 0; i < kRun / 4; ++i) v[e][i] = 0;
                     }
 #pragma unroll
                     for (int i = 0; i < kRun / 4; ++i) {
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {  // elements 4 i + 2 h and the next: bytes of two keys side by side
-                            const uint32_t a = __byte_perm(v[0][i], v[1][i], h ? 0x7362 : 0x5140);
-                            const uint32_t b = __byte_perm(v[2][i], v[3][i], h ? 0x7362 : 0x5140);
-                            mma16816<false>(o[4 * i + 2 * h], pa, cr_e4m3_pair(a) & keep[0], cr_e4m3_pair(b) & keep[1]);
-                            mma16816<false>(o[4 * i + 2 * h + 1], pa, cr_e4m3_pair(a >> 16) & keep[0], cr_e4m3_pair(b >> 16) & keep[1]);
+                            const uint32_t lo = __byte_perm(v[0][i], v[1][i], h ? 0x7362 : 0x5140);
+                            const uint32_t hi = __byte_perm(v[2][i], v[3][i], h ? 0x7362 : 0x5140);
+                            const uint32_t a[4] = {cr_e4m3_pair(lo), cr_e4m3_pair(lo >> 16), cr_e4m3_pair(hi), cr_e4m3_pair(hi >> 16)};
+#pragma unroll
+                            for (int n = 0; n < kN; ++n) mma16816<false>(o[n][2 * i + h], a, pb[n][0], pb[n][1]);
                         }
                     }
                 }
@@ -1957,31 +2087,40 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                     phase ^= 1;
                 }
             }
-            // ---- the four warps' states join: eight rows and 64 columns at a time, four columns a thread ----
-            const float unit = E * 0x1p-15f;
+            // ---- the four warps' states join: eight heads and 64 columns at a time, four columns a thread ----
+            const float unit = E * 0x1p-7f;
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                l[r] += __shfl_xor_sync(~0u, l[r], 1);
-                l[r] += __shfl_xor_sync(~0u, l[r], 2);
-                if (q4 == 0) join_ml[warp][r4 + 8 * r] = make_float2(m[r], l[r]);
-            }
+            for (int n = 0; n < kN; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float x = l[n][e];
+                    x += __shfl_xor_sync(~0u, x, 4);
+                    x += __shfl_xor_sync(~0u, x, 8);
+                    x += __shfl_xor_sync(~0u, x, 16);
+                    if (r4 == 0) join_ml[warp][8 * n + 2 * q4 + e] = make_float2(x == 0.f ? -INFINITY : m[n][e], x);
+                }
             const int slot = w.slot();
             // a whole block that a shared prefix still joins has a place of its own
             const bool to_own = slot < 0 && w.k.lo > 0;
             const uint64_t place = to_own ? (uint64_t)w.k.row0 * A.few_heads + w.h : (uint64_t)slot;
             float *part = to_own ? A.own : A.part, *part_ml = to_own ? A.own_ml : A.part_ml;
 #pragma unroll
-            for (int pass = 0; pass < (int)kR * (D / 64); ++pass) {
-                const int r = pass / (D / 64), ch = pass % (D / 64);
-                if (rows <= 8u * r) break;
-                // place (i, run): element run * kRun + ch * 8 + i
+            for (int pass = 0; pass < kN * (D / 64); ++pass) {
+                const int n = pass / (D / 64), ch = pass % (D / 64);
+                if (rows <= 8u * n) break;
+                // column 8 r + i: element r kRun + ch * 8 + i
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    *reinterpret_cast<float2 *>(join + (warp * 8 + r4) * 64 + i * 8 + q4 * 2) =
-                        make_float2(o[ch * 8 + i][2 * r] * unit, o[ch * 8 + i][2 * r + 1] * unit);
+                for (int e = 0; e < 2; ++e) {
+                    float *to = join + (warp * 8 + 2 * q4 + e) * cfg::kJoinRow + r4 * 8;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        *reinterpret_cast<float4 *>(to + 4 * i) =
+                            make_float4(o[n][ch * 4 + 2 * i][e] * unit, o[n][ch * 4 + 2 * i][2 + e] * unit,
+                                        o[n][ch * 4 + 2 * i + 1][e] * unit, o[n][ch * 4 + 2 * i + 1][2 + e] * unit);
+                }
                 if (!meet()) goto out;
-                const uint32_t rr = threadIdx.x >> 4, col = threadIdx.x & 15, i0 = (col & 1) * 4, run = col >> 1, row = 8 * r + rr;
-                const uint32_t d4 = (run * kRun + ch * 8 + i0) / 4;
+                const uint32_t rr = threadIdx.x >> 4, col = threadIdx.x & 15, row = 8 * n + rr;
+                const uint32_t d4 = ((col >> 1) * kRun + ch * 8 + (col & 1) * 4) / 4;
                 if (row < rows) {
                     const uint64_t oh = (uint64_t)w.k.row0 * A.q_heads + h0 + row;
                     float mm = -INFINITY, ll = 0.f;
@@ -1991,12 +2130,12 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                     for (int v = 0; v < kFewWarps; ++v) {
                         const float2 ml = join_ml[v][row];
                         const float f = ml.x == -INFINITY ? 0.f : cr_exp2(ml.x - mm);
-                        const float *x = join + (v * 8 + rr) * 64 + i0 * 8 + run;
+                        const float4 x = *reinterpret_cast<const float4 *>(join + (v * 8 + rr) * cfg::kJoinRow + 4 * col);
                         ll += ml.y * f;
-                        s.x += x[0] * f;
-                        s.y += x[8] * f;
-                        s.z += x[16] * f;
-                        s.w += x[24] * f;
+                        s.x += x.x * f;
+                        s.y += x.y * f;
+                        s.z += x.z * f;
+                        s.w += x.w * f;
                     }
                     if (slot >= 0 || to_own) {
                         reinterpret_cast<float4 *>(part)[(place * (D / 4) + d4) * 16 + row] = s;
