@@ -545,22 +545,23 @@ struct rows_cfg {
     static constexpr int kPieces = kXch + 4 * kRowsTile * 4, kBars = kPieces + 2 * 48;
     static constexpr int kScales = kBars + 8 * (26 + 2 * kStages + 2 * kCodes);
     static constexpr int kRefs = kScales + 64 * kCodes;  // of eight tiles, keys and values
-    static constexpr int kSmem = kRefs + (E8 ? 64 : 0) + 16;
+    static constexpr int kUp = kRefs + (E8 ? 64 : 0);    // of each query row, the power of two it was multiplied by
+    static constexpr int kSmem = kUp + (E8 ? 2 * kRowsTile : 0) + 16;
     static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
 };
 // Warps 0-15: softmax (tile, half of the keys, 32 rows); 16: products; 17: copies; 18, 19 make the
 // warpgroup whole, whose registers go to the softmax threads: 512 x 104 + 128 x 64 = 640 x 96.
 constexpr int kRowsThreads = 640;
-// Keys and values in 8 bits: warps 18 and 19 make tiles of halves of them, and zeros of what is behind the sequence; the
+// Keys and values in 8 bits: warps 18 to 21 make tiles of halves of them, and zeros of what is behind the sequence; the
 // products are of halves whatever the queries' type.  So that these are enough, each tile's largest power of two R
 // becomes 2^7 in the tile: the others are exact while they are above 2^-22 R, and off by less than 2^-31 R otherwise.
 // The softmax threads multiply scores by R of the keys' tile; values' R is the largest of the piece so far, and as it grows
-// the accumulator is scaled.  They also bring each row of bfloat16 queries to 2^14 .. 2^15 by a power of two (k_attn_few8),
-// and hold weights 2^6 times larger, so that those below the row's largest by 2^20 are still rounded to 11 bits.
-// (Tiles of bfloat16, exact without R: twice the instructions, two warps could not keep up: 40 suffixes of 1 to 128
-// tokens over prefixes to 16,384, 32/4 heads of 128: 249 us.)
-constexpr int kRowsWiden = 2;
+// the accumulator is scaled.  They hold weights 2^6 times larger, so that those below the row's largest by 2^20 are still
+// rounded to 11 bits, and bring each row of bfloat16 queries to 2^14 .. 2^15 by a power of two (k_attn_few8).
+// Tiles of bfloat16 would be exact without R, at twice the instructions.  Registers: 512 x 96 + 256 x 48 = 768 x 80.
+constexpr int kRowsWiden = 4;
 constexpr float kLift = 6.f;  // of the weights' logarithms
+__host__ __device__ constexpr int rows_threads(bool e8) { return e8 ? 768 : kRowsThreads; }
 
 enum { B_QFULL, B_QEMPTY, B_DONE, B_SFULL, B_PREADY = B_SFULL + 2, B_OFULL = B_PREADY + 4, B_OEMPTY = B_OFULL + 2,
        B_PFULL = B_OEMPTY + 2, B_PEMPTY = B_PFULL + 2, B_LREAD = B_PEMPTY + 2, B_QREADY = B_LREAD + 8, B_FULL };
@@ -570,13 +571,12 @@ struct rows_piece {
     int row0, ntok, klen, diag;
     int h, t0, n, slot;  // n: key tiles, 0: no more pieces
     int stage, phase;    // of the ring, at its first keys
-    int tiles;           // of pieces before
-    int pad;
+    int pad[2];
 };
 static_assert(sizeof(rows_piece) == 48, "shared memory of the pieces");
 
 template <int D, bool BF16, bool E8>
-__global__ void __launch_bounds__(kRowsThreads, 1)
+__global__ void __launch_bounds__(rows_threads(E8), 1)
     k_attn_rows(const __grid_constant__ attn_in A, const __grid_constant__ CUtensorMap map_q,
                 const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
 {
@@ -634,7 +634,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     }
     // query rows that no copy writes (128 is not a multiple of G) are zeros
     if (A.G * A.tq < kRowsTile)
-        for (uint32_t i = threadIdx.x; i < 2u * cfg::kTile / 16; i += kRowsThreads)
+        for (uint32_t i = threadIdx.x; i < 2u * cfg::kTile / 16; i += rows_threads(E8))
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(sq + 16 * i), "r"(0));
     cr_fence_async_smem();
     if (warp == 16) cr_tmem_alloc(cr_smem(&tmem_at), 512);
@@ -647,11 +647,16 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
 
     uint32_t pieces = 0;  // their number so far; they take two places in turn
 
-    if (warp >= 16) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (warp >= 16) {
+        if (E8)
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        else
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    }
     if (warp == 17) {
         // ---- copies ----
         const uint32_t q_bytes = A.G * A.tq * 128 * cfg::kChunks;
-        uint32_t stage = 0, phase = 0, tiles = 0;
+        uint32_t stage = 0, phase = 0;
         walk w;
         w.begin(A.start + blockIdx.x, A.blk);
         for (;;) {
@@ -670,13 +675,11 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                     p->slot = w.slot();
                     p->stage = (int)stage;
                     p->phase = (int)phase;
-                    if (E8) p->tiles = (int)tiles;
                 }
                 cr_bar_arrive(BAR(B_PFULL + (pieces & 1)));
             }
             __syncwarp();
             if (!more) break;
-            tiles += w.t1 - w.t0;
             if (A.to_pfx && lane == 0) {
                 const uint64_t at = (uint64_t)w.k.row0 * A.kv_heads + w.h;
                 if (w.t0 == 0) A.first_cta[at] = (int)blockIdx.x;
@@ -845,7 +848,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         }
         cr_tc_commit(BAR(B_DONE), me);  // the shared memory is in use until the last product has ended
         cr_bar_wait(BAR(B_DONE), 0, &gave_up);
-    } else if (E8 && warp >= 18) {
+    } else if (E8 && warp >= 18 && warp < 18 + kRowsWiden) {
         // ---- tiles of halves: a lane widens rows of its own ----
         uint32_t stage = 0, phase = 0, code = 0, cphase = 0, tile = 0;
         for (;; ++pieces) {
@@ -866,34 +869,43 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                 if (j & 1) ref = top = fmaxf(top, ref);
                 if (ref == 0.f) ref = 1.f;  // no keys
                 const float per = 128.f / ref;
+                const bool whole = left >= kRowsTile && __all_sync(~0u, r != 0);  // a scale of 0: no page
                 if (!cr_bar_wait(EMPTY(stage), phase ^ 1, &gave_up)) goto out;
                 if (warp == 18 && lane == 0)
                     asm volatile("st.shared.f32 [%0], %1;" ::"r"(sq + cfg::kRefs + (j & 1) * 32 + (tile & 7) * 4), "f"(ref * 0x1p-7f)
                                  : "memory");
-#pragma unroll 1
-                for (uint32_t row = (warp - 18) * 32 + lane; row < (uint32_t)kRowsTile; row += 32 * kRowsWiden) {
-                    float scale;  // 0: no page
-                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(scale) : "r"(sc + (row >> 3) * 4));
-                    const bool live = (int)row < left && scale != 0.f;
-                    const __half2 f = __float2half2_rn(scale * per);
-                    const uint32_t src = sq + cfg::kCode0 + code * cfg::kCodeTile + row * D, turn = D == 128 ? row & 7 : (row >> 1) & 3;
-                    const uint32_t dst = ring + stage * cfg::kTile + row * 128;
-                    uint32_t q[D / 16][4];
+                const uint32_t row = (warp - 18) * 32 + lane;
+                float scale;
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(scale) : "r"(sc + (row >> 3) * 4));
+                const __half2 f = __float2half2_rn(scale * per);
+                const uint32_t src = sq + cfg::kCode0 + code * cfg::kCodeTile + row * D, turn = D == 128 ? row & 7 : (row >> 1) & 3;
+                const uint32_t dst = ring + stage * cfg::kTile + row * 128;
+                const bool none = !whole && ((int)row >= left || scale == 0.f);
 #pragma unroll
-                    for (uint32_t c = 0; c < D / 16; ++c)
+                for (uint32_t c0 = 0; c0 < D / 16; c0 += 4) {
+                    uint32_t q[4][4];
+#pragma unroll
+                    for (uint32_t c = 0; c < 4; ++c)
                         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
                                      : "=r"(q[c][0]), "=r"(q[c][1]), "=r"(q[c][2]), "=r"(q[c][3])
-                                     : "r"(src + ((c ^ turn) << 4)));
+                                     : "r"(src + (((c0 + c) ^ turn) << 4)));
+                    if (none) {
 #pragma unroll
-                    for (uint32_t c = 0; c < D / 16; ++c) {
+                        for (uint32_t c = 0; c < 4; ++c) q[c][0] = q[c][1] = q[c][2] = q[c][3] = 0;
+                    }
+#pragma unroll
+                    for (uint32_t c = 0; c < 4; ++c) {
                         uint32_t o[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const uint32_t h = cr_e4m3_pair(e & 1 ? q[c][e / 2] >> 16 : q[c][e / 2]);
-                            const __half2 y = __hmul2(*reinterpret_cast<const __half2 *>(&h), f);
-                            o[e] = live ? *reinterpret_cast<const uint32_t *>(&y) : 0u;
+                        for (int e = 0; e < 4; ++e) {
+                            cr_e4m3_halves(q[c][e], o[2 * e], o[2 * e + 1]);
+#pragma unroll
+                            for (int h = 2 * e; h < 2 * e + 2; ++h) {
+                                const __half2 y = __hmul2(*reinterpret_cast<const __half2 *>(&o[h]), f);
+                                o[h] = *reinterpret_cast<const uint32_t *>(&y);
+                            }
                         }
-                        const uint32_t to = dst + (c >> 2) * (kRowsTile * 128), u = (c & 3) * 2;
+                        const uint32_t to = dst + (c0 >> 2) * (kRowsTile * 128), u = c * 2;
                         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((u ^ (row & 7)) << 4)), "r"(o[0]),
                                      "r"(o[1]), "r"(o[2]), "r"(o[3])
                                      : "memory");
@@ -924,7 +936,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         }
     } else if (warp < 16) {
         // ---- softmax: two threads a row ----
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+        if (E8)
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
+        else
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
         const int x = (int)(warp >> 3), half = (int)(warp >> 2) & 1;
         const uint32_t row = (warp & 3) * 32 + lane;
         // this warp's lanes of tensor memory, its scores (and weights), its columns of the accumulator
@@ -944,25 +959,20 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             meet();
             return xch[x * 2 + (half ^ 1)][row];
         };
-        for (uint32_t ophase = 0;; ++pieces) {
-            if (!cr_bar_wait(BAR(B_PFULL + (pieces & 1)), (pieces >> 1) & 1, &gave_up)) goto left;
-            const volatile rows_piece *p = piece + (pieces & 1);
-            const int n = p->n;
-            if (n == 0) break;
-            if (x == 1 && p->ntok <= (int)A.tq) {
-                __syncwarp();
-                if (lane == 0) {
-                    cr_bar_arrive(BAR(B_PEMPTY + (pieces & 1)));
-                    if (E8 && BF16) cr_bar_arrive(BAR(B_QREADY));
-                }
-                continue;
-            }
-            float cq = A.c;
-            if constexpr (E8 && BF16) {
-                if (!cr_bar_wait(BAR(B_QFULL), pieces & 1, &gave_up)) goto left;
+        // 8 bits: a piece's bfloat16 queries as halves, each row brought to 2^14 .. 2^15; two lanes a row, and the two
+        // warps that share 32 rows half of them each.  Done as soon as the piece before has no more weights to make, so
+        // that its result is written while the products go on (after that result: 0.5 us a piece more).
+        float next_c = A.c;
+        uint32_t tile = 0;  // 8 bits: key tiles so far
+        auto halve = [&](uint32_t i) {
+            if (!cr_bar_wait(BAR(B_PFULL + (i & 1)), (i >> 1) & 1, &gave_up)) return false;
+            const volatile rows_piece *p = piece + (i & 1);
+            if (p->n == 0) return true;
+            if (!cr_bar_wait(BAR(B_QFULL), i & 1, &gave_up)) return false;  // also who has no rows: no phase is left out
+            if (x == 0 || p->ntok > (int)A.tq) {
                 constexpr int kC = D / 16;  // chunks of eight elements
-                const uint32_t at = sq + x * cfg::kTile + (D == 128 ? half * (kRowsTile * 128) : half * 64) + row * 128;
-                const uint32_t turn = row & (D == 128 ? 7 : 3);
+                const uint32_t r = (warp & 3) * 32 + half * 16 + (lane & 15), h = lane >> 4, turn = r & (D == 128 ? 7 : 3);
+                const uint32_t at = sq + x * cfg::kTile + r * 128 + (D == 128 ? h * (kRowsTile * 128) : ((h * 4) ^ (r & 4)) * 16);
                 uint32_t q[kC][4], most = 0;
 #pragma unroll
                 for (uint32_t k = 0; k < kC; ++k) {
@@ -972,10 +982,9 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) most = max(most, max(q[k][e] << 16 & 0x7fffffffu, q[k][e] & 0x7fff0000u));
                 }
-                most = max(most, __float_as_uint(exchange(__uint_as_float(most))));
+                most = max(most, __shfl_xor_sync(~0u, most, 16));
                 const int up = max(-113, min(113, 14 + 127 - (int)(most >> 23)));
                 const float f = __uint_as_float((uint32_t)(127 + up) << 23);
-                cq *= __uint_as_float((uint32_t)(127 - up) << 23);
 #pragma unroll
                 for (uint32_t k = 0; k < kC; ++k) {
 #pragma unroll
@@ -985,10 +994,32 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                                  "r"(q[k][2]), "r"(q[k][3])
                                  : "memory");
                 }
+                const uint32_t ups = sq + cfg::kUp + x * kRowsTile;
+                if (h == 0) asm volatile("st.shared.b8 [%0], %1;" ::"r"(ups + r), "r"(up) : "memory");
                 cr_fence_async_smem();
-                __syncwarp();
-                if (lane == 0) cr_bar_arrive(BAR(B_QREADY));
+                meet();
+                int mine;
+                asm volatile("ld.shared.s8 %0, [%1];" : "=r"(mine) : "r"(ups + row) : "memory");
+                next_c = A.c * __uint_as_float((uint32_t)(127 - mine) << 23);
             }
+            __syncwarp();
+            if (lane == 0) cr_bar_arrive(BAR(B_QREADY));
+            return true;
+        };
+        if (E8 && BF16 && !halve(0)) goto left;
+        for (uint32_t ophase = 0;; ++pieces) {
+            if (!cr_bar_wait(BAR(B_PFULL + (pieces & 1)), (pieces >> 1) & 1, &gave_up)) goto left;
+            const volatile rows_piece *p = piece + (pieces & 1);
+            const int n = p->n;
+            if (n == 0) break;
+            if (x == 1 && p->ntok <= (int)A.tq) {
+                __syncwarp();
+                if (lane == 0) cr_bar_arrive(BAR(B_PEMPTY + (pieces & 1)));
+                tile += (uint32_t)n;
+                if (E8 && BF16 && !halve(pieces + 1)) goto left;
+                continue;
+            }
+            const float cq = next_c;
             float unit = 0.f;  // of the accumulator
             // keys that this row sees, from the first tile's on; the tile with the sequence's end
             int seen = p->klen - p->t0 * kRowsTile - half * 64;
@@ -1017,15 +1048,14 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                     mx[i] = fmaxf(mx[i], __uint_as_float(s[60 + i]));
                 }
                 float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-                top = fmaxf(top, exchange(top));
-                unsigned long long c2 = cr_pair(c, c);
+                float ct = c, now = 0.f;
                 if (E8) {
-                    float ct;
-                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ct) : "r"(sq + cfg::kRefs + ((p->tiles + j) & 7) * 4));
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ct) : "r"(sq + cfg::kRefs + (tile & 7) * 4));
                     ct *= cq;
-                    top *= ct;
-                    c2 = cr_pair(ct, ct);
                 }
+                top = fmaxf(top, exchange(top));
+                if (E8) top *= ct;
+                const unsigned long long c2 = cr_pair(ct, ct);
                 // The maximum may lag by 2^8: weights stay below 2^8, sums below 2^31, and the
                 // accumulator is scaled a few times per row instead of at every tile.
                 const bool grow = j == 0 || !((top - m) * c <= 8.f || top == m);
@@ -1064,7 +1094,13 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                     cr_fence_async_smem();
                 }
                 float off = m == -INFINITY ? 0.f : -m * c;
-                if (E8) off += kLift;
+                if (E8) {
+                    off += kLift;
+                    const uint32_t at = 2 * tile + 1;  // the values' R
+                    if (!cr_bar_wait(FULL(at % cfg::kStages), (at / cfg::kStages) & 1, &gave_up)) goto left;
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(now) : "r"(sq + cfg::kRefs + 32 + (tile & 7) * 4));
+                    ++tile;
+                }
                 const unsigned long long off2 = cr_pair(off, off);
                 unsigned long long sum[2] = {0ull, 0ull};
 #pragma unroll
@@ -1082,10 +1118,6 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                     }
                     cr_tmem_st16(ts + part * 16, w);
                     if (E8 && part == 0) {
-                        const uint32_t tile = (uint32_t)p->tiles + j, at = 2 * tile + 1;
-                        if (!cr_bar_wait(FULL(at % cfg::kStages), (at / cfg::kStages) & 1, &gave_up)) goto left;
-                        float now;
-                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(now) : "r"(sq + cfg::kRefs + 32 + (tile & 7) * 4));
                         if (now != unit && j > 0) {
                             const float f = unit / now;
 #pragma unroll 1
@@ -1119,6 +1151,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             __syncwarp();
             if (lane == 0) cr_bar_arrive(BAR(B_LREAD + pair - 1));
             l = half ? l2 + l : l + l2;
+            if (E8 && BF16 && !halve(pieces + 1)) goto left;
             const bool valid = hd >= 0 && tok < p->ntok;
             const int slot = p->slot;
             const int head = p->h * (int)A.G + hd;
@@ -1994,8 +2027,9 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                     float s[kN][2][4] = {};  // two sums, so that a product does not wait for the one before
 #pragma unroll
                     for (int i = 0; i < D / 16; ++i) {
-                        const uint32_t a[4] = {cr_e4m3_pair(c4[0][i]), cr_e4m3_pair(c4[1][i]), cr_e4m3_pair(c4[0][i] >> 16),
-                                               cr_e4m3_pair(c4[1][i] >> 16)};
+                        uint32_t a[4];
+                        cr_e4m3_halves(c4[0][i], a[0], a[2]);
+                        cr_e4m3_halves(c4[1][i], a[1], a[3]);
 #pragma unroll
                         for (int n = 0; n < kN; ++n) mma16816<false>(s[n][i & 1], a, qb[n][i][0], qb[n][i][1]);
                     }
@@ -2074,7 +2108,9 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                         for (int h = 0; h < 2; ++h) {  // elements 4 i + 2 h and the next: bytes of two keys side by side
                             const uint32_t lo = __byte_perm(v[0][i], v[1][i], h ? 0x7362 : 0x5140);
                             const uint32_t hi = __byte_perm(v[2][i], v[3][i], h ? 0x7362 : 0x5140);
-                            const uint32_t a[4] = {cr_e4m3_pair(lo), cr_e4m3_pair(lo >> 16), cr_e4m3_pair(hi), cr_e4m3_pair(hi >> 16)};
+                            uint32_t a[4];
+                            cr_e4m3_halves(lo, a[0], a[1]);
+                            cr_e4m3_halves(hi, a[2], a[3]);
 #pragma unroll
                             for (int n = 0; n < kN; ++n) mma16816<false>(o[n][2 * i + h], a, pb[n][0], pb[n][1]);
                         }
@@ -2363,7 +2399,7 @@ int launch_rows(cr_ctx *ctx, const attn_in &A, const kv_desc &K, const cr_attn_a
     auto kern = k_attn_rows<D, BF16, E8>;
     static unsigned long long raised = 0;
     CR_TRY(raise_smem(ctx, kern, rows_cfg<D, E8>::kSmem, raised));
-    CR_TRY(cr_launch_early(ctx, "k_attn_rows", kern, dim3(ctas), kRowsThreads, rows_cfg<D, E8>::kSmem, A, mq, mk, mv));
+    CR_TRY(cr_launch_early(ctx, "k_attn_rows", kern, dim3(ctas), rows_threads(E8), rows_cfg<D, E8>::kSmem, A, mq, mk, mv));
     if (ctas > 1 && !A.to_pfx)
         CR_TRY(cr_launch_early(ctx, "k_attn_join", k_attn_join<D, BF16, 2 * kRowsTile>, dim3(4 * ctx->num_sms), 256, 0, A));
     return CR_OK;

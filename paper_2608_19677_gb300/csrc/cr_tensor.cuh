@@ -243,26 +243,10 @@ __device__ __forceinline__ uint32_t cr_pack16(float lo, float hi)
 }
 
 // ---- e4m3 ------------------------------------------------------------------------------------
-// two e4m3 numbers, the first in the low byte, as half numbers (exact; not-a-number stays one)
-__device__ __forceinline__ uint32_t cr_e4m3_pair(uint32_t v)
+// Four e4m3 numbers, the first lowest, as halves (exact; not-a-number stays one).
+__device__ __forceinline__ void cr_e4m3_halves(uint32_t v, uint32_t &lo, uint32_t &hi)
 {
-    uint32_t r;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)v));
-    return r;
-}
-// Four e4m3 numbers times a power of two in the 16-bit type.  With the powers that a block may have this is exact.
-template <bool BF16>
-__device__ __forceinline__ void cr_widen4(uint32_t v, float scale, uint32_t &lo, uint32_t &hi)
-{
-    const uint32_t a = cr_e4m3_pair(v), b = cr_e4m3_pair(v >> 16);
-    if (BF16) {
-        const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&a)), y = __half22float2(*reinterpret_cast<const __half2 *>(&b));
-        lo = cr_pack16<true>(x.x * scale, x.y * scale);
-        hi = cr_pack16<true>(y.x * scale, y.y * scale);
-    } else {
-        const __half2 s = __float2half2_rn(scale);
-        const __half2 x = __hmul2(*reinterpret_cast<const __half2 *>(&a), s), y = __hmul2(*reinterpret_cast<const __half2 *>(&b), s);
-        lo = *reinterpret_cast<const uint32_t *>(&x);
-        hi = *reinterpret_cast<const uint32_t *>(&y);
-    }
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+        : "=r"(lo), "=r"(hi)
+        : "r"(v));
 }
