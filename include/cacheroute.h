@@ -621,10 +621,16 @@ typedef struct {
  * alike; 16-byte aligned, strides multiples of 8), head_dim a multiple of 8, 8..128.
  * d_out may be d_x with the same strides; else they do not overlap.
  *   d_pos   int32[n_tokens]: position of each token (may be negative)
+ *   dtype   CR_DTYPE_BF16 or CR_DTYPE_FP16
  * Errors: CR_EINVAL, CR_ECUDA. */
-CR_API int cr_rope(cr_ctx *ctx, const cr_rotary *rotary, uint32_t dtype, const void *d_x, uint64_t x_token, uint64_t x_head,
-                   void *d_out, uint64_t o_token, uint64_t o_head, uint32_t n_tokens, uint32_t heads, uint32_t head_dim,
-                   const int32_t *d_pos);
+typedef struct {
+    const void *d_x;
+    void *d_out;
+    const int32_t *d_pos;
+    uint64_t x_token, x_head, o_token, o_head; /* elements */
+    uint32_t n_tokens, heads, head_dim, dtype;
+} cr_rope_args;
+CR_API int cr_rope(cr_ctx *ctx, const cr_rotary *rotary, const cr_rope_args *args);
 
 /* cr_kv_write with the new tokens' queries and keys rotated to their positions in
  * their rows (the first token of a row is at 0): keys go rotated into the pages
@@ -650,9 +656,13 @@ CR_API int cr_kv_append(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t layer, c
  * d_seqs[i] (NULL: of row i); d_start NULL: the row's last ones.  Tokens that fall
  * outside their row become zeros (CR_EINVAL by the next blocking call).  Keys come as
  * they are held: rotated, where they were written so.  Errors: CR_EINVAL, CR_ECUDA. */
-CR_API int cr_kv_read(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t layer, void *d_k, uint64_t k_token, uint64_t k_head,
-                      void *d_v, uint64_t v_token, uint64_t v_head, const int32_t *d_cu, const int32_t *d_seqs,
-                      const int32_t *d_start, uint32_t n, uint32_t n_tokens);
+typedef struct {
+    void *d_k, *d_v;
+    const int32_t *d_cu, *d_seqs, *d_start;
+    uint64_t k_token, k_head, v_token, v_head; /* elements */
+    uint32_t n, n_tokens;
+} cr_read_args;
+CR_API int cr_kv_read(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t layer, const cr_read_args *args);
 
 /* ==== attention ======================================================== */
 /*

@@ -163,9 +163,9 @@ def lib() -> C.CDLL:
         "cr_pages_free": ([vp, vp, vp, u32], i32),
         "cr_pages_compact": ([vp, vp, vp, vp, vp, vp], i32),
         "cr_kv_write": ([vp, vp, u32, vp, u64, u64, vp, u64, u64, vp, vp, u32, u32], i32),
-        "cr_rope": ([vp, vp, u32, vp, u64, u64, vp, u64, u64, u32, u32, u32, vp], i32),
+        "cr_rope": ([vp, vp, vp], i32),
         "cr_kv_append": ([vp, vp, u32, vp, vp], i32),
-        "cr_kv_read": ([vp, vp, u32, vp, u64, u64, vp, u64, u64, vp, vp, vp, u32, u32], i32),
+        "cr_kv_read": ([vp, vp, u32, vp], i32),
         "cr_attn_packed": ([vp, vp, u32, u32, u32, vp, u64, u64, vp, u64, u64, vp, u32], i32),
         "cr_attn_paged": ([vp, vp, u32, vp], i32),
         "cr_attn_decode": ([vp, vp, u32, vp, vp, vp, u32], i32),
@@ -823,19 +823,26 @@ class Rotary:
         return r
 
 
+_pack_rope = struct.Struct("@3P4Q4I").pack    # cr_rope_args
+
+
 def rope(ctx: Context, x, rotary: Rotary, pos, out=None):
     """Rotate tokens x [tokens, heads, head_dim] (bfloat16 or float16) to positions ``pos`` int32[tokens] (cr_rope).
     ``out`` may be ``x``."""
     dtype, shape = x.dtype, x.shape
-    code = _dtype_code(dtype)
+    code = _codes.get(dtype)
+    if code is None:
+        code = _dtype_code(dtype)
     if x.requires_grad or (out is not None and out.requires_grad):
         _no_gradient(x, *(() if out is None else (out,)))
     xp, xt, xh = _heads("x", x, dtype, shape, None, None, None)
     T, heads, dim = shape
     if out is None:
         out = _out(ctx, shape, x, dtype)
-    op, ot, oh = _heads("out", out, dtype, out.shape, T, heads, dim)
-    st = lib().cr_rope(ctx._h, rotary._addr, code, xp, xt, xh, op, ot, oh, T, heads, dim, _int32("pos", pos, T))
+        op, ot, oh = out.data_ptr(), heads * dim, dim
+    else:
+        op, ot, oh = _heads("out", out, dtype, out.shape, T, heads, dim)
+    st = lib().cr_rope(ctx._h, rotary._addr, _pack_rope(xp, op, _int32("pos", pos, T), xt, xh, ot, oh, T, heads, dim, code))
     if st:
         ctx.check(st, "cr_rope")
     return out
@@ -861,7 +868,9 @@ def kv_append(ctx: Context, pages: KVPages, layer: int, q, k, v, rotary: Rotary,
         heads = q.shape[1]
         if out is None:
             out = _out(ctx, q.shape, q, dtype)
-        op, ot, oh = _heads("out", out, dtype, out.shape, T, heads, dim)
+            op, ot, oh = out.data_ptr(), heads * dim, dim
+        else:
+            op, ot, oh = _heads("out", out, dtype, out.shape, T, heads, dim)
     elif out is not None:
         raise ValueError("out without queries")
     a = _pack_append(qp, op, kp, vp, qt, qh, ot, oh, kt, kh, vt, vh, _int32("cu", cu),
@@ -872,25 +881,32 @@ def kv_append(ctx: Context, pages: KVPages, layer: int, q, k, v, rotary: Rotary,
     return out
 
 
+_pack_read = struct.Struct("@5P4Q2I").pack    # cr_read_args
+
+
 def kv_read(ctx: Context, pages: KVPages, layer: int, cu, seqs=None, start=None, tokens: Optional[int] = None, out=None):
     """Keys and values of cached tokens, [tokens, kv_heads, head_dim] each (cr_kv_read): entry i's are cu[i] .. cu[i+1]-1
     of them, and tokens start[i] .. of row seqs[i] (None: the row's last ones; row i).  ``tokens``: cu's last value, which
     is read from the GPU where neither it nor ``out`` (a pair of tensors) is given."""
     n = max(cu.numel() - 1, 0)
+    heads, dim = pages.kv_heads, pages.head_dim
     if out is None:
         if tokens is None:
             tokens = int(cu[-1]) if n else 0
-        shape = (tokens, pages.kv_heads, pages.head_dim)
-        out = _out(ctx, shape, pages.cache, pages.dtype), _out(ctx, shape, pages.cache, pages.dtype)
-    k, v = out
-    if k.requires_grad or v.requires_grad:
-        _no_gradient(k, v)
-    kp, kt, kh = _heads("k", k, pages.dtype, k.shape, tokens, pages.kv_heads, pages.head_dim)
-    T = k.shape[0]
-    vp, vt, vh = _heads("v", v, pages.dtype, v.shape, T, pages.kv_heads, pages.head_dim)
-    st = lib().cr_kv_read(ctx._h, pages._addr, layer, kp, kt, kh, vp, vt, vh, _int32("cu", cu),
-                          None if seqs is None else _int32("seqs", seqs, n),
-                          None if start is None else _int32("start", start, n), n, T)
+        T, kt, kh = tokens, heads * dim, dim
+        k = _out(ctx, (T, heads, dim), pages.cache, pages.dtype)
+        v = _out(ctx, (T, heads, dim), pages.cache, pages.dtype)
+        kp, vp, vt, vh = k.data_ptr(), v.data_ptr(), kt, kh
+    else:
+        k, v = out
+        if k.requires_grad or v.requires_grad:
+            _no_gradient(k, v)
+        kp, kt, kh = _heads("k", k, pages.dtype, k.shape, tokens, heads, dim)
+        T = k.shape[0]
+        vp, vt, vh = _heads("v", v, pages.dtype, v.shape, T, heads, dim)
+    a = _pack_read(kp, vp, _int32("cu", cu), 0 if seqs is None else _int32("seqs", seqs, n),
+                   0 if start is None else _int32("start", start, n), kt, kh, vt, vh, n, T)
+    st = lib().cr_kv_read(ctx._h, pages._addr, layer, a)
     if st:
         ctx.check(st, "cr_kv_read")
     return k, v

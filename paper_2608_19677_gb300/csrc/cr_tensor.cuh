@@ -230,6 +230,12 @@ __device__ __forceinline__ unsigned long long cr_add2(unsigned long long a, unsi
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
+__device__ __forceinline__ unsigned long long cr_mul2(unsigned long long a, unsigned long long b)
+{
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
 // two floats rounded to the 16-bit type, the first in the low half
 template <bool BF16>
 __device__ __forceinline__ uint32_t cr_pack16(float lo, float hi)

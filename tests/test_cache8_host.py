@@ -19,6 +19,14 @@ PROGRAM = r"""
 int main(void)
 {
     printf("cr_kv_pages %zu\ncr_rotary %zu\ncr_append_args %zu\n", sizeof(cr_kv_pages), sizeof(cr_rotary), sizeof(cr_append_args));
+    printf("cr_rope_args %zu\ncr_read_args %zu\n", sizeof(cr_rope_args), sizeof(cr_read_args));
+    F(cr_rope_args, d_x); F(cr_rope_args, d_out); F(cr_rope_args, d_pos); F(cr_rope_args, x_token); F(cr_rope_args, x_head);
+    F(cr_rope_args, o_token); F(cr_rope_args, o_head); F(cr_rope_args, n_tokens); F(cr_rope_args, heads);
+    F(cr_rope_args, head_dim); F(cr_rope_args, dtype);
+    F(cr_read_args, d_k); F(cr_read_args, d_v); F(cr_read_args, d_cu); F(cr_read_args, d_seqs); F(cr_read_args, d_start);
+    F(cr_read_args, k_token); F(cr_read_args, k_head); F(cr_read_args, v_token); F(cr_read_args, v_head);
+    F(cr_read_args, n); F(cr_read_args, n_tokens);
+    F(cr_append_args, q_head); F(cr_append_args, o_head); F(cr_append_args, k_head); F(cr_append_args, v_token);
     F(cr_kv_pages, d_scale); F(cr_kv_pages, block); F(cr_kv_pages, reserved);
     F(cr_rotary, d_turn); F(cr_rotary, pairs); F(cr_rotary, layout); F(cr_rotary, inverse); F(cr_rotary, scale);
     F(cr_append_args, d_q); F(cr_append_args, d_q_out); F(cr_append_args, d_k); F(cr_append_args, d_v);
@@ -48,15 +56,18 @@ def test_structures_are_laid_out_as_the_header_declares_them(header):
             if key.startswith(name + "."):
                 field = getattr(kind, key.split(".")[1])
                 assert place == (field.offset, field.size), key
-    names = ("d_q", "d_q_out", "d_k", "d_v", "q_token", "q_head", "o_token", "o_head", "k_token", "k_head", "v_token",
-             "v_head", "d_cu", "d_seqs", "n", "n_tokens", "q_heads", "reserved")
-    packed = P._pack_append(*range(1, len(names) + 1))
-    assert header["cr_append_args"] == (len(packed),)
-    for key, place in header.items():
-        if key.startswith("cr_append_args."):
-            at, size = place
+    for name, pack, fields in (
+            ("cr_append_args", P._pack_append, "d_q d_q_out d_k d_v q_token q_head o_token o_head k_token k_head v_token v_head "
+                                               "d_cu d_seqs n n_tokens q_heads reserved"),
+            ("cr_rope_args", P._pack_rope, "d_x d_out d_pos x_token x_head o_token o_head n_tokens heads head_dim dtype"),
+            ("cr_read_args", P._pack_read, "d_k d_v d_cu d_seqs d_start k_token k_head v_token v_head n n_tokens")):
+        fields = fields.split()
+        packed = pack(*range(1, len(fields) + 1))
+        assert header[name] == (len(packed),)
+        for field in fields:
+            at, size = header[f"{name}.{field}"]
             value = struct.unpack({4: "<I", 8: "<Q"}[size], packed[at:at + size])[0]
-            assert value == names.index(key.split(".")[1]) + 1, key
+            assert value == fields.index(field) + 1, (name, field)
 
 
 def test_calls_refuse_a_missing_context():
@@ -64,9 +75,9 @@ def test_calls_refuse_a_missing_context():
     __graft_entry__.build()
     import paper_2608_19677_gb300 as P
     L = P.lib()
-    assert L.cr_rope(None, None, 0, None, 0, 0, None, 0, 0, 0, 0, 0, None) == P.CR_EINVAL
+    assert L.cr_rope(None, None, None) == P.CR_EINVAL
     assert L.cr_kv_append(None, None, 0, None, None) == P.CR_EINVAL
-    assert L.cr_kv_read(None, None, 0, None, 0, 0, None, 0, 0, None, None, None, 0, 0) == P.CR_EINVAL
+    assert L.cr_kv_read(None, None, 0, None) == P.CR_EINVAL
 
 
 # ---- frequencies ---------------------------------------------------------------------------------------------------
