@@ -8,10 +8,13 @@ those prefixes in pages of a key/value cache, one table row each:
           values and attends over prefix and suffix;
   step    one more token for every running request; requests of one key stand together, so that their prefix is read
           once for all of them (``attn_decode``);
-  finish  rows of finished requests become empty; ``compact`` moves live pages to the front.
+  finish  rows of finished requests become empty; ``compact`` moves live pages to the front;
+  export  a prefix' keys and values, and ``install`` takes them at another destination, as prefixes move when a plan
+          changes.
 
 The model is the caller's: ``layers``, ``embed(tokens) -> x``, ``qkv(layer, x) -> q, k, v`` ([tokens, heads, head_dim])
-and ``mix(layer, x, out) -> x``.  Bookkeeping of rows is on the host; nothing here waits for the GPU.
+and ``mix(layer, x, out) -> x``.  One with ``rotary`` (a ``Rotary``) has its queries and keys rotated to their positions
+(``kv_append``).  The pool may hold 16 or 8 bits.  Bookkeeping of rows is on the host; nothing here waits for the GPU.
 
 Every call runs on the context's stream, the model's passes among it: after what torch's current stream has when the
 call is made, and before what that stream gets next.
@@ -22,8 +25,8 @@ import functools
 from collections import OrderedDict
 from typing import Dict, List, Sequence, Tuple
 
-from . import (Context, KVPages, attn_decode, attn_paged, kv_write, pages_compact, pages_extend, pages_fork,
-               pages_free)
+from . import (Context, KVPages, attn_decode, attn_paged, kv_append, kv_read, kv_write, pages_compact, pages_extend,
+               pages_fork, pages_free)
 
 
 def _on_context_stream(call):
@@ -94,11 +97,15 @@ class Destination:
     def _forward(self, tokens, cu, rows, groups=None):
         """One pass of the model, without gradients, over new tokens that the rows' lengths already count."""
         import torch
+        rotary = getattr(self.model, "rotary", None)
         with torch.no_grad():
             x = self.model.embed(tokens)
             for layer in range(self.model.layers):
                 q, k, v = self.model.qkv(layer, x)
-                kv_write(self.ctx, self.pages, layer, k, v, cu, seqs=rows)
+                if rotary is None:
+                    kv_write(self.ctx, self.pages, layer, k, v, cu, seqs=rows)
+                else:
+                    q = kv_append(self.ctx, self.pages, layer, q, k, v, rotary, cu, seqs=rows)
                 if groups is None:
                     out = attn_paged(self.ctx, q, self.pages, layer, cu, seqs=rows)
                 else:
@@ -241,6 +248,41 @@ class Destination:
             return
         self._free(list(rows))
         self._leave(gone)
+
+    @_on_context_stream
+    def export(self, key: int):
+        """The keys and values of a prefix that is held, (k, v) [tokens, kv_heads, head_dim] for each layer, keys rotated
+        where the model rotates them."""
+        if key not in self.prefixes:
+            raise ValueError(f"key {key} is not held")
+        row, n = self.prefixes[key]
+        self.prefixes.move_to_end(key)
+        cu, seqs = self._ints([0, n]), self._ints([row])
+        return [kv_read(self.ctx, self.pages, layer, cu, seqs=seqs, tokens=n) for layer in range(self.model.layers)]
+
+    @_on_context_stream
+    def install(self, key: int, layers) -> None:
+        """Hold a prefix whose keys and values another destination has exported.  Idle prefixes leave for it; if a call
+        fails, it is given up.  Pools in 8 bits with blocks of the same size hold the same numbers then."""
+        if key in self.prefixes:
+            raise ValueError(f"key {key} is held already")
+        if len(layers) != self.model.layers:
+            raise ValueError(f"keys and values of {len(layers)} layers for a model of {self.model.layers}")
+        n = int(layers[0][0].shape[0])
+        if n < 1 or any(int(t.shape[0]) != n for kv in layers for t in kv):
+            raise ValueError("keys and values of a prefix have its tokens, one at least, in every layer")
+        self._check_width(n)
+        self._make_room(1, self._pages(n), {key})
+        row = self._take(n, self._pages(n))
+        self.prefixes[key] = (row, n)
+        try:
+            rows, cu = self._ints([row]), self._ints([0, n])
+            pages_extend(self.ctx, self.pages, rows, self._ints([n]))
+            for layer, (k, v) in enumerate(layers):
+                kv_write(self.ctx, self.pages, layer, k, v, cu, seqs=rows)
+        except BaseException:
+            self._give_up([row])
+            raise
 
     @_on_context_stream
     def compact(self):

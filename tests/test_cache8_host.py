@@ -195,3 +195,72 @@ def test_no_load_takes_the_path_for_data_that_nothing_writes():
     for name in ("cr_kv.cu", "cr_pages.cuh"):
         text = open(os.path.join(CSRC, name)).read()
         assert not [w for w in ("__ldg(", "ld.global.nc", "__restrict__") if w in text], name
+
+
+# ---- a destination that rotates, and prefixes that move ----------------------------------------------------------------
+def test_a_model_with_rotary_positions_is_appended(monkeypatch):
+    torch = pytest.importorskip("torch")
+    from test_destination_host import Model, Pool, text
+    from paper_2608_19677_gb300 import destination as D
+
+    class Turning(Model):
+        rotary = object()
+
+    pool, said = Pool(64, 16, 8, 8), []
+
+    def append(ctx, pages, layer, q, k, v, rotary, cu, seqs=None):
+        said.append(rotary)
+        pool.write(ctx, pages, layer, k, v, cu, seqs=seqs)
+        return -q
+
+    def paged(ctx, q, pages, layer, cu, seqs=None):
+        assert (q <= 0).all(), "the rotated queries"
+        return q
+
+    for name in ("extend", "fork", "free"):
+        monkeypatch.setattr(D, f"pages_{name}", getattr(pool, name))
+    monkeypatch.setattr(D, "kv_append", append)
+    monkeypatch.setattr(D, "kv_write", lambda *a, **k: pytest.fail("keys that are not rotated"))
+    monkeypatch.setattr(D, "attn_paged", paged)
+    d = D.Destination(None, pool, Turning())
+    (row,), _ = d.admit([(5, text(1, 40), 32)])
+    assert pool.read(row, 40) == text(1, 40).tolist()
+    assert len(said) == 2 and all(r is Turning.rotary for r in said)
+
+
+def test_prefixes_move_between_destinations(monkeypatch):
+    torch = pytest.importorskip("torch")
+    from test_destination_host import Model, Pool, text
+    from paper_2608_19677_gb300 import destination as D
+    pools = [Pool(12, 16, 4, 4) for _ in range(2)]
+    for name in ("extend", "fork", "free"):
+        monkeypatch.setattr(D, f"pages_{name}", lambda ctx, pages, *a, name=name: getattr(pages, name)(ctx, pages, *a))
+    monkeypatch.setattr(D, "kv_write", lambda ctx, pages, *a, **k: pages.write(ctx, pages, *a, **k))
+    monkeypatch.setattr(D, "attn_paged", lambda ctx, q, pages, *a, **k: q)
+
+    def read(ctx, pages, layer, cu, seqs=None, tokens=None):
+        assert cu.tolist() == [0, tokens]
+        x = torch.tensor(pages.read(int(seqs[0]), tokens))[:, None, None]
+        return x, x
+
+    monkeypatch.setattr(D, "kv_read", read)
+    a, b = (D.Destination(None, p, Model()) for p in pools)
+    rows, _ = a.admit([(5, text(1, 40), 37)])
+    a.finish(rows)
+    kv = a.export(5)
+    b.install(5, kv)
+    row, n = b.prefixes[5]
+    assert n == 37 and pools[1].read(row, 37) == text(1, 37).tolist() and b.free_pages == 12 - 3
+    (mine,), _ = b.admit([(5, torch.cat([text(1, 37), text(2, 4)]), 37)])
+    assert pools[1].read(mine, 41) == text(1, 37).tolist() + text(2, 4).tolist()
+    before = dict(b.prefixes), b.free_pages, list(b.free_rows)
+    for wrong in (lambda: b.install(5, kv), lambda: b.install(6, kv + kv), lambda: b.install(6, [(kv[0][0], kv[0][1][:3])]),
+                  lambda: b.install(6, [(kv[0][0][:0], kv[0][1][:0])]), lambda: a.export(6)):
+        with pytest.raises(ValueError):
+            wrong()
+    with pytest.raises(RuntimeError):
+        b.install(6, [(text(3, 65)[:, None, None],) * 2])    # wider than a row
+    monkeypatch.setattr(D, "kv_write", lambda *a, **k: (_ for _ in ()).throw(ValueError("another shape")))
+    with pytest.raises(ValueError):
+        b.install(6, kv)                                      # given up
+    assert (dict(b.prefixes), b.free_pages, sorted(b.free_rows)) == (before[0], before[1], sorted(before[2]))
