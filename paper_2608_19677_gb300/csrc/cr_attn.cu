@@ -9,8 +9,8 @@
 // laid end to end; every CTA takes an equal stretch of it, wherever that begins or ends.  What a
 // CTA has of a block that it shares with others goes to scratch, and a second kernel joins the
 // pieces in order (k_attn_plan, one CTA, writes the list and the stretches, but for a few single tokens,
-// whose list k_attn_few makes).  A block counts for its tiles and for kExtra more: its queries, its first
-// scores and its result, which no other work hides.
+// whose list k_attn_few makes).  A block counts for its tiles and for some more
+// (extra): its queries, its first scores and its result, which no other work hides.
 //
 // Two kernels do the work:
 //   k_attn_rows  many query rows per key head: 256 rows (tokens x grouped heads) against tiles of
@@ -28,6 +28,8 @@ constexpr int kRowsTile = 128;  // query rows of a tile, and keys of one
 constexpr int kFewTile = 64;    // keys of a tile of k_attn_few
 constexpr int kFewWarps = 4;
 constexpr uint32_t kExtra = 1;
+// Single tokens over 8 bits: a tile takes half of the time, and a block's beginning and end the same.
+constexpr uint32_t kFewExtra8 = 4;
 
 // A block of query rows of one key head.
 struct __align__(16) attn_blk {
@@ -62,6 +64,7 @@ struct plan_in {
     uint32_t max_len;      // paged: tokens that a row can hold
     uint32_t min_tiles;    // key tiles that a CTA is worth
     uint32_t piece_cost;   // what a piece costs, in key tiles
+    uint32_t extra;        // what a block does
     attn_blk *blk;
     attn_start *start;        // [max_cta + 1]
     uint32_t *joins;          // [max_cta + 1] number of blocks with several pieces, and their first stretches
@@ -168,7 +171,7 @@ __device__ __forceinline__ unsigned long long div_by(unsigned long long a, unsig
 // How the work is cut: N units in stretches of equal length, or one stretch for each block.
 struct plan_cut {
     unsigned long long N, Nb, snap;
-    uint32_t nblk, ncta;
+    uint32_t nblk, ncta, extra;
     bool one_each;
 };
 // Nb: of a head; filled: blocks that have keys; longest: their most tiles.
@@ -176,6 +179,7 @@ __device__ __forceinline__ plan_cut cut_work(const plan_in &A, unsigned long lon
                                              uint32_t longest)
 {
     plan_cut C;
+    C.extra = A.extra;
     C.Nb = Nb;
     C.nblk = nblk;
     C.N = Nb * A.heads;  // N < 2^54
@@ -188,7 +192,7 @@ __device__ __forceinline__ plan_cut cut_work(const plan_in &A, unsigned long lon
     C.one_each = false;
     if (blocks && blocks <= A.max_cta) {
         const unsigned long long most_now = div_by(C.N, C.ncta) + A.piece_cost;
-        if (filled == nblk && longest + kExtra <= most_now) {
+        if (filled == nblk && longest + A.extra <= most_now) {
             C.one_each = true;
             C.ncta = (uint32_t)blocks;
         } else if (blocks <= C.ncta) {
@@ -215,8 +219,8 @@ __device__ __forceinline__ attn_start stretch(const plan_cut &C, const unsigned 
         const unsigned long long rem = s.pos - s.head * C.Nb;
         s.blk = at_or_below(cum, C.nblk, rem);
         const unsigned long long t = rem - cum[s.blk], left = cum[s.blk + 1] - rem;
-        s.tile = (uint32_t)(t - kExtra);
-        if (t <= C.snap || t <= kExtra) {
+        s.tile = (uint32_t)(t - C.extra);
+        if (t <= C.snap || t <= C.extra) {
             s.pos -= t;
             s.tile = 0;
         } else if (left <= C.snap) {
@@ -337,7 +341,7 @@ __device__ void plan_build(const plan_in &A, plan_shared &S, uint32_t *status)
                 for (int t = 0; t < k.ntok; ++t) A.of_token[k.row0 + t] = k.row0;
         }
         filled += __syncthreads_count(nt > 0);
-        const unsigned long long at = base + scan_cta<NT>(nt ? nt + kExtra : 0, S.part, &total);
+        const unsigned long long at = base + scan_cta<NT>(nt ? nt + A.extra : 0, S.part, &total);
         if (b < nblk) {
             cum[b] = at;
             A.blk[b] = k;
@@ -361,7 +365,7 @@ __device__ void plan_build(const plan_in &A, plan_shared &S, uint32_t *status)
     __syncthreads();
     // the first stretch that begins inside a block joins its pieces
     for (uint32_t c = 1 + tid; c < C.ncta; c += NT) {
-        if (S.end[c] == 0 || S.pos[c - 1] > S.pos[c] - S.first_tile[c] - kExtra) continue;
+        if (S.end[c] == 0 || S.pos[c - 1] > S.pos[c] - S.first_tile[c] - A.extra) continue;
         A.start[c].pieces = at_or_below(S.pos, A.max_cta, S.end[c] - 1) + 1 - (c - 1);
         A.joins[1 + atomicAdd(&S.joins, 1)] = c;  // in any order
     }
@@ -403,6 +407,7 @@ struct attn_in {
     uint32_t to_pfx;       // k_attn_rows, its join: write those instead of o
     uint32_t o_wide;       // rows of o begin at multiples of 32 bytes
     uint32_t *status;
+    uint32_t extra;        // of a block, in the list of work
     uint32_t own_list;     // k_attn_few, its join: every CTA makes the list of work itself, from
     plan_in plan;
     // keys and values in 8 bits: their blocks' scales in this layer, [n_pages][kv_heads][1 << nb_log2]
@@ -433,7 +438,7 @@ __device__ __forceinline__ plan_cut make_list(const plan_in &P, own_list *L, uin
         k.kbase = row < 0 ? 0 : row;
         k.klen = keys_of(P, row);
         k.nt = (int)cr_few_tiles(0, k.klen, kFewTile);
-        at = (uint32_t)k.nt + kExtra;
+        at = (uint32_t)k.nt + P.extra;
     }
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -461,7 +466,7 @@ __device__ __forceinline__ plan_cut make_list(const plan_in &P, own_list *L, uin
 __device__ __forceinline__ void count_pieces(const plan_in &P, const plan_cut &C, const own_list *L)
 {
     const attn_start &s = L->start[0];
-    if (s.tile == 0 || s.pos >= C.N || L->before > s.pos - s.tile - kExtra) return;
+    if (s.tile == 0 || s.pos >= C.N || L->before > s.pos - s.tile - P.extra) return;
     const unsigned long long end = s.pos - s.tile + (uint32_t)s.k.nt;
     // stretches that begin before the block's end: none of them begins a whole stretch from its even share
     const uint32_t near = (uint32_t)div_by(end * C.ncta, C.N), c0 = near > 8 ? near - 8 : 0, c = c0 + (threadIdx.x & 31);
@@ -472,7 +477,7 @@ __device__ __forceinline__ void count_pieces(const plan_in &P, const plan_cut &C
 // A CTA's stretch, a block at a time; the next block's description is on its way while one is worked on.
 struct walk {
     unsigned long long left;
-    uint32_t h, next_h, b, t0, t1, begin_tile, nblk;  // b: of next_k
+    uint32_t extra, h, next_h, b, t0, t1, begin_tile, nblk;  // b: of next_k
     attn_blk k, next_k;
     const attn_blk *blk;
     __device__ __forceinline__ void fetch(uint32_t i)
@@ -483,9 +488,10 @@ struct walk {
         d[1] = g[1];
     }
     // s: this CTA's beginning, and the next one's
-    __device__ __forceinline__ void begin(const attn_start *s, const attn_blk *list)
+    __device__ __forceinline__ void begin(const attn_start *s, const attn_blk *list, uint32_t of_block)
     {
         blk = list;
+        extra = of_block;
         next_h = s->head;
         b = s->blk;
         begin_tile = s->tile;
@@ -501,7 +507,7 @@ struct walk {
         h = next_h;
         t0 = begin_tile;
         begin_tile = 0;
-        if (t0 == 0) left -= kExtra;
+        if (t0 == 0) left -= extra;
         t1 = (uint32_t)k.nt - t0 < left ? (uint32_t)k.nt : t0 + (uint32_t)left;
         left -= t1 - t0;
         if (left) step();  // a piece that does not end its block is the last
@@ -658,7 +664,7 @@ __global__ void __launch_bounds__(rows_threads(E8), 1)
         const uint32_t q_bytes = A.G * A.tq * 128 * cfg::kChunks;
         uint32_t stage = 0, phase = 0;
         walk w;
-        w.begin(A.start + blockIdx.x, A.blk);
+        w.begin(A.start + blockIdx.x, A.blk, A.extra);
         for (;;) {
             const bool more = w.next();
             if (!cr_bar_wait(BAR(B_PEMPTY + (pieces & 1)), ((pieces >> 1) & 1) ^ 1, &gave_up)) goto out;
@@ -1571,9 +1577,9 @@ __global__ void __launch_bounds__(kFewThreads, 2)
     if (A.own_list) {
         if (warp == kFewWarps) cut = make_list(A.plan, &list, A.status);
         __syncthreads();
-        w.begin(list.start, list.blk);
+        w.begin(list.start, list.blk, A.extra);
     } else {
-        w.begin(A.start + blockIdx.x, A.blk);
+        w.begin(A.start + blockIdx.x, A.blk, A.extra);
     }
     uint32_t stage = 0, phase = 0, qphase = 0;
     if (warp == kFewWarps) {
@@ -1868,9 +1874,9 @@ __global__ void __launch_bounds__(kFewThreads, 2)
     if (A.own_list) {
         if (warp == kFewWarps) cut = make_list(A.plan, &list, A.status);
         __syncthreads();
-        w.begin(list.start, list.blk);
+        w.begin(list.start, list.blk, A.extra);
     } else {
-        w.begin(A.start + blockIdx.x, A.blk);
+        w.begin(A.start + blockIdx.x, A.blk, A.extra);
     }
     uint32_t stage = 0, phase = 0, qphase = 0;
     if (warp == kFewWarps) {
@@ -2317,6 +2323,7 @@ struct plan_mem {
         a.last_cta = a.first_cta + n_marks;
         p.of_token = reinterpret_cast<int32_t *>(base + of_token);
         a.start = p.start;
+        a.extra = p.extra;
         a.ncta = p.max_cta;
         a.of_token = p.of_token;
     }
@@ -2476,7 +2483,9 @@ int part_mem(cr_ctx *ctx, int slot, attn_in &A, uint32_t ctas, uint32_t rows_per
 
 // Two tiles a CTA at least (64 tokens over 2,048 cached: 24.4 us a call with four, 20.9 with two); a piece costs about
 // as much as three tiles of 128 keys, or six of 64.
-constexpr uint32_t kRowsMinTiles = 2, kFewMinTiles = 2, kRowsPieceCost = 3, kFewPieceCost = 6;
+constexpr uint32_t kRowsMinTiles = 2, kFewMinTiles = 2, kRowsPieceCost = 3, kFewPieceCost = 6, kFewPieceCost8 = 8;
+
+constexpr uint64_t kAloneTiles = 8192;
 
 int attn_many(cr_ctx *ctx, const cr_attn_args *a, const kv_desc &K)
 {
@@ -2498,6 +2507,7 @@ int attn_many(cr_ctx *ctx, const cr_attn_args *a, const kv_desc &K)
     p.max_blk = a->n_tokens / p.tok_blk + (a->n < a->n_tokens ? a->n : a->n_tokens);
     p.min_tiles = kRowsMinTiles;
     p.piece_cost = kRowsPieceCost;
+    p.extra = kExtra;
     if (K.paged) {
         p.lens = K.pg->d_lens;
         p.n_seqs = K.pg->n_seqs;
@@ -2594,6 +2604,10 @@ extern "C" int cr_attn_decode(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t la
     if (n_groups > (1u << 24)) return cr_fail(ctx, CR_EINVAL, "cr_attn_decode: %u groups", n_groups);
     if (args->n == 0) return CR_OK;
     if (args->n == 1) n_groups = 0;  // nobody to share with
+    // 8 bits: where the rows cannot hold much, every sequence reads its prefix itself, which saves two kernels.  Both take
+    // equally long at about 8,300 tiles of 64 keys and a key head, whatever they are made of (heads of 64 and 128, 2 and 8 key heads, 4 to 128
+    // sequences: 13 to 20 us so and 25 to 37 in groups at 4,000 tiles and fewer; at 33,000 83 to 100 and 34 to 50).
+    if (K.e4m3 && (uint64_t)args->n * K.heads * cr_key_tiles((int)(pages->max_pages * pages->page), kFewTile) <= kAloneTiles) n_groups = 0;
 
     const uint32_t D = K.dim <= 64 ? 64 : 128;
     attn_in F = {}, R = {};
@@ -2619,7 +2633,8 @@ extern "C" int cr_attn_decode(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t la
     f.heads = F.few_heads = K.heads * F.nsub;
     f.max_cta = min(2 * (uint32_t)ctx->num_sms, kMaxCtas);
     f.min_tiles = kFewMinTiles;
-    f.piece_cost = kFewPieceCost;
+    f.piece_cost = K.e4m3 ? kFewPieceCost8 : kFewPieceCost;
+    f.extra = K.e4m3 ? kFewExtra8 : kExtra;
     plan_in g = f;
     g.cu_q = d_group_off;
     g.heads = K.heads;
@@ -2628,6 +2643,7 @@ extern "C" int cr_attn_decode(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t la
     g.max_cta = min((uint32_t)ctx->num_sms, kMaxCtas);
     g.min_tiles = kRowsMinTiles;
     g.piece_cost = kRowsPieceCost;
+    g.extra = kExtra;
 
     const bool grouped = n_groups > 0;
     const plan_mem mf(f.max_blk, f.max_cta, f.n, 0, grouped ? (uint64_t)f.n * F.few_heads : 0),

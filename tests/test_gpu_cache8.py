@@ -673,13 +673,14 @@ def check(out, lse, parts, cu):
         assert ((gl - l).abs()[~none] <= bl[~none]).all(), f"sequence {b}: lse"
 
 
-def fill8(P, ctx, g, page, block, lens, heads, d, dtype, layers=1, order="token", shared=None, group=None, spread=None):
+def fill8(P, ctx, g, page, block, lens, heads, d, dtype, layers=1, order="token", shared=None, group=None, spread=None,
+          width=0):
     """Rows in a pool whose other places hold not-a-number; rows of a group share its first shared[group] tokens
     (whole pages).  Returns the pages and the (k, v) that each row stands for, in 64 bits."""
     r = np.random.default_rng(page + sum(lens))
     need = [-(-n // page) for n in lens]
     total = sum(need) + 5
-    pg = pool8(P, page, block, total, len(lens), max(need + [1]) + 1, layers, heads, d, dtype, order)
+    pg = pool8(P, page, block, total, len(lens), max(need + [1, width]) + 1, layers, heads, d, dtype, order)
     order_of = r.permutation(total)
     table, at, first = np.full(tuple(pg.table.shape), -1, np.int64), 0, {}
     begin = [0] * len(lens)
@@ -751,14 +752,19 @@ GROUPED = [
 ]
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("page,block,hkv,hq,d,dtype,shared,members", GROUPED)
-def test_decode8_groups(P, ctx, page, block, hkv, hq, d, dtype, shared, members):
+def test_decode8_groups(P, ctx, page, block, hkv, hq, d, dtype, shared, members, wide):
+    """Rows that can hold little read their prefixes themselves; of those that can hold more, a group's is read once."""
     g = gen(page + hq)
     group = [i for i, m in enumerate(members) for _ in m]
     lens = [shared[i] + n for i, m in enumerate(members) for n in m]
-    pg, rows = fill8(P, ctx, g, page, block, lens, hkv, d, dtype, shared=shared, group=group)
+    pg, rows = fill8(P, ctx, g, page, block, lens, hkv, d, dtype, shared=shared, group=group,
+                     width=8192 * 64 // (len(lens) * hkv * page) + 1 if wide else 0)
     q = randn(g, len(lens), hq, d, dtype=dtype)
+    before = ctx.launches
     out, lse = P.attn_decode(ctx, q, pg, 0, group_off=cum([len(m) for m in members]), shared=ints(shared), lse=True)
+    assert ctx.launches - before == (4 if wide else 2)
     alone, alse = P.attn_decode(ctx, q, pg, 0, lse=True)
     ctx.sync()
     n = len(lens)
