@@ -814,6 +814,15 @@ class Rotary:
     def _bind(self, inverse: int):
         d = RotaryDesc(_ptr(self.turn), self.dims // 2, 0 if self.layout == "half" else 1, inverse, self.scale)
         self._desc, self._addr, self._inverse = d, C.addressof(d), inverse
+        self._device = self.turn.device.index if self.turn.is_cuda else None
+
+    def _on(self, ctx: Context) -> int:
+        """Address of cr_rotary, for a call on ctx's stream: the frequencies stay until that stream has passed it."""
+        if self._device != ctx.device:
+            raise ValueError(f"the rotation's frequencies are on {self.turn.device}, the context on GPU {ctx.device}")
+        if ctx._raw_stream != _torch._C._cuda_getCurrentRawStream(ctx.device):
+            self.turn.record_stream(ctx._stream_obj)
+        return self._addr
 
     def inverse(self) -> "Rotary":
         """Turns by the opposite angles (and multiplies by the same scale): the gradient of the rotation."""
@@ -842,7 +851,7 @@ def rope(ctx: Context, x, rotary: Rotary, pos, out=None):
         op, ot, oh = out.data_ptr(), heads * dim, dim
     else:
         op, ot, oh = _heads("out", out, dtype, out.shape, T, heads, dim)
-    st = lib().cr_rope(ctx._h, rotary._addr, _pack_rope(xp, op, _int32("pos", pos, T), xt, xh, ot, oh, T, heads, dim, code))
+    st = lib().cr_rope(ctx._h, rotary._on(ctx), _pack_rope(xp, op, _int32("pos", pos, T), xt, xh, ot, oh, T, heads, dim, code))
     if st:
         ctx.check(st, "cr_rope")
     return out
@@ -875,7 +884,7 @@ def kv_append(ctx: Context, pages: KVPages, layer: int, q, k, v, rotary: Rotary,
         raise ValueError("out without queries")
     a = _pack_append(qp, op, kp, vp, qt, qh, ot, oh, kt, kh, vt, vh, _int32("cu", cu),
                      0 if seqs is None else _int32("seqs", seqs, n), n, T, heads, 0)
-    st = lib().cr_kv_append(ctx._h, pages._addr, layer, rotary._addr, a)
+    st = lib().cr_kv_append(ctx._h, pages._addr, layer, rotary._on(ctx), a)
     if st:
         ctx.check(st, "cr_kv_append")
     return out

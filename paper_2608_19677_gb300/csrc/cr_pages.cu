@@ -663,6 +663,8 @@ extern "C" int cr_kv_write(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t layer
     if (n > (1u << 24) || n_tokens > (1u << 30)) return cr_fail(ctx, CR_EINVAL, "cr_kv_write: too many entries or tokens");
     if (!n || !n_tokens) return CR_OK;
     if (!d_k || !d_v || !d_cu) return cr_fail(ctx, CR_EINVAL, "cr_kv_write: NULL pointer");
+    if (((uintptr_t)d_k & 15) || ((uintptr_t)d_v & 15) || ((k_token | k_head | v_token | v_head) & 7))
+        return cr_fail(ctx, CR_EINVAL, "cr_kv_write: keys and values must be 16-byte aligned, strides multiples of 8");
     if (cr_in_8bit(pages->dtype)) {
         cr_append_args A = {};
         A.d_k = d_k;
@@ -677,8 +679,6 @@ extern "C" int cr_kv_write(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t layer
         A.n_tokens = n_tokens;
         return cr_append(ctx, "cr_kv_write", pages, layer, nullptr, &A);
     }
-    if (((uintptr_t)d_k & 15) || ((uintptr_t)d_v & 15) || ((k_token | k_head | v_token | v_head) & 7))
-        return cr_fail(ctx, CR_EINVAL, "cr_kv_write: keys and values must be 16-byte aligned, strides multiples of 8");
     const pages_in P = cr_pages_input(ctx, pages);
     write_in W = {static_cast<const uint16_t *>(d_k), static_cast<const uint16_t *>(d_v), k_token, k_head, v_token, v_head,
                   d_cu, d_seqs, n, n_tokens, 0};

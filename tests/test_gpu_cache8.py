@@ -977,6 +977,35 @@ def test_on_a_stream_that_is_not_the_current_one(P):
     there.close()
 
 
+def test_write8_refuses_what_is_not_aligned(P, ctx):
+    """Through the C entry, which no check of tensors stands before."""
+    pg = P.KVPages.empty(4, 16, 1, 4, 1, 2, 64, dtype=BF, device=DEV, bits=8)
+    k, cu = torch.zeros(2, 3, 2, 64, dtype=BF, device=DEV), ints([0, 1])
+    before = pg.cache.view(torch.uint8).clone()
+    for bump, token, head in ((2, 128, 64), (8, 128, 64), (0, 130, 64), (0, 128, 65)):
+        for bad_v in (False, True):
+            good = (k[0].data_ptr(), 128, 64)
+            bad = (k[0].data_ptr() + bump, token, head)
+            first, second = (good, bad) if bad_v else (bad, good)
+            st = P.lib().cr_kv_write(ctx._h, pg._addr, 0, *first, *second, cu.data_ptr(), None, 1, 1)
+            with pytest.raises(Exception, match="aligned"):
+                ctx.check(st, "cr_kv_write")
+    torch.cuda.synchronize()
+    assert torch.equal(pg.cache.view(torch.uint8), before)
+
+
+def test_rotary_of_another_device_is_refused(P, ctx):
+    x, pos = torch.zeros(1, 2, 64, dtype=BF, device=DEV), ints([0])
+    rot = P.Rotary(64, device="cpu")
+    with pytest.raises(ValueError, match="frequencies are on cpu"):
+        P.rope(ctx, x, rot, pos)
+    with pytest.raises(ValueError, match="frequencies are on cpu"):
+        P.rope(ctx, x, rot.inverse(), pos)
+    pg = P.KVPages.empty(4, 16, 1, 4, 1, 2, 64, dtype=BF, device=DEV, bits=8)
+    with pytest.raises(ValueError, match="frequencies are on cpu"):
+        P.kv_append(ctx, pg, 0, None, x, x, rot, ints([0, 1]))
+
+
 def test_offsets_past_32_bits(P, ctx):
     """Pages whose numbers begin past 2^32 bytes of the cache."""
     g = gen(43)
