@@ -531,7 +531,8 @@ CR_API int cr_replay_import_state(cr_ctx *ctx, cr_replay *rp, uint32_t rep, uint
  * (at the largest e numbers stay within 240).  Tokens that are added to a block may raise its
  * power; the tokens before them in the block are then rounded again, which changes
  * only those that become subnormal.  It is never lowered while the block is in use;
- * the call that writes a block's first token chooses it anew.  An infinity, or what
+ * the call that writes a block's first token chooses it anew: a row's tokens are
+ * written in order, without gaps.  An infinity, or what
  * would be one in the 16-bit type, is held as not-a-number and does not count for
  * the power.  head_dim a multiple of 16, 16..128, strides multiples of 16 elements;
  * block a power of two, 8..page.
@@ -675,6 +676,9 @@ CR_API int cr_kv_read(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t layer, con
  * token sees every key.  A query that sees no key gets o = 0 and lse = -infinity.
  * Products are of 16-bit operands with 32-bit sums; the softmax is in 32 bits, its
  * weights are rounded to the 16-bit type for the product with v, o once at the end.
+ * Over pages in 8 bits the operands are halves, whatever the type of q: a row of
+ * bfloat16 queries times a power of two, numbers of the pages exactly, and weights
+ * that are rounded to 11 bits.
  * Nothing behind a sequence's end is read into its result, whatever it holds.  A
  * NaN or infinity in k_j or v_j reaches the queries that see j, and may reach
  * others of the same sequence.
@@ -714,7 +718,8 @@ CR_API int cr_attn_paged(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t layer, 
 /* One query token per entry (d_cu_q and causal are not read, n_tokens = n).  With
  * n_groups > 0 the entries d_group_off[g] .. d_group_off[g+1]-1 (int32[n_groups+1],
  * ascending from 0 to n) are sequences whose first d_shared[g] tokens lie in the same
- * pages: these are read once for all of them.  d_shared[g] is at most the shortest
+ * pages: these are read once for all of them (pages in 8 bits: where the rows can hold
+ * so much that it is faster).  d_shared[g] is at most the shortest
  * of their lengths. */
 CR_API int cr_attn_decode(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t layer, const cr_attn_args *args,
                           const int32_t *d_group_off, const int32_t *d_shared, uint32_t n_groups);

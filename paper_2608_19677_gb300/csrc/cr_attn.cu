@@ -565,6 +565,9 @@ constexpr int kRowsThreads = 640;
 // the accumulator is scaled.  They hold weights 2^6 times larger, so that those below the row's largest by 2^20 are still
 // rounded to 11 bits, and bring each row of bfloat16 queries to 2^14 .. 2^15 by a power of two (k_attn_few8).
 // Tiles of bfloat16 would be exact without R, at twice the instructions.  Registers: 512 x 96 + 256 x 48 = 768 x 80.
+// Measured (one GB300, 40 suffixes of 1 to 128 tokens over prefixes to 16,384, 32/4 heads of 128): 153 us a call, with two
+// widening warps 170, with tiles of bfloat16 249.  Tensor cores at work in 47% of the cycles (16-bit pages: 60%); a copy of
+// the kernel that leaves the widening out takes 18 us less.
 constexpr int kRowsWiden = 4;
 constexpr float kLift = 6.f;  // of the weights' logarithms
 __host__ __device__ constexpr int rows_threads(bool e8) { return e8 ? 768 : kRowsThreads; }
@@ -1811,6 +1814,8 @@ out:
 // and so is that of the rows: a lane takes what lies together, for scores D/4 consecutive elements of two keys, for
 // values D/8 consecutive elements of four keys, whose bytes it pairs up.
 // A head's maximum may lag by 2^8: then a step needs no exchange between lanes but one vote.
+// Bound by HBM and latency: 64 contexts to 32,768, 28/4 heads of 128, 89 us (538 MB, 6.0 TB/s) of the call's 141; with
+// heads as the 16-row operand and maxima that do not lag the call took 161.  One token over 2,112: 9 to 10 us cold.
 template <int D>
 struct few8_cfg {
     static constexpr int kTile = kFewTile * D;            // bytes of 64 keys
@@ -2605,8 +2610,9 @@ extern "C" int cr_attn_decode(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t la
     if (args->n == 0) return CR_OK;
     if (args->n == 1) n_groups = 0;  // nobody to share with
     // 8 bits: where the rows cannot hold much, every sequence reads its prefix itself, which saves two kernels.  Both take
-    // equally long at about 8,300 tiles of 64 keys and a key head, whatever they are made of (heads of 64 and 128, 2 and 8 key heads, 4 to 128
-    // sequences: 13 to 20 us so and 25 to 37 in groups at 4,000 tiles and fewer; at 33,000 83 to 100 and 34 to 50).
+    // equally long at about 8,300 tiles of 64 keys and a key head, whatever they are made of (heads of 64 and 128, 2 and
+    // 8 key heads, 4 to 128 sequences: 13 to 20 us so and 25 to 37 in groups at 4,000 tiles and fewer; at 33,000 83 to 100
+    // and 34 to 50).
     if (K.e4m3 && (uint64_t)args->n * K.heads * cr_key_tiles((int)(pages->max_pages * pages->page), kFewTile) <= kAloneTiles) n_groups = 0;
 
     const uint32_t D = K.dim <= 64 ? 64 : 128;
