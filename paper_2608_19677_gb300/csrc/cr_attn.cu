@@ -1060,7 +1060,9 @@ __global__ void __launch_bounds__(rows_threads(E8), 1)
                 float ct = c, now = 0.f;
                 if (E8) {
                     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ct) : "r"(sq + cfg::kRefs + (tile & 7) * 4));
-                    ct *= cq;
+                    // above 0, as what it multiplies may be masked, minus infinity; sums are below 2^40, so that scores which
+                    // this enlarges are still below 2^-86
+                    ct = fmaxf(ct * cq, 0x1p-126f);
                 }
                 top = fmaxf(top, exchange(top));
                 if (E8) top *= ct;
