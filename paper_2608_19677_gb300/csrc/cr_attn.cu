@@ -1996,7 +1996,9 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                 for (int i = 0; i < D / 16; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[n][i][e] = 0.f;
-                m[n][0] = m[n][1] = -1e30f;  // below every score: the first that is seen is above it by more than may be
+                // the lowest finite number: a score is that or above it by more than may be, and one that is not seen,
+                // minus infinity, has weight 0 beside it
+                m[n][0] = m[n][1] = -0x1.fffffep127f;
                 l[n][0] = l[n][1] = 0.f;
             }
             float E = 0.f, per_E = 0.f;  // per_E: 2^7 / E

@@ -79,3 +79,34 @@ def test_zeros_in_a_shared_prefix(P, ctx, dtype):
     assert ctx.launches - before == 4
     ctx.sync()
     sequences(out, lse, q, rows, range(len(lens) + 1), False, 0.125)
+
+
+# ---- scores of any size --------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("hq", [4, 16])
+@pytest.mark.parametrize("sign", [-1.0, 1.0])
+@pytest.mark.parametrize("call,bits", [("decode", 8)])
+def test_scores_of_any_finite_size(P, ctx, call, bits, hq, sign):
+    """Equal keys, so that every weight is the same however large the score: the mean of the values, and lse = score + log n.
+    Scores from 2^21 to -+2^112: below -1e30 and above 1e30; off by 2^-18 of their size, and lse by a few 32-bit roundings."""
+    g, d, lens = gen(7), 64, [700, 40]
+    key = randn(g, 1, 1, d).abs().clamp_min(0.5)
+    if bits == 8:
+        pg, rows = fill8(P, ctx, g, 16, 16, lens, 1, d, BF, spread=lambda k, v: ((key * 2.0 ** 50).expand_as(k).contiguous(), v))
+    else:
+        pg = P.KVPages.empty(60, 16, 2, 50, 1, 1, d)
+        k, v = (key * 2.0 ** 50).expand(740, 1, d).contiguous(), randn(g, 740, 1, d)
+        P.pages_extend(ctx, pg, ints([0, 1]), ints(lens))
+        P.kv_write(ctx, pg, 0, k, v, cum(lens))
+        rows = [(k[:700].double(), v[:700].double()), (k[700:].double(), v[700:].double())]
+    q = (sign * key.expand(2, hq, d).double() * 2.0 ** torch.linspace(-32, 59, hq, device=DEV).double()[None, :, None]).to(BF)
+    if call == "decode":
+        out, lse = P.attn_decode(ctx, q, pg, 0, scale=0.125, lse=True)
+    else:
+        out, lse = P.attn_paged(ctx, q, pg, 0, ints([0, 1, 2]), scale=0.125, lse=True)
+    ctx.sync()
+    for i, (k, v) in enumerate(rows):
+        mean, size = v.mean(0), v.abs().mean(0)
+        assert ((out[i].double() - mean).abs() <= 2.0 ** -8 * (mean.abs() + size) * 1.01 + 2.0 ** -19 * size).all()
+        s = 0.125 * (q[i].double() * k[0]).sum(-1)
+        assert (s[-1] * sign > 1e30).all()
+        assert ((lse[i].double() - s).abs() <= s.abs() * 2.0 ** -17).all()
