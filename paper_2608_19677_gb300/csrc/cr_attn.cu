@@ -28,6 +28,12 @@ constexpr int kRowsTile = 128;  // query rows of a tile, and keys of one
 constexpr int kFewTile = 64;    // keys of a tile of k_attn_few
 constexpr int kFewWarps = 4;
 constexpr uint32_t kExtra = 1;
+// Weights are exp2 of one fused operation, score * c - maximum * c, whose second product is a rounded one.  Where that is
+// beyond this size (a base-2 logarithm) what the rounding drops is no longer small in an exponent, and even the largest
+// weight could overflow or vanish.  There c becomes its power of two, with which both products are exact: distinct scores
+// are still 2^-3 or more apart, and have 32-bit sums' errors of 2^4 at least.
+constexpr float kFar = 0x1p22f;
+inline float coarse(float c) { return fmaxf(ldexpf(0.5f, ilogbf(c) + 1), 0x1p-126f); }
 // Single tokens over 8 bits: a tile takes half of the time, and a block's beginning and end the same.
 constexpr uint32_t kFewExtra8 = 4;
 
@@ -396,6 +402,8 @@ struct attn_in {
     uint32_t max_pages, page_log2, box_rows, box_log2;
     uint32_t paged, causal, G, nsub, tq, q_heads, head_dim;
     float c;               // scale * log2(e)
+    float c_pow, c_rest;   // its power of two, which stands for it beyond kFar, and what that leaves
+    float far;             // kFar / c
     void *o;
     float *lse;
     uint64_t o_token, o_head;
@@ -955,7 +963,8 @@ __global__ void __launch_bounds__(rows_threads(E8), 1)
         const uint32_t ts = tmem + ((warp & 3) << 21) + x * 128 + half * 64;
         const uint32_t to = tmem + ((warp & 3) << 21) + 256 + x * D + half * (D / 2);
         const uint32_t pair = 1 + x * 4 + (warp & 3);  // barrier of the two warps that share rows
-        const float c = E8 ? 1.f : A.c;  // 8 bits: scores are scaled as they come, m is a base-2 logarithm
+        // 8 bits: sums are scaled by powers of two as they come, that of A.c among them, which leaves less than 2
+        const float c = E8 ? A.c_rest : A.c, c_far = E8 ? 1.f : A.c_pow;
         const int tok = x * (int)A.tq + (int)(row / A.G), hd = row < A.G * A.tq ? (int)(row % A.G) : -1;
         uint32_t sphase = 0;
         // The other half's value of this row.  The next value is written only after the other warp has read this
@@ -971,7 +980,7 @@ __global__ void __launch_bounds__(rows_threads(E8), 1)
         // 8 bits: a piece's bfloat16 queries as halves, each row brought to 2^14 .. 2^15; two lanes a row, and the two
         // warps that share 32 rows half of them each.  Done as soon as the piece before has no more weights to make, so
         // that its result is written while the products go on (after that result: 0.5 us a piece more).
-        float next_c = A.c;
+        float next_c = A.c_pow;
         uint32_t tile = 0;  // 8 bits: key tiles so far
         auto halve = [&](uint32_t i) {
             if (!cr_bar_wait(BAR(B_PFULL + (i & 1)), (i >> 1) & 1, &gave_up)) return false;
@@ -1009,7 +1018,7 @@ __global__ void __launch_bounds__(rows_threads(E8), 1)
                 meet();
                 int mine;
                 asm volatile("ld.shared.s8 %0, [%1];" : "=r"(mine) : "r"(ups + row) : "memory");
-                next_c = A.c * __uint_as_float((uint32_t)(127 - mine) << 23);
+                next_c = A.c_pow * __uint_as_float((uint32_t)(127 - mine) << 23);
             }
             __syncwarp();
             if (lane == 0) cr_bar_arrive(BAR(B_QREADY));
@@ -1057,7 +1066,7 @@ __global__ void __launch_bounds__(rows_threads(E8), 1)
                     mx[i] = fmaxf(mx[i], __uint_as_float(s[60 + i]));
                 }
                 float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-                float ct = c, now = 0.f;
+                float ct = 1.f, now = 0.f;
                 if (E8) {
                     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ct) : "r"(sq + cfg::kRefs + (tile & 7) * 4));
                     // above 0, as what it multiplies may be masked, minus infinity; sums are below 2^40, so that scores which
@@ -1066,10 +1075,9 @@ __global__ void __launch_bounds__(rows_threads(E8), 1)
                 }
                 top = fmaxf(top, exchange(top));
                 if (E8) top *= ct;
-                const unsigned long long c2 = cr_pair(ct, ct);
                 // The maximum may lag by 2^8: weights stay below 2^8, sums below 2^31, and the
                 // accumulator is scaled a few times per row instead of at every tile.
-                const bool grow = j == 0 || !((top - m) * c <= 8.f || top == m);
+                const bool grow = j == 0 || !(E8 ? (top - m) * c < 8.f || top == m : (top - m) * c <= 8.f || top == m);
                 if (__any_sync(~0u, grow)) {
                     const float m_new = fmaxf(m, top);
                     if (j > 0) {
@@ -1104,9 +1112,11 @@ __global__ void __launch_bounds__(rows_threads(E8), 1)
                     }
                     cr_fence_async_smem();
                 }
-                float off = m == -INFINITY ? 0.f : -m * c;
+                const float by = fabsf(m) > (E8 ? kFar : A.far) ? c_far : c;
+                const unsigned long long c2 = E8 ? cr_pair(ct * by, ct * by) : cr_pair(by, by);
+                constexpr float lift = E8 ? kLift : 0.f;
+                const float off = m == -INFINITY ? lift : E8 ? fmaf(-m, by, lift) : -m * by;
                 if (E8) {
-                    off += kLift;
                     const uint32_t at = 2 * tile + 1;  // the values' R
                     if (!cr_bar_wait(FULL(at % cfg::kStages), (at / cfg::kStages) & 1, &gave_up)) goto left;
                     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(now) : "r"(sq + cfg::kRefs + 32 + (tile & 7) * 4));
@@ -1191,7 +1201,7 @@ __global__ void __launch_bounds__(rows_threads(E8), 1)
                 }
                 if (half == 0)
                     reinterpret_cast<float2 *>(A.part_ml)[(uint64_t)slot * RP + r] =
-                        make_float2(m == -INFINITY ? m : (E8 ? m - kLift : m * c), l);
+                        make_float2(m == -INFINITY ? m : (E8 ? fmaf(m, c, -kLift) : m * c), l);
             } else {
                 if (!A.to_pfx && A.o_wide && A.head_dim == D) {
                     // Lanes of a group of C hold C chunks of 32 bytes of a row each; the chunks change places, so that a
@@ -1263,7 +1273,7 @@ __global__ void __launch_bounds__(rows_threads(E8), 1)
                     }
                 }
                 if (valid && half == 0) {
-                    const float lse2 = l == 0.f ? -INFINITY : (E8 ? m - kLift : m * c) + log2f(l);
+                    const float lse2 = l == 0.f ? -INFINITY : (E8 ? fmaf(m, c, -kLift) : m * c) + log2f(l);
                     if (A.to_pfx)
                         A.pfx_lse[tk * A.q_heads + head] = lse2;
                     else if (A.lse)
@@ -1710,10 +1720,11 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                             }
                             m[r] = m_new;
                         }
-                        const float off = m[r] == -INFINITY ? 0.f : -m[r] * c;
+                        const float by = fabsf(m[r]) > A.far ? A.c_pow : c;
+                        const float off = m[r] == -INFINITY ? 0.f : -m[r] * by;
                         float p[4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) p[i] = cr_exp2(fmaf(s[i >> 1][2 * r + (i & 1)], c, off));
+                        for (int i = 0; i < 4; ++i) p[i] = cr_exp2(fmaf(s[i >> 1][2 * r + (i & 1)], by, off));
                         l[r] += (p[0] + p[1]) + (p[2] + p[3]);
                         pa[r] = cr_pack16<BF16>(p[0], p[1]);
                         pa[2 + r] = cr_pack16<BF16>(p[2], p[3]);
@@ -2364,7 +2375,10 @@ void fill_common(attn_in &A, cr_ctx *ctx, const cr_attn_args *a, const kv_desc &
     A.q_heads = a->q_heads;
     A.kv_heads = K.heads;
     A.head_dim = K.dim;
-    A.c = a->scale * 1.44269504088896341f;
+    A.c = fminf(a->scale * 1.44269504088896341f, 0x1.fffffep127f);
+    A.c_pow = coarse(A.c);
+    A.c_rest = A.c / A.c_pow;
+    A.far = kFar / A.c;
     A.causal = a->causal != 0;
     A.o = a->d_o;
     A.o_token = a->o_token;

@@ -82,31 +82,67 @@ def test_zeros_in_a_shared_prefix(P, ctx, dtype):
 
 
 # ---- scores of any size --------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [BF, HF])
 @pytest.mark.parametrize("hq", [4, 16])
 @pytest.mark.parametrize("sign", [-1.0, 1.0])
-@pytest.mark.parametrize("call,bits", [("decode", 8)])
-def test_scores_of_any_finite_size(P, ctx, call, bits, hq, sign):
+@pytest.mark.parametrize("call,bits", [("decode", 8), ("paged", 8), ("decode", 16), ("paged", 16), ("packed", 16)])
+def test_scores_of_any_finite_size(P, ctx, call, bits, hq, sign, dtype):
     """Equal keys, so that every weight is the same however large the score: the mean of the values, and lse = score + log n.
-    Scores from 2^21 to -+2^112: below -1e30 and above 1e30; off by 2^-18 of their size, and lse by a few 32-bit roundings."""
+    Scores from 2^21 to -+2^112 (half: 2^13 to 2^26): below -1e30 and above 1e30; off by 2^-18 of their size, and lse by a
+    few 32-bit roundings."""
     g, d, lens = gen(7), 64, [700, 40]
-    key = randn(g, 1, 1, d).abs().clamp_min(0.5)
+    up, low, high = (50, -32, 59) if dtype == BF else (10, 0, 13)
+    key = randn(g, 1, 1, d, dtype=dtype).abs().clamp_min(0.5)
     if bits == 8:
-        pg, rows = fill8(P, ctx, g, 16, 16, lens, 1, d, BF, spread=lambda k, v: ((key * 2.0 ** 50).expand_as(k).contiguous(), v))
+        pg, rows = fill8(P, ctx, g, 16, 16, lens, 1, d, dtype, spread=lambda k, v: ((key * 2.0 ** up).expand_as(k).contiguous(), v))
     else:
-        pg = P.KVPages.empty(60, 16, 2, 50, 1, 1, d)
-        k, v = (key * 2.0 ** 50).expand(740, 1, d).contiguous(), randn(g, 740, 1, d)
+        pg = P.KVPages.empty(60, 16, 2, 50, 1, 1, d, dtype=dtype)
+        k, v = (key * 2.0 ** up).expand(740, 1, d).contiguous(), randn(g, 740, 1, d, dtype=dtype)
         P.pages_extend(ctx, pg, ints([0, 1]), ints(lens))
         P.kv_write(ctx, pg, 0, k, v, cum(lens))
         rows = [(k[:700].double(), v[:700].double()), (k[700:].double(), v[700:].double())]
-    q = (sign * key.expand(2, hq, d).double() * 2.0 ** torch.linspace(-32, 59, hq, device=DEV).double()[None, :, None]).to(BF)
+    q = (sign * key.expand(2, hq, d).double() * 2.0 ** torch.linspace(low, high, hq, device=DEV).double()[None, :, None]).to(dtype)
     if call == "decode":
         out, lse = P.attn_decode(ctx, q, pg, 0, scale=0.125, lse=True)
-    else:
+    elif call == "paged":
         out, lse = P.attn_paged(ctx, q, pg, 0, ints([0, 1, 2]), scale=0.125, lse=True)
+    else:
+        out, lse = P.attn_packed(ctx, q, k, v, ints([0, 1, 2]), cu_k=cum(lens), scale=0.125, lse=True)
     ctx.sync()
     for i, (k, v) in enumerate(rows):
         mean, size = v.mean(0), v.abs().mean(0)
-        assert ((out[i].double() - mean).abs() <= 2.0 ** -8 * (mean.abs() + size) * 1.01 + 2.0 ** -19 * size).all()
+        u = 2.0 ** -8 if dtype == BF else 2.0 ** -11
+        assert ((out[i].double() - mean).abs() <= u * (mean.abs() + size) * 1.01 + 2.0 ** -19 * size).all()
         s = 0.125 * (q[i].double() * k[0]).sum(-1)
-        assert (s[-1] * sign > 1e30).all()
-        assert ((lse[i].double() - s).abs() <= s.abs() * 2.0 ** -17).all()
+        assert s[-1] * sign > (1e30 if dtype == BF else 2.0 ** 24)
+        assert ((lse[i].double() - (s + math.log(len(k)))).abs() <= s.abs() * 2.0 ** -17).all()
+
+
+@pytest.mark.parametrize("size", [2.0 ** 18, 2.0 ** 21, 2.0 ** 30, 2.0 ** 90])
+@pytest.mark.parametrize("bits,call", [(8, "decode"), (8, "paged"), (16, "decode"), (16, "paged")])
+def test_scores_far_apart(P, ctx, bits, call, size):
+    """Keys of ordinary scores behind ones that are far below: the softmax of the former.  Equal keys far above, behind those:
+    the mean of their values."""
+    g, d, lens = gen(8), 64, [600, 300]
+    key = randn(g, 1, 1, d).abs().clamp_min(0.5)
+    k, v = randn(g, 900, 1, d), randn(g, 900, 1, d)
+    k[:256], k[856:] = -size * key, size * key
+    if bits == 8:
+        pg, rows = fill8(P, ctx, g, 16, 16, lens, 1, d, BF, spread=lambda *_: (k, v))
+    else:
+        pg = P.KVPages.empty(60, 16, 2, 40, 1, 1, d)
+        P.pages_extend(ctx, pg, ints([0, 1]), ints(lens))
+        P.kv_write(ctx, pg, 0, k, v, cum(lens))
+        rows = [(k[:600].double(), v[:600].double()), (k[600:].double(), v[600:].double())]
+    q = randn(g, 2, 8, d).abs().clamp_min(0.25)
+    if call == "decode":
+        out, lse = P.attn_decode(ctx, q, pg, 0, lse=True)
+    else:
+        out, lse = P.attn_paged(ctx, q, pg, 0, ints([0, 1, 2]), lse=True)
+    ctx.sync()
+    seen = [tuple(x[256:] for x in rows[0])]
+    check(out[:1], lse[:1], [reference(q[:1], *seen[0], False, d ** -0.5)], [0, 1])
+    mean, sizes = rows[1][1][256:].mean(0), rows[1][1][256:].abs().mean(0)
+    assert ((out[1].double() - mean).abs() <= 2.0 ** -8 * (mean.abs() + sizes) * 1.01 + 2.0 ** -19 * sizes).all()
+    s = d ** -0.5 * (q[1].double() * rows[1][0][-1]).sum(-1)
+    assert ((lse[1].double() - (s + math.log(44))).abs() <= s * 2.0 ** -17).all()
