@@ -1916,16 +1916,17 @@ __global__ void __launch_bounds__(kFewThreads, 2)
             }
             const int32_t *row = A.table + (uint64_t)w.k.kbase * A.max_pages;
             const uint32_t tile0 = (uint32_t)w.k.lo / kFewTile;
-            auto page_of = [&](uint32_t t) {  // n_pages: none
+            // behind the sequence's end: ~0; n_pages stands for what is no page, whose copy is of zeros
+            auto page_of = [&](uint32_t t) {
                 const uint32_t at = (tile0 + t) * kFewTile + group * 8;
-                return t < w.t1 && (int)at < w.k.klen ? (uint32_t)row[at >> A.page_log2] : A.n_pages;
+                return t < w.t1 && (int)at < w.k.klen ? min((uint32_t)row[at >> A.page_log2], A.n_pages) : ~0u;
             };
             uint32_t next = page_of(w.t0);
             for (uint32_t t = w.t0; t < w.t1; ++t) {
                 const uint32_t in_page = ((tile0 + t) * kFewTile + group * 8) & ((1u << A.page_log2) - 1);
                 const uint32_t page = next;
                 next = page_of(t + 1);  // on its way while this tile waits for its place
-                const bool on = page < A.n_pages, brings = lane < 8 && on && (group * 8 & (A.box_rows - 1)) == 0;
+                const bool on = page < A.n_pages, brings = lane < 8 && page != ~0u && (group * 8 & (A.box_rows - 1)) == 0;
                 const uint32_t bytes = 2 * __popc(__ballot_sync(~0u, brings)) * A.box_rows * D;
                 const uint64_t scale = on ? (((uint64_t)page * A.kv_heads + kv) << A.nb_log2) + (in_page >> A.block_log2) : 0;
                 if (!cr_bar_wait(EMPTY(stage), phase ^ 1, &gave_up)) goto out;

@@ -146,3 +146,32 @@ def test_scores_far_apart(P, ctx, bits, call, size):
     assert ((out[1].double() - mean).abs() <= 2.0 ** -8 * (mean.abs() + sizes) * 1.01 + 2.0 ** -19 * sizes).all()
     s = d ** -0.5 * (q[1].double() * rows[1][0][-1]).sum(-1)
     assert ((lse[1].double() - (s + math.log(44))).abs() <= s * 2.0 ** -17).all()
+
+
+# ---- tables of the caller's own ------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [8, 16, 64, 128])
+def test_pages_outside_the_pool_are_zeros(P, ctx, dtype, d, page):
+    """A table of the caller's own that names no page within a row's length: keys and values of zeros, as over 16 bits,
+    whatever the memory held that they would have come to."""
+    g, n = gen(page + d), 900
+    full, _ = fill8(P, ctx, g, page, 8, [40000], 2, d, dtype)
+    full.cache.view(torch.uint8).fill_(0x7f)              # not-a-number into every place of shared memory
+    full.scale.fill_(1.0)
+    pg, rows = fill8(P, ctx, g, page, 8, [n, n], 2, d, dtype)
+    gone = [1, 3, n // page - 1, n // page]                # the last one holds the row's end
+    for j, p in zip(gone, (-1, pg.n_pages, 2 ** 31 - 1, -2 ** 31)):
+        pg.table[0, j] = p
+        for x in rows[0]:
+            x[j * page:(j + 1) * page] = 0
+    q = randn(g, 2, 8, d, dtype=dtype)
+    P.attn_decode(ctx, randn(g, 1, 8, d, dtype=dtype), full, 0)
+    one, olse = P.attn_decode(ctx, q, pg, 0, lse=True)
+    P.attn_paged(ctx, randn(g, 1, 8, d, dtype=dtype), full, 0, ints([0, 1]))
+    many, mlse = P.attn_paged(ctx, q, pg, 0, ints([0, 1, 2]), lse=True)
+    again = P.attn_decode(ctx, q, pg, 0)
+    ctx.sync()
+    sequences(one, olse, q, rows, range(3), False, d ** -0.5)
+    sequences(many, mlse, q, rows, range(3), False, d ** -0.5)
+    assert torch.equal(one, again)
