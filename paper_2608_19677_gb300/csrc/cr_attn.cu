@@ -578,6 +578,7 @@ constexpr int kRowsThreads = 640;
 // the kernel that leaves the widening out takes 18 us less.
 constexpr int kRowsWiden = 4;
 constexpr float kLift = 6.f;  // of the weights' logarithms
+constexpr float kUnlift = 0x1p-6f;
 __host__ __device__ constexpr int rows_threads(bool e8) { return e8 ? 768 : kRowsThreads; }
 
 enum { B_QFULL, B_QEMPTY, B_DONE, B_SFULL, B_PREADY = B_SFULL + 2, B_OFULL = B_PREADY + 4, B_OEMPTY = B_OFULL + 2,
@@ -1190,9 +1191,9 @@ __global__ void __launch_bounds__(rows_threads(E8), 1)
                     uint32_t o[16];
                     cr_tmem_ld16(to + i, o);
                     cr_tmem_ld_wait();
-                    if (E8) {
+                    if (E8) {  // sums of weights as they are: values near the type's largest leave no room for more
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * unit);
+                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * (unit * kUnlift));
                     }
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
@@ -1201,7 +1202,7 @@ __global__ void __launch_bounds__(rows_threads(E8), 1)
                 }
                 if (half == 0)
                     reinterpret_cast<float2 *>(A.part_ml)[(uint64_t)slot * RP + r] =
-                        make_float2(m == -INFINITY ? m : (E8 ? fmaf(m, c, -kLift) : m * c), l);
+                        make_float2(m == -INFINITY ? m : E8 ? fmaf(m, c, -kLift) + kLift : m * c, E8 ? l * kUnlift : l);
             } else {
                 if (!A.to_pfx && A.o_wide && A.head_dim == D) {
                     // Lanes of a group of C hold C chunks of 32 bytes of a row each; the chunks change places, so that a

@@ -175,3 +175,21 @@ def test_pages_outside_the_pool_are_zeros(P, ctx, dtype, d, page):
     sequences(one, olse, q, rows, range(3), False, d ** -0.5)
     sequences(many, mlse, q, rows, range(3), False, d ** -0.5)
     assert torch.equal(one, again)
+
+
+# ---- pieces --------------------------------------------------------------------------------------------------------
+def test_pieces_hold_values_as_large_as_16_bits_do(P, ctx):
+    """2,048 keys of equal weight, values near 2^115, cut into pieces whose unnormalised sums stay finite."""
+    g, n, d = gen(11), 2048, 128
+    spread = lambda k, v: (k, (v.abs().double() * 2.0 ** 115).to(BF))  # noqa: E731
+    pg, rows = fill8(P, ctx, g, 16, 16, [n], 2, d, BF, spread=spread)
+    wide = P.KVPages.empty(n // 16, 16, 1, n // 16, 1, 2, d)
+    P.pages_extend(ctx, wide, ints([0]), ints([n]))
+    P.kv_write(ctx, wide, 0, *(x.to(BF) for x in rows[0]), ints([0, n]))
+    q = torch.zeros((1, 4, d), dtype=BF, device=DEV)
+    for pool in (wide, pg):
+        many, mlse = P.attn_paged(ctx, q, pool, 0, ints([0, 1]), lse=True)
+        one, olse = P.attn_decode(ctx, q, pool, 0, lse=True)
+        ctx.sync()
+        sequences(many, mlse, q, rows, [0, 1], False, d ** -0.5)
+        sequences(one, olse, q, rows, [0, 1], False, d ** -0.5)
