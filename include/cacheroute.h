@@ -589,7 +589,9 @@ CR_API int cr_pages_compact(cr_ctx *ctx, const cr_kv_pages *pages, int32_t *d_re
  * that fall outside their row, or into a page that other rows name too (as those of
  * a forked row do that could not be extended), are skipped and reported as CR_EINVAL
  * by the next blocking call: a row's tokens are written before it is forked, in
- * every layer.  Errors: CR_EINVAL, CR_ECUDA. */
+ * every layer.  Into a pool in 8 bits, a row that stands in the list twice is written
+ * by the first of its entries that has tokens (CR_EINVAL by the next blocking call for
+ * the others that have some).  Errors: CR_EINVAL, CR_ENOMEM, CR_ECUDA. */
 CR_API int cr_kv_write(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t layer, const void *d_k, uint64_t k_token,
                        uint64_t k_head, const void *d_v, uint64_t v_token, uint64_t v_head, const int32_t *d_cu,
                        const int32_t *d_seqs, uint32_t n, uint32_t n_tokens);
@@ -639,8 +641,8 @@ CR_API int cr_rope(cr_ctx *ctx, const cr_rotary *rotary, const cr_rope_args *arg
  * (strides as cr_rope's; it may be d_q).  q_heads = 0: no queries.  Tokens whose page
  * other rows name have their queries rotated all the same; queries of tokens that
  * fall outside their row become zeros.  A row that stands in the list twice is
- * written by the first of its entries (CR_EINVAL by the next blocking call; its
- * queries are rotated in every entry).  Errors: CR_EINVAL, CR_ENOMEM, CR_ECUDA. */
+ * written by the first of its entries that has tokens (CR_EINVAL by the next blocking
+ * call for the others that have some; queries are rotated in every entry).  Errors: CR_EINVAL, CR_ENOMEM, CR_ECUDA. */
 typedef struct {
     const void *d_q;
     void *d_q_out;

@@ -55,7 +55,7 @@ enum cr_scratch_slot {
     SCR_ATTN_PART,     // attention: pieces of blocks that several CTAs share
     SCR_ATTN_FEW,      //   of single tokens
     SCR_ATTN_PFX,      // attention: results over shared prefixes
-    SCR_KV_CLAIM,      // long lists of rows that are written: the first entry of each row
+    SCR_KV_CLAIM,      // long lists of rows that are written: the first entry of each row that has tokens
     SCR_NUM
 };
 

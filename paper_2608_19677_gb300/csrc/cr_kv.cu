@@ -326,7 +326,7 @@ struct append_in {
     uint16_t *qo;
     uint64_t q_token, q_head, o_token, o_head, k_token, k_head, v_token, v_head;
     const int32_t *cu, *seqs;
-    const int32_t *claim;  // long lists: the first entry of each row
+    const int32_t *claim;  // long lists: the first entry of each row that has tokens
     uint32_t n, n_tokens, q_heads, step_log2;  // step: positions of a slot
     uint32_t kv_split;     // blockIdx.y below: a share of the key heads, the others one of the query heads
 };
@@ -340,13 +340,13 @@ __global__ void __launch_bounds__(256) k_claim_clear(int32_t *claim, const int32
         if (row >= 0 && (uint32_t)row < n_seqs) claim[row] = 0x7fffffff;
     }
 }
-__global__ void __launch_bounds__(256) k_claim(int32_t *claim, const int32_t *seqs, uint32_t n, uint32_t n_seqs)
+__global__ void __launch_bounds__(256) k_claim(int32_t *claim, const int32_t *seqs, const int32_t *cu, uint32_t n, uint32_t n_seqs)
 {
     cr_launch_next();
     cr_wait_previous();
     for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
         const int row = seqs[i];
-        if (row >= 0 && (uint32_t)row < n_seqs) atomicMin(claim + row, (int)i);
+        if (row >= 0 && (uint32_t)row < n_seqs && cu[i] < cu[i + 1]) atomicMin(claim + row, (int)i);
     }
 }
 
@@ -399,9 +399,9 @@ __device__ __forceinline__ int page_of_slot(const pages_in &P, const append_in &
         if (p >= 0 && (uint32_t)p < P.n_pages && P.ref[p] <= 1) page = p;
         if (A.claim && A.claim[W.row] != (int)W.entry) page = -1;
     }
-    if (A.seqs && !A.claim) {  // a row that an entry before this one names is that one's
+    if (A.seqs && !A.claim) {  // a row that an entry before this one names is that one's, if it has tokens
         bool twice = false;
-        for (uint32_t i = threadIdx.x; i < W.entry; i += kThreads) twice |= A.seqs[i] == W.row;
+        for (uint32_t i = threadIdx.x; i < W.entry; i += kThreads) twice |= A.seqs[i] == W.row && A.cu[i] < A.cu[i + 1];
         if (__syncthreads_or(twice)) page = -1;
     }
     if (page < 0 && threadIdx.x == 0) atomicOr(P.status, CR_FLAG_BADPAGES);
@@ -813,7 +813,7 @@ int cr_append(cr_ctx *ctx, const char *who, const cr_kv_pages *pg, uint32_t laye
         int32_t *claim = static_cast<int32_t *>(p);
         const uint32_t blocks = cr_blocks(A.n, 256, 2 * ctx->num_sms);
         CR_TRY(cr_launch_early(ctx, "k_claim_clear", k_claim_clear, dim3(blocks), 256, 0, claim, A.seqs, A.n, P.n_seqs));
-        CR_TRY(cr_launch_early(ctx, "k_claim", k_claim, dim3(blocks), 256, 0, claim, A.seqs, A.n, P.n_seqs));
+        CR_TRY(cr_launch_early(ctx, "k_claim", k_claim, dim3(blocks), 256, 0, claim, A.seqs, A.cu, A.n, P.n_seqs));
         A.claim = claim;
     }
     // Shares of the heads.  8 bits: as many key heads as 48 KB of shared memory hold for a slice (three CTAs an SM);

@@ -193,3 +193,27 @@ def test_pieces_hold_values_as_large_as_16_bits_do(P, ctx):
         ctx.sync()
         sequences(many, mlse, q, rows, [0, 1], False, d ** -0.5)
         sequences(one, olse, q, rows, [0, 1], False, d ** -0.5)
+
+
+# ---- rows that stand in a list twice -------------------------------------------------------------------------------
+@pytest.mark.parametrize("many", [False, True])
+@pytest.mark.parametrize("bits", [8, 16])
+def test_entries_without_tokens_do_not_claim_a_row(P, ctx, bits, many):
+    """As the padding of a batch names a row: only an entry that has tokens writes it."""
+    g, rot = gen(13), P.Rotary(64)
+    pg = P.KVPages.empty(40, 16, 4, 8, 1, 2, 64, bits=bits)
+    P.pages_extend(ctx, pg, ints([1, 2]), ints([20, 5]))
+    k, v, q = randn(g, 25, 2, 64), randn(g, 25, 2, 64), randn(g, 25, 4, 64)
+    pad = 1500 if many else 3
+    seqs, cu = [2] * pad + [1, 2, 1], [0] * pad + [0, 20, 25, 25]
+    want = P.rope(ctx, q, rot, ints(list(range(20)) + list(range(5))))
+    assert torch.equal(P.kv_append(ctx, pg, 0, q, k, v, rot, ints(cu), seqs=ints(seqs)), want)
+    ctx.sync()
+    _, got = P.kv_read(ctx, pg, 0, ints([0, 20, 25]), seqs=ints([1, 2]))
+    P.kv_write(ctx, pg, 0, v, k, ints(cu), seqs=ints(seqs))
+    ctx.sync()
+    _, back = P.kv_read(ctx, pg, 0, ints([0, 20, 25]), seqs=ints([1, 2]))
+    ctx.sync()
+    tol = 2.0 ** -4 if bits == 8 else 0.0
+    for x, y in ((got, v), (back, k)):
+        assert ((x - y).abs().double() <= y.abs().double() * tol + (2.0 ** -9 if bits == 8 else 0)).all()
