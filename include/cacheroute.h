@@ -657,8 +657,9 @@ CR_API int cr_kv_append(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t layer, c
 /* Tokens of cached rows back, in the 16-bit type: those of entry i are tokens d_cu[i] ..
  * d_cu[i+1]-1 of d_k and d_v (strides as cr_kv_write's), and tokens d_start[i] .. of row
  * d_seqs[i] (NULL: of row i); d_start NULL: the row's last ones.  Tokens that fall
- * outside their row become zeros (CR_EINVAL by the next blocking call).  Keys come as
- * they are held: rotated, where they were written so.  Errors: CR_EINVAL, CR_ECUDA. */
+ * outside their row, and those of no entry, become zeros (CR_EINVAL by the next
+ * blocking call).  Keys come as they are held: rotated, where they were written so.
+ * Errors: CR_EINVAL, CR_ECUDA. */
 typedef struct {
     void *d_k, *d_v;
     const int32_t *d_cu, *d_seqs, *d_start;

@@ -636,7 +636,7 @@ __global__ void __launch_bounds__(kThreads) k_kv_read(const __grid_constant__ pa
             else
                 hi = m;
         }
-        const int a = A.cu[lo], b = A.cu[lo + 1];
+        const int a = A.n ? A.cu[lo] : 0, b = A.n ? A.cu[lo + 1] : 0;
         uint2 w = make_uint2(~0u, 0);
         if (a <= t && t < b) {
             const int row = A.seqs ? A.seqs[lo] : (int)lo;
@@ -865,8 +865,8 @@ extern "C" int cr_kv_read(cr_ctx *ctx, const cr_kv_pages *pages, uint32_t layer,
     if (layer >= pages->layers) return cr_fail(ctx, CR_EINVAL, "cr_kv_read: layer %u of %u", layer, pages->layers);
     const uint32_t n_tokens = a->n_tokens;
     if (a->n > (1u << 24) || n_tokens > (1u << 30)) return cr_fail(ctx, CR_EINVAL, "cr_kv_read: too many entries or tokens");
-    if (!a->n || !n_tokens) return CR_OK;
-    if (!a->d_k || !a->d_v || !a->d_cu) return cr_fail(ctx, CR_EINVAL, "cr_kv_read: NULL pointer");
+    if (!n_tokens) return CR_OK;
+    if (!a->d_k || !a->d_v || (a->n && !a->d_cu)) return cr_fail(ctx, CR_EINVAL, "cr_kv_read: NULL pointer");
     if (!aligned(a->d_k, a->k_token, a->k_head) || !aligned(a->d_v, a->v_token, a->v_head))
         return cr_fail(ctx, CR_EINVAL, "cr_kv_read: keys and values must be 16-byte aligned, strides multiples of 8");
     const pages_in P = cr_pages_input(ctx, pages);

@@ -217,3 +217,16 @@ def test_entries_without_tokens_do_not_claim_a_row(P, ctx, bits, many):
     tol = 2.0 ** -4 if bits == 8 else 0.0
     for x, y in ((got, v), (back, k)):
         assert ((x - y).abs().double() <= y.abs().double() * tol + (2.0 ** -9 if bits == 8 else 0)).all()
+
+
+# ---- reading back --------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("bits", [8, 16])
+def test_reading_for_no_rows(P, ctx, bits):
+    """Tokens of no entry are zeros, and reported, as those behind the last entry are."""
+    pg = P.KVPages.empty(4, 16, 2, 2, 1, 2, 64, bits=bits)
+    for cu in (ints([0]), ints([])):
+        k, v = (torch.full((5, 2, 64), math.nan, dtype=BF, device=DEV) for _ in range(2))
+        fails(P, ctx, P.CR_EINVAL, lambda: P.kv_read(ctx, pg, 0, cu, out=(k, v)))
+        assert bool((k == 0).all()) and bool((v == 0).all())
+        assert P.kv_read(ctx, pg, 0, cu)[0].shape == (0, 2, 64)
+    ctx.sync()
