@@ -28,6 +28,7 @@ What a destination does with the prefixes it holds:
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
 import os
 import struct
@@ -761,6 +762,26 @@ def kv_write(ctx: Context, pages: KVPages, layer: int, k, v, cu, seqs=None):
         ctx.check(st, "cr_kv_write")
 
 
+@functools.lru_cache(None)
+def _pi(bits: int) -> int:
+    """pi * 2^bits, off by a unit at most (Machin: pi = 16 atan(1/5) - 4 atan(1/239))."""
+    def atan_inverse(n):
+        total, power, k, sign = 0, (1 << bits + 32) // n, 1, 1
+        while power:
+            total += sign * (power // k)
+            power, k, sign = power // (n * n), k + 2, -sign
+        return total
+    return (16 * atan_inverse(5) - 4 * atan_inverse(239)) >> 32
+
+
+def _share(f: float) -> int:
+    """f radians as a share of a full turn, times 2^64, whole turns left out: the nearest integer.  A double is below
+    2^1024: with 1,280 bits of pi, the quotient is exact to 2^-190."""
+    num, den = f.as_integer_ratio()
+    num, den = num << 1280 + 64, 2 * den * _pi(1280)
+    return (2 * num + den) // (2 * den) % 2 ** 64
+
+
 class Rotary:
     """Rotary positions: pair i of the first ``dims`` elements of a head turns by position * f_i, f_i = base^(-2i/dims).
 
@@ -769,7 +790,9 @@ class Rotary:
     leaves pairs that turn more than ``fast`` times within ``original`` tokens, divides those that turn less than ``slow``
     times, and goes from one to the other linearly in the turns, and multiplies the rotated elements by
     0.1 ln(factor) + 1 (Peng et al., arXiv 2309.00071).  ``scale`` gives that multiplier instead.  ``frequencies`` gives
-    the f_i (radians a token, ``dims`` / 2 of them) instead of the base.  ``inverse()`` turns back."""
+    the f_i (radians a token, ``dims`` / 2 of them) instead of the base.  ``inverse()`` turns back.
+
+    The f_i are doubles (``frequencies``); angles are exact for these to 2^-32 turns at every position."""
 
     def __init__(self, dims: int, base: float = 10000.0, layout: str = "half", scaling: Optional[str] = None,
                  factor: float = 1.0, original: int = 0, slow: float = 1.0, fast: float = 32.0,
@@ -784,9 +807,12 @@ class Rotary:
         if not (base > 0 and factor > 0) or not (math.isfinite(base) and math.isfinite(factor)):
             raise ValueError("base and factor must be positive")
         if frequencies is None:
-            if scaling == "ntk":
-                base *= factor ** (dims / (dims - 2))
-            f = [base ** (-2.0 * i / dims) for i in range(dims // 2)]
+            try:
+                if scaling == "ntk":
+                    base *= factor ** (dims / (dims - 2))
+                f = [base ** (-2.0 * i / dims) if math.isfinite(base) else math.inf for i in range(dims // 2)]
+            except OverflowError:
+                f = [math.inf]
         else:
             f = [float(x) for x in frequencies]
             if scaling == "ntk":
@@ -805,9 +831,11 @@ class Rotary:
         scale = 1.0 if scale is None else float(scale)
         if not abs(scale) <= 3.4028234663852886e38:
             raise ValueError("scale must be finite")
+        if not all(map(math.isfinite, f)):
+            raise ValueError("base and factor give frequencies that are not finite")
         self.dims, self.layout, self.scale, self.frequencies = dims, layout, scale, f
-        # shares of a full turn, times 2^64; position times share drops whole turns by itself
-        turn = [round(x / (2 * math.pi) * 2.0 ** 64) % 2 ** 64 for x in f]
+        # position times share drops whole turns by itself
+        turn = [_share(x) for x in f]
         self.turn = torch.tensor([t - 2 ** 64 if t >= 2 ** 63 else t for t in turn], dtype=torch.int64, device=device)
         self._bind(0)
 

@@ -2,8 +2,9 @@
 // (include/cacheroute.h).
 //
 // Angles.  The k-th pair's frequency is held as a 64-bit share of a full turn, so position times frequency is an integer
-// product whose overflow drops whole turns: the angle of the furthest position is as exact as the nearest one's, where a
-// 32-bit product would be off by 2^-24 of all the turns made.
+// product whose overflow drops whole turns: the angle of the furthest position is exact for that share to the 2^-32 turns
+// that are used of it (a share is off by 2^-65 turns, the furthest position's product by 2^-34), where a 32-bit product would
+// be off by 2^-24 of all the turns made.
 //
 // All three calls move each element once (2 bytes in, 2 or 1 out) and are bound by that, or by the latency of their
 // dependent reads (list, length, table, page) where there are few tokens.  A lane holds V consecutive elements of a
@@ -40,8 +41,8 @@ struct rope_shared {
 // Cosine and sine of t * 2^-32 turns, each within 0.73 units in the last place of a 32-bit number in the first octant: what
 // they multiply is rounded to three bits later on, and a cosine that is off by 2^-23 decides one number in a million
 // differently.  Whole quarters are dropped as integers; the angle of what is left, |r| <= 2^29, is the sum of th, the
-// 32-bit product, and e, what that product lacks; then the Taylor series at th (behind the last term: 1e-9 of the angle,
-// 1e-9) and e times the other function.
+// 32-bit product, and e, what that product lacks; then the Taylor series at th (behind the last term, at pi / 4: 2.3e-9 of
+// the angle for the sine, 1.2e-10 for the cosine) and e times the other function.
 __device__ __forceinline__ void cos_sin_turn(uint32_t t, float &c, float &s)
 {
     constexpr float kHi = 0x1.921fb6p-30f, kLo = -0x1.777a5cp-55f;  // 2 pi * 2^-32
