@@ -25,8 +25,8 @@ import functools
 from collections import OrderedDict
 from typing import Dict, List, Sequence, Tuple
 
-from . import (Context, KVPages, attn_decode, attn_paged, kv_append, kv_read, kv_write, pages_compact, pages_extend,
-               pages_fork, pages_free)
+from . import (Context, KVPages, _heads, _no_gradient, attn_decode, attn_paged, kv_append, kv_read, kv_write, pages_compact,
+               pages_extend, pages_fork, pages_free)
 
 
 def _on_context_stream(call):
@@ -90,6 +90,16 @@ class Destination:
         width = self.pages.table.shape[1] * self.pages.page
         if tokens > width:
             raise RuntimeError(f"a row of {width} tokens has no room for {tokens}")
+
+    def _check_kv(self, tokens: int, layers) -> None:
+        """What ``kv_write`` would refuse, before idle prefixes leave for it."""
+        p = self.pages
+        for k, v in layers:
+            for name, t in (("keys", k), ("values", v)):
+                at, *strides = _heads(name, t, p.dtype, t.shape, tokens, p.kv_heads, p.head_dim)
+                if t.device != p.lens.device or at % 16 or any(s % 8 for s in strides):
+                    raise ValueError(f"{name} must be on {p.lens.device}, 16-byte aligned, with strides that are multiples of 8")
+            _no_gradient(k, v)
 
     def _pages(self, tokens: int) -> int:
         return -(-tokens // self.pages.page)
@@ -262,8 +272,9 @@ class Destination:
 
     @_on_context_stream
     def install(self, key: int, layers) -> None:
-        """Hold a prefix whose keys and values another destination has exported.  Idle prefixes leave for it; if a call
-        fails, it is given up.  Pools in 8 bits with blocks of the same size hold the same numbers then."""
+        """Hold a prefix whose keys and values another destination has exported.  Tensors that the pool cannot take are
+        refused before anything changes.  Idle prefixes leave for it; if a call fails, it is given up.  Pools in 8 bits with
+        blocks of the same size hold the same numbers then."""
         if key in self.prefixes:
             raise ValueError(f"key {key} is held already")
         if len(layers) != self.model.layers:
@@ -271,6 +282,8 @@ class Destination:
         n = int(layers[0][0].shape[0])
         if n < 1 or any(int(t.shape[0]) != n for kv in layers for t in kv):
             raise ValueError("keys and values of a prefix have its tokens, one at least, in every layer")
+        if self.pages.lens.is_cuda:
+            self._check_kv(n, layers)
         self._check_width(n)
         self._make_room(1, self._pages(n), {key})
         row = self._take(n, self._pages(n))

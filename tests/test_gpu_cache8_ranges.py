@@ -230,3 +230,29 @@ def test_reading_for_no_rows(P, ctx, bits):
         assert bool((k == 0).all()) and bool((v == 0).all())
         assert P.kv_read(ctx, pg, 0, cu)[0].shape == (0, 2, 64)
     ctx.sync()
+
+
+# ---- prefixes that move --------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("bits", [8, 16])
+def test_install_refuses_before_idle_prefixes_leave(P, ctx, bits):
+    from examples.serve_prefixes import TinyAttention
+    from paper_2608_19677_gb300.destination import Destination
+    model = TinyAttention(torch, DEV)
+    pages = P.KVPages.empty(8, 16, 3, 8, model.layers, model.kv_heads, model.dim, bits=bits)
+    d = Destination(ctx, pages, model)
+    text = torch.arange(70, device=DEV)
+    rows, _ = d.admit([(1, text, 64)])
+    d.finish(rows)                                   # an idle prefix of four pages; five more do not fit beside it
+    kv = [tuple(randn(gen(5), 80, model.kv_heads, model.dim) for _ in range(2)) for _ in range(model.layers)]
+    k, v = kv[1]
+    free = d.free_pages, sorted(d.free_rows)
+    for wrong in ((k.half(), v), (k, v.float()), (k[:, :1], v[:, :1]), (k[..., :32], v[..., :32]), (k, v[..., None]), (k.cpu(), v.cpu()),
+                  (k, v, v), (k, v.transpose(1, 2).contiguous().transpose(1, 2)), (k, v.clone().requires_grad_()),
+                  (k, torch.cat([v, v], -1)[..., 4:4 + model.dim])):
+        with pytest.raises(ValueError):
+            d.install(2, [kv[0], wrong])
+        assert list(d.prefixes) == [1] and (d.free_pages, sorted(d.free_rows)) == free
+    with torch.no_grad():
+        d.install(2, [kv[0], (k, v.clone().requires_grad_())])
+    assert list(d.prefixes) == [2]
+    ctx.sync()
