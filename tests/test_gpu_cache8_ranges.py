@@ -12,7 +12,7 @@ if not torch.cuda.is_available():
 else:
     pytestmark = pytest.mark.gpu
 
-from test_gpu_cache8 import BF, DEV, HF, P, check, ctx, cum, fails, fill8, gen, ints, randn, reference  # noqa: E402,F401
+from test_gpu_cache8 import BF, DEV, HF, P, check, ctx, cum, fails, fill8, gen, ints, randn, reference, turned  # noqa: E402,F401
 
 
 def sequences(out, lse, q, rows, cu, causal, scale, extra=0.0):
@@ -256,3 +256,106 @@ def test_install_refuses_before_idle_prefixes_leave(P, ctx, bits):
         d.install(2, [kv[0], (k, v.clone().requires_grad_())])
     assert list(d.prefixes) == [2]
     ctx.sync()
+
+
+# ---- powers far apart ----------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("hq", [2, 16])
+def test_many_rows_over_blocks_of_very_different_size(P, ctx, dtype, hq):
+    """Several causal tokens over lengths off a tile; values' powers 2^18 apart, keys' 2^4, whole blocks and tiles of zeros,
+    queries from zero and 2^-40 (bfloat16) to 2^3: outputs and the kernel's own lse.
+
+    The bound has a term more, derived before its first run: the kernel's weights are halves of 2^6 times the row's own, so
+    each is off by 2^-31 of the row's largest at most (half of a half's last subnormal place, 2^-25, over 2^6), and numbers
+    are off by 2^-31 of the largest power so far; a row's sum is at least its largest weight.  Together (n + 1) 2^-31 of the
+    largest value."""
+    g, d = gen(29), 64
+    lens, new = [500, 129, 777], [130, 3, 64]
+    n = sum(lens)
+
+    def spread(k, v):
+        i = torch.arange(n, device=DEV) // 16
+        k = (k * 2.0 ** (i % 5 - 3)[:, None, None]).to(dtype)
+        v = (v.double() * 2.0 ** ((i * 7 % 19) - 14).double()[:, None, None]).to(dtype)
+        k[i % 11 == 4], v[i % 13 == 2] = 0, 0
+        k[640:1100] = 0
+        return k, v
+
+    pg, rows = fill8(P, ctx, g, 16, 16, lens, 1, d, dtype, spread=spread)
+    q = randn(g, sum(new), hq, d, dtype=dtype, spread=0.5)
+    if dtype == BF:
+        q = (q.double() * 2.0 ** torch.linspace(-40, 3, hq, device=DEV).double()[None, :, None]).to(dtype)
+    q[::7] = 0
+    cu = np.concatenate([[0], np.cumsum(new)])
+    for causal in (True, False):
+        out, lse = P.attn_paged(ctx, q, pg, 0, cum(new), causal=causal, scale=0.25, lse=True)
+        ctx.sync()
+        most = max(float(v.abs().max()) for _, v in rows)
+        sequences(out, lse, q, rows, cu, causal, 0.25, extra=(max(lens) + 1) * 2.0 ** -31 * most)
+
+
+# ---- a server ------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("rotary", [True, False])
+def test_destination_holds_the_models_keys_and_values(P, ctx, bits, rotary):
+    """After every pass, a row's new tokens are the model's keys, rotated to their positions, and its values: rounded once, by
+    2^-4 (8 bits) or 2^-8 (rotated keys) of themselves, or by 2^-10 of their block's power, which is below 2^-7 times the
+    row's largest magnitude (448 2^e is less than twice its block's)."""
+    from examples.serve_prefixes import TinyAttention
+    from paper_2608_19677_gb300.destination import Destination
+    rot = P.Rotary(64, scaling="ramp", factor=4.0, original=256) if rotary else None
+    met = []
+
+    class Watched(TinyAttention):
+        def qkv(self, layer, x):
+            self.kv = super().qkv(layer, x)[1:]
+            return *super().qkv(layer, x)[:1], *self.kv
+
+        def mix(self, layer, x, out):
+            ctx.sync()
+            at = 0
+            for row, m in met[-1]:
+                n = int(pages.lens[row])
+                held = P.kv_read(ctx, pages, layer, ints([0, n]), seqs=ints([row]))
+                ctx.sync()
+                k, v = (t[at:at + m] for t in self.kv)
+                k, off = turned(k, np.arange(n - m, n), rot) if rot is not None else (k.double(), 0.0)
+                for got, want, slack, exact in ((held[0], k, off, rot is None), (held[1], v.double(), 0.0, True)):
+                    near = 2.0 ** -4 if bits == 8 else 0.0 if exact else 2.0 ** -8
+                    small = 2.0 ** -17 * 1.07 * float(got.abs().max()) if bits == 8 else 0.0
+                    assert ((got[n - m:].double() - want).abs() <= near * want.abs() * 1.01 + slack * 1.07 + small).all(), (layer, row)
+                at += m
+            assert at == out.shape[0]
+            return super().mix(layer, x, out)
+
+    model = Watched(torch, DEV, rotary=rot)
+    pages = P.KVPages.empty(200, 16, 12, 12, model.layers, model.kv_heads, model.dim, bits=bits)
+    d = Destination(ctx, pages, model)
+    forward = d._forward
+
+    def watched(tokens, cu, rows, groups=None):
+        met.append(list(zip(rows.tolist(), np.diff(cu.tolist()).tolist())))
+        return forward(tokens, cu, rows, groups)
+
+    d._forward = watched
+    g = gen(61)
+    text = lambda n: torch.randint(0, 4096, (n,), generator=g, device=DEV)  # noqa: E731
+    a, b = text(100), text(33)
+    d.admit([(1, torch.cat([a, text(5)]), 100), (2, torch.cat([b[:30], text(40)]), 30), (1, torch.cat([a[:64], text(1)]), 64)])
+    for _ in range(3):
+        d.step(text(3))
+    d.compact()
+    d.step(text(3))
+    assert len(met) == 6
+
+
+def test_example_in_8_bits():
+    """Keys and values are off by 2^-4 / sqrt(3) of themselves in the mean square at most, independently; the model's scores
+    have a spread of 1, so that this moves a layer's attention by sqrt(2) times as much of itself, through its values and
+    through its weights.  Attention is at most as large as what it is added to.  The second layer is off by that again, and
+    by what the first layer's error does to its queries, keys and values: sqrt(1 + 1 + 3) in all; twice that for the worst of
+    the requests, and the bound of 16 bits beside it."""
+    import examples.serve_prefixes as m
+    bound = 2 * 2.0 ** -4 / math.sqrt(3) * math.sqrt(2) * math.sqrt(5) + 2.0 ** -9 * math.sqrt(12) * 2
+    for rotary in (True, False):
+        assert m.main(48, 3, log=lambda *_: None, rotary=rotary, bits=8) < bound
