@@ -572,10 +572,11 @@ constexpr int kRowsThreads = 640;
 // The softmax threads multiply scores by R of the keys' tile; values' R is the largest of the piece so far, and as it grows
 // the accumulator is scaled.  They hold weights 2^6 times larger, so that those below the row's largest by 2^20 are still
 // rounded to 11 bits, and bring each row of bfloat16 queries to 2^14 .. 2^15 by a power of two (k_attn_few8).
-// Tiles of bfloat16 would be exact without R, at twice the instructions.  Registers: 512 x 96 + 256 x 48 = 768 x 80.
-// Measured (one GB300, 40 suffixes of 1 to 128 tokens over prefixes to 16,384, 32/4 heads of 128): 153 us a call, with two
-// widening warps 170, with tiles of bfloat16 249.  Tensor cores at work in 47% of the cycles (16-bit pages: 60%); a copy of
-// the kernel that leaves the widening out takes 18 us less.
+// Tiles of bfloat16 would be exact without R, at twice the instructions.  Registers: 512 x 96 + 256 x 48 = 768 x 80, and 20
+// to 48 bytes of spill stores.
+// Measured (one GB300, 40 suffixes of 1 to 128 tokens over prefixes to 16,384, 32/4 heads of 128): 155 us a call (153 before
+// scores beyond kFar were looked after), with two widening warps 170, with tiles of bfloat16 249.  Tensor cores at work in
+// 47% of the cycles (16-bit pages: 60%); a copy of the kernel that leaves the widening out takes 18 us less.
 constexpr int kRowsWiden = 4;
 constexpr float kLift = 6.f;  // of the weights' logarithms
 constexpr float kUnlift = 0x1p-6f;
@@ -1830,6 +1831,7 @@ out:
 // A head's maximum may lag by 2^8: then a step needs no exchange between lanes but one vote.
 // Bound by HBM and latency: 64 contexts to 32,768, 28/4 heads of 128, 89 us (538 MB, 6.0 TB/s) of the call's 141; with
 // heads as the 16-row operand and maxima that do not lag the call took 161.  One token over 2,112: 9 to 10 us cold.
+// Registers: 114 to 156; WIDE 152 to 168, which at head size 128 leaves 148 (half) or 192 (bfloat16) bytes of spill stores.
 template <int D>
 struct few8_cfg {
     static constexpr int kTile = kFewTile * D;            // bytes of 64 keys
