@@ -792,7 +792,7 @@ class Rotary:
     0.1 ln(factor) + 1 (Peng et al., arXiv 2309.00071).  ``scale`` gives that multiplier instead.  ``frequencies`` gives
     the f_i (radians a token, ``dims`` / 2 of them) instead of the base.  ``inverse()`` turns back.
 
-    The f_i are doubles (``frequencies``); angles are exact for these to 2^-32 turns at every position."""
+    The f_i are doubles (``frequencies``); at every position, angles are within 2^-31 turns of theirs."""
 
     def __init__(self, dims: int, base: float = 10000.0, layout: str = "half", scaling: Optional[str] = None,
                  factor: float = 1.0, original: int = 0, slow: float = 1.0, fast: float = 32.0,
